@@ -105,7 +105,8 @@ typedef enum {
     TWINKV_ERR_TIMEOUT = 5,       /* a device-side wait gave up; outputs are undefined */
     TWINKV_ERR_WORKSPACE = 6,     /* workspace missing, misaligned or too small */
     TWINKV_ERR_TOO_LARGE = 7      /* more than TWINKV_NOALLOC_MAX_POSITIONS positions were
-                                     given to twinkv_repair_select_noalloc */
+                                     given to twinkv_repair_select_noalloc; more slots than a
+                                     unit has pages (twinkv_cache_*) */
 } twinkv_status;
 
 typedef enum { TWINKV_BF16 = 0, TWINKV_F32 = 1 } twinkv_dtype;
@@ -362,6 +363,178 @@ twinkv_status twinkv_policy(const void* keys, twinkv_shape s, const int32_t* bud
                             float threshold, const twinkv_params* params, uint8_t* out_mask,
                             int32_t* out_count, int32_t* out_status, void* workspace,
                             size_t workspace_bytes, void* stream);
+
+/* ==== The cache that the repair leaves: pages of 4-bit codes ==========================
+ *
+ * The calls below make the keys that the pass audits (twinkv_qk_norm_rope), keep the
+ * keys and values that a mask retains (twinkv_cache_pack), add new tokens
+ * (twinkv_cache_append), evict again (twinkv_cache_read for the audit,
+ * twinkv_cache_compact) and attend over what is kept (twinkv_cache_attend).  Streams,
+ * workspaces, CUDA graphs and errors are as above; the kernels wait on nothing.
+ *
+ * Rounding.  A row (one position's key or value in one head) is rounded in groups of 64
+ * values, float32 values to bf16 first:
+ *     lo = min(0, smallest), hi = max(0, largest), s = bf16((hi - lo) / 15),
+ *     z = min(15, rint(-lo / s)), c = min(15, rint(x / s) + z)
+ * (s below 2^-126: s = z = c = 0; rint to nearest, ties to even; the results are those of
+ * exact arithmetic).  The group keeps s (bf16), z and the 64 codes c, and stands for the
+ * values s (c - z), within about 0.53 s of x.  Values must be finite and below 2^120.
+ *
+ * Pages.  A page holds TWINKV_PAGE_SLOTS slots of one unit (a sequence or layer, and one
+ * KV head): their codes, scales, zeros and positions, twinkv_cache_page_bytes(d) bytes (148
+ * a slot at d = 128, 76 at d = 64), in the order in which the attention reads them.  The
+ * caller owns the pool of pages and says which page has which slots: entry j of a unit's
+ * row of `table` ([units][max_pages] int32) is the page of slots [64 j, 64 j + 64), and
+ * lens[u] slots are in use.  Units may have different lengths.  Since the repair keeps
+ * exactly its budget, the pages a unit needs, ceil(budget / 64), are known before the
+ * call.  A page may be in several rows of tables (sequences that share a beginning) as
+ * long as no call writes it.
+ *
+ * Data errors, in out_status[u]: TWINKV_ERR_INVALID_ARG for a length outside
+ * [0, 64 max_pages], a mask byte above 1 or a page number outside the pool;
+ * TWINKV_ERR_TOO_LARGE for more slots than the unit's row of `table` has pages.  No
+ * such unit makes a kernel read or write outside the caller's arrays.
+ */
+#define TWINKV_PAGE_SLOTS 64
+
+typedef struct {
+    void* pages;         /* [n_pages][twinkv_cache_page_bytes(d)] device, 16-byte aligned */
+    int32_t n_pages;
+    int32_t d;           /* 64 or 128 */
+} twinkv_pool;
+
+/* Bytes of a page (0 for another d). */
+size_t twinkv_cache_page_bytes(int32_t d);
+
+/* Heads of queries and keys: strides in elements, multiples of 16 bytes. */
+typedef struct {
+    int32_t tokens, heads_q, heads_k, d, dtype;
+    int32_t rows;                          /* of the table of cosines and sines */
+    int64_t q_token, q_head, k_token, k_head;
+    int64_t out_q_token, out_q_head, out_k_token, out_k_head;
+} twinkv_heads;
+
+/*
+ * Norms of queries and keys per head and their rotation by position, in one pass: what
+ * turns a layer's projections into queries and into the post-RoPE keys of Sec. 3.2.
+ *   y = x / sqrt(mean(x^2) + eps) * w         (w NULL: y = x)
+ *   out[j] = y[j] cos - y[j + d/2] sin,  out[j + d/2] = y[j] sin + y[j + d/2] cos
+ * in float32, rounded once.
+ *   q, k        [tokens][heads][d] of s.dtype, 16-byte aligned, strides in s (views into a
+ *               fused projection, or a dense cache [H][N][d]); heads_q or heads_k may be 0
+ *   wq, wk      [d] of s.dtype, 16-byte aligned, or NULL (no norm)
+ *   cos_sin     [rows][d] float32: d/2 cosines, then d/2 sines, of each position
+ *   positions   [tokens] int32, in [0, rows)
+ *   out_q, out_k  strides in s; may be q and k themselves (with the same strides)
+ *   out_status  [tokens] int32 or NULL: TWINKV_ERR_INVALID_ARG where the position is outside
+ *               the table (that token's outputs are 0)
+ */
+twinkv_status twinkv_qk_norm_rope(const void* q, const void* k, twinkv_heads s, const void* wq,
+                                  const void* wk, float eps, const float* cos_sin,
+                                  const int32_t* positions, void* out_q, void* out_k,
+                                  int32_t* out_status, void* stream);
+
+/* Workspace of twinkv_cache_pack and twinkv_cache_compact with a mask of `units` rows of N. */
+size_t twinkv_cache_move_workspace(int32_t units, int32_t N);
+
+/*
+ * The retained rows of a dense cache into pages: slot r of unit u becomes its r-th retained
+ * position, key and value (S1 of the repair, Sec. 3.4, or any mask).
+ *   keys, values   [L][H][N][d] device, s.dtype, 16-byte aligned; only retained rows are read
+ *   retained_mask  [L][H][N] uint8, or NULL: every row is kept (no workspace then)
+ *   table          [L*H][max_pages]; the pages a unit fills must be in no other row
+ *   out_lens       [L*H] int32: rows kept (0 for a unit with a data error)
+ *   out_status     [L*H] int32, or NULL
+ */
+twinkv_status twinkv_cache_pack(const void* keys, const void* values, twinkv_shape s,
+                                const uint8_t* retained_mask, twinkv_pool pool,
+                                const int32_t* table, int32_t max_pages, int32_t* out_lens,
+                                int32_t* out_status, void* workspace, size_t workspace_bytes,
+                                void* stream);
+
+/* New rows: strides in elements, multiples of 16 bytes. */
+typedef struct {
+    int32_t B, H, n, dtype;
+    int64_t k_batch, k_token, k_head, v_batch, v_token, v_head;
+} twinkv_rows;
+
+/*
+ * The rows of n <= 64 new tokens behind each unit's last slot.
+ *   keys, values  [B][n][H][d] of s.dtype, 16-byte aligned, strides in s
+ *   positions     [B][n] int32, at least 0, ascending and above those already stored
+ *   table, lens   of the B*H units; the pages from slot lens[u] on must be in no other row
+ *   out_lens      [B*H] int32: lens + n, or lens for a unit with a data error (nothing is
+ *                 written to its pages); may be `lens` itself
+ *   out_status    [B*H] int32, or NULL
+ * More than 64 tokens: TWINKV_ERR_UNSUPPORTED.
+ */
+twinkv_status twinkv_cache_append(const void* keys, const void* values, twinkv_rows s,
+                                  const int32_t* positions, twinkv_pool pool,
+                                  const int32_t* table, int32_t max_pages, const int32_t* lens,
+                                  int32_t* out_lens, int32_t* out_status, void* stream);
+
+/*
+ * The kept slots of each unit into other pages, in order, codes and positions as they are.
+ *   table, lens   of the source
+ *   keep          [units][N] uint8, N at least the longest unit; bytes from lens[u] on are not
+ *                 looked at.  NULL: every slot is kept (a copy; no workspace).  A fork that
+ *                 shares its full pages copies its last one so
+ *   new_table     [units][new_max_pages]: pages that are in no other row, nor in `table`
+ *   out_lens      [units] int32: slots kept (0 for a unit with a data error, which includes
+ *                 lens[u] > N); not `lens`
+ *   out_status    [units] int32, or NULL
+ */
+twinkv_status twinkv_cache_compact(twinkv_pool pool, const int32_t* table, int32_t max_pages,
+                                   const int32_t* lens, int32_t units, const uint8_t* keep,
+                                   int32_t N, const int32_t* new_table, int32_t new_max_pages,
+                                   int32_t* out_lens, int32_t* out_status, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+
+/*
+ * The first (last != 0: the last) `rows` slots of each unit as bf16 rows, as the audit of
+ * a cache in pages reads its keys.  Row r is slot r (last: slot max(0, lens[u] - rows) + r);
+ * rows without a slot, or with a page number outside the pool, are 0 at position -1.
+ *   out_keys, out_values  [units][rows][d] bf16, 16-byte aligned
+ *   out_positions         [units][rows] int32, or NULL
+ *   out_status            [units] int32, or NULL
+ */
+twinkv_status twinkv_cache_read(twinkv_pool pool, const int32_t* table, int32_t max_pages,
+                                const int32_t* lens, int32_t units, int32_t rows, int32_t last,
+                                void* out_keys, void* out_values, int32_t* out_positions,
+                                int32_t* out_status, void* stream);
+
+/* Queries of B sequences, n tokens and Hq heads over H KV heads: strides in elements. */
+typedef struct {
+    int32_t B, H, Hq, n;
+    int64_t q_batch, q_token, q_head;
+} twinkv_queries;
+
+size_t twinkv_cache_attend_workspace(twinkv_queries s, int32_t d);
+
+/*
+ * Attention of each sequence's newest n <= 64 tokens over its pages.  Token i is the one in
+ * slot lens[u] - n + i (append first); query head h reads KV head h / (Hq / H).  Token i sees
+ * the slots up to its own and, with window > 0, of those only the ones whose position is
+ * above its own minus `window` or below n_sink (the sinks and the recent region of Sec. 3.2).
+ *   o = sum_j softmax_j(scale q . k_j) v_j      float32 sums; a token that sees nothing: 0
+ * Precision: codes and queries enter exactly; a probability times its slot's value scale is
+ * rounded to bf16, then the result to bf16.
+ *   q           [B][n][Hq][d] bf16, 16-byte aligned, strides in s (multiples of 8)
+ *   scale       finite, above 0
+ *   window      0: none (n_sink is then not used)
+ *   table, lens of the B*H units, unit b*H + h; the positions of a unit's slots ascend
+ *   out         [B][n][Hq][d] bf16, 16-byte aligned
+ *   out_lse     [B][n][Hq] float32 log of the softmax's denominator (-inf: nothing seen), or
+ *               NULL; attention over several caches is joined with it
+ *   out_status  [B*H] int32, or NULL; pages outside the pool count as unseen
+ * Limits (TWINKV_ERR_UNSUPPORTED beyond): n <= 64, Hq / H <= 256, B*H and
+ * B*H*ceil(n Hq / H / 16) <= 65535.
+ */
+twinkv_status twinkv_cache_attend(const void* q, twinkv_queries s, float scale, int32_t window,
+                                  int32_t n_sink, twinkv_pool pool, const int32_t* table,
+                                  int32_t max_pages, const int32_t* lens, void* out,
+                                  float* out_lse, int32_t* out_status, void* workspace,
+                                  size_t workspace_bytes, void* stream);
 
 /* Static description of a status code. */
 const char* twinkv_status_string(twinkv_status st);

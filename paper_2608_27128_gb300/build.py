@@ -21,8 +21,9 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libtwinkv.so")
 SOURCES = ["twk_api.cu", "twk_audit.cu", "twk_prep.cu", "twk_refine.cu", "twk_repair.cu",
-           "twk_policy.cu"]
-HEADERS = ["twk_internal.h", "twk_ptx.cuh", "twk_df.cuh", "twk_bound.cuh"]
+           "twk_policy.cu", "twk_rope.cu", "twk_cache.cu", "twk_attend.cu", "twk_cache_api.cu"]
+HEADERS = ["twk_internal.h", "twk_ptx.cuh", "twk_df.cuh", "twk_bound.cuh", "twk_cache.cuh",
+           "twk_cache_internal.h"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
 

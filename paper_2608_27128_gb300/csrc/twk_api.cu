@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "twinkv.h"
+#include "twk_cache_internal.h"
 #include "twk_internal.h"
 
 namespace twk {
@@ -427,6 +428,17 @@ twinkv_status noalloc_scratch(void** out)
 }
 
 }  // namespace
+
+twinkv_status device_facts(int* sms)
+{
+    DeviceInfo* dev = nullptr;
+    const twinkv_status r = device_info(&dev);
+    if (r == TWINKV_OK) *sms = dev->sms;
+    return r;
+}
+
+twinkv_status cuda_result(cudaError_t e) { return cuda_status(e); }
+
 }  // namespace twk
 
 using namespace twk;
@@ -470,8 +482,8 @@ const char* twinkv_status_string(twinkv_status st)
     case TWINKV_ERR_TIMEOUT: return "a device-side wait timed out";
     case TWINKV_ERR_WORKSPACE: return "workspace missing, misaligned or too small";
     case TWINKV_ERR_TOO_LARGE:
-        return "L*H*N exceeds TWINKV_NOALLOC_MAX_POSITIONS (the fixed scratch of "
-               "twinkv_repair_select_noalloc)";
+        return "too large: L*H*N exceeds TWINKV_NOALLOC_MAX_POSITIONS (the fixed scratch of "
+               "twinkv_repair_select_noalloc), or a unit's slots its pages";
     }
     return "unknown status";
 }

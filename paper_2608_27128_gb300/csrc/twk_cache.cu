@@ -1,0 +1,662 @@
+// twk_cache.cu -- writing, moving and reading the pages of a cache held in 4 bits
+// (layout and rounding: twk_cache.cuh).
+//
+//   index_kernel    the kept rows of every unit in order, from a mask
+//   pack_kernel     kept rows of a dense cache -> codes -> pages
+//   append_kernel   the rows of new tokens -> codes -> the slots after a unit's last
+//   compact_kernel  kept slots of pages -> other pages, codes as they are
+//   read_kernel     pages -> bf16 rows
+//
+// All are bound by memory, or by latency where the call is small.  Keys are stored slot by slot.
+// Values are stored for the attention kernel with eight slots of one dimension to a word, while
+// rounding, moving and reading want eight dimensions of one slot: the word held by both sides is
+// an 8 x 8 block of codes, transposed in registers in 32 instructions (transpose8).
+#include "twk_cache.cuh"
+#include "twk_cache_internal.h"
+#include "twk_internal.h"
+#include "twk_ptx.cuh"
+
+namespace twk {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
+constexpr int kInvalid = TWINKV_ERR_INVALID_ARG;
+constexpr int kTooLarge = TWINKV_ERR_TOO_LARGE;
+
+// out[i] nibble n = in[n] nibble i
+__device__ __forceinline__ void transpose8(uint32_t (&r)[8])
+{
+    uint32_t a[8], b[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        a[i] = __byte_perm(r[i], r[i + 4], 0x5410);
+        a[i + 4] = __byte_perm(r[i], r[i + 4], 0x7632);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; i += 4)
+#pragma unroll
+        for (int j = i; j < i + 2; ++j) {
+            b[j] = __byte_perm(a[j], a[j + 2], 0x6240);
+            b[j + 2] = __byte_perm(a[j], a[j + 2], 0x7351);
+        }
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+        r[i] = (b[i] & 0x0f0f0f0fu) | ((b[i + 1] << 4) & 0xf0f0f0f0u);
+        r[i + 1] = ((b[i] >> 4) & 0x0f0f0f0fu) | (b[i + 1] & 0xf0f0f0f0u);
+    }
+}
+
+// A slot's words of eight value codes (dimensions 8 j .. 8 j + 7, in the key words' order of
+// nibbles) are kept in shared memory at slot * kSlotWords + j, the stride odd against bank
+// conflicts.
+template <int D>
+constexpr int kSlotWords = D / 8 + 1;
+
+// One block of transpose8: the values of dimensions [8 j, 8 j + 8) at the eight slots with the
+// given t and a (slot = 32 a + 16 c + 8 k + 2 t + b).
+struct Block8 {
+    int j, t, a;
+    // consecutive blocks are the 16 words of a page's row (m, g), then the next m
+    __device__ explicit Block8(int i) : j(i / 16 * 2 + i / 2 % 2), t(i / 4 % 4), a(i % 2) {}
+    __device__ int slot(int n) const
+    {
+        return 32 * a + n / 2 % 2 * 16 + n % 2 * 8 + 2 * t + n / 4;
+    }
+    // word of the page's value codes with dimension 8 j + g
+    __device__ int word(int g) const
+    {
+        return ((j / 2 * 8 + g) * 4 + t) * 4 + j % 2 * 2 + a;
+    }
+    // nibble of a slot's word that holds dimension 8 j + g
+    __device__ static constexpr int nibble(int g) { return g / 2 + 4 * (g % 2); }
+};
+
+// ---------------------------------------------------------------- index
+
+constexpr int kVecChunk = kThreads;       // 16-byte vectors of a block
+
+// Vector v of a unit's mask: the bytes at positions [16 v - mis, +16) of the row, those outside
+// [0, limit) zero.  Rows start at any address: mis makes the vectors' addresses multiples of 16.
+__device__ __forceinline__ uint4 mask_vector(const uint8_t* row, int mis, int64_t v, int limit)
+{
+    const int64_t p = 16 * v - mis;
+    if (p >= 0 && p + 16 <= limit) return *reinterpret_cast<const uint4*>(row + p);
+    uint32_t w[4] = {};
+    for (int i = 0; i < 16; ++i)
+        if (p + i >= 0 && p + i < limit)
+            w[i / 4] |= static_cast<uint32_t>(row[p + i]) << (8 * (i % 4));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+__device__ __forceinline__ int mask_count(const uint4& v)
+{
+    return __popc((v.x & 0x01010101u) | (v.y & 0x01010101u) << 1 | (v.z & 0x01010101u) << 2 |
+                  (v.w & 0x01010101u) << 3);
+}
+
+// A block per 4096 positions of a unit.  Each counts what lies before its own positions by itself
+// (masks are small against the rows: at 131072 positions a unit's blocks read 2 MB of L2 where
+// its rows are 32 MB), so that one launch does it; the unit's last block, which thus sees the
+// whole mask, also checks it, the length and the page numbers.
+__global__ void __launch_bounds__(kThreads) index_kernel(const IndexArgs a)
+{
+    __shared__ int s_sum[kWarps], s_bad[kWarps], s_scan[kWarps];
+    wait_for_previous();
+    const int u = blockIdx.y, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    int limit = a.limit ? a.limit[u] : a.N;
+    int status = 0;
+    if (limit < 0 || limit > a.limit_most) {
+        status = kInvalid;
+        limit = 0;
+    }
+    const uint8_t* row = a.mask ? a.mask + static_cast<int64_t>(u) * a.N : nullptr;
+    const int mis = static_cast<int>(reinterpret_cast<uintptr_t>(row) & 15);
+    const int64_t vectors = row ? (static_cast<int64_t>(limit) + mis + 15) / 16 : 0;
+    const int64_t v0 = static_cast<int64_t>(blockIdx.x) * kVecChunk;
+    const int last = vectors > 0 ? static_cast<int>((vectors - 1) / kVecChunk) : 0;
+    if (static_cast<int>(blockIdx.x) > last) return;
+    int total = limit;
+    bool bad = false;
+    if (row) {
+        int before = 0;
+#pragma unroll 4
+        for (int64_t v = threadIdx.x; v < v0; v += kThreads) {
+            const uint4 x = mask_vector(row, mis, v, limit);
+            before += mask_count(x);
+            bad |= ((x.x | x.y | x.z | x.w) & 0xfefefefeu) != 0;
+        }
+        const int64_t v = v0 + threadIdx.x;
+        const uint4 x = v < vectors ? mask_vector(row, mis, v, limit) : make_uint4(0, 0, 0, 0);
+        bad |= ((x.x | x.y | x.z | x.w) & 0xfefefefeu) != 0;
+        const int own = mask_count(x);
+        int scan = own;
+#pragma unroll
+        for (int m = 1; m < 32; m *= 2) {
+            const int y = __shfl_up_sync(0xffffffffu, scan, m);
+            if (lane >= m) scan += y;
+        }
+        before = __reduce_add_sync(0xffffffffu, before);
+        bad = __any_sync(0xffffffffu, bad);
+        if (lane == 31) s_scan[warp] = scan;
+        if (lane == 0) {
+            s_sum[warp] = before;
+            s_bad[warp] = bad;
+        }
+        __syncthreads();
+        int base = 0;
+        total = 0;
+        bad = false;
+        for (int i = 0; i < kWarps; ++i) {
+            base += s_sum[i] + (i < warp ? s_scan[i] : 0);
+            total += s_sum[i] + s_scan[i];
+            bad |= s_bad[i] != 0;
+        }
+        int rank = base + scan - own;
+        int* out = a.index + static_cast<int64_t>(u) * a.N;
+        const int p = static_cast<int>(16 * v - mis);
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (w[i / 4] >> (8 * (i % 4)) & 1) out[rank++] = p + i;
+        __syncthreads();
+    }
+    if (static_cast<int>(blockIdx.x) != last) return;
+    if (bad) status = kInvalid;
+    if (status == 0 && total > static_cast<int64_t>(a.dst_max_pages) * kPage) status = kTooLarge;
+    if (status) total = 0;
+    bool off = false;
+    for (int j = threadIdx.x; j < (total + kPage - 1) / kPage; j += kThreads)
+        off |= static_cast<unsigned>(a.dst_table[static_cast<int64_t>(u) * a.dst_max_pages + j]) >=
+               static_cast<unsigned>(a.n_pages);
+    if (a.src_table && total)
+        for (int j = threadIdx.x; j < (limit + kPage - 1) / kPage; j += kThreads)
+            off |= static_cast<unsigned>(
+                       a.src_table[static_cast<int64_t>(u) * a.src_max_pages + j]) >=
+                   static_cast<unsigned>(a.n_pages);
+    if (__syncthreads_or(off)) {
+        status = kInvalid;
+        total = 0;
+    }
+    if (threadIdx.x == 0) {
+        a.out_lens[u] = total;
+        if (a.out_status) a.out_status[u] = status;
+    }
+}
+
+// ---------------------------------------------------------------- pages in shared memory
+
+// The page is put together in shared memory and leaves in 16-byte stores.
+template <int D>
+struct PageImage {
+    alignas(16) uint8_t bytes[PageLayout<D>::kBytes];
+    uint32_t slots[kPage * kSlotWords<D>];   // value codes by slot
+};
+
+template <int D>
+__device__ __forceinline__ void put_key(uint8_t* page, int slot, int j, uint32_t word, float scale,
+                                        int zero)
+{
+    using P = PageLayout<D>;
+    *reinterpret_cast<uint32_t*>(page + P::key_word(slot, j)) = word;
+    if (j % 8 == 0)
+        *reinterpret_cast<uint32_t*>(page + P::kKeyGroups + (slot * P::kGroups + j / 8) * 4) =
+            (__float_as_uint(scale) >> 16) | (0xc3000000u + (static_cast<uint32_t>(zero) << 16));
+}
+
+// the group's part of a value row (its codes go elsewhere)
+template <int D>
+__device__ __forceinline__ void put_value_group(uint8_t* page, int slot, int j, float scale,
+                                                int zero)
+{
+    using P = PageLayout<D>;
+    if (j % 8 == 0) {
+        reinterpret_cast<uint16_t*>(page + P::kValScales)[slot * P::kGroups + j / 8] =
+            static_cast<uint16_t>(__float_as_uint(scale) >> 16);
+        reinterpret_cast<uint16_t*>(page + P::kValZeros)[P::val_zero(j / 8, slot)] =
+            static_cast<uint16_t>(0xc300 + zero);
+    }
+}
+
+// the value codes of the page from the slots' words
+template <int D>
+__device__ __forceinline__ void slots_to_page(PageImage<D>& im)
+{
+    uint32_t* codes = reinterpret_cast<uint32_t*>(im.bytes + PageLayout<D>::kValCodes);
+    for (int i = threadIdx.x; i < D; i += kThreads) {
+        const Block8 b(i);
+        uint32_t r[8];
+#pragma unroll
+        for (int n = 0; n < 8; ++n) r[n] = im.slots[b.slot(n) * kSlotWords<D> + b.j];
+        transpose8(r);
+#pragma unroll
+        for (int g = 0; g < 8; ++g) codes[b.word(g)] = r[Block8::nibble(g)];
+    }
+}
+
+template <int D>
+__device__ __forceinline__ void store_page(const PageImage<D>& im, uint8_t* page)
+{
+    constexpr int kVec = PageLayout<D>::kBytes / 16;
+#pragma unroll
+    for (int i = threadIdx.x; i < kVec; i += kThreads)
+        reinterpret_cast<uint4*>(page)[i] = reinterpret_cast<const uint4*>(im.bytes)[i];
+}
+
+// eight values of a row, float32 ones rounded to bf16
+template <typename T>
+struct Values8;
+
+template <>
+struct Values8<uint16_t> {
+    uint4 v = {};
+    __device__ void load(const uint16_t* p) { v = __ldg(reinterpret_cast<const uint4*>(p)); }
+    __device__ void get(float (&x)[8]) const
+    {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = bf16_lo(w[i]);
+            x[2 * i + 1] = bf16_hi(w[i]);
+        }
+    }
+};
+
+template <>
+struct Values8<float> {
+    float4 a = {}, b = {};
+    __device__ void load(const float* p)
+    {
+        a = __ldg(reinterpret_cast<const float4*>(p));
+        b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+    }
+    __device__ void get(float (&x)[8]) const
+    {
+        const float f[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t w = bf16_pair(f[2 * i], f[2 * i + 1]);
+            x[2 * i] = bf16_lo(w);
+            x[2 * i + 1] = bf16_hi(w);
+        }
+    }
+};
+
+// ---------------------------------------------------------------- pack
+
+// A block per page to fill.  D / 8 lanes hold a row, eight values each; a thread loads all of its
+// rows before it rounds the first.
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads) pack_kernel(const PackArgs a)
+{
+    using P = PageLayout<D>;
+    constexpr int kLanes = D / 8, kStep = kThreads / kLanes, kSteps = kPage / kStep;
+    __shared__ PageImage<D> im;
+    wait_for_previous();
+    const int u = blockIdx.y, first = blockIdx.x * kPage;
+    const int count = min(kPage, a.lens[u] - first);
+    if (count <= 0) return;
+    const int j = threadIdx.x % kLanes, s0 = threadIdx.x / kLanes;
+    const T* keys = static_cast<const T*>(a.keys) + static_cast<int64_t>(u) * a.N * D + 8 * j;
+    const T* values = static_cast<const T*>(a.values) + static_cast<int64_t>(u) * a.N * D + 8 * j;
+    const int* index = a.index ? a.index + static_cast<int64_t>(u) * a.N + first : nullptr;
+    int row[kSteps];
+    Values8<T> k[kSteps], v[kSteps];
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+        const int s = s0 + i * kStep;
+        row[i] = s >= count ? -1 : index ? index[s] : first + s;
+    }
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i)
+        if (row[i] >= 0) k[i].load(keys + static_cast<int64_t>(row[i]) * D);
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i)
+        if (row[i] >= 0) v[i].load(values + static_cast<int64_t>(row[i]) * D);
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+        const int s = s0 + i * kStep;
+        float x[8], scale;
+        int zero;
+        k[i].get(x);
+        uint32_t w = quantize8(x, &scale, &zero);
+        put_key<D>(im.bytes, s, j, w, scale, zero);
+        if (j == 0) reinterpret_cast<int*>(im.bytes + P::kPos)[s] = row[i];
+        v[i].get(x);
+        w = quantize8(x, &scale, &zero);
+        im.slots[s * kSlotWords<D> + j] = w;
+        put_value_group<D>(im.bytes, s, j, scale, zero);
+    }
+    __syncthreads();
+    slots_to_page(im);
+    __syncthreads();
+    const int page = a.to.table[static_cast<int64_t>(u) * a.to.max_pages + blockIdx.x];
+    store_page(im, a.to.base + static_cast<int64_t>(page) * P::kBytes);
+}
+
+// ---------------------------------------------------------------- append
+
+constexpr int kAppendMost = kPage;   // new rows of a unit: they reach two pages at most
+
+// A block per unit.  Rows are rounded side by side; the value codes, whose words hold eight
+// slots, are then written word by word, each by one thread, which keeps the other slots' codes.
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads) append_kernel(const AppendArgs a)
+{
+    using P = PageLayout<D>;
+    constexpr int kLanes = D / 8;
+    __shared__ uint32_t slots[kAppendMost * kSlotWords<D>];
+    const int u = blockIdx.x, b = u / a.H, h = u % a.H;
+    const int len = a.lens[u];
+    const int* table = a.to.table + static_cast<int64_t>(u) * a.to.max_pages;
+    int status = len < 0 ? kInvalid
+                 : static_cast<int64_t>(len) + a.n > static_cast<int64_t>(a.to.max_pages) * kPage
+                     ? kTooLarge
+                     : 0;
+    uint8_t* page[2] = {};
+    const int p0 = len / kPage;
+    if (status == 0) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (len + a.n > (p0 + i) * kPage) {
+                const int id = table[p0 + i];
+                if (static_cast<unsigned>(id) >= static_cast<unsigned>(a.to.n_pages))
+                    status = kInvalid;
+                else
+                    page[i] = a.to.base + static_cast<int64_t>(id) * P::kBytes;
+            }
+    }
+    __syncthreads();                 // out_lens may be lens
+    if (threadIdx.x == 0) {
+        a.out_lens[u] = status ? len : len + a.n;
+        if (a.out_status) a.out_status[u] = status;
+    }
+    if (status) return;
+    const int at = len % kPage;      // the first new row's slot of page[0]
+    for (int i0 = 0; i0 < a.n; i0 += kThreads / kLanes) {
+        const int i = i0 + threadIdx.x / kLanes, j = threadIdx.x % kLanes;
+        const bool on = i < a.n;
+        Values8<T> k, v;
+        if (on) {
+            k.load(static_cast<const T*>(a.keys) + b * a.k_batch + i * a.k_token + h * a.k_head +
+                   8 * j);
+            v.load(static_cast<const T*>(a.values) + b * a.v_batch + i * a.v_token +
+                   h * a.v_head + 8 * j);
+        }
+        float x[8], scale;
+        int zero;
+        uint8_t* to = page[(at + i) / kPage ? 1 : 0];
+        const int s = (at + i) % kPage;
+        k.get(x);
+        uint32_t w = quantize8(x, &scale, &zero);
+        if (on) {
+            put_key<D>(to, s, j, w, scale, zero);
+            if (j == 0)
+                reinterpret_cast<int*>(to + P::kPos)[s] =
+                    a.positions[static_cast<int64_t>(b) * a.n + i];
+        }
+        v.get(x);
+        w = quantize8(x, &scale, &zero);
+        if (on) {
+            slots[i * kSlotWords<D> + j] = w;
+            put_value_group<D>(to, s, j, scale, zero);
+        }
+    }
+    __syncthreads();
+    const int blocks = at + a.n > kPage ? 2 * D : D;
+    for (int i = threadIdx.x; i < blocks; i += kThreads) {
+        const Block8 blk(i % D);
+        const int base = (i / D) * kPage - at;   // the page's first slot, counted in new rows
+        uint32_t r[8], fresh = 0;
+#pragma unroll
+        for (int n = 0; n < 8; ++n) {
+            const int row = base + blk.slot(n);
+            r[n] = 0;
+            if (row >= 0 && row < a.n) {
+                r[n] = slots[row * kSlotWords<D> + blk.j];
+                fresh |= 15u << (4 * n);
+            }
+        }
+        if (!fresh) continue;
+        transpose8(r);
+        uint32_t* codes = reinterpret_cast<uint32_t*>(page[i / D] + P::kValCodes);
+#pragma unroll
+        for (int g = 0; g < 8; ++g) {
+            uint32_t* w = codes + blk.word(g);
+            *w = (*w & ~fresh) | r[Block8::nibble(g)];
+        }
+    }
+}
+
+// ---------------------------------------------------------------- compact
+
+// A block per page to fill.  Its slots come from a run of source pages in ascending order (two
+// or three where half of the slots are kept): their value codes are turned to slot order one page
+// per 128 or 64 threads, and only the kept slots' words are put down.
+template <int D>
+__global__ void __launch_bounds__(kThreads) compact_kernel(const CompactArgs a)
+{
+    using P = PageLayout<D>;
+    __shared__ PageImage<D> im;
+    __shared__ int s_src[kPage];             // source slot of each slot
+    __shared__ const uint8_t* s_page[kPage]; // and its page
+    wait_for_previous();
+    const int u = blockIdx.y, first = blockIdx.x * kPage;
+    const int count = min(kPage, a.lens[u] - first);
+    if (count <= 0) return;
+    const int* table = a.from.table + static_cast<int64_t>(u) * a.from.max_pages;
+    if (threadIdx.x < kPage) {
+        const int s = threadIdx.x;
+        int src = -1;
+        const uint8_t* page = nullptr;
+        if (s < count) {
+            src = a.index ? a.index[static_cast<int64_t>(u) * a.N + first + s] : first + s;
+            page = a.from.base + static_cast<int64_t>(table[src / kPage]) * P::kBytes;
+        }
+        s_src[s] = src;
+        s_page[s] = page;
+    }
+    for (int i = threadIdx.x; i < kPage * kSlotWords<D>; i += kThreads) im.slots[i] = 0;
+    __syncthreads();
+    // what is stored by slot
+    constexpr int kVecs = P::kRow / 16;
+    for (int i = threadIdx.x; i < kPage * kVecs; i += kThreads) {
+        const int s = i / kVecs, src = s_src[s] % kPage;
+        uint4 v = {};
+        if (s < count)
+            v = *reinterpret_cast<const uint4*>(s_page[s] + src * P::kRow + i % kVecs * 16);
+        *reinterpret_cast<uint4*>(im.bytes + s * P::kRow + i % kVecs * 16) = v;
+    }
+    if (threadIdx.x < kPage * P::kGroups) {
+        const int s = threadIdx.x / P::kGroups, G = threadIdx.x % P::kGroups;
+        const int src = s_src[s] % kPage;
+        uint32_t kg = 0xc3000000u;
+        uint16_t vs = 0, vz = 0xc300;
+        if (s < count) {
+            const uint8_t* p = s_page[s];
+            kg = reinterpret_cast<const uint32_t*>(p + P::kKeyGroups)[src * P::kGroups + G];
+            vs = reinterpret_cast<const uint16_t*>(p + P::kValScales)[src * P::kGroups + G];
+            vz = reinterpret_cast<const uint16_t*>(p + P::kValZeros)[P::val_zero(G, src)];
+        }
+        reinterpret_cast<uint32_t*>(im.bytes + P::kKeyGroups)[s * P::kGroups + G] = kg;
+        reinterpret_cast<uint16_t*>(im.bytes + P::kValScales)[s * P::kGroups + G] = vs;
+        reinterpret_cast<uint16_t*>(im.bytes + P::kValZeros)[P::val_zero(G, s)] = vz;
+        if (G == 0)
+            reinterpret_cast<int*>(im.bytes + P::kPos)[s] =
+                s < count ? reinterpret_cast<const int*>(s_page[s] + P::kPos)[src] : -1;
+    }
+    // value codes, by source page
+    constexpr int kPagesAtOnce = kThreads / D;
+    const int p0 = s_src[0] / kPage, p1 = s_src[count - 1] / kPage;
+    for (int p = p0 + threadIdx.x / D; p <= p1; p += kPagesAtOnce) {
+        // this page's slots are [lo, hi) of the new one
+        int lo = 0, hi = count;
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (s_src[mid] < p * kPage) lo = mid + 1;
+            else hi = mid;
+        }
+        if (lo >= count || s_src[lo] >= (p + 1) * kPage) continue;
+        const Block8 blk(threadIdx.x % D);
+        const uint32_t* codes = reinterpret_cast<const uint32_t*>(s_page[lo] + P::kValCodes);
+        uint32_t r[8], turned[8];
+#pragma unroll
+        for (int g = 0; g < 8; ++g) turned[Block8::nibble(g)] = codes[blk.word(g)];
+#pragma unroll
+        for (int n = 0; n < 8; ++n) r[n] = turned[n];
+        transpose8(r);                       // r[n]: the word of slot(n)
+        for (int s = lo; s < count && s_src[s] < (p + 1) * kPage; ++s) {
+            const int src = s_src[s] - p * kPage;
+            if (src / 32 != blk.a || src % 8 / 2 != blk.t) continue;
+            const int n = PageLayout<D>::val_nibble(src);
+            uint32_t w = r[0];
+#pragma unroll
+            for (int k = 1; k < 8; ++k) w = n == k ? r[k] : w;
+            im.slots[s * kSlotWords<D> + blk.j] = w;
+        }
+    }
+    __syncthreads();
+    slots_to_page(im);
+    __syncthreads();
+    const int page = a.to.table[static_cast<int64_t>(u) * a.to.max_pages + blockIdx.x];
+    store_page(im, a.to.base + static_cast<int64_t>(page) * P::kBytes);
+}
+
+// ---------------------------------------------------------------- read
+
+// Eight codes as bf16 values s (c - z), one 16-byte store.  The product of the bf16 s and an
+// integer below 16 is exact in float32 and rounded once.
+__device__ __forceinline__ uint4 decode8(uint32_t word, float scale, float neg_zero)
+{
+    uint32_t o[4];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const uint32_t c = code_pair(word, p);
+        o[p] = bf16_pair((bf16_lo(c) + neg_zero) * scale, (bf16_hi(c) + neg_zero) * scale);
+    }
+    return make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+// A block per page that the rows touch.
+template <int D>
+__global__ void __launch_bounds__(kThreads) read_kernel(const ReadArgs a)
+{
+    using P = PageLayout<D>;
+    constexpr int kLanes = D / 8;
+    __shared__ uint32_t slots[kPage * kSlotWords<D>];
+    const int u = blockIdx.y;
+    int len = a.lens[u], status = 0;
+    if (len < 0 || len > static_cast<int64_t>(a.from.max_pages) * kPage) {
+        len = 0;
+        status = kInvalid;
+    }
+    const int first = a.last ? max(0, len - a.rows) : 0;
+    const int64_t end = static_cast<int64_t>(first) + a.rows;         // past the last row's slot
+    const int* table = a.from.table + static_cast<int64_t>(u) * a.from.max_pages;
+    if (blockIdx.x == 0 && a.out_status) {
+        bool off = false;
+        for (int p = first / kPage + threadIdx.x; p * kPage < min(static_cast<int64_t>(len), end);
+             p += kThreads)
+            off |= static_cast<unsigned>(table[p]) >= static_cast<unsigned>(a.from.n_pages);
+        off = __syncthreads_or(off);
+        if (threadIdx.x == 0) a.out_status[u] = off ? kInvalid : status;
+    }
+    const int64_t base = (static_cast<int64_t>(first / kPage) + blockIdx.x) * kPage;
+    if (base >= end) return;
+    const uint8_t* page = nullptr;
+    if (base < len) {
+        const int id = table[base / kPage];
+        if (static_cast<unsigned>(id) < static_cast<unsigned>(a.from.n_pages))
+            page = a.from.base + static_cast<int64_t>(id) * P::kBytes;
+    }
+    if (page)
+        for (int i = threadIdx.x; i < D; i += kThreads) {
+            const Block8 blk(i);
+            const uint32_t* codes = reinterpret_cast<const uint32_t*>(page + P::kValCodes);
+            uint32_t r[8];
+#pragma unroll
+            for (int g = 0; g < 8; ++g) r[Block8::nibble(g)] = codes[blk.word(g)];
+            transpose8(r);
+#pragma unroll
+            for (int n = 0; n < 8; ++n) slots[blk.slot(n) * kSlotWords<D> + blk.j] = r[n];
+        }
+    __syncthreads();
+#pragma unroll 2
+    for (int i = threadIdx.x; i < kPage * kLanes; i += kThreads) {
+        const int s = i / kLanes, j = i % kLanes;
+        const int64_t slot = base + s, row = slot - first;
+        if (row < 0 || row >= a.rows) continue;
+        uint4 k = {}, v = {};
+        const bool held = page && slot < len;
+        if (held) {
+            const uint32_t kg =
+                reinterpret_cast<const uint32_t*>(page + P::kKeyGroups)[s * P::kGroups + j / 8];
+            k = decode8(*reinterpret_cast<const uint32_t*>(page + P::key_word(s, j)), bf16_lo(kg),
+                        bf16_hi(kg));
+            const uint16_t vs =
+                reinterpret_cast<const uint16_t*>(page + P::kValScales)[s * P::kGroups + j / 8];
+            const uint16_t vz =
+                reinterpret_cast<const uint16_t*>(page + P::kValZeros)[P::val_zero(j / 8, s)];
+            v = decode8(slots[s * kSlotWords<D> + j], bf16_lo(vs), bf16_lo(vz));
+        }
+        const int64_t at = (static_cast<int64_t>(u) * a.rows + row) * D + 8 * j;
+        *reinterpret_cast<uint4*>(a.out_keys + at) = k;
+        *reinterpret_cast<uint4*>(a.out_values + at) = v;
+        if (j == 0 && a.out_positions)
+            a.out_positions[static_cast<int64_t>(u) * a.rows + row] =
+                held ? reinterpret_cast<const int*>(page + P::kPos)[s] : -1;
+    }
+}
+
+unsigned pages_of(int64_t slots) { return static_cast<unsigned>((slots + kPage - 1) / kPage); }
+
+}  // namespace
+
+cudaError_t launch_index(const IndexArgs& a, cudaStream_t st)
+{
+    const int64_t vectors = a.mask ? (static_cast<int64_t>(a.N) + 30) / 16 : 1;
+    const dim3 grid(static_cast<unsigned>((vectors + kVecChunk - 1) / kVecChunk), a.units);
+    index_kernel<<<grid, kThreads, 0, st>>>(a);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_pack(const PackArgs& a, int d, bool f32, cudaStream_t st)
+{
+    const dim3 grid(std::min<unsigned>(a.to.max_pages, pages_of(a.N)), a.units);
+    if (d == 128)
+        return f32 ? launch_dependent(pack_kernel<float, 128>, grid, kThreads, 0, st, a)
+                   : launch_dependent(pack_kernel<uint16_t, 128>, grid, kThreads, 0, st, a);
+    return f32 ? launch_dependent(pack_kernel<float, 64>, grid, kThreads, 0, st, a)
+               : launch_dependent(pack_kernel<uint16_t, 64>, grid, kThreads, 0, st, a);
+}
+
+cudaError_t launch_append(const AppendArgs& a, int d, bool f32, cudaStream_t st)
+{
+    const unsigned grid = static_cast<unsigned>(a.B) * a.H;
+    if (d == 128) {
+        if (f32) append_kernel<float, 128><<<grid, kThreads, 0, st>>>(a);
+        else append_kernel<uint16_t, 128><<<grid, kThreads, 0, st>>>(a);
+    } else {
+        if (f32) append_kernel<float, 64><<<grid, kThreads, 0, st>>>(a);
+        else append_kernel<uint16_t, 64><<<grid, kThreads, 0, st>>>(a);
+    }
+    return cudaGetLastError();
+}
+
+cudaError_t launch_compact(const CompactArgs& a, int d, cudaStream_t st)
+{
+    const dim3 grid(std::min<unsigned>(a.to.max_pages, pages_of(a.N)), a.units);
+    return d == 128 ? launch_dependent(compact_kernel<128>, grid, kThreads, 0, st, a)
+                    : launch_dependent(compact_kernel<64>, grid, kThreads, 0, st, a);
+}
+
+cudaError_t launch_read(const ReadArgs& a, int d, cudaStream_t st)
+{
+    // the last rows need not start with a page
+    const dim3 grid(pages_of(a.rows) + (a.last ? 1 : 0), a.units);
+    if (d == 128) read_kernel<128><<<grid, kThreads, 0, st>>>(a);
+    else read_kernel<64><<<grid, kThreads, 0, st>>>(a);
+    return cudaGetLastError();
+}
+
+}  // namespace twk

@@ -1,0 +1,124 @@
+// twk_cache.cuh -- the pages of a cache held in 4 bits: layout, and the rounding of a group of
+// values to codes.
+//
+// A page holds kPage slots of one unit.  Rows (one slot's key or value, D values) are held in
+// groups of 64: per group a bf16 scale s, a zero z in 0..15, and a code c in 0..15 per value,
+// which stands for s (c - z).
+//
+// The layout is the one in which the attention kernel's threads find their operands.  In an
+// m16n8k16 multiplication thread 4 g + t of a warp holds rows g and g + 8 of the left operand, and
+// of each row the columns 2 t, 2 t + 1, 2 t + 8, 2 t + 9 (sums may take the columns in any order,
+// as long as both operands do).
+//   keys     rows are slots, columns are dimensions.  A slot's codes are D / 2 bytes; thread t's
+//            share of them, the dimensions 64 G + 16 t + [0, 16) of every group G, is contiguous.
+//            The 8 codes of a word are pairs (2 p, 2 p + 1) in nibbles p and 4 + p, so that
+//            (word >> 4 p) & 0x000f000f holds a pair in two halves.
+//   values   rows are dimensions, columns are slots: 16 bytes of thread (g, t) hold the dimensions
+//            16 m + g and 16 m + 8 + g of 16 slots each, the 8 codes of a word again as 4 pairs.
+//   zeros    -(128 + z) as bf16: what a code's operand 128 + c (below) has too much.  Beside the
+//            scale for keys; for values in the order of the slots in the operand.
+#pragma once
+#include <cstdint>
+
+namespace twk {
+
+constexpr int kPage = 64;   // slots
+
+template <int D>
+struct PageLayout {
+    static constexpr int kGroups = D / 64;
+    static constexpr int kRow = D / 2;                              // a slot's key codes, bytes
+    static constexpr int kKeyGroups = kPage * kRow;                 // u32 [slot][G]
+    static constexpr int kValCodes = kKeyGroups + kPage * kGroups * 4;
+    static constexpr int kValScales = kValCodes + kPage * kRow;     // bf16 [slot][G]
+    static constexpr int kValZeros = kValScales + kPage * kGroups * 2;
+    static constexpr int kPos = kValZeros + kPage * kGroups * 2;    // int32 [slot]
+    static constexpr int kBytes = kPos + kPage * 4;
+
+    // byte offset of the word with a slot's key dimensions 8 j .. 8 j + 7
+    __host__ __device__ static constexpr int key_word(int slot, int j)
+    {
+        return slot * kRow + (j % 8 / 2) * (8 * kGroups) + (j / 8) * 8 + (j & 1) * 4;
+    }
+    // word (of kValCodes) and nibble of a value
+    __host__ __device__ static constexpr int val_word(int dim, int slot)
+    {
+        return (((dim / 16) * 8 + dim % 8) * 4 + slot % 8 / 2) * 4 + dim % 16 / 8 * 2 + slot / 32;
+    }
+    __host__ __device__ static constexpr int val_nibble(int slot)
+    {
+        return 4 * (slot & 1) + 2 * (slot % 32 / 16) + slot % 16 / 8;
+    }
+    // element of kValZeros
+    __host__ __device__ static constexpr int val_zero(int group, int slot)
+    {
+        return group * kPage + slot % 8 / 2 * 16 + slot / 16 * 4 + slot % 16 / 8 * 2 + (slot & 1);
+    }
+};
+
+// a pair of codes as bf16 numbers 128 + c: the code sits in the last bits of 128's fraction
+__device__ __forceinline__ uint32_t code_pair(uint32_t word, int p)
+{
+    return ((word >> (4 * p)) & 0x000f000fu) | 0x43004300u;
+}
+
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+// f32 -> bf16 bits, nearest even; two values, the first in the low half
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// 8 values of a group as one word of codes (pairs as above), and the group's scale and zero.
+// The lanes l, l ^ 1, l ^ 2, l ^ 4 hold the group's other values.  x: values of bf16 numbers.
+//
+//   lo = min(0, x..), hi = max(0, x..), s = bf16((hi - lo) / 15) (0 below 2^-126),
+//   z = rint(-lo / s), c = min(15, rint(x / s) + z); rint: to nearest, ties to even.
+//
+// The result is that of exact arithmetic, though x / s is computed as x r, r = 1 / s rounded:
+// x and s have 8-bit significands and |x / s| <= 15.06, so x / s is k + 1/2 exactly or more than
+// 2^-10 away from it.  x r is within 2^-19 of x / s.  Adding 12288 in one rounding with the
+// product gives a multiple of 2^-10: a tie becomes a tie again, and nothing else becomes one or
+// crosses one; adding up to 2^23 + 2^22 then rounds to an integer, ties to even.  s: hi - lo is
+// exact in float32 unless the two are 2^15 apart, and then (hi - lo) / 15 is not near a point
+// where the rounding to bf16 turns (15 times such a point has more significant bits than hi).
+// Codes need no lower clamp: rint is odd, and -lo is among the values; NaN and infinities give
+// some code (the & 15).
+__device__ __forceinline__ uint32_t quantize8(const float (&x)[8], float* scale, int* zero)
+{
+    float lo = 0.0f, hi = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        lo = fminf(lo, x[i]);
+        hi = fmaxf(hi, x[i]);
+    }
+#pragma unroll
+    for (int m = 1; m < 8; m *= 2) {
+        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, m));
+        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, m));
+    }
+    float s = __uint_as_float(bf16_pair(__fdiv_rn(hi - lo, 15.0f), 0.0f) << 16);
+    const bool flat = !(s >= 0x1p-126f);
+    s = flat ? 0.0f : s;
+    const float r = flat ? 0.0f : __frcp_rn(s);
+    constexpr float kFine = 12288.0f, kUnit = 12582912.0f;
+    constexpr int kBase = 0x4B400000;   // the bits of kUnit
+    const int z = min(15, __float_as_int(fmaf(-lo, r, kFine) + (kUnit - kFine)) - kBase) & 15;
+    int c[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        c[i] = min(__float_as_int(fmaf(x[i], r, kFine) + (kUnit - kFine)) - kBase + z, 15) & 15;
+    *scale = s;
+    *zero = z;
+    uint32_t w = 0;
+#pragma unroll
+    for (int p = 0; p < 4; ++p)
+        w |= static_cast<uint32_t>(c[2 * p] << (4 * p) | c[2 * p + 1] << (16 + 4 * p));
+    return w;
+}
+
+}  // namespace twk

@@ -10,6 +10,7 @@ Sec. 3.4 (Eq. 4, orphans, donors, the budget-exact swap).
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import functools
 import math
@@ -38,7 +39,13 @@ EXPORTED = (
     "twinkv_repair_host",
     "twinkv_policy", "twinkv_repair_dedup", "twinkv_repair_select_dedup",
     "twinkv_redundancy_symmetric",
+    "twinkv_cache_page_bytes", "twinkv_cache_move_workspace", "twinkv_cache_attend_workspace",
+    "twinkv_qk_norm_rope", "twinkv_cache_pack", "twinkv_cache_append", "twinkv_cache_compact",
+    "twinkv_cache_read", "twinkv_cache_attend",
 )
+PAGE_SLOTS = 64                                 # slots of a page (TWINKV_PAGE_SLOTS)
+PAGE_BYTES = {64: 4864, 128: 9472}              # twinkv_cache_page_bytes by head dimension
+_PAGE_DIM = {v: k for k, v in PAGE_BYTES.items()}
 
 
 class Shape(ctypes.Structure):
@@ -49,6 +56,29 @@ class Shape(ctypes.Structure):
 class Params(ctypes.Structure):
     _fields_ = [("threshold", ctypes.c_float), ("window", ctypes.c_int32),
                 ("n_sink", ctypes.c_int32), ("n_recent", ctypes.c_int32)]
+
+
+class Pool(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_void_p), ("n_pages", ctypes.c_int32), ("d", ctypes.c_int32)]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("tokens", "heads_q", "heads_k", "d", "dtype",
+                                              "rows")] + \
+               [(n, ctypes.c_int64) for n in ("q_token", "q_head", "k_token", "k_head",
+                                              "out_q_token", "out_q_head", "out_k_token",
+                                              "out_k_head")]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "H", "n", "dtype")] + \
+               [(n, ctypes.c_int64) for n in ("k_batch", "k_token", "k_head", "v_batch",
+                                              "v_token", "v_head")]
+
+
+class Queries(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "H", "Hq", "n")] + \
+               [(n, ctypes.c_int64) for n in ("q_batch", "q_token", "q_head")]
 
 
 class TwinKVError(RuntimeError):
@@ -112,6 +142,26 @@ def load(build_if_missing: bool = True):
                                                    ctypes.c_size_t, _P]
         lib.twinkv_policy.argtypes = [_P, Shape, _P, ctypes.c_float, ctypes.POINTER(Params),
                                       _P, _P, _P, _P, ctypes.c_size_t, _P]
+        i32 = ctypes.c_int32
+        lib.twinkv_cache_page_bytes.argtypes = [i32]
+        lib.twinkv_cache_page_bytes.restype = ctypes.c_size_t
+        lib.twinkv_cache_move_workspace.argtypes = [i32, i32]
+        lib.twinkv_cache_move_workspace.restype = ctypes.c_size_t
+        lib.twinkv_cache_attend_workspace.argtypes = [Queries, i32]
+        lib.twinkv_cache_attend_workspace.restype = ctypes.c_size_t
+        lib.twinkv_qk_norm_rope.argtypes = [_P, _P, Heads, _P, _P, ctypes.c_float, _P, _P, _P,
+                                            _P, _P, _P]
+        lib.twinkv_cache_pack.argtypes = [_P, _P, Shape, _P, Pool, _P, i32, _P, _P, _P,
+                                          ctypes.c_size_t, _P]
+        lib.twinkv_cache_append.argtypes = [_P, _P, Rows, _P, Pool, _P, i32, _P, _P, _P, _P]
+        lib.twinkv_cache_compact.argtypes = [Pool, _P, i32, _P, i32, _P, i32, _P, i32, _P, _P,
+                                             _P, ctypes.c_size_t, _P]
+        lib.twinkv_cache_read.argtypes = [Pool, _P, i32, _P, i32, i32, i32, _P, _P, _P, _P, _P]
+        lib.twinkv_cache_attend.argtypes = [_P, Queries, ctypes.c_float, i32, i32, Pool, _P, i32,
+                                            _P, _P, _P, _P, _P, ctypes.c_size_t, _P]
+        for name in ("twinkv_qk_norm_rope", "twinkv_cache_pack", "twinkv_cache_append",
+                     "twinkv_cache_compact", "twinkv_cache_read", "twinkv_cache_attend"):
+            getattr(lib, name).restype = ctypes.c_int
         lib.twinkv_status_string.argtypes = [ctypes.c_int]
         lib.twinkv_status_string.restype = ctypes.c_char_p
         lib.twinkv_set_wait_timeout_ns.argtypes = [ctypes.c_uint64]
@@ -555,6 +605,314 @@ def twinkv_repair_host(keys, retained_mask, budget=None, threshold=None, params=
         _ptr(o.get("twin_all")), _ptr(o["status"]), int(chunk_units), _ptr(arena),
         arena.numel(), _stream(stream))
     _check(st, "twinkv_repair_host")
+    return o
+
+
+# ---- the cache in pages of 4-bit codes --------------------------------------------------
+#
+# What the calls make themselves (outputs that ``out`` does not hold, workspaces) is allocated on
+# the stream they run on.  Tensors that the caller passes must stay alive until that stream is done.
+
+def cache_pool(n_pages: int, d: int, device="cuda") -> torch.Tensor:
+    """A pool of pages for head dimension d: uint8 [n_pages, PAGE_BYTES[d]]."""
+    if d not in PAGE_BYTES:
+        raise ValueError("d must be 64 or 128")
+    return torch.zeros((int(n_pages), PAGE_BYTES[d]), dtype=torch.uint8, device=device)
+
+
+def cache_move_workspace(units: int, N: int, device) -> torch.Tensor:
+    """A workspace for twinkv_cache_pack and twinkv_cache_compact with a mask [units, N]."""
+    n = int(load().twinkv_cache_move_workspace(int(units), int(N)))
+    if n == 0:
+        raise ValueError("invalid number of units or positions")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+@functools.lru_cache(maxsize=1024)
+def _attend_workspace_size(B, n, Hq, H, d) -> int:
+    return int(load().twinkv_cache_attend_workspace(Queries(B, H, Hq, n, 0, 0, 0), d))
+
+
+def cache_attend_workspace(q_shape, H: int, device) -> torch.Tensor:
+    """A workspace for twinkv_cache_attend with queries of q_shape [B, n, Hq, d], H KV heads."""
+    B, n, Hq, d = (int(x) for x in q_shape)
+    size = _attend_workspace_size(B, n, Hq, int(H), d)
+    if size == 0:
+        raise ValueError("unsupported queries")
+    return torch.empty(size, dtype=torch.uint8, device=device)
+
+
+def _on(stream):
+    """Where a call's own tensors are allocated."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _pool(pool):
+    if not isinstance(pool, torch.Tensor):
+        raise TypeError("pool must be a torch tensor")
+    d = _PAGE_DIM.get(pool.shape[-1]) if pool.dim() == 2 else None
+    if d is None:
+        raise ValueError("pool must be [n_pages, PAGE_BYTES[d]]")
+    dev = pool.device
+    _need(pool, "pool", torch.uint8, pool.shape, dev)
+    if dev.index != torch.cuda.current_device():
+        raise ValueError(f"pool must live on the current device, not on {dev}")
+    return Pool(pool.data_ptr(), pool.shape[0], d), d, dev
+
+
+def _table(table, name, units, dev):
+    """A page table [*units, max_pages] and its last size."""
+    if not isinstance(table, torch.Tensor) or table.dim() != len(units) + 1:
+        raise ValueError(f"{name} must be [{', '.join(map(str, units))}, max_pages]")
+    _need(table, name, torch.int32, (*units, table.shape[-1]), dev)
+    return table.shape[-1]
+
+
+def _dense(t, name, dtype, shape, dev):
+    """A tensor of rows: any strides but the last, 16-byte aligned rows."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if t.device != dev or t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{name} must be {dtype} {tuple(shape)} on {dev}, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
+    # a dimension of one has no stride
+    strides = [x if n > 1 else 0 for x, n in zip(t.stride(), shape)]
+    step = 4 if dtype is torch.float32 else 8
+    if t.stride(-1) != 1 or t.data_ptr() % 16 or any(x % step for x in strides[:-1]):
+        raise ValueError(f"{name}'s rows must be contiguous and start on 16-byte boundaries")
+    return strides
+
+
+def _rows_dtype(t, name):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if t.dtype is torch.bfloat16:
+        return BF16
+    if t.dtype is torch.float32:
+        return F32
+    raise ValueError(f"{name} must be bfloat16 or float32")
+
+
+def twinkv_qk_norm_rope(q, k, wq, wk, cos_sin, positions, eps=1e-6, *, out=None,
+                        stream=None) -> dict:
+    """Norms of queries and keys per head and their rotation by position, in one pass.
+
+    q [T,Hq,d] and k [T,H,d], bf16 or float32, any strides that keep rows on 16-byte boundaries
+    (views into a fused projection); either may be None.  wq, wk [d] of the same dtype, or None
+    (no norm).  cos_sin [rows,d] float32, cosines then sines; positions [T] int32.  Returns a
+    dict: q, k (dense unless ``out`` holds tensors with other strides; ``out`` may hold q and k
+    themselves) and status [T] int32 (1 where a position is outside the table; that token is 0).
+    """
+    x = k if q is None else q
+    dtype = _rows_dtype(x, "q" if q is not None else "k")
+    if x.dim() != 3:
+        raise ValueError("q and k must be [T, heads, d]")
+    T, d, dev = x.shape[0], x.shape[2], x.device
+    if dev.type != "cuda" or dev.index != torch.cuda.current_device():
+        raise ValueError(f"tensors must live on the current CUDA device, not on {dev}")
+    o = {}
+    given = out or {}
+    strides, ptrs, heads = [0] * 8, [None] * 4, [0, 0]
+    for i, (t, name) in enumerate(((q, "q"), (k, "k"))):
+        if t is None:
+            continue
+        if t.dim() != 3:
+            raise ValueError("q and k must be [T, heads, d]")
+        heads[i] = t.shape[1]
+        shape = (T, heads[i], d)
+        strides[2 * i], strides[2 * i + 1], _ = _dense(t, name, x.dtype, shape, dev)
+        y = given.get(name)
+        if y is None:
+            with _on(stream):
+                y = torch.empty(shape, dtype=x.dtype, device=dev)
+        strides[4 + 2 * i], strides[5 + 2 * i], _ = _dense(y, f"out {name}", x.dtype, shape, dev)
+        o[name] = y
+        ptrs[i], ptrs[2 + i] = t.data_ptr(), y.data_ptr()
+    for w, name in ((wq, "wq"), (wk, "wk")):
+        if w is not None:
+            _need(w, name, x.dtype, (d,), dev)
+    if not isinstance(cos_sin, torch.Tensor) or cos_sin.dim() != 2:
+        raise ValueError("cos_sin must be [rows, d]")
+    _need(cos_sin, "cos_sin", torch.float32, (cos_sin.shape[0], d), dev)
+    _need(positions, "positions", torch.int32, (T,), dev)
+    with _on(stream):
+        o["status"] = _out(given.get("status"), "status", torch.int32, (T,), dev)
+    s = Heads(T, heads[0], heads[1], d, dtype, cos_sin.shape[0], *strides)
+    st = load().twinkv_qk_norm_rope(ptrs[0], ptrs[1], s, _ptr(wq), _ptr(wk), float(eps),
+                                    cos_sin.data_ptr(), positions.data_ptr(), ptrs[2], ptrs[3],
+                                    o["status"].data_ptr(), _stream(stream))
+    _check(st, "twinkv_qk_norm_rope")
+    return o
+
+
+def _lens_status(out, units, dev, stream):
+    out = out or {}
+    with _on(stream):
+        return {"lens": _out(out.get("lens"), "lens", torch.int32, units, dev),
+                "status": _out(out.get("status"), "status", torch.int32, units, dev)}
+
+
+def _move_ws(ws, units, N, dev, stream):
+    need = units * N * 4
+    if ws is None:
+        with _on(stream):
+            ws = cache_move_workspace(units, N, dev)
+    if not ws.is_cuda or ws.device != dev or ws.dtype != torch.uint8 or ws.numel() < need:
+        raise ValueError(f"workspace must be a uint8 tensor of {need} bytes on {dev}")
+    return ws
+
+
+def twinkv_cache_pack(keys, values, retained_mask, pool, table, *, out=None, ws=None,
+                      stream=None) -> dict:
+    """The retained rows of a dense cache into pages, rounded to 4 bits.
+
+    keys, values [L,H,N,d] bf16 or float32; retained_mask [L,H,N] uint8 or None (every row);
+    pool as cache_pool makes it; table [L,H,max_pages] int32, the pages of each unit.  Returns a
+    dict: lens [L,H] int32 and status [L,H] int32.
+    """
+    s = shape_of(keys)
+    p, d, dev = _pool(pool)
+    _need(keys, "keys", keys.dtype, keys.shape, dev)
+    _need(values, "values", keys.dtype, keys.shape, dev)
+    if s.d != d:
+        raise ValueError(f"the pool's pages hold rows of {d} values, the keys have {s.d}")
+    units = (s.L, s.H)
+    pages = _table(table, "table", units, dev)
+    if retained_mask is not None:
+        _need(retained_mask, "retained_mask", torch.uint8, (s.L, s.H, s.N), dev)
+        ws = _move_ws(ws, s.L * s.H, s.N, dev, stream)
+    o = _lens_status(out, units, dev, stream)
+    st = load().twinkv_cache_pack(
+        keys.data_ptr(), values.data_ptr(), s, _ptr(retained_mask), p, table.data_ptr(), pages,
+        o["lens"].data_ptr(), o["status"].data_ptr(), _ptr(ws), 0 if ws is None else ws.numel(),
+        _stream(stream))
+    _check(st, "twinkv_cache_pack")
+    return o
+
+
+def twinkv_cache_append(k, v, positions, pool, table, lens, *, out=None, stream=None) -> dict:
+    """The rows of new tokens behind each unit's last slot.
+
+    k, v [B,n,H,d] bf16 or float32, any strides that keep rows on 16-byte boundaries; positions
+    [B,n] int32; table [B,H,max_pages]; lens [B,H] int32.  Returns a dict: lens [B,H], the new
+    lengths (``out`` may hold ``lens`` itself), and status [B,H].
+    """
+    p, d, dev = _pool(pool)
+    dtype = _rows_dtype(k, "k")
+    if k.dim() != 4:
+        raise ValueError("k must be [B, n, H, d]")
+    B, n, H, _ = k.shape
+    shape = (B, n, H, d)
+    kb, kt, kh, _ = _dense(k, "k", k.dtype, shape, dev)
+    vb, vt, vh, _ = _dense(v, "v", k.dtype, shape, dev)
+    _need(positions, "positions", torch.int32, (B, n), dev)
+    pages = _table(table, "table", (B, H), dev)
+    _need(lens, "lens", torch.int32, (B, H), dev)
+    o = _lens_status(out, (B, H), dev, stream)
+    st = load().twinkv_cache_append(
+        k.data_ptr(), v.data_ptr(), Rows(B, H, n, dtype, kb, kt, kh, vb, vt, vh),
+        positions.data_ptr(), p, table.data_ptr(), pages, lens.data_ptr(),
+        o["lens"].data_ptr(), o["status"].data_ptr(), _stream(stream))
+    _check(st, "twinkv_cache_append")
+    return o
+
+
+def twinkv_cache_compact(pool, table, lens, keep, new_table, *, out=None, ws=None,
+                         stream=None) -> dict:
+    """The kept slots of each unit into other pages, in order.
+
+    table [...,max_pages] and lens [...] of the units; keep [...,N] uint8 over their slots, N at
+    least the longest, or None (a copy); new_table [...,new_max_pages], pages that no table uses.
+    Returns a dict: lens and status, shaped as ``lens``.
+    """
+    p, _, dev = _pool(pool)
+    if not isinstance(lens, torch.Tensor):
+        raise TypeError("lens must be a torch tensor")
+    units = tuple(lens.shape)
+    _need(lens, "lens", torch.int32, units, dev)
+    pages, new_pages = (_table(table, "table", units, dev),
+                        _table(new_table, "new_table", units, dev))
+    U, N = lens.numel(), pages * PAGE_SLOTS
+    if keep is not None:
+        if not isinstance(keep, torch.Tensor) or keep.dim() != len(units) + 1:
+            raise ValueError("keep must be [units, N]")
+        N = keep.shape[-1]
+        _need(keep, "keep", torch.uint8, (*units, N), dev)
+        ws = _move_ws(ws, U, N, dev, stream)
+    o = _lens_status(out, units, dev, stream)
+    st = load().twinkv_cache_compact(
+        p, table.data_ptr(), pages, lens.data_ptr(), U, _ptr(keep), N, new_table.data_ptr(),
+        new_pages, o["lens"].data_ptr(), o["status"].data_ptr(), _ptr(ws),
+        0 if ws is None else ws.numel(), _stream(stream))
+    _check(st, "twinkv_cache_compact")
+    return o
+
+
+def twinkv_cache_read(pool, table, lens, rows: int, *, last=False, out=None,
+                      stream=None) -> dict:
+    """The first (or last) ``rows`` slots of each unit as bf16 rows.
+
+    table [...,max_pages] and lens [...] of the units.  Returns a dict: keys and values
+    [...,rows,d] bf16, positions [...,rows] int32 (-1, and rows of 0, where there is no slot) and
+    status [...] int32.
+    """
+    p, d, dev = _pool(pool)
+    if not isinstance(lens, torch.Tensor):
+        raise TypeError("lens must be a torch tensor")
+    units, rows, given = tuple(lens.shape), int(rows), out or {}
+    _need(lens, "lens", torch.int32, units, dev)
+    pages = _table(table, "table", units, dev)
+    with _on(stream):
+        o = {"keys": _out(given.get("keys"), "keys", torch.bfloat16, (*units, rows, d), dev),
+             "values": _out(given.get("values"), "values", torch.bfloat16, (*units, rows, d),
+                            dev),
+             "positions": _out(given.get("positions"), "positions", torch.int32, (*units, rows),
+                               dev),
+             "status": _out(given.get("status"), "status", torch.int32, units, dev)}
+    st = load().twinkv_cache_read(
+        p, table.data_ptr(), pages, lens.data_ptr(), lens.numel(), rows, int(bool(last)),
+        o["keys"].data_ptr(), o["values"].data_ptr(), o["positions"].data_ptr(),
+        o["status"].data_ptr(), _stream(stream))
+    _check(st, "twinkv_cache_read")
+    return o
+
+
+def twinkv_cache_attend(q, pool, table, lens, *, scale=None, window=0, n_sink=0, want_lse=False,
+                        out=None, ws=None, stream=None) -> dict:
+    """Attention of each sequence's newest n tokens over its pages (append them first).
+
+    q [B,n,Hq,d] bf16, any strides that keep rows on 16-byte boundaries; table [B,H,max_pages];
+    lens [B,H] int32; scale: d ** -0.5 by default; window > 0: a token sees only the slots whose
+    position is above its own minus ``window``, and those below ``n_sink``.  Returns a dict: out
+    [B,n,Hq,d] bf16, status [B,H] int32 and, with want_lse, lse [B,n,Hq] float32.
+    """
+    p, d, dev = _pool(pool)
+    if not isinstance(q, torch.Tensor) or q.dim() != 4:
+        raise ValueError("q must be [B, n, Hq, d]")
+    B, n, Hq, _ = q.shape
+    qb, qt, qh, _ = _dense(q, "q", torch.bfloat16, (B, n, Hq, d), dev)
+    if not isinstance(lens, torch.Tensor) or lens.dim() != 2:
+        raise ValueError("lens must be [B, H]")
+    H = lens.shape[1]
+    _need(lens, "lens", torch.int32, (B, H), dev)
+    pages = _table(table, "table", (B, H), dev)
+    given = out or {}
+    need = _attend_workspace_size(B, n, Hq, H, d) if H > 0 else 0
+    with _on(stream):
+        o = {"out": _out(given.get("out"), "out", torch.bfloat16, (B, n, Hq, d), dev),
+             "status": _out(given.get("status"), "status", torch.int32, (B, H), dev)}
+        if want_lse:
+            o["lse"] = _out(given.get("lse"), "lse", torch.float32, (B, n, Hq), dev)
+        if ws is None:
+            ws = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
+    if ws.device != dev or ws.dtype != torch.uint8 or ws.numel() < need:
+        raise ValueError(f"workspace must be a uint8 tensor of {need} bytes on {dev}")
+    st = load().twinkv_cache_attend(
+        q.data_ptr(), Queries(B, H, Hq, n, qb, qt, qh), d ** -0.5 if scale is None else scale,
+        int(window), int(n_sink), p, table.data_ptr(), pages, lens.data_ptr(),
+        o["out"].data_ptr(), _ptr(o.get("lse")), o["status"].data_ptr(), ws.data_ptr(),
+        ws.numel(), _stream(stream))
+    _check(st, "twinkv_cache_attend")
     return o
 
 
