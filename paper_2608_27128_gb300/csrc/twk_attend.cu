@@ -89,6 +89,24 @@ __device__ __forceinline__ Visit visit_of(const AttendParams& p, int unit)
     return v;
 }
 
+// floats of a part: outputs, maxima, sums
+template <int D, int NT>
+constexpr int kPartSize = 8 * NT * D + 16 * NT;
+
+// row of out and out_lse
+__device__ __forceinline__ int64_t out_row(const AttendParams& p, int unit, int row)
+{
+    const int b = unit / p.a.H, h = unit % p.a.H;
+    return (static_cast<int64_t>(b) * p.a.n + row / p.a.G) * (p.a.H * p.a.G) + h * p.a.G +
+           row % p.a.G;
+}
+
+// log of the softmax's denominator
+__device__ __forceinline__ float log_sum(const AttendParams& p, float top, float sum)
+{
+    return sum > 0.0f ? top * p.a.scale + logf(sum) : -INFINITY;
+}
+
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -194,6 +212,8 @@ __global__ void __launch_bounds__(32 * Config<D, NT>::kWarps, 1)
     constexpr int G = P::kGroups, M = D / 16;
     constexpr int kRows = 8 * NT;
     extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ int s_pair[C::kWarps], s_slot[C::kWarps];
+    __shared__ bool s_begins[C::kWarps], s_ends[C::kWarps];
     int* chunk_pages = reinterpret_cast<int*>(smem + C::kWarps * C::kRing);
     wait_for_previous();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, g = lane / 4, t = lane % 4;
@@ -224,16 +244,20 @@ __global__ void __launch_bounds__(32 * Config<D, NT>::kWarps, 1)
     }
     __syncthreads();
     const int64_t total = chunk_pages[p.chunks];
-    // every worker has a page; neighbours are on different SMs
-    const int workers = static_cast<int>(min(total, static_cast<int64_t>(gridDim.x) * C::kWarps));
-    const int worker = warp * gridDim.x + blockIdx.x;
-    if (worker >= workers) return;
-    const int64_t begin = total * worker / workers, end = total * (worker + 1) / workers;
-    int todo = static_cast<int>(end - begin);
+    // Blocks, and warps within a block, that have a page each, as even as can be; the spans of a
+    // block's warps follow one another.
+    const int64_t blocks = min(total, static_cast<int64_t>(gridDim.x));
+    const int64_t workers = min(total, static_cast<int64_t>(gridDim.x) * C::kWarps);
+    if (blockIdx.x >= blocks) return;
+    const int64_t index = workers * blockIdx.x / blocks + warp;
+    const bool has_span = index < workers * (blockIdx.x + 1) / blocks;
+    const int worker = blockIdx.x * C::kWarps + warp;
+    const int64_t begin = has_span ? total * index / workers : 0;
+    int todo = has_span ? static_cast<int>(total * (index + 1) / workers - begin) : 0;
 
     // the span's first page
-    Place at;
-    {
+    Place at = {};
+    if (has_span) {
         int lo = 0, hi = p.chunks - 1;       // last chunk that starts at or before `begin`
         while (lo < hi) {
             const int mid = (lo + hi + 1) / 2;
@@ -361,19 +385,10 @@ __global__ void __launch_bounds__(32 * Config<D, NT>::kWarps, 1)
         all_from = seen ? seen[1 + last_token] : 0;
     };
 
-    auto finish_unit = [&]() {
-        const int unit = at.pair / p.parts, r0 = at.pair % p.parts * kRows;
-        const bool whole = seg_begin == 0 && at.j == at.v.count;
-        const int slot = 2 * worker + (first_seg ? 0 : 1);
-        first_seg = false;
-        if (lane == 0) {
-            if (seg_begin == 0) p.spans[at.pair].x = slot;
-            if (at.j == at.v.count) p.spans[at.pair].y = whole ? -1 : worker;
-        }
-        float* part = p.part + static_cast<int64_t>(slot) * (kRows * D + 2 * kRows);
+    // the sums of the lanes that share a row; the zeros' part joins the output
+    auto close_rows = [&]() {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            float inv[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 float s = sum[nt][e];
@@ -381,56 +396,71 @@ __global__ void __launch_bounds__(32 * Config<D, NT>::kWarps, 1)
                 s += __shfl_xor_sync(0xffffffffu, s, 8);
                 s += __shfl_xor_sync(0xffffffffu, s, 16);
                 sum[nt][e] = s;
-                inv[e] = s > 0.0f ? 1.0f / s : 0.0f;
             }
-            if (whole) {
-                const int b = unit / p.a.H, h = unit % p.a.H, r = r0 + 8 * nt + g;
-                const int64_t head =
-                    (static_cast<int64_t>(b) * p.a.n + r / p.a.G) * (p.a.H * p.a.G) + h * p.a.G +
-                    r % p.a.G;
 #pragma unroll
-                for (int m = 0; m < M; ++m)
+            for (int m = 0; m < M; ++m)
 #pragma unroll
-                    for (int e = 0; e < 4; e += 2) {
-                        const float x = o[nt][m][e] + zero_part[nt][m / 4][0];
-                        const float y = o[nt][m][e + 1] + zero_part[nt][m / 4][1];
-                        const uint32_t w = transpose16(bf16_pair(x * inv[0], y * inv[1]));
-                        if (r < p.rows)
-                            *reinterpret_cast<uint32_t*>(p.a.out + head * D + 16 * m + 4 * e +
-                                                         2 * t) = w;
-                    }
-                if (p.a.out_lse && g == 0) {
+                for (int e = 0; e < 4; ++e) o[nt][m][e] += zero_part[nt][m / 4][e % 2];
+        }
+    };
+    // rows as maxima, sums and outputs [kRows][D], [kRows], [kRows]
+    auto put_part = [&](float* part) {
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int row = r0 + 8 * nt + 2 * t + e;
-                        if (row < p.rows)
-                            p.a.out_lse[(static_cast<int64_t>(b) * p.a.n + row / p.a.G) *
-                                            (p.a.H * p.a.G) + h * p.a.G + row % p.a.G] =
-                                sum[nt][e] > 0.0f
-                                    ? top[nt][e] * p.a.scale + logf(sum[nt][e])
-                                    : -INFINITY;
-                    }
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int m = 0; m < M; ++m)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    part[(8 * nt + 2 * t + e % 2) * D + 16 * m + 8 * (e / 2) + g] = o[nt][m][e];
+            if (g == 0) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    part[kRows * D + 8 * nt + 2 * t + e] = top[nt][e];
+                    part[kRows * D + kRows + 8 * nt + 2 * t + e] = sum[nt][e];
                 }
-            } else {
+            }
+        }
+    };
+    // a unit that ends inside the span: written at once if it began there
+    auto finish_unit = [&]() {
+        close_rows();
+        if (seg_begin > 0) {
+            put_part(p.part + static_cast<int64_t>(2 * worker) * kPartSize<D, NT>);
+            if (lane == 0) p.spans[at.pair].y = worker;
+            return;
+        }
+        if (lane == 0) p.spans[at.pair] = make_int2(0, -1);
+        const int r0 = at.pair % p.parts * kRows;
 #pragma unroll
-                for (int m = 0; m < M; ++m)
+        for (int nt = 0; nt < NT; ++nt) {
+            float inv[2];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        part[(8 * nt + 2 * t + e % 2) * D + 16 * m + 8 * (e / 2) + g] =
-                            o[nt][m][e] + zero_part[nt][m / 4][e % 2];
-                if (g == 0) {
+            for (int e = 0; e < 2; ++e) inv[e] = sum[nt][e] > 0.0f ? 1.0f / sum[nt][e] : 0.0f;
+            const int row = r0 + 8 * nt + g;
+            uint16_t* out = p.a.out + out_row(p, at.pair / p.parts, row) * D;
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        part[kRows * D + 8 * nt + 2 * t + e] = top[nt][e];
-                        part[kRows * D + kRows + 8 * nt + 2 * t + e] = sum[nt][e];
-                    }
+            for (int m = 0; m < M; ++m)
+#pragma unroll
+                for (int e = 0; e < 4; e += 2) {
+                    const uint32_t w =
+                        transpose16(bf16_pair(o[nt][m][e] * inv[0], o[nt][m][e + 1] * inv[1]));
+                    if (row < p.rows)
+                        *reinterpret_cast<uint32_t*>(out + 16 * m + 4 * e + 2 * t) = w;
+                }
+            if (p.a.out_lse && g == 0) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int r = r0 + 8 * nt + 2 * t + e;
+                    if (r < p.rows)
+                        p.a.out_lse[out_row(p, at.pair / p.parts, r)] =
+                            log_sum(p, top[nt][e], sum[nt][e]);
                 }
             }
         }
     };
 
-    start_unit();
-    for (int stage = 0;;) {
+    if (todo > 0) start_unit();
+    for (int stage = 0; todo > 0;) {
         const int page = at.j + (at.j < at.v.sink_pages ? 0 : at.v.skip);
         const int base = page * kPage;
         const bool gone = absent >> stage & 1;
@@ -627,9 +657,9 @@ __global__ void __launch_bounds__(32 * Config<D, NT>::kWarps, 1)
         stage = stage + 1 == C::kStages ? 0 : stage + 1;
         ++at.j;
         --todo;
-        if (todo == 0 || at.j == at.v.count) {
+        if (todo > 0 && at.j == at.v.count) {
             finish_unit();
-            if (todo == 0) break;
+            first_seg = false;
             do {
                 ++at.pair;
                 at.v = visit_of(p, at.pair / p.parts);
@@ -638,24 +668,91 @@ __global__ void __launch_bounds__(32 * Config<D, NT>::kWarps, 1)
             start_unit();
         }
     }
+
+    // ---- the spans' last units: the warps of the block that end in the same one join their parts
     cp_async_wait<0>();
+    __syncwarp();
+    if (has_span) {
+        close_rows();
+        put_part(reinterpret_cast<float*>(smem + warp * C::kRing));
+    }
+    if (lane == 0) {
+        s_pair[warp] = has_span ? at.pair : -1;
+        s_slot[warp] = 2 * worker + (first_seg ? 0 : 1);
+        s_begins[warp] = seg_begin == 0;
+        s_ends[warp] = at.j == at.v.count;
+    }
+    __syncthreads();
+    for (int w0 = 0, w1; w0 < C::kWarps && s_pair[w0] >= 0; w0 = w1) {
+        const int pair = s_pair[w0], unit = pair / p.parts, r0 = pair % p.parts * kRows;
+        for (w1 = w0 + 1; w1 < C::kWarps && s_pair[w1] == pair; ++w1) {}
+        const bool begins = s_begins[w0], ends = s_ends[w1 - 1], whole = begins && ends;
+        float* part = p.part + static_cast<int64_t>(s_slot[w0]) * kPartSize<D, NT>;
+        for (int i = threadIdx.x; i < kRows * D / 4; i += 32 * C::kWarps) {
+            const int r = 4 * i / D, x = 4 * i % D;
+            float m = -INFINITY, l = 0.0f;
+            float4 acc = {};
+            for (int w = w0; w < w1; ++w)
+                m = fmaxf(m, reinterpret_cast<const float*>(smem + w * C::kRing)[kRows * D + r]);
+            for (int w = w0; w < w1 && m > -INFINITY; ++w) {
+                const float* from_warp = reinterpret_cast<const float*>(smem + w * C::kRing);
+                const float f = exp2_approx((from_warp[kRows * D + r] - m) * p.c);
+                const float4 y = *reinterpret_cast<const float4*>(from_warp + 4 * i);
+                l = fmaf(from_warp[kRows * D + kRows + r], f, l);
+                acc.x = fmaf(y.x, f, acc.x);
+                acc.y = fmaf(y.y, f, acc.y);
+                acc.z = fmaf(y.z, f, acc.z);
+                acc.w = fmaf(y.w, f, acc.w);
+            }
+            if (!whole) {
+                *reinterpret_cast<float4*>(part + 4 * i) = acc;
+                if (x == 0) {
+                    part[kRows * D + r] = m;
+                    part[kRows * D + kRows + r] = l;
+                }
+            } else if (r0 + r < p.rows) {
+                const int64_t row = out_row(p, unit, r0 + r);
+                const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+                *reinterpret_cast<uint2*>(p.a.out + row * D + x) = make_uint2(
+                    bf16_pair(acc.x * inv, acc.y * inv), bf16_pair(acc.z * inv, acc.w * inv));
+                if (p.a.out_lse && x == 0) p.a.out_lse[row] = log_sum(p, m, l);
+            }
+        }
+        if (threadIdx.x == 0) {
+            if (whole) p.spans[pair] = make_int2(0, -1);
+            if (!whole && begins) p.spans[pair].x = s_slot[w0];
+            if (!whole && ends) p.spans[pair].y = blockIdx.x * C::kWarps + w1 - 1;
+        }
+        // merge_kernel looks at the unit's last worker, whose part is in the run's first one's
+        if (!whole && ends && w1 - w0 > 1)
+            for (int r = threadIdx.x; r < 2 * kRows; r += 32 * C::kWarps)
+                p.part[static_cast<int64_t>(s_slot[w1 - 1]) * kPartSize<D, NT> + kRows * D + r] =
+                    r < kRows ? -INFINITY : 0.0f;
+    }
 }
 
-// One block per (unit, part) pair and row: joins the parts of a unit that several warps took, in
-// the order of its slots, and writes the rows of units without slots.  Block 0 of a unit also
-// checks its length and page numbers.
+// One block per (unit, part) pair and row: joins the parts of a unit that several blocks took, in
+// the order of its slots, and writes the rows of units without slots.  Its parts are those of the
+// warp it begins in, of the first warp of every block after that, and of the warp it ends in.  The
+// warps take them in turn, their sums are added in order.  The first block of a unit also checks
+// its length and page numbers.
+constexpr int kMergeWarps = 4;
+
 template <int D, int NT>
-__global__ void __launch_bounds__(D) merge_kernel(const __grid_constant__ AttendParams p)
+__global__ void __launch_bounds__(32 * kMergeWarps)
+    merge_kernel(const __grid_constant__ AttendParams p)
 {
-    constexpr int kRows = 8 * NT, kSize = kRows * D + 2 * kRows;
+    constexpr int kRows = 8 * NT, kWarps = Config<D, NT>::kWarps, kVec = D / 32;
+    __shared__ float s_acc[kMergeWarps][D];
+    __shared__ float s_top[kMergeWarps], s_sum[kMergeWarps];
     wait_for_previous();
     const int pair = blockIdx.x, unit = pair / p.parts, r = blockIdx.y;
-    const int row = pair % p.parts * kRows + r;
+    const int row = pair % p.parts * kRows + r, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     if (pair % p.parts == 0 && r == 0 && p.a.out_status) {
         const int len = p.a.lens[unit];
         bool bad = len < 0 || len > static_cast<int64_t>(p.a.from.max_pages) * kPage;
         if (!bad)
-            for (int j = threadIdx.x; j * kPage < len; j += D)
+            for (int j = threadIdx.x; j * kPage < len; j += 32 * kMergeWarps)
                 bad |= static_cast<unsigned>(
                            p.a.from.table[static_cast<int64_t>(unit) * p.a.from.max_pages + j]) >=
                        static_cast<unsigned>(p.a.from.n_pages);
@@ -663,30 +760,69 @@ __global__ void __launch_bounds__(D) merge_kernel(const __grid_constant__ Attend
         if (threadIdx.x == 0) p.a.out_status[unit] = bad ? TWINKV_ERR_INVALID_ARG : TWINKV_OK;
     }
     if (row >= p.rows) return;
-    float top = -INFINITY, sum = 0.0f, acc = 0.0f;
+    int n = 0;
+    int2 span = make_int2(0, 0);
     if (visit_of(p, unit).count > 0) {
-        const int2 span = p.spans[pair];
-        if (span.y < 0) return;       // one warp has written it
-        const int first = span.x / 2, n = span.y - first + 1;
-        auto part = [&](int i) {
-            return p.part + static_cast<int64_t>(i == 0 ? span.x : 2 * (first + i)) * kSize;
-        };
-        for (int i = 0; i < n; ++i) top = fmaxf(top, part(i)[kRows * D + r]);
-        if (top > -INFINITY)
-            for (int i = 0; i < n; ++i) {
-                const float* x = part(i);
-                const float f = exp2_approx((x[kRows * D + r] - top) * p.c);
-                sum = fmaf(x[kRows * D + kRows + r], f, sum);
-                acc = fmaf(x[r * D + threadIdx.x], f, acc);
-            }
+        span = p.spans[pair];
+        if (span.y < 0) return;       // written already
+        n = span.y / kWarps - span.x / 2 / kWarps + 1;
     }
-    const int b = unit / p.a.H, h = unit % p.a.H;
-    const int64_t head = (static_cast<int64_t>(b) * p.a.n + row / p.a.G) * (p.a.H * p.a.G) +
-                         h * p.a.G + row % p.a.G;
-    p.a.out[head * D + threadIdx.x] =
-        static_cast<uint16_t>(bf16_pair(sum > 0.0f ? acc / sum : 0.0f, 0.0f));
-    if (p.a.out_lse && threadIdx.x == 0)
-        p.a.out_lse[head] = sum > 0.0f ? top * p.a.scale + logf(sum) : -INFINITY;
+    const bool own_end = n > 0 && span.y % kWarps != 0 && span.y != span.x / 2;
+    const int parts = n + own_end;
+    auto part = [&](int i) {
+        const int slot = i == 0  ? span.x
+                         : i < n ? 2 * kWarps * (span.x / 2 / kWarps + i)
+                                 : 2 * span.y;
+        return p.part + static_cast<int64_t>(slot) * kPartSize<D, NT>;
+    };
+    float top = -INFINITY;
+    for (int i = threadIdx.x; i < parts; i += 32 * kMergeWarps)
+        top = fmaxf(top, part(i)[kRows * D + r]);
+#pragma unroll
+    for (int m = 1; m < 32; m *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
+    if (lane == 0) s_top[warp] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kMergeWarps; ++w) top = fmaxf(top, s_top[w]);
+    float sum = 0.0f, acc[kVec] = {};
+    if (top > -INFINITY) {
+#pragma unroll 4
+        for (int i = warp; i < parts; i += kMergeWarps) {
+            const float* x = part(i);
+            const float m = x[kRows * D + r];
+            if (m == -INFINITY) continue;     // an empty part has no outputs
+            const float f = exp2_approx((m - top) * p.c);
+            sum = fmaf(x[kRows * D + kRows + r], f, sum);
+            float y[kVec];
+            if constexpr (D == 128) {
+                const float4 v = *reinterpret_cast<const float4*>(x + r * D + 4 * lane);
+                y[0] = v.x, y[1] = v.y, y[2] = v.z, y[3] = v.w;
+            } else {
+                const float2 v = *reinterpret_cast<const float2*>(x + r * D + 2 * lane);
+                y[0] = v.x, y[1] = v.y;
+            }
+#pragma unroll
+            for (int k = 0; k < kVec; ++k) acc[k] = fmaf(y[k], f, acc[k]);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kVec; ++k) s_acc[warp][kVec * lane + k] = acc[k];
+    if (lane == 0) s_sum[warp] = sum;
+    __syncthreads();
+    if (threadIdx.x < D / 2) {
+        float a = 0.0f, b = 0.0f;
+        sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kMergeWarps; ++w) {
+            a += s_acc[w][2 * threadIdx.x];
+            b += s_acc[w][2 * threadIdx.x + 1];
+            sum += s_sum[w];
+        }
+        const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+        const int64_t at = out_row(p, unit, row);
+        reinterpret_cast<uint32_t*>(p.a.out + at * D)[threadIdx.x] = bf16_pair(a * inv, b * inv);
+        if (p.a.out_lse && threadIdx.x == 0) p.a.out_lse[at] = log_sum(p, top, sum);
+    }
 }
 
 // ---------------------------------------------------------------- windows
@@ -761,7 +897,8 @@ cudaError_t launch(AttendParams& p, int sms, cudaStream_t st)
     }
     if (e != cudaSuccess) return e;
     return launch_dependent(merge_kernel<D, NT>,
-                            dim3(p.units * p.parts, std::min(p.rows, 8 * NT)), D, 0, st, p);
+                            dim3(p.units * p.parts, std::min(p.rows, 8 * NT)), 32 * kMergeWarps, 0,
+                            st, p);
 }
 
 }  // namespace

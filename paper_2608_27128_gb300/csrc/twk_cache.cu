@@ -431,95 +431,116 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendArgs a)
 // ---------------------------------------------------------------- compact
 
 // A block per page to fill.  Its slots come from a run of source pages in ascending order (two
-// or three where half of the slots are kept): their value codes are turned to slot order one page
-// per 128 or 64 threads, and only the kept slots' words are put down.
+// or three where half of the slots are kept).  Of each source page the kept slots are a 64-bit
+// mask: D threads turn the page's value codes to slot order and put down the words of those in the
+// mask, each behind as many as the mask has before it.
 template <int D>
 __global__ void __launch_bounds__(kThreads) compact_kernel(const CompactArgs a)
 {
     using P = PageLayout<D>;
+    constexpr int kVecs = P::kRow / 16, kPagesAtOnce = kThreads / D;
     __shared__ PageImage<D> im;
-    __shared__ int s_src[kPage];             // source slot of each slot
-    __shared__ const uint8_t* s_page[kPage]; // and its page
+    __shared__ int s_src[kPage];                       // source slot of each slot
+    __shared__ const uint8_t* s_page[kPage];           // and its page
+    __shared__ const uint8_t* s_run_page[kPage];       // the run's pages: where, which slots, and
+    __shared__ unsigned long long s_run_mask[kPage];   // the first slot that they go to
+    __shared__ int s_run_first[kPage];
+    __shared__ unsigned s_changes[2];
     wait_for_previous();
     const int u = blockIdx.y, first = blockIdx.x * kPage;
     const int count = min(kPage, a.lens[u] - first);
     if (count <= 0) return;
     const int* table = a.from.table + static_cast<int64_t>(u) * a.from.max_pages;
+    const int* index = a.index ? a.index + static_cast<int64_t>(u) * a.N + first : nullptr;
+    int src = -1;
+    const uint8_t* page = nullptr;
+    bool change = false;
     if (threadIdx.x < kPage) {
         const int s = threadIdx.x;
-        int src = -1;
-        const uint8_t* page = nullptr;
+        s_run_mask[s] = 0;
         if (s < count) {
-            src = a.index ? a.index[static_cast<int64_t>(u) * a.N + first + s] : first + s;
+            src = index ? index[s] : first + s;
+            const int before = s == 0 ? -1 : index ? index[s - 1] : first + s - 1;
+            change = s == 0 || before / kPage != src / kPage;
             page = a.from.base + static_cast<int64_t>(table[src / kPage]) * P::kBytes;
         }
         s_src[s] = src;
         s_page[s] = page;
+        const unsigned changes = __ballot_sync(0xffffffffu, change);
+        if (s % 32 == 0) s_changes[s / 32] = changes;
     }
     for (int i = threadIdx.x; i < kPage * kSlotWords<D>; i += kThreads) im.slots[i] = 0;
     __syncthreads();
+    const int runs = __popc(s_changes[0]) + __popc(s_changes[1]);
+    if (threadIdx.x < count) {
+        const int s = threadIdx.x;
+        const int run = (s < 32 ? 0 : __popc(s_changes[0])) +
+                        __popc(s_changes[s / 32] & (0xffffffffu >> (31 - s % 32))) - 1;
+        if (change) {
+            s_run_page[run] = page;
+            s_run_first[run] = s;
+        }
+        atomicOr(&s_run_mask[run], 1ull << (src % kPage));
+    }
     // what is stored by slot
-    constexpr int kVecs = P::kRow / 16;
-    for (int i = threadIdx.x; i < kPage * kVecs; i += kThreads) {
-        const int s = i / kVecs, src = s_src[s] % kPage;
-        uint4 v = {};
-        if (s < count)
-            v = *reinterpret_cast<const uint4*>(s_page[s] + src * P::kRow + i % kVecs * 16);
-        *reinterpret_cast<uint4*>(im.bytes + s * P::kRow + i % kVecs * 16) = v;
+    constexpr int kCopies = (kPage * kVecs + kThreads - 1) / kThreads;
+    uint4 copy[kCopies];
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) {
+        const int at = threadIdx.x + i * kThreads, s = at / kVecs;
+        copy[i] = make_uint4(0, 0, 0, 0);
+        if (s < count)                      // count is at most kPage
+            copy[i] = *reinterpret_cast<const uint4*>(s_page[s] + s_src[s] % kPage * P::kRow +
+                                                      at % kVecs * 16);
     }
-    if (threadIdx.x < kPage * P::kGroups) {
-        const int s = threadIdx.x / P::kGroups, G = threadIdx.x % P::kGroups;
-        const int src = s_src[s] % kPage;
-        uint32_t kg = 0xc3000000u;
-        uint16_t vs = 0, vz = 0xc300;
-        if (s < count) {
-            const uint8_t* p = s_page[s];
-            kg = reinterpret_cast<const uint32_t*>(p + P::kKeyGroups)[src * P::kGroups + G];
-            vs = reinterpret_cast<const uint16_t*>(p + P::kValScales)[src * P::kGroups + G];
-            vz = reinterpret_cast<const uint16_t*>(p + P::kValZeros)[P::val_zero(G, src)];
-        }
-        reinterpret_cast<uint32_t*>(im.bytes + P::kKeyGroups)[s * P::kGroups + G] = kg;
-        reinterpret_cast<uint16_t*>(im.bytes + P::kValScales)[s * P::kGroups + G] = vs;
-        reinterpret_cast<uint16_t*>(im.bytes + P::kValZeros)[P::val_zero(G, s)] = vz;
-        if (G == 0)
-            reinterpret_cast<int*>(im.bytes + P::kPos)[s] =
-                s < count ? reinterpret_cast<const int*>(s_page[s] + P::kPos)[src] : -1;
+    uint32_t kg = 0xc3000000u;
+    uint16_t vs = 0, vz = 0xc300;
+    int pos = -1;
+    const int gs = threadIdx.x / P::kGroups, G = threadIdx.x % P::kGroups;
+    if (gs < count) {
+        const uint8_t* p = s_page[gs];
+        const int from = s_src[gs] % kPage;
+        kg = reinterpret_cast<const uint32_t*>(p + P::kKeyGroups)[from * P::kGroups + G];
+        vs = reinterpret_cast<const uint16_t*>(p + P::kValScales)[from * P::kGroups + G];
+        vz = reinterpret_cast<const uint16_t*>(p + P::kValZeros)[P::val_zero(G, from)];
+        pos = reinterpret_cast<const int*>(p + P::kPos)[from];
     }
+    __syncthreads();
     // value codes, by source page
-    constexpr int kPagesAtOnce = kThreads / D;
-    const int p0 = s_src[0] / kPage, p1 = s_src[count - 1] / kPage;
-    for (int p = p0 + threadIdx.x / D; p <= p1; p += kPagesAtOnce) {
-        // this page's slots are [lo, hi) of the new one
-        int lo = 0, hi = count;
-        while (lo < hi) {
-            const int mid = (lo + hi) / 2;
-            if (s_src[mid] < p * kPage) lo = mid + 1;
-            else hi = mid;
-        }
-        if (lo >= count || s_src[lo] >= (p + 1) * kPage) continue;
-        const Block8 blk(threadIdx.x % D);
-        const uint32_t* codes = reinterpret_cast<const uint32_t*>(s_page[lo] + P::kValCodes);
-        uint32_t r[8], turned[8];
+    const Block8 blk(threadIdx.x % D);
+    for (int run = threadIdx.x / D; run < runs; run += kPagesAtOnce) {
+        const uint32_t* codes = reinterpret_cast<const uint32_t*>(s_run_page[run] + P::kValCodes);
+        uint32_t r[8];
 #pragma unroll
-        for (int g = 0; g < 8; ++g) turned[Block8::nibble(g)] = codes[blk.word(g)];
-#pragma unroll
-        for (int n = 0; n < 8; ++n) r[n] = turned[n];
+        for (int g = 0; g < 8; ++g) r[Block8::nibble(g)] = codes[blk.word(g)];
+        const unsigned long long mask = s_run_mask[run];
+        const int at = s_run_first[run];
         transpose8(r);                       // r[n]: the word of slot(n)
-        for (int s = lo; s < count && s_src[s] < (p + 1) * kPage; ++s) {
-            const int src = s_src[s] - p * kPage;
-            if (src / 32 != blk.a || src % 8 / 2 != blk.t) continue;
-            const int n = PageLayout<D>::val_nibble(src);
-            uint32_t w = r[0];
 #pragma unroll
-            for (int k = 1; k < 8; ++k) w = n == k ? r[k] : w;
-            im.slots[s * kSlotWords<D> + blk.j] = w;
+        for (int n = 0; n < 8; ++n) {
+            const unsigned long long bit = 1ull << blk.slot(n);
+            if (mask & bit)
+                im.slots[(at + __popcll(mask & (bit - 1))) * kSlotWords<D> + blk.j] = r[n];
         }
+    }
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) {
+        const int at = threadIdx.x + i * kThreads;
+        if (at < kPage * kVecs)
+            *reinterpret_cast<uint4*>(im.bytes + at / kVecs * P::kRow + at % kVecs * 16) =
+                copy[i];
+    }
+    if (gs < kPage) {
+        reinterpret_cast<uint32_t*>(im.bytes + P::kKeyGroups)[gs * P::kGroups + G] = kg;
+        reinterpret_cast<uint16_t*>(im.bytes + P::kValScales)[gs * P::kGroups + G] = vs;
+        reinterpret_cast<uint16_t*>(im.bytes + P::kValZeros)[P::val_zero(G, gs)] = vz;
+        if (G == 0) reinterpret_cast<int*>(im.bytes + P::kPos)[gs] = pos;
     }
     __syncthreads();
     slots_to_page(im);
     __syncthreads();
-    const int page = a.to.table[static_cast<int64_t>(u) * a.to.max_pages + blockIdx.x];
-    store_page(im, a.to.base + static_cast<int64_t>(page) * P::kBytes);
+    const int to = a.to.table[static_cast<int64_t>(u) * a.to.max_pages + blockIdx.x];
+    store_page(im, a.to.base + static_cast<int64_t>(to) * P::kBytes);
 }
 
 // ---------------------------------------------------------------- read
@@ -569,42 +590,55 @@ __global__ void __launch_bounds__(kThreads) read_kernel(const ReadArgs a)
         if (static_cast<unsigned>(id) < static_cast<unsigned>(a.from.n_pages))
             page = a.from.base + static_cast<int64_t>(id) * P::kBytes;
     }
-    if (page)
-        for (int i = threadIdx.x; i < D; i += kThreads) {
-            const Block8 blk(i);
-            const uint32_t* codes = reinterpret_cast<const uint32_t*>(page + P::kValCodes);
-            uint32_t r[8];
+    // everything is loaded before anything is used
+    constexpr int kItems = kPage * kLanes / kThreads;
+    const int j = threadIdx.x % kLanes, s0 = threadIdx.x / kLanes;
+    const Block8 blk(threadIdx.x % D);
+    uint32_t r[8], kw[kItems] = {}, kg[kItems] = {};
+    uint16_t vs[kItems] = {}, vz[kItems] = {};
+    int pos = -1;
+    const bool turns = page && threadIdx.x < D;
+    if (turns) {
+        const uint32_t* codes = reinterpret_cast<const uint32_t*>(page + P::kValCodes);
 #pragma unroll
-            for (int g = 0; g < 8; ++g) r[Block8::nibble(g)] = codes[blk.word(g)];
-            transpose8(r);
+        for (int g = 0; g < 8; ++g) r[Block8::nibble(g)] = codes[blk.word(g)];
+    }
+    if (page) {
 #pragma unroll
-            for (int n = 0; n < 8; ++n) slots[blk.slot(n) * kSlotWords<D> + blk.j] = r[n];
+        for (int i = 0; i < kItems; ++i) {
+            const int s = s0 + i * (kThreads / kLanes), x = s * P::kGroups + j / 8;
+            kw[i] = *reinterpret_cast<const uint32_t*>(page + P::key_word(s, j));
+            kg[i] = reinterpret_cast<const uint32_t*>(page + P::kKeyGroups)[x];
+            vs[i] = reinterpret_cast<const uint16_t*>(page + P::kValScales)[x];
+            vz[i] = reinterpret_cast<const uint16_t*>(page + P::kValZeros)[P::val_zero(j / 8, s)];
         }
+        if (threadIdx.x < kPage) pos = reinterpret_cast<const int*>(page + P::kPos)[threadIdx.x];
+    }
+    if (turns) {
+        transpose8(r);
+#pragma unroll
+        for (int n = 0; n < 8; ++n) slots[blk.slot(n) * kSlotWords<D> + blk.j] = r[n];
+    }
+    if (threadIdx.x < kPage && a.out_positions) {
+        const int64_t slot = base + threadIdx.x, row = slot - first;
+        if (row >= 0 && row < a.rows)
+            a.out_positions[static_cast<int64_t>(u) * a.rows + row] =
+                page && slot < len ? pos : -1;
+    }
     __syncthreads();
-#pragma unroll 2
-    for (int i = threadIdx.x; i < kPage * kLanes; i += kThreads) {
-        const int s = i / kLanes, j = i % kLanes;
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+        const int s = s0 + i * (kThreads / kLanes);
         const int64_t slot = base + s, row = slot - first;
         if (row < 0 || row >= a.rows) continue;
         uint4 k = {}, v = {};
-        const bool held = page && slot < len;
-        if (held) {
-            const uint32_t kg =
-                reinterpret_cast<const uint32_t*>(page + P::kKeyGroups)[s * P::kGroups + j / 8];
-            k = decode8(*reinterpret_cast<const uint32_t*>(page + P::key_word(s, j)), bf16_lo(kg),
-                        bf16_hi(kg));
-            const uint16_t vs =
-                reinterpret_cast<const uint16_t*>(page + P::kValScales)[s * P::kGroups + j / 8];
-            const uint16_t vz =
-                reinterpret_cast<const uint16_t*>(page + P::kValZeros)[P::val_zero(j / 8, s)];
-            v = decode8(slots[s * kSlotWords<D> + j], bf16_lo(vs), bf16_lo(vz));
+        if (page && slot < len) {
+            k = decode8(kw[i], bf16_lo(kg[i]), bf16_hi(kg[i]));
+            v = decode8(slots[s * kSlotWords<D> + j], bf16_lo(vs[i]), bf16_lo(vz[i]));
         }
         const int64_t at = (static_cast<int64_t>(u) * a.rows + row) * D + 8 * j;
         *reinterpret_cast<uint4*>(a.out_keys + at) = k;
         *reinterpret_cast<uint4*>(a.out_values + at) = v;
-        if (j == 0 && a.out_positions)
-            a.out_positions[static_cast<int64_t>(u) * a.rows + row] =
-                held ? reinterpret_cast<const int*>(page + P::kPos)[s] : -1;
     }
 }
 
