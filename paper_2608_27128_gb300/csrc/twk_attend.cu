@@ -10,20 +10,30 @@
 // Bound by memory: 144 bytes a slot (d = 128) against 512 operations per query row, and a unit has
 // G n rows, 4 to 16 as a rule.  So what a slot costs in instructions counts, and the design is for
 // few of them:
-//   - Codes enter the tensor cores as the bf16 numbers 128 + c (exact), three instructions for two
-//     pairs; nothing is subtracted or scaled per element.  With Q_G the sum of q over a group,
-//         q . k = sum_G s_G (sum q (128 + c) - (128 + z_G) Q_G):
+//   - Key codes enter the tensor cores as f16 bit patterns as they are: a code c in the last bits of a
+//     half is the number c 2^-24, and 16 c one place up, so that a word of 8 codes gives 4 operand
+//     registers in 5 instructions; the query values that meet the second kind are divided by 16.
+//     Queries are scaled by a power of two per row, which leaves them exact.  Nothing is subtracted or
+//     scaled per element: with Q_G the sum of q over a group,
+//         q . k = sum_G s_G (sum q c - z_G Q_G):
 //     the second term is the accumulator's start value, the scale one multiplication per group.
-//     For values the scale goes into the probabilities, P s rounded to bf16 (2^-9 relative, as
-//     large as the output's own rounding, and independent from slot to slot), and the zeros into
-//     one more product with the same rounded numbers, so that no rounding error is multiplied by 128.
+//   - Value codes enter as the bf16 numbers 128 + c (exact; 7 instructions a word), since the
+//     probabilities, which take the slots' scales with them, need bf16's range.  P s is rounded to bf16
+//     (2^-8, the output's own rounding, and independent from slot to slot), and the zeros go
+//     into one more product with the same rounded numbers, so that no rounding is multiplied by 128.
 //   - mma.sync m16n8k16 with the cache as the 16-row operand (slots for keys, dimensions for values)
 //     and up to 8 query rows as the other one: 18 multiplications for 16 slots at d = 128.  With
 //     tcgen05 the cache would have to be written to shared memory again as bf16, four times its
 //     bytes, for a 128-row operand; here codes go from the page to registers to the multiplication.
+//     (e4m3 operands, where a code's byte is c 2^-9 in 3 instructions a word and q a high and a low
+//     part, are taken apart again into f16 by this part's mma.sync: 90 us where f16 takes 82, and up to
+//     twice the time with more rows.)
 //   - A warp works alone: it takes pages in order, keeps the running maxima, sums and outputs of its
 //     rows in registers, and has its pages' bytes copied into its own ring in shared memory (cp.async,
-//     16 bytes a lane), two pages ahead.  No block barrier after the start.
+//     16 bytes a lane), two pages ahead.  No block barrier after the start.  (One bulk copy per half
+//     page and a barrier instead: 92 us where this takes 82; 16 warps with 3 half pages each instead
+//     of 12 with 4: 88.)
+//   Times here: 32 x 8 units of 4k to 16k slots, d = 128, 4 query rows, at successive steps.
 //
 // The pages of all units in one sequence are divided evenly among all warps of the grid, whatever
 // the units' lengths: a warp's span may begin and end inside a unit.  A unit that lies in
@@ -31,6 +41,7 @@
 // output), and merge_kernel joins them in the order of the slots.
 #include <algorithm>
 #include <climits>
+#include <type_traits>
 
 #include "twk_cache.cuh"
 #include "twk_cache_internal.h"
@@ -40,10 +51,11 @@
 namespace twk {
 namespace {
 
-template <int D, int NT>
+// R: query rows of a part (4, 8 or 16), in NT groups of 8 columns.  Column 2 t of a group is row t, and
+// column 2 t + 1 row t + 4: with 4 rows a lane has one of them and no idle second.
+template <int D, int R>
 struct Config {
-    // NT: groups of 8 query rows.  A warp's registers: 32 NT (d = 128) of output, 16 NT of queries,
-    // 32 NT of scores and probabilities.
+    static constexpr int NT = (R + 7) / 8, E = R == 4 ? 1 : 2;   // E: rows of a lane in a group
     static constexpr int kWarps = NT == 1 ? 12 : 8;
     static constexpr int kHalf = PageLayout<D>::kValCodes;        // bytes of a page's keys
     static constexpr int kStages = (NT == 1 ? 2 : 3) * (128 / D); // pages of a warp's ring
@@ -90,8 +102,8 @@ __device__ __forceinline__ Visit visit_of(const AttendParams& p, int unit)
 }
 
 // floats of a part: outputs, maxima, sums
-template <int D, int NT>
-constexpr int kPartSize = 8 * NT * D + 16 * NT;
+template <int D, int R>
+constexpr int kPartSize = Config<D, R>::NT * (8 * D + 16);
 
 // row of out and out_lse
 __device__ __forceinline__ int64_t out_row(const AttendParams& p, int unit, int row)
@@ -129,6 +141,25 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
         "{%8,%9}, {%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// The same with f16 operands.
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
+                                        uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+        "{%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// x and y as f16, x in the low half
+__device__ __forceinline__ uint32_t f16_pair(float x, float y)
+{
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(y), "f"(x));
+    return r;
 }
 
 // 8 x 8 block of 16-bit numbers, thread (g, t) holding row g, columns 2 t and 2 t + 1: transposed
@@ -203,13 +234,13 @@ struct Place {
     Visit v;
 };
 
-template <int D, int NT>
-__global__ void __launch_bounds__(32 * Config<D, NT>::kWarps, 1)
+template <int D, int R>
+__global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
     attend_kernel(const __grid_constant__ AttendParams p)
 {
     using P = PageLayout<D>;
-    using C = Config<D, NT>;
-    constexpr int G = P::kGroups, M = D / 16;
+    using C = Config<D, R>;
+    constexpr int G = P::kGroups, M = D / 16, NT = C::NT, E = C::E;
     constexpr int kRows = 8 * NT;
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ int s_pair[C::kWarps], s_slot[C::kWarps];
@@ -219,31 +250,51 @@ __global__ void __launch_bounds__(32 * Config<D, NT>::kWarps, 1)
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, g = lane / 4, t = lane % 4;
     const int pairs = p.units * p.parts;
 
-    // pages before each chunk of 32 pairs
-    for (int c = warp; c < p.chunks; c += C::kWarps) {
-        const int pair = 32 * c + lane;
-        int n = pair < pairs ? visit_of(p, pair / p.parts).count : 0;
-        n = __reduce_add_sync(0xffffffffu, n);
-        if (lane == 0) chunk_pages[c] = n;
-    }
-    __syncthreads();
-    if (warp == 0) {
-        int before = 0;
-        for (int c0 = 0; c0 < p.chunks; c0 += 32) {
-            const int n = c0 + lane < p.chunks ? chunk_pages[c0 + lane] : 0;
-            int scan = n;
+    int64_t total;
+    // Pages before each chunk of 32 pairs: up to kFewChunks of them by every warp for itself, without
+    // a barrier, more by the block.
+    constexpr int kFewChunks = 8;
+    int few[kFewChunks];
+    if (p.chunks <= kFewChunks) {
 #pragma unroll
-            for (int m = 1; m < 32; m *= 2) {
-                const int y = __shfl_up_sync(0xffffffffu, scan, m);
-                if (lane >= m) scan += y;
-            }
-            if (c0 + lane < p.chunks) chunk_pages[c0 + lane] = before + scan - n;
-            before += __shfl_sync(0xffffffffu, scan, 31);
+        for (int c = 0; c < kFewChunks; ++c) {
+            const int pair = 32 * c + lane;
+            few[c] = pair < pairs ? visit_of(p, pair / p.parts).count : 0;
         }
-        if (lane == 0) chunk_pages[p.chunks] = before;
+        int before = 0;
+#pragma unroll
+        for (int c = 0; c < kFewChunks; ++c) {
+            const int n = __reduce_add_sync(0xffffffffu, few[c]);
+            few[c] = before;
+            before += n;
+        }
+        total = before;
+    } else {
+        for (int c = warp; c < p.chunks; c += C::kWarps) {
+            const int pair = 32 * c + lane;
+            int n = pair < pairs ? visit_of(p, pair / p.parts).count : 0;
+            n = __reduce_add_sync(0xffffffffu, n);
+            if (lane == 0) chunk_pages[c] = n;
+        }
+        __syncthreads();
+        if (warp == 0) {
+            int before = 0;
+            for (int c0 = 0; c0 < p.chunks; c0 += 32) {
+                const int n = c0 + lane < p.chunks ? chunk_pages[c0 + lane] : 0;
+                int scan = n;
+#pragma unroll
+                for (int m = 1; m < 32; m *= 2) {
+                    const int y = __shfl_up_sync(0xffffffffu, scan, m);
+                    if (lane >= m) scan += y;
+                }
+                if (c0 + lane < p.chunks) chunk_pages[c0 + lane] = before + scan - n;
+                before += __shfl_sync(0xffffffffu, scan, 31);
+            }
+            if (lane == 0) chunk_pages[p.chunks] = before;
+        }
+        __syncthreads();
+        total = chunk_pages[p.chunks];
     }
-    __syncthreads();
-    const int64_t total = chunk_pages[p.chunks];
     // Blocks, and warps within a block, that have a page each, as even as can be; the spans of a
     // block's warps follow one another.
     const int64_t blocks = min(total, static_cast<int64_t>(gridDim.x));
@@ -258,11 +309,21 @@ __global__ void __launch_bounds__(32 * Config<D, NT>::kWarps, 1)
     // the span's first page
     Place at = {};
     if (has_span) {
-        int lo = 0, hi = p.chunks - 1;       // last chunk that starts at or before `begin`
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) / 2;
-            if (chunk_pages[mid] <= begin) lo = mid;
-            else hi = mid - 1;
+        int lo = 0, before = 0;              // last chunk that starts at or before `begin`
+        if (p.chunks <= kFewChunks) {
+#pragma unroll
+            for (int c = 1; c < kFewChunks; ++c)
+                if (c < p.chunks && few[c] <= begin) {
+                    lo = c;
+                    before = few[c];
+                }
+        } else {
+            for (int hi = p.chunks - 1; lo < hi;) {
+                const int mid = (lo + hi + 1) / 2;
+                if (chunk_pages[mid] <= begin) lo = mid;
+                else hi = mid - 1;
+            }
+            before = chunk_pages[lo];
         }
         const int pair = 32 * lo + lane;
         const int n = pair < pairs ? visit_of(p, pair / p.parts).count : 0;
@@ -272,7 +333,7 @@ __global__ void __launch_bounds__(32 * Config<D, NT>::kWarps, 1)
             const int y = __shfl_up_sync(0xffffffffu, scan, m);
             if (lane >= m) scan += y;
         }
-        const int rest = static_cast<int>(begin - chunk_pages[lo]);
+        const int rest = static_cast<int>(begin - before);
         const unsigned past = __ballot_sync(0xffffffffu, scan > rest);
         const int l = __ffs(past) - 1;
         at.pair = 32 * lo + l;
@@ -283,18 +344,32 @@ __global__ void __launch_bounds__(32 * Config<D, NT>::kWarps, 1)
     // ---- copies: the page `ahead` is one past those in the ring; its number is already loaded
     Place ahead = at;
     int ahead_todo = todo;
+    const int* ahead_row = p.a.from.table +
+                           static_cast<int64_t>(at.pair / p.parts) * p.a.from.max_pages;
     auto next_id = [&]() -> int {
         if (ahead_todo == 0) return -1;
         --ahead_todo;
-        while (ahead.j >= ahead.v.count) {
-            ++ahead.pair;
-            ahead.v = visit_of(p, ahead.pair / p.parts);
+        if (ahead.j >= ahead.v.count) {
+            do {
+                ++ahead.pair;
+                ahead.v = visit_of(p, ahead.pair / p.parts);
+            } while (ahead.v.count == 0);
             ahead.j = 0;
+            ahead_row = p.a.from.table +
+                        static_cast<int64_t>(ahead.pair / p.parts) * p.a.from.max_pages;
         }
         const int page = ahead.j + (ahead.j < ahead.v.sink_pages ? 0 : ahead.v.skip);
         ++ahead.j;
-        return p.a.from.table[static_cast<int64_t>(ahead.pair / p.parts) * p.a.from.max_pages +
-                              page];
+        return ahead_row[page];
+    };
+    // in registers: an instruction takes one constant of its own, the codes' take two
+    uint32_t code_mask, code_one;
+    asm volatile("mov.u32 %0, 0x000f000f;" : "=r"(code_mask));
+    asm volatile("mov.u32 %0, 0x43004300;" : "=r"(code_one));
+    auto pair_of = [&](uint32_t w, int i) {
+        uint32_t r;
+        asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w >> (4 * i)), "r"(code_mask), "r"(code_one));
+        return r;
     };
     const uint32_t ring = smem_u32(smem + warp * C::kRing);
     auto copy_half = [&](int id, int stage, int half) {
@@ -319,11 +394,11 @@ __global__ void __launch_bounds__(32 * Config<D, NT>::kWarps, 1)
         id = next_id();
     }
 
-    // ---- state of the unit's rows: thread (g, t) has the columns 2 t and 2 t + 1 of every 8 rows
+    // ---- state of the unit's rows: thread (g, t) has the rows t and t + 4 of every 8
     uint32_t q[NT][G][8];
-    float qsum[NT][G][2];
-    float o[NT][M][4], zero_part[NT][G][4], top[NT][2], sum[NT][2];
-    int limit[NT][2], from[NT][2];    // row sees slots < limit that are >= from or < sinks
+    float qsum[NT][G][E], unit_of[NT][E];   // sums of q, and what a score's unit is, see below
+    float o[NT][M][4], zero_part[NT][G][4], top[NT][E], sum[NT][E];
+    int limit[NT][E], from[NT][E];    // row sees slots < limit that are >= from or < sinks
     int sinks = 0, all_limit = 0, all_from = 0;
     int seg_begin = 0;
     bool first_seg = true;
@@ -335,15 +410,17 @@ __global__ void __launch_bounds__(32 * Config<D, NT>::kWarps, 1)
         const int* seen =
             p.seen ? p.seen + static_cast<int64_t>(unit) * (1 + p.a.n) : nullptr;
         sinks = seen ? seen[0] : 0;
-        all_limit = INT_MAX;
-        all_from = 0;
+        // Queries as f16: a row is scaled by a power of two, 2^k, so that its largest value is in
+        // [2^14, 2^15); values down to 2^-28 of it stay exact.  Its scores are sums of 2^(k - 24) q c.
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int r = r0 + 8 * nt + g;
+            const int in_group = g / 2 + g % 2 * 4, r = r0 + 8 * nt + in_group;   // of column g
             const uint16_t* src = nullptr;
-            if (r < p.rows)
+            if (r < p.rows && in_group < R)
                 src = p.a.q + b * p.a.q_batch + r / p.a.G * p.a.q_token +
                       (h * p.a.G + r % p.a.G) * p.a.q_head;
+            uint32_t w[G][8];
+            uint32_t most = 0;
 #pragma unroll
             for (int G_ = 0; G_ < G; ++G_) {
                 uint4 v0 = {}, v1 = {};
@@ -351,32 +428,56 @@ __global__ void __launch_bounds__(32 * Config<D, NT>::kWarps, 1)
                     v0 = *reinterpret_cast<const uint4*>(src + 64 * G_ + 16 * t);
                     v1 = *reinterpret_cast<const uint4*>(src + 64 * G_ + 16 * t + 8);
                 }
-                const uint32_t w[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
+                w[G_][0] = v0.x, w[G_][1] = v0.y, w[G_][2] = v0.z, w[G_][3] = v0.w;
+                w[G_][4] = v1.x, w[G_][5] = v1.y, w[G_][6] = v1.z, w[G_][7] = v1.w;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    most = max(most, max(w[G_][i] & 0x7fffu, w[G_][i] >> 16 & 0x7fffu));
+            }
+            most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+            most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+            // rows of exponents outside [-100, 100] are scaled as those
+            const int exponent = min(max(static_cast<int>(most >> 7) - 127, -100), 100);
+            const float up = __uint_as_float(static_cast<uint32_t>(127 + 14 - exponent) << 23);
+            const float down = __uint_as_float(static_cast<uint32_t>(127 + 10 + exponent) << 23);
+#pragma unroll
+            for (int G_ = 0; G_ < G; ++G_) {
                 float s = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    q[nt][G_][i] = w[i];
-                    s += bf16_lo(w[i]) + bf16_hi(w[i]);
+                    // the odd pairs of a word's codes enter times 16
+                    const float x = bf16_lo(w[G_][i]) * up, y = bf16_hi(w[G_][i]) * up;
+                    const float f = i % 2 ? 0.0625f : 1.0f;
+                    q[nt][G_][i] = f16_pair(x * f, y * f);
+                    s += x + y;
                 }
                 s += __shfl_xor_sync(0xffffffffu, s, 1);
                 s += __shfl_xor_sync(0xffffffffu, s, 2);
-                qsum[nt][G_][0] = __shfl_sync(0xffffffffu, s, 8 * t);
-                qsum[nt][G_][1] = __shfl_sync(0xffffffffu, s, 8 * t + 4);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) zero_part[nt][G_][i] = 0.0f;
+                for (int e = 0; e < E; ++e)
+                    qsum[nt][G_][e] = __shfl_sync(0xffffffffu, s, 8 * t + 4 * e) * 0x1p-24f;
             }
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int row = r0 + 8 * nt + 2 * t + e, token = row / p.a.G;
+            for (int e = 0; e < E; ++e)
+                unit_of[nt][e] = __shfl_sync(0xffffffffu, down, 8 * t + 4 * e);
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const int row = r0 + 8 * nt + 4 * e + t, token = row / p.a.G;
                 limit[nt][e] = row < p.rows ? at.v.len - p.a.n + token + 1 : INT_MAX;
                 from[nt][e] = row < p.rows && seen ? seen[1 + token] : 0;
                 top[nt][e] = -INFINITY;
                 sum[nt][e] = 0.0f;
             }
 #pragma unroll
-            for (int m = 0; m < M; ++m)
+            for (int i = 0; i < 4; ++i) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[nt][m][i] = 0.0f;
+                for (int m = 0; m < M; ++m) o[nt][m][i] = 0.0f;
+#pragma unroll
+                for (int G_ = 0; G_ < G; ++G_) zero_part[nt][G_][i] = 0.0f;
+            }
         }
         // every row of the part: the first token sees least at the end, the last at the window's
         // begin
@@ -390,12 +491,13 @@ __global__ void __launch_bounds__(32 * Config<D, NT>::kWarps, 1)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
+            for (int e = 0; e < E; ++e) {
                 float s = sum[nt][e];
                 s += __shfl_xor_sync(0xffffffffu, s, 4);
                 s += __shfl_xor_sync(0xffffffffu, s, 8);
                 s += __shfl_xor_sync(0xffffffffu, s, 16);
                 sum[nt][e] = s;
+                top[nt][e] *= unit_of[nt][e];
             }
 #pragma unroll
             for (int m = 0; m < M; ++m)
@@ -403,29 +505,31 @@ __global__ void __launch_bounds__(32 * Config<D, NT>::kWarps, 1)
                 for (int e = 0; e < 4; ++e) o[nt][m][e] += zero_part[nt][m / 4][e % 2];
         }
     };
-    // rows as maxima, sums and outputs [kRows][D], [kRows], [kRows]
+    // rows as outputs [kRows][D], maxima and sums [kRows] (rows past the lanes' own: nothing seen)
     auto put_part = [&](float* part) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int m = 0; m < M; ++m)
+            for (int e = 0; e < 2; ++e) {
+                const int r = 8 * nt + 4 * e + t;
+                if (e < E) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    part[(8 * nt + 2 * t + e % 2) * D + 16 * m + 8 * (e / 2) + g] = o[nt][m][e];
-            if (g == 0) {
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    part[kRows * D + 8 * nt + 2 * t + e] = top[nt][e];
-                    part[kRows * D + kRows + 8 * nt + 2 * t + e] = sum[nt][e];
+                    for (int m = 0; m < M; ++m) {
+                        part[r * D + 16 * m + g] = o[nt][m][e];
+                        part[r * D + 16 * m + 8 + g] = o[nt][m][2 + e];
+                    }
+                }
+                if (g == 0) {
+                    part[kRows * D + r] = e < E ? top[nt][e % E] : -INFINITY;
+                    part[kRows * D + kRows + r] = e < E ? sum[nt][e % E] : 0.0f;
                 }
             }
-        }
     };
     // a unit that ends inside the span: written at once if it began there
     auto finish_unit = [&]() {
         close_rows();
         if (seg_begin > 0) {
-            put_part(p.part + static_cast<int64_t>(2 * worker) * kPartSize<D, NT>);
+            put_part(p.part + static_cast<int64_t>(2 * worker) * kPartSize<D, R>);
             if (lane == 0) p.spans[at.pair].y = worker;
             return;
         }
@@ -433,10 +537,10 @@ __global__ void __launch_bounds__(32 * Config<D, NT>::kWarps, 1)
         const int r0 = at.pair % p.parts * kRows;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            float inv[2];
+            float inv[2] = {};
 #pragma unroll
-            for (int e = 0; e < 2; ++e) inv[e] = sum[nt][e] > 0.0f ? 1.0f / sum[nt][e] : 0.0f;
-            const int row = r0 + 8 * nt + g;
+            for (int e = 0; e < E; ++e) inv[e] = sum[nt][e] > 0.0f ? 1.0f / sum[nt][e] : 0.0f;
+            const int row = r0 + 8 * nt + g / 2 + g % 2 * 4;     // of column g
             uint16_t* out = p.a.out + out_row(p, at.pair / p.parts, row) * D;
 #pragma unroll
             for (int m = 0; m < M; ++m)
@@ -449,8 +553,8 @@ __global__ void __launch_bounds__(32 * Config<D, NT>::kWarps, 1)
                 }
             if (p.a.out_lse && g == 0) {
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int r = r0 + 8 * nt + 2 * t + e;
+                for (int e = 0; e < E; ++e) {
+                    const int r = r0 + 8 * nt + 4 * e + t;
                     if (r < p.rows)
                         p.a.out_lse[out_row(p, at.pair / p.parts, r)] =
                             log_sum(p, top[nt][e], sum[nt][e]);
@@ -472,11 +576,11 @@ __global__ void __launch_bounds__(32 * Config<D, NT>::kWarps, 1)
         // ---- scores of 64 slots
         cp_async_wait<2 * C::kStages - 1>();
         __syncwarp();
-        float s[NT][4][4];
+        float s[NT][E][4][2];               // slots g and g + 8 of each tile
 #pragma unroll
         for (int tile = 0; tile < 4; ++tile) {
             const int lo = 16 * tile + g;
-            uint32_t a0[4 * G / 2], a1[4 * G / 2];    // words of slots lo and lo + 8
+            uint32_t a0[2 * G], a1[2 * G];    // words of slots lo and lo + 8
             if constexpr (D == 128) {
                 const uint4 u = lds128(keys + lo * P::kRow + 16 * t);
                 const uint4 w = lds128(keys + (lo + 8) * P::kRow + 16 * t);
@@ -493,34 +597,34 @@ __global__ void __launch_bounds__(32 * Config<D, NT>::kWarps, 1)
             load_groups<D>(keys + P::kKeyGroups + (lo + 8) * 4 * G, k1);
 #pragma unroll
             for (int G_ = 0; G_ < G; ++G_) {
-                float acc[NT][4];
+                float acc[NT][4] = {};       // -z Q at first
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        acc[nt][e] = bf16_hi(k0[G_]) * qsum[nt][G_][e];
-                        acc[nt][2 + e] = bf16_hi(k1[G_]) * qsum[nt][G_][e];
+                    for (int e = 0; e < E; ++e) {
+                        const float all = 128.0f * qsum[nt][G_][e];
+                        acc[nt][e] = fmaf(bf16_hi(k0[G_]), qsum[nt][G_][e], all);
+                        acc[nt][2 + e] = fmaf(bf16_hi(k1[G_]), qsum[nt][G_][e], all);
                     }
 #pragma unroll
                 for (int w = 0; w < 2; ++w)
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        const uint32_t u = a0[2 * G_ + w], v = a1[2 * G_ + w];
-                        const uint32_t r0 = code_pair(u, 2 * x), r1 = code_pair(v, 2 * x);
-                        const uint32_t r2 = code_pair(u, 2 * x + 1), r3 = code_pair(v, 2 * x + 1);
+                        const uint32_t u = a0[2 * G_ + w] >> (8 * x), v = a1[2 * G_ + w] >> (8 * x);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
-                            mma_bf16(acc[nt], r0, r1, r2, r3, q[nt][G_][4 * w + 2 * x],
-                                     q[nt][G_][4 * w + 2 * x + 1]);
+                            mma_f16(acc[nt], u & 0x000f000fu, v & 0x000f000fu, u & 0x00f000f0u,
+                                    v & 0x00f000f0u, q[nt][G_][4 * w + 2 * x],
+                                    q[nt][G_][4 * w + 2 * x + 1]);
                     }
                 const float s0 = bf16_lo(k0[G_]), s1 = bf16_lo(k1[G_]);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float f = e < 2 ? s0 : s1;
-                        s[nt][tile][e] = G_ == 0 ? acc[nt][e] * f
-                                                 : fmaf(acc[nt][e], f, s[nt][tile][e]);
+                    for (int e = 0; e < E; ++e) {
+                        float(&y)[2] = s[nt][e][tile];
+                        y[0] = G_ == 0 ? acc[nt][e] * s0 : fmaf(acc[nt][e], s0, y[0]);
+                        y[1] = G_ == 0 ? acc[nt][2 + e] * s1 : fmaf(acc[nt][2 + e], s1, y[1]);
                     }
             }
         }
@@ -530,87 +634,96 @@ __global__ void __launch_bounds__(32 * Config<D, NT>::kWarps, 1)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int tile = 0; tile < 4; ++tile)
+                for (int e = 0; e < E; ++e)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int slot = base + 16 * tile + 8 * (e / 2) + g;
-                        const bool see = !gone && slot < min(limit[nt][e % 2], at.v.len) &&
-                                         (slot >= from[nt][e % 2] || slot < sinks);
-                        if (!see) s[nt][tile][e] = -INFINITY;
+                    for (int i = 0; i < 8; ++i) {
+                        const int slot = base + 8 * i + g;
+                        const bool see = !gone && slot < min(limit[nt][e], at.v.len) &&
+                                         (slot >= from[nt][e] || slot < sinks);
+                        if (!see) s[nt][e][i / 2][i % 2] = -INFINITY;
                     }
         }
 
         // ---- running maxima; probabilities
         bool grown = false;
-        float shift[NT][2], shrink[NT][2];
+        float shrink[NT][E];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                float m = fmaxf(s[nt][0][e], s[nt][0][2 + e]);
+            for (int e = 0; e < E; ++e) {
+                float(&y)[4][2] = s[nt][e];
+                const float last = top[nt][e], c = p.c * unit_of[nt][e];
+                float m = last;
 #pragma unroll
-                for (int tile = 1; tile < 4; ++tile)
-                    m = fmaxf(m, fmaxf(s[nt][tile][e], s[nt][tile][2 + e]));
+                for (int tile = 0; tile < 4; ++tile) m = fmaxf(m, fmaxf(y[tile][0], y[tile][1]));
                 m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
                 m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
                 m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
-                m = fmaxf(m, top[nt][e]);
-                grown |= m > top[nt][e];
+                grown |= m > last;
                 // a row that has seen nothing yet keeps -inf, and its probabilities are 0
-                shift[nt][e] = m == -INFINITY ? 0.0f : m * p.c;
-                shrink[nt][e] = top[nt][e] == -INFINITY ? 0.0f
-                                                        : exp2_approx((top[nt][e] - m) * p.c);
+                const float shift = m == -INFINITY ? 0.0f : m * c;
+                const float f = last == -INFINITY ? 0.0f : exp2_approx((last - m) * c);
+                shrink[nt][e] = f;
                 top[nt][e] = m;
+                float l = 0.0f;
+#pragma unroll
+                for (int tile = 0; tile < 4; ++tile)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        y[tile][i] = exp2_approx(fmaf(y[tile][i], c, -shift));
+                        l += y[tile][i];
+                    }
+                sum[nt][e] = fmaf(sum[nt][e], f, l);
             }
         if (__any_sync(0xffffffffu, grown)) {
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) sum[nt][e] *= shrink[nt][e];
+                for (int e = 0; e < E; ++e) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                    for (int m = 0; m < M; ++m) {
+                        o[nt][m][e] *= shrink[nt][e];
+                        o[nt][m][2 + e] *= shrink[nt][e];
+                    }
 #pragma unroll
-                    for (int m = 0; m < M; ++m) o[nt][m][i] *= shrink[nt][i % 2];
-#pragma unroll
-                    for (int G_ = 0; G_ < G; ++G_) zero_part[nt][G_][i] *= shrink[nt][i % 2];
+                    for (int G_ = 0; G_ < G; ++G_) {
+                        zero_part[nt][G_][e] *= shrink[nt][e];
+                        zero_part[nt][G_][2 + e] *= shrink[nt][e];
+                    }
                 }
-            }
         }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int tile = 0; tile < 4; ++tile)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float x = exp2_approx(fmaf(s[nt][tile][e], p.c, -shift[nt][e % 2]));
-                    s[nt][tile][e] = x;
-                    sum[nt][e % 2] += x;
-                }
 
         // ---- values
         cp_async_wait<2 * C::kStages - 1>();
         __syncwarp();
         uint32_t prob[NT][4][G][2];      // P s, bf16, slots in the order of the value codes
+        auto weigh = [&](auto masked) {
 #pragma unroll
-        for (int tile = 0; tile < 4; ++tile) {
-            float v0[G], v1[G];
-            load_scales<D>(values + P::kValScales - P::kValCodes + (16 * tile + g) * 2 * G, v0);
-            load_scales<D>(values + P::kValScales - P::kValCodes + (16 * tile + 8 + g) * 2 * G, v1);
+            for (int tile = 0; tile < 4; ++tile) {
+                float v[2][G];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+                for (int i = 0; i < 2; ++i)
+                    load_scales<D>(values + P::kValScales - P::kValCodes +
+                                       (16 * tile + 8 * i + g) * 2 * G, v[i]);
 #pragma unroll
-                for (int G_ = 0; G_ < G; ++G_) {
-                    float x[4];
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        x[e] = s[nt][tile][e] * (e < 2 ? v0[G_] : v1[G_]);
-                        // what an unseen slot holds may be anything
-                        if (!full && s[nt][tile][e] == 0.0f) x[e] = 0.0f;
-                    }
-                    prob[nt][tile][G_][0] = transpose16(bf16_pair(x[0], x[1]));
-                    prob[nt][tile][G_][1] = transpose16(bf16_pair(x[2], x[3]));
-                }
-        }
+                    for (int G_ = 0; G_ < G; ++G_)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            float x[2] = {};        // rows t and t + 4
+#pragma unroll
+                            for (int e = 0; e < E; ++e) {
+                                const float y = s[nt][e][tile][i];
+                                // what an unseen slot holds may be anything
+                                x[e] = decltype(masked)::value && y == 0.0f ? 0.0f : y * v[i][G_];
+                            }
+                            prob[nt][tile][G_][i] = transpose16(bf16_pair(x[0], x[1]));
+                        }
+            }
+        };
+        if (full) weigh(std::false_type{});
+        else weigh(std::true_type{});
 #pragma unroll
         for (int G_ = 0; G_ < G; ++G_)
 #pragma unroll
@@ -639,8 +752,8 @@ __global__ void __launch_bounds__(32 * Config<D, NT>::kWarps, 1)
                 const uint32_t lo = a ? w.y : w.x, hi = a ? w.w : w.z;
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                    const uint32_t r0 = code_pair(lo, 2 * c), r1 = code_pair(hi, 2 * c);
-                    const uint32_t r2 = code_pair(lo, 2 * c + 1), r3 = code_pair(hi, 2 * c + 1);
+                    const uint32_t r0 = pair_of(lo, 2 * c), r1 = pair_of(hi, 2 * c);
+                    const uint32_t r2 = pair_of(lo, 2 * c + 1), r3 = pair_of(hi, 2 * c + 1);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
                         mma_bf16(o[nt][m], r0, r1, r2, r3, prob[nt][2 * a + c][m / 4][0],
@@ -687,7 +800,7 @@ __global__ void __launch_bounds__(32 * Config<D, NT>::kWarps, 1)
         const int pair = s_pair[w0], unit = pair / p.parts, r0 = pair % p.parts * kRows;
         for (w1 = w0 + 1; w1 < C::kWarps && s_pair[w1] == pair; ++w1) {}
         const bool begins = s_begins[w0], ends = s_ends[w1 - 1], whole = begins && ends;
-        float* part = p.part + static_cast<int64_t>(s_slot[w0]) * kPartSize<D, NT>;
+        float* part = p.part + static_cast<int64_t>(s_slot[w0]) * kPartSize<D, R>;
         for (int i = threadIdx.x; i < kRows * D / 4; i += 32 * C::kWarps) {
             const int r = 4 * i / D, x = 4 * i % D;
             float m = -INFINITY, l = 0.0f;
@@ -726,29 +839,31 @@ __global__ void __launch_bounds__(32 * Config<D, NT>::kWarps, 1)
         // merge_kernel looks at the unit's last worker, whose part is in the run's first one's
         if (!whole && ends && w1 - w0 > 1)
             for (int r = threadIdx.x; r < 2 * kRows; r += 32 * C::kWarps)
-                p.part[static_cast<int64_t>(s_slot[w1 - 1]) * kPartSize<D, NT> + kRows * D + r] =
+                p.part[static_cast<int64_t>(s_slot[w1 - 1]) * kPartSize<D, R> + kRows * D + r] =
                     r < kRows ? -INFINITY : 0.0f;
     }
 }
 
 // One block per (unit, part) pair and row: joins the parts of a unit that several blocks took, in
 // the order of its slots, and writes the rows of units without slots.  Its parts are those of the
-// warp it begins in, of the first warp of every block after that, and of the warp it ends in.  The
-// warps take them in turn, their sums are added in order.  The first block of a unit also checks
-// its length and page numbers.
-constexpr int kMergeWarps = 4;
+// warp it begins in, of the first warp of every block after that, and of the warp it ends in.
+// Bound by latency: lengths and spans are read together, then every warp reads four parts at once,
+// maxima, sums and outputs, and joins them as it would pages; the warps' results are joined in order.
+// The last row of blocks checks lengths and page numbers.
+constexpr int kMergeWarps = 4, kMergeParts = 4;
 
-template <int D, int NT>
+template <int D, int R>
 __global__ void __launch_bounds__(32 * kMergeWarps)
     merge_kernel(const __grid_constant__ AttendParams p)
 {
-    constexpr int kRows = 8 * NT, kWarps = Config<D, NT>::kWarps, kVec = D / 32;
+    constexpr int kRows = 8 * Config<D, R>::NT, kWarps = Config<D, R>::kWarps, kVec = D / 32;
     __shared__ float s_acc[kMergeWarps][D];
     __shared__ float s_top[kMergeWarps], s_sum[kMergeWarps];
     wait_for_previous();
     const int pair = blockIdx.x, unit = pair / p.parts, r = blockIdx.y;
     const int row = pair % p.parts * kRows + r, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    if (pair % p.parts == 0 && r == 0 && p.a.out_status) {
+    if (blockIdx.y == gridDim.y - 1) {
+        if (pair % p.parts != 0 || !p.a.out_status) return;
         const int len = p.a.lens[unit];
         bool bad = len < 0 || len > static_cast<int64_t>(p.a.from.max_pages) * kPage;
         if (!bad)
@@ -758,65 +873,77 @@ __global__ void __launch_bounds__(32 * kMergeWarps)
                        static_cast<unsigned>(p.a.from.n_pages);
         bad = __syncthreads_or(bad);
         if (threadIdx.x == 0) p.a.out_status[unit] = bad ? TWINKV_ERR_INVALID_ARG : TWINKV_OK;
+        return;
     }
     if (row >= p.rows) return;
+    const int2 span = p.spans[pair];   // of a unit with pages
     int n = 0;
-    int2 span = make_int2(0, 0);
     if (visit_of(p, unit).count > 0) {
-        span = p.spans[pair];
-        if (span.y < 0) return;       // written already
+        if (span.y < 0) return;        // written already
         n = span.y / kWarps - span.x / 2 / kWarps + 1;
     }
-    const bool own_end = n > 0 && span.y % kWarps != 0 && span.y != span.x / 2;
-    const int parts = n + own_end;
-    auto part = [&](int i) {
-        const int slot = i == 0  ? span.x
-                         : i < n ? 2 * kWarps * (span.x / 2 / kWarps + i)
-                                 : 2 * span.y;
-        return p.part + static_cast<int64_t>(slot) * kPartSize<D, NT>;
-    };
-    float top = -INFINITY;
-    for (int i = threadIdx.x; i < parts; i += 32 * kMergeWarps)
-        top = fmaxf(top, part(i)[kRows * D + r]);
+    const int parts = n + (n > 0 && span.y % kWarps != 0 && span.y != span.x / 2);
+    float top = -INFINITY, sum = 0.0f, acc[kVec] = {};
+    for (int i0 = warp; i0 < parts; i0 += kMergeWarps * kMergeParts) {
+        float m[kMergeParts], l[kMergeParts], y[kMergeParts][kVec];
 #pragma unroll
-    for (int m = 1; m < 32; m *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
-    if (lane == 0) s_top[warp] = top;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kMergeWarps; ++w) top = fmaxf(top, s_top[w]);
-    float sum = 0.0f, acc[kVec] = {};
-    if (top > -INFINITY) {
-#pragma unroll 4
-        for (int i = warp; i < parts; i += kMergeWarps) {
-            const float* x = part(i);
-            const float m = x[kRows * D + r];
-            if (m == -INFINITY) continue;     // an empty part has no outputs
-            const float f = exp2_approx((m - top) * p.c);
-            sum = fmaf(x[kRows * D + kRows + r], f, sum);
-            float y[kVec];
+        for (int k = 0; k < kMergeParts; ++k) {
+            const int i = i0 + k * kMergeWarps;
+            m[k] = -INFINITY;
+            if (i >= parts) continue;
+            const int slot = i == 0  ? span.x
+                             : i < n ? 2 * kWarps * (span.x / 2 / kWarps + i)
+                                     : 2 * span.y;
+            const float* x = p.part + static_cast<int64_t>(slot) * kPartSize<D, R>;
+            m[k] = x[kRows * D + r];
+            l[k] = x[kRows * D + kRows + r];
             if constexpr (D == 128) {
                 const float4 v = *reinterpret_cast<const float4*>(x + r * D + 4 * lane);
-                y[0] = v.x, y[1] = v.y, y[2] = v.z, y[3] = v.w;
+                y[k][0] = v.x, y[k][1] = v.y, y[k][2] = v.z, y[k][3] = v.w;
             } else {
                 const float2 v = *reinterpret_cast<const float2*>(x + r * D + 2 * lane);
-                y[0] = v.x, y[1] = v.y;
+                y[k][0] = v.x, y[k][1] = v.y;
             }
+        }
+        float most = top;
 #pragma unroll
-            for (int k = 0; k < kVec; ++k) acc[k] = fmaf(y[k], f, acc[k]);
+        for (int k = 0; k < kMergeParts; ++k) most = fmaxf(most, m[k]);
+        if (top > -INFINITY) {
+            const float f = exp2_approx((top - most) * p.c);
+            sum *= f;
+#pragma unroll
+            for (int v = 0; v < kVec; ++v) acc[v] *= f;
+        }
+        top = most;
+#pragma unroll
+        for (int k = 0; k < kMergeParts; ++k) {
+            if (m[k] == -INFINITY) continue;       // an empty part has no outputs
+            const float f = exp2_approx((m[k] - top) * p.c);
+            sum = fmaf(l[k], f, sum);
+#pragma unroll
+            for (int v = 0; v < kVec; ++v) acc[v] = fmaf(y[k][v], f, acc[v]);
         }
     }
 #pragma unroll
-    for (int k = 0; k < kVec; ++k) s_acc[warp][kVec * lane + k] = acc[k];
-    if (lane == 0) s_sum[warp] = sum;
+    for (int v = 0; v < kVec; ++v) s_acc[warp][kVec * lane + v] = acc[v];
+    if (lane == 0) {
+        s_top[warp] = top;
+        s_sum[warp] = sum;
+    }
     __syncthreads();
     if (threadIdx.x < D / 2) {
+        top = s_top[0];
+#pragma unroll
+        for (int w = 1; w < kMergeWarps; ++w) top = fmaxf(top, s_top[w]);
         float a = 0.0f, b = 0.0f;
         sum = 0.0f;
 #pragma unroll
         for (int w = 0; w < kMergeWarps; ++w) {
-            a += s_acc[w][2 * threadIdx.x];
-            b += s_acc[w][2 * threadIdx.x + 1];
-            sum += s_sum[w];
+            if (s_top[w] == -INFINITY) continue;
+            const float f = exp2_approx((s_top[w] - top) * p.c);
+            sum = fmaf(s_sum[w], f, sum);
+            a = fmaf(s_acc[w][2 * threadIdx.x], f, a);
+            b = fmaf(s_acc[w][2 * threadIdx.x + 1], f, b);
         }
         const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
         const int64_t at = out_row(p, unit, row);
@@ -875,12 +1002,12 @@ size_t up256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
 int part_rows(int rows) { return rows <= 8 ? 8 : 16; }
 
-template <int D, int NT>
+template <int D, int R>
 cudaError_t launch(AttendParams& p, int sms, cudaStream_t st)
 {
-    using C = Config<D, NT>;
+    using C = Config<D, R>;
     const size_t smem = static_cast<size_t>(C::kWarps) * C::kRing + (p.chunks + 1) * 4;
-    cudaError_t e = cudaFuncSetAttribute(attend_kernel<D, NT>,
+    cudaError_t e = cudaFuncSetAttribute(attend_kernel<D, R>,
                                          cudaFuncAttributeMaxDynamicSharedMemorySize,
                                          static_cast<int>(smem));
     if (e != cudaSuccess) return e;
@@ -890,14 +1017,14 @@ cudaError_t launch(AttendParams& p, int sms, cudaStream_t st)
         window_kernel<D><<<(warps + 3) / 4, 128, 0, st>>>(p.a, p.units,
                                                           const_cast<int*>(p.seen));
         if ((e = cudaGetLastError()) != cudaSuccess) return e;
-        e = launch_dependent(attend_kernel<D, NT>, grid, 32 * C::kWarps, smem, st, p);
+        e = launch_dependent(attend_kernel<D, R>, grid, 32 * C::kWarps, smem, st, p);
     } else {
-        attend_kernel<D, NT><<<grid, 32 * C::kWarps, smem, st>>>(p);
+        attend_kernel<D, R><<<grid, 32 * C::kWarps, smem, st>>>(p);
         e = cudaGetLastError();
     }
     if (e != cudaSuccess) return e;
-    return launch_dependent(merge_kernel<D, NT>,
-                            dim3(p.units * p.parts, std::min(p.rows, 8 * NT)), 32 * kMergeWarps, 0,
+    return launch_dependent(merge_kernel<D, R>,
+                            dim3(p.units * p.parts, std::min(p.rows, 8 * C::NT) + 1), 32 * kMergeWarps, 0,
                             st, p);
 }
 
@@ -907,9 +1034,9 @@ cudaError_t launch(AttendParams& p, int sms, cudaStream_t st)
 size_t attend_workspace(int units, int rows, int n, int d)
 {
     const int pr = part_rows(rows), parts = (rows + pr - 1) / pr;
-    const int warps = kAttendBlocks * (pr == 8 ? Config<128, 1>::kWarps : Config<128, 2>::kWarps);
-    static_assert(Config<64, 1>::kWarps == Config<128, 1>::kWarps &&
-                  Config<64, 2>::kWarps == Config<128, 2>::kWarps);
+    const int warps = kAttendBlocks * (pr == 8 ? Config<128, 8>::kWarps : Config<128, 16>::kWarps);
+    static_assert(Config<64, 8>::kWarps == Config<128, 4>::kWarps &&
+                  Config<64, 16>::kWarps == Config<128, 16>::kWarps);
     return up256(static_cast<size_t>(units) * parts * sizeof(int2)) +
            up256(static_cast<size_t>(units) * (1 + n) * 4) +
            up256(static_cast<size_t>(2) * warps * (pr * d + 2 * pr) * 4);
@@ -931,8 +1058,13 @@ cudaError_t launch_attend(const AttendArgs& a, int sms, cudaStream_t st)
     p.seen = a.window > 0 ? reinterpret_cast<const int*>(ws) : nullptr;
     ws += up256(static_cast<size_t>(p.units) * (1 + a.n) * 4);
     p.part = reinterpret_cast<float*>(ws);
-    if (a.d == 128) return pr == 8 ? launch<128, 1>(p, sms, st) : launch<128, 2>(p, sms, st);
-    return pr == 8 ? launch<64, 1>(p, sms, st) : launch<64, 2>(p, sms, st);
+    if (a.d == 128)
+        return p.rows <= 4   ? launch<128, 4>(p, sms, st)
+               : p.rows <= 8 ? launch<128, 8>(p, sms, st)
+                             : launch<128, 16>(p, sms, st);
+    return p.rows <= 4   ? launch<64, 4>(p, sms, st)
+           : p.rows <= 8 ? launch<64, 8>(p, sms, st)
+                         : launch<64, 16>(p, sms, st);
 }
 
 }  // namespace twk
