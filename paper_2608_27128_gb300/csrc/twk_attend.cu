@@ -40,6 +40,7 @@
 // one span is written at once; of the others each warp writes its part (maximum, sum, unnormalised
 // output), and merge_kernel joins them in the order of the slots.
 #include <algorithm>
+#include <atomic>
 #include <climits>
 #include <type_traits>
 
@@ -1006,11 +1007,18 @@ template <int D, int R>
 cudaError_t launch(AttendParams& p, int sms, cudaStream_t st)
 {
     using C = Config<D, R>;
-    const size_t smem = static_cast<size_t>(C::kWarps) * C::kRing + (p.chunks + 1) * 4;
-    cudaError_t e = cudaFuncSetAttribute(attend_kernel<D, R>,
-                                         cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         static_cast<int>(smem));
+    constexpr int kRings = C::kWarps * C::kRing, kMostChunks = 2048;
+    static std::atomic<bool> allowed[64];     // by device
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
+    if (dev >= 64 || !allowed[dev].load(std::memory_order_relaxed)) {
+        e = cudaFuncSetAttribute(attend_kernel<D, R>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 kRings + (kMostChunks + 1) * 4);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) allowed[dev].store(true, std::memory_order_relaxed);
+    }
+    const size_t smem = kRings + (p.chunks + 1) * 4;
     const dim3 grid(std::min(sms, kAttendBlocks));
     if (p.seen) {
         const int warps = p.units * (1 + p.a.n);

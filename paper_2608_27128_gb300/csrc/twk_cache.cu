@@ -219,11 +219,11 @@ __device__ __forceinline__ void put_value_group(uint8_t* page, int slot, int j, 
 }
 
 // the value codes of the page from the slots' words
-template <int D>
+template <int D, int kBlock>
 __device__ __forceinline__ void slots_to_page(PageImage<D>& im)
 {
     uint32_t* codes = reinterpret_cast<uint32_t*>(im.bytes + PageLayout<D>::kValCodes);
-    for (int i = threadIdx.x; i < D; i += kThreads) {
+    for (int i = threadIdx.x; i < D; i += kBlock) {
         const Block8 b(i);
         uint32_t r[8];
 #pragma unroll
@@ -234,16 +234,16 @@ __device__ __forceinline__ void slots_to_page(PageImage<D>& im)
     }
 }
 
-template <int D>
+template <int D, int kBlock>
 __device__ __forceinline__ void store_page(const PageImage<D>& im, uint8_t* page)
 {
     constexpr int kVec = PageLayout<D>::kBytes / 16;
 #pragma unroll
-    for (int i = threadIdx.x; i < kVec; i += kThreads)
+    for (int i = threadIdx.x; i < kVec; i += kBlock)
         reinterpret_cast<uint4*>(page)[i] = reinterpret_cast<const uint4*>(im.bytes)[i];
 }
 
-// eight values of a row, float32 ones rounded to bf16
+// eight values of a row as bf16 pairs, float32 ones rounded
 template <typename T>
 struct Values8;
 
@@ -251,15 +251,7 @@ template <>
 struct Values8<uint16_t> {
     uint4 v = {};
     __device__ void load(const uint16_t* p) { v = __ldg(reinterpret_cast<const uint4*>(p)); }
-    __device__ void get(float (&x)[8]) const
-    {
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[2 * i] = bf16_lo(w[i]);
-            x[2 * i + 1] = bf16_hi(w[i]);
-        }
-    }
+    __device__ void get(uint32_t (&x)[4]) const { x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w; }
 };
 
 template <>
@@ -270,15 +262,10 @@ struct Values8<float> {
         a = __ldg(reinterpret_cast<const float4*>(p));
         b = __ldg(reinterpret_cast<const float4*>(p) + 1);
     }
-    __device__ void get(float (&x)[8]) const
+    __device__ void get(uint32_t (&x)[4]) const
     {
-        const float f[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t w = bf16_pair(f[2 * i], f[2 * i + 1]);
-            x[2 * i] = bf16_lo(w);
-            x[2 * i + 1] = bf16_hi(w);
-        }
+        x[0] = bf16_pair(a.x, a.y), x[1] = bf16_pair(a.z, a.w);
+        x[2] = bf16_pair(b.x, b.y), x[3] = bf16_pair(b.z, b.w);
     }
 };
 
@@ -316,7 +303,8 @@ __global__ void __launch_bounds__(kThreads) pack_kernel(const PackArgs a)
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
         const int s = s0 + i * kStep;
-        float x[8], scale;
+        uint32_t x[4];
+        float scale;
         int zero;
         k[i].get(x);
         uint32_t w = quantize8(x, &scale, &zero);
@@ -328,10 +316,10 @@ __global__ void __launch_bounds__(kThreads) pack_kernel(const PackArgs a)
         put_value_group<D>(im.bytes, s, j, scale, zero);
     }
     __syncthreads();
-    slots_to_page(im);
+    slots_to_page<D, kThreads>(im);
     __syncthreads();
     const int page = a.to.table[static_cast<int64_t>(u) * a.to.max_pages + blockIdx.x];
-    store_page(im, a.to.base + static_cast<int64_t>(page) * P::kBytes);
+    store_page<D, kThreads>(im, a.to.base + static_cast<int64_t>(page) * P::kBytes);
 }
 
 // ---------------------------------------------------------------- append
@@ -383,7 +371,8 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendArgs a)
             v.load(static_cast<const T*>(a.values) + b * a.v_batch + i * a.v_token +
                    h * a.v_head + 8 * j);
         }
-        float x[8], scale;
+        uint32_t x[4];
+        float scale;
         int zero;
         uint8_t* to = page[(at + i) / kPage ? 1 : 0];
         const int s = (at + i) % kPage;
@@ -433,17 +422,21 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendArgs a)
 // A block per page to fill.  Its slots come from a run of source pages in ascending order (two
 // or three where half of the slots are kept).  Of each source page the kept slots are a 64-bit
 // mask: D threads turn the page's value codes to slot order and put down the words of those in the
-// mask, each behind as many as the mask has before it.
+// mask, each behind as many as the mask has before it.  Blocks of 128 threads, so that many are at
+// different steps on an SM.
+constexpr int kCompactThreads = 128;
+
 template <int D>
-__global__ void __launch_bounds__(kThreads) compact_kernel(const CompactArgs a)
+__global__ void __launch_bounds__(kCompactThreads) compact_kernel(const CompactArgs a)
 {
     using P = PageLayout<D>;
-    constexpr int kVecs = P::kRow / 16, kPagesAtOnce = kThreads / D;
+    constexpr int kVecs = P::kRow / 16, kPagesAtOnce = kCompactThreads / D;
+    static_assert(kPagesAtOnce >= 1 && kCompactThreads >= kPage * P::kGroups);
     __shared__ PageImage<D> im;
-    __shared__ int s_src[kPage];                       // source slot of each slot
-    __shared__ const uint8_t* s_page[kPage];           // and its page
-    __shared__ const uint8_t* s_run_page[kPage];       // the run's pages: where, which slots, and
-    __shared__ unsigned long long s_run_mask[kPage];   // the first slot that they go to
+    __shared__ const uint8_t* s_from[kPage];     // page of each slot, and the slot in it
+    __shared__ uint8_t s_slot[kPage];
+    __shared__ const uint8_t* s_run_page[kPage]; // the run's pages, which of their slots are kept,
+    __shared__ uint32_t s_run_mask[kPage][2];    // and the first slot that they go to
     __shared__ int s_run_first[kPage];
     __shared__ unsigned s_changes[2];
     wait_for_previous();
@@ -452,24 +445,26 @@ __global__ void __launch_bounds__(kThreads) compact_kernel(const CompactArgs a)
     if (count <= 0) return;
     const int* table = a.from.table + static_cast<int64_t>(u) * a.from.max_pages;
     const int* index = a.index ? a.index + static_cast<int64_t>(u) * a.N + first : nullptr;
+    const int to = a.to.table[static_cast<int64_t>(u) * a.to.max_pages + blockIdx.x];
     int src = -1;
     const uint8_t* page = nullptr;
     bool change = false;
     if (threadIdx.x < kPage) {
         const int s = threadIdx.x;
-        s_run_mask[s] = 0;
+        s_run_mask[s][0] = s_run_mask[s][1] = 0;
         if (s < count) {
             src = index ? index[s] : first + s;
             const int before = s == 0 ? -1 : index ? index[s - 1] : first + s - 1;
             change = s == 0 || before / kPage != src / kPage;
             page = a.from.base + static_cast<int64_t>(table[src / kPage]) * P::kBytes;
         }
-        s_src[s] = src;
-        s_page[s] = page;
+        s_from[s] = page;
+        s_slot[s] = static_cast<uint8_t>(src & (kPage - 1));
         const unsigned changes = __ballot_sync(0xffffffffu, change);
         if (s % 32 == 0) s_changes[s / 32] = changes;
     }
-    for (int i = threadIdx.x; i < kPage * kSlotWords<D>; i += kThreads) im.slots[i] = 0;
+    if (count < kPage)
+        for (int i = threadIdx.x; i < kPage * kSlotWords<D>; i += kCompactThreads) im.slots[i] = 0;
     __syncthreads();
     const int runs = __popc(s_changes[0]) + __popc(s_changes[1]);
     if (threadIdx.x < count) {
@@ -480,17 +475,17 @@ __global__ void __launch_bounds__(kThreads) compact_kernel(const CompactArgs a)
             s_run_page[run] = page;
             s_run_first[run] = s;
         }
-        atomicOr(&s_run_mask[run], 1ull << (src % kPage));
+        atomicOr(&s_run_mask[run][src / 32 % 2], 1u << (src % 32));
     }
     // what is stored by slot
-    constexpr int kCopies = (kPage * kVecs + kThreads - 1) / kThreads;
+    constexpr int kCopies = kPage * kVecs / kCompactThreads;
     uint4 copy[kCopies];
 #pragma unroll
     for (int i = 0; i < kCopies; ++i) {
-        const int at = threadIdx.x + i * kThreads, s = at / kVecs;
+        const int at = threadIdx.x + i * kCompactThreads, s = at / kVecs;
         copy[i] = make_uint4(0, 0, 0, 0);
-        if (s < count)                      // count is at most kPage
-            copy[i] = *reinterpret_cast<const uint4*>(s_page[s] + s_src[s] % kPage * P::kRow +
+        if (s < count)
+            copy[i] = *reinterpret_cast<const uint4*>(s_from[s] + s_slot[s] * P::kRow +
                                                       at % kVecs * 16);
     }
     uint32_t kg = 0xc3000000u;
@@ -498,37 +493,45 @@ __global__ void __launch_bounds__(kThreads) compact_kernel(const CompactArgs a)
     int pos = -1;
     const int gs = threadIdx.x / P::kGroups, G = threadIdx.x % P::kGroups;
     if (gs < count) {
-        const uint8_t* p = s_page[gs];
-        const int from = s_src[gs] % kPage;
+        const uint8_t* p = s_from[gs];
+        const int from = s_slot[gs];
         kg = reinterpret_cast<const uint32_t*>(p + P::kKeyGroups)[from * P::kGroups + G];
         vs = reinterpret_cast<const uint16_t*>(p + P::kValScales)[from * P::kGroups + G];
         vz = reinterpret_cast<const uint16_t*>(p + P::kValZeros)[P::val_zero(G, from)];
-        pos = reinterpret_cast<const int*>(p + P::kPos)[from];
+        if (G == 0) pos = reinterpret_cast<const int*>(p + P::kPos)[from];
     }
     __syncthreads();
-    // value codes, by source page
+    // value codes, by source page: the next one's are loaded while one is turned
     const Block8 blk(threadIdx.x % D);
-    for (int run = threadIdx.x / D; run < runs; run += kPagesAtOnce) {
+    uint32_t ahead[8] = {};
+    auto load = [&](int run) {
         const uint32_t* codes = reinterpret_cast<const uint32_t*>(s_run_page[run] + P::kValCodes);
+#pragma unroll
+        for (int g = 0; g < 8; ++g) ahead[Block8::nibble(g)] = codes[blk.word(g)];
+    };
+    int run = threadIdx.x / D;
+    if (run < runs) load(run);
+    for (; run < runs; run += kPagesAtOnce) {
         uint32_t r[8];
 #pragma unroll
-        for (int g = 0; g < 8; ++g) r[Block8::nibble(g)] = codes[blk.word(g)];
-        const unsigned long long mask = s_run_mask[run];
-        const int at = s_run_first[run];
+        for (int n = 0; n < 8; ++n) r[n] = ahead[n];
+        if (run + kPagesAtOnce < runs) load(run + kPagesAtOnce);
+        const uint32_t low = s_run_mask[run][0], mask = blk.a ? s_run_mask[run][1] : low;
+        const int at = s_run_first[run] + (blk.a ? __popc(low) : 0);
         transpose8(r);                       // r[n]: the word of slot(n)
 #pragma unroll
-        for (int n = 0; n < 8; ++n) {
-            const unsigned long long bit = 1ull << blk.slot(n);
-            if (mask & bit)
-                im.slots[(at + __popcll(mask & (bit - 1))) * kSlotWords<D> + blk.j] = r[n];
+        for (int n = 0; n < 4; ++n) {        // slots b and b + 1 of the half page
+            const int b = n / 2 * 16 + n % 2 * 8 + 2 * blk.t;
+            const uint32_t rest = mask >> b;
+            uint32_t* dst = im.slots + (at + __popc(mask & ~(~0u << b))) * kSlotWords<D> + blk.j;
+            if (rest & 1) *dst = r[n];
+            if (rest & 2) dst[(rest & 1) * kSlotWords<D>] = r[n + 4];
         }
     }
 #pragma unroll
     for (int i = 0; i < kCopies; ++i) {
-        const int at = threadIdx.x + i * kThreads;
-        if (at < kPage * kVecs)
-            *reinterpret_cast<uint4*>(im.bytes + at / kVecs * P::kRow + at % kVecs * 16) =
-                copy[i];
+        const int at = threadIdx.x + i * kCompactThreads;
+        *reinterpret_cast<uint4*>(im.bytes + at / kVecs * P::kRow + at % kVecs * 16) = copy[i];
     }
     if (gs < kPage) {
         reinterpret_cast<uint32_t*>(im.bytes + P::kKeyGroups)[gs * P::kGroups + G] = kg;
@@ -537,10 +540,9 @@ __global__ void __launch_bounds__(kThreads) compact_kernel(const CompactArgs a)
         if (G == 0) reinterpret_cast<int*>(im.bytes + P::kPos)[gs] = pos;
     }
     __syncthreads();
-    slots_to_page(im);
+    slots_to_page<D, kCompactThreads>(im);
     __syncthreads();
-    const int to = a.to.table[static_cast<int64_t>(u) * a.to.max_pages + blockIdx.x];
-    store_page(im, a.to.base + static_cast<int64_t>(to) * P::kBytes);
+    store_page<D, kCompactThreads>(im, a.to.base + static_cast<int64_t>(to) * P::kBytes);
 }
 
 // ---------------------------------------------------------------- read
@@ -680,8 +682,8 @@ cudaError_t launch_append(const AppendArgs& a, int d, bool f32, cudaStream_t st)
 cudaError_t launch_compact(const CompactArgs& a, int d, cudaStream_t st)
 {
     const dim3 grid(std::min<unsigned>(a.to.max_pages, pages_of(a.N)), a.units);
-    return d == 128 ? launch_dependent(compact_kernel<128>, grid, kThreads, 0, st, a)
-                    : launch_dependent(compact_kernel<64>, grid, kThreads, 0, st, a);
+    return d == 128 ? launch_dependent(compact_kernel<128>, grid, kCompactThreads, 0, st, a)
+                    : launch_dependent(compact_kernel<64>, grid, kCompactThreads, 0, st, a);
 }
 
 cudaError_t launch_read(const ReadArgs& a, int d, cudaStream_t st)

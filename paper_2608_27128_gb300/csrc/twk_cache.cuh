@@ -73,51 +73,76 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi)
     return r;
 }
 
-// 8 values of a group as one word of codes (pairs as above), and the group's scale and zero.
-// The lanes l, l ^ 1, l ^ 2, l ^ 4 hold the group's other values.  x: values of bf16 numbers.
+// two bf16 numbers at a time; a NaN gives way to a number
+__device__ __forceinline__ uint32_t min_pair(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("min.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ float rcp_approx(float x)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// 8 values of a group (bf16 pairs) as one word of codes (pairs as above), and the group's scale and
+// zero.  The lanes l, l ^ 1, l ^ 2, l ^ 4 hold the group's other values.
 //
 //   lo = min(0, x..), hi = max(0, x..), s = bf16((hi - lo) / 15) (0 below 2^-126),
 //   z = rint(-lo / s), c = min(15, rint(x / s) + z); rint: to nearest, ties to even.
 //
-// The result is that of exact arithmetic, though x / s is computed as x r, r = 1 / s rounded:
-// x and s have 8-bit significands and |x / s| <= 15.06, so x / s is k + 1/2 exactly or more than
-// 2^-10 away from it.  x r is within 2^-19 of x / s.  Adding 12288 in one rounding with the
-// product gives a multiple of 2^-10: a tie becomes a tie again, and nothing else becomes one or
-// crosses one; adding up to 2^23 + 2^22 then rounds to an integer, ties to even.  s: hi - lo is
-// exact in float32 unless the two are 2^15 apart, and then (hi - lo) / 15 is not near a point
-// where the rounding to bf16 turns (15 times such a point has more significant bits than hi).
-// Codes need no lower clamp: rint is odd, and -lo is among the values; NaN and infinities give
-// some code (the & 15).
-__device__ __forceinline__ uint32_t quantize8(const float (&x)[8], float* scale, int* zero)
+// The result is that of exact arithmetic, without a division:
+//   x / s    x and s have 8-bit significands and |x / s| <= 15.06, so x / s is k + 1/2 exactly or more
+//            than 2^-10 away from it.  x r, r about 1 / s, is within 2^-17 of x / s.  Adding 12288 in
+//            one rounding with the product gives a multiple of 2^-10: a tie becomes a tie again, and
+//            nothing else becomes one or crosses one; adding up to 2^23 + 2^22 then rounds to an
+//            integer, ties to even, in the sum's last bits.
+//   s        hi - lo is exact in float32 unless the two are 2^15 apart, and then (hi - lo) / 15 is not
+//            near a point where the rounding to bf16 turns (15 times such a point has more
+//            significant bits than hi).  The quotient is correctly rounded: the product with RN(1 / 15) and
+//            one step with its exact remainder (Markstein 1990).
+// Codes need no lower clamp: rint is odd, and -lo is among the values.
+__device__ __forceinline__ uint32_t quantize8(const uint32_t (&x)[4], float* scale, int* zero)
 {
-    float lo = 0.0f, hi = 0.0f;
+    const uint32_t low = min_pair(min_pair(x[0], x[1]), min_pair(x[2], x[3]));
+    const uint32_t high = max_pair(max_pair(x[0], x[1]), max_pair(x[2], x[3]));
+    // (largest, -smallest) of the lane's values and 0, then of the group's
+    uint32_t ends = max_pair(max_pair(__byte_perm(high, low, 0x5410) ^ 0x80000000u,
+                                      __byte_perm(high, low, 0x7632) ^ 0x80000000u), 0u);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        lo = fminf(lo, x[i]);
-        hi = fmaxf(hi, x[i]);
-    }
-#pragma unroll
-    for (int m = 1; m < 8; m *= 2) {
-        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, m));
-        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, m));
-    }
-    float s = __uint_as_float(bf16_pair(__fdiv_rn(hi - lo, 15.0f), 0.0f) << 16);
+    for (int m = 1; m < 8; m *= 2) ends = max_pair(ends, __shfl_xor_sync(0xffffffffu, ends, m));
+    const float up = bf16_lo(ends), down = bf16_hi(ends), range = up + down;
+    constexpr float kFifteenth = 1.0f / 15.0f;
+    const float q = range * kFifteenth;
+    float s = fmaf(fmaf(-15.0f, q, range), kFifteenth, q);
+    s = bf16_hi(bf16_pair(0.0f, s));
     const bool flat = !(s >= 0x1p-126f);
     s = flat ? 0.0f : s;
-    const float r = flat ? 0.0f : __frcp_rn(s);
+    const float r = flat ? 0.0f : rcp_approx(s);
     constexpr float kFine = 12288.0f, kUnit = 12582912.0f;
-    constexpr int kBase = 0x4B400000;   // the bits of kUnit
-    const int z = min(15, __float_as_int(fmaf(-lo, r, kFine) + (kUnit - kFine)) - kBase) & 15;
-    int c[8];
+    constexpr uint32_t kBase = 0x4B400000u;   // the bits of kUnit
+    auto rounded = [&](float v) {             // kBase + rint(v / s)
+        return __float_as_int(fmaf(v, r, kFine) + (kUnit - kFine));
+    };
+    const int z = min(static_cast<int>(rounded(down) - kBase), 15) & 15;
+    const int most = static_cast<int>(kBase) + 15 - z;
+    // codes are the sums' last bits less kBase, plus z: taken off all eight at once
+    uint32_t w = (z - kBase) * 0x11111111u;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        c[i] = min(__float_as_int(fmaf(x[i], r, kFine) + (kUnit - kFine)) - kBase + z, 15) & 15;
+    for (int p = 0; p < 4; ++p) {
+        w += static_cast<uint32_t>(min(rounded(bf16_lo(x[p])), most)) << (4 * p);
+        w += static_cast<uint32_t>(min(rounded(bf16_hi(x[p])), most)) << (16 + 4 * p);
+    }
     *scale = s;
     *zero = z;
-    uint32_t w = 0;
-#pragma unroll
-    for (int p = 0; p < 4; ++p)
-        w |= static_cast<uint32_t>(c[2 * p] << (4 * p) | c[2 * p + 1] << (16 + 4 * p));
     return w;
 }
 

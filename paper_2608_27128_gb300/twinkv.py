@@ -10,7 +10,6 @@ Sec. 3.4 (Eq. 4, orphans, donors, the budget-exact swap).
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import functools
 import math
@@ -197,7 +196,8 @@ def _ptr(t):
 
 def _stream(stream):
     if stream is None:
-        stream = torch.cuda.current_stream()
+        # torch.cuda.current_stream().cuda_stream without the Stream object (1.5 us less a call)
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream.cuda_stream
 
 
@@ -642,55 +642,112 @@ def cache_attend_workspace(q_shape, H: int, device) -> torch.Tensor:
     return torch.empty(size, dtype=torch.uint8, device=device)
 
 
-def _on(stream):
-    """Where a call's own tensors are allocated."""
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+# The checks of a call with small tensors cost as much as its kernels, so what depends on types,
+# shapes and strides alone is checked once per combination (the cached functions below), and the
+# rest in as few steps as it takes.
+
+def _same(t, name, dtype, shape, dev: int):
+    """A contiguous tensor of the given type and shape on CUDA device number `dev`."""
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape
+            and t.get_device() == dev and t.is_contiguous()):
+        return t
+    return _need(t, name, dtype, shape, torch.device("cuda", dev))
+
+
+def _made(t, name, dtype, shape, dev: int, stream):
+    """An output: the caller's, or a new one, allocated on the stream the call runs on."""
+    if t is not None:
+        return _same(t, name, dtype, shape, dev)
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=dev)
+
+
+def _bytes(ws, need, dev: int, stream):
+    """A workspace: the caller's, or a new one, allocated on the stream the call runs on."""
+    if ws is None:
+        return _made(None, "workspace", torch.uint8, (max(need, 1),), dev, stream)
+    if ws.get_device() != dev or ws.dtype is not torch.uint8 or ws.numel() < need:
+        raise ValueError(f"workspace must be a uint8 tensor of {need} bytes on CUDA device {dev}")
+    return ws
 
 
 def _pool(pool):
+    """(Pool, head dimension, CUDA device number) of a pool on the current device."""
     if not isinstance(pool, torch.Tensor):
         raise TypeError("pool must be a torch tensor")
-    d = _PAGE_DIM.get(pool.shape[-1]) if pool.dim() == 2 else None
+    shape = pool.shape
+    d = _PAGE_DIM.get(shape[1]) if len(shape) == 2 else None
     if d is None:
         raise ValueError("pool must be [n_pages, PAGE_BYTES[d]]")
-    dev = pool.device
-    _need(pool, "pool", torch.uint8, pool.shape, dev)
-    if dev.index != torch.cuda.current_device():
-        raise ValueError(f"pool must live on the current device, not on {dev}")
-    return Pool(pool.data_ptr(), pool.shape[0], d), d, dev
+    dev = torch._C._cuda_getDevice() if pool.is_cuda else -1
+    if pool.get_device() != dev or dev < 0:
+        raise ValueError(f"pool must live on the current CUDA device, not on {pool.device}")
+    _same(pool, "pool", torch.uint8, shape, dev)
+    return Pool(pool.data_ptr(), shape[0], d), d, dev
 
 
-def _table(table, name, units, dev):
-    """A page table [*units, max_pages] and its last size."""
+def _table(table, name, units, dev: int):
+    """A page table [*units, max_pages]; its last size."""
     if not isinstance(table, torch.Tensor) or table.dim() != len(units) + 1:
         raise ValueError(f"{name} must be [{', '.join(map(str, units))}, max_pages]")
-    _need(table, name, torch.int32, (*units, table.shape[-1]), dev)
-    return table.shape[-1]
+    pages = table.shape[-1]
+    _same(table, name, torch.int32, (*units, pages), dev)
+    return pages
 
 
-def _dense(t, name, dtype, shape, dev):
-    """A tensor of rows: any strides but the last, 16-byte aligned rows."""
+def _kind(t, name):
+    """Type, shape, strides of a tensor of rows."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch tensor")
-    if t.device != dev or t.dtype is not dtype or t.shape != shape:
-        raise ValueError(f"{name} must be {dtype} {tuple(shape)} on {dev}, got {t.dtype} "
-                         f"{tuple(t.shape)} on {t.device}")
+    return t.dtype, t.shape, t.stride()
+
+
+def _row_strides(kind, name, dtype, shape):
+    """Strides of a tensor of rows: any but the last, each row on a 16-byte boundary."""
+    if kind[0] is not dtype or tuple(kind[1]) != tuple(shape):
+        raise ValueError(f"{name} must be {dtype} {tuple(shape)}, got {kind[0]} {tuple(kind[1])}")
     # a dimension of one has no stride
-    strides = [x if n > 1 else 0 for x, n in zip(t.stride(), shape)]
+    strides = [x if n > 1 else 0 for x, n in zip(kind[2], shape)][:-1]
     step = 4 if dtype is torch.float32 else 8
-    if t.stride(-1) != 1 or t.data_ptr() % 16 or any(x % step for x in strides[:-1]):
+    if kind[2][-1] != 1 or any(x % step for x in strides):
         raise ValueError(f"{name}'s rows must be contiguous and start on 16-byte boundaries")
     return strides
 
 
-def _rows_dtype(t, name):
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name} must be a torch tensor")
-    if t.dtype is torch.bfloat16:
+def _rows_dtype(dtype, name):
+    if dtype is torch.bfloat16:
         return BF16
-    if t.dtype is torch.float32:
+    if dtype is torch.float32:
         return F32
     raise ValueError(f"{name} must be bfloat16 or float32")
+
+
+def _on(dev: int, *named):
+    for t, name in named:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"{name} must live on CUDA device {dev}, not on {t.device}")
+
+
+@functools.lru_cache(maxsize=1024)
+def _rope_plan(q, k, out_q, out_k, cs):
+    dtype, shape = (k if q is None else q)[:2]
+    code = _rows_dtype(dtype, "q and k")
+    if len(shape) != 3 or (k is not None and len(k[1]) != 3):
+        raise ValueError("q and k must be [T, heads, d]")
+    T, _, d = shape
+    if cs[0] is not torch.float32 or len(cs[1]) != 2 or cs[1][1] != d or cs[2] != (d, 1):
+        raise ValueError("cos_sin must be contiguous float32 [rows, d]")
+    heads, strides = [0, 0], [0] * 8
+    for i, (x, y, name) in enumerate(((q, out_q, "q"), (k, out_k, "k"))):
+        if x is None:
+            continue
+        heads[i] = x[1][1]
+        want = (T, heads[i], d)
+        strides[2 * i:2 * i + 2] = _row_strides(x, name, dtype, want)
+        strides[4 + 2 * i:6 + 2 * i] = _row_strides(y, f"out {name}", dtype, want)
+    return Heads(T, heads[0], heads[1], d, code, cs[1][0], *strides), dtype, T, d
 
 
 def twinkv_qk_norm_rope(q, k, wq, wk, cos_sin, positions, eps=1e-6, *, out=None,
@@ -704,62 +761,53 @@ def twinkv_qk_norm_rope(q, k, wq, wk, cos_sin, positions, eps=1e-6, *, out=None,
     themselves) and status [T] int32 (1 where a position is outside the table; that token is 0).
     """
     x = k if q is None else q
-    dtype = _rows_dtype(x, "q" if q is not None else "k")
-    if x.dim() != 3:
-        raise ValueError("q and k must be [T, heads, d]")
-    T, d, dev = x.shape[0], x.shape[2], x.device
-    if dev.type != "cuda" or dev.index != torch.cuda.current_device():
-        raise ValueError(f"tensors must live on the current CUDA device, not on {dev}")
-    o = {}
+    if not isinstance(x, torch.Tensor):
+        raise TypeError("q and k must be torch tensors")
+    dev = torch._C._cuda_getDevice() if x.is_cuda else -1
+    if dev < 0:
+        raise ValueError("q and k must be CUDA tensors")
     given = out or {}
-    strides, ptrs, heads = [0] * 8, [None] * 4, [0, 0]
-    for i, (t, name) in enumerate(((q, "q"), (k, "k"))):
-        if t is None:
-            continue
-        if t.dim() != 3:
-            raise ValueError("q and k must be [T, heads, d]")
-        heads[i] = t.shape[1]
-        shape = (T, heads[i], d)
-        strides[2 * i], strides[2 * i + 1], _ = _dense(t, name, x.dtype, shape, dev)
-        y = given.get(name)
-        if y is None:
-            with _on(stream):
-                y = torch.empty(shape, dtype=x.dtype, device=dev)
-        strides[4 + 2 * i], strides[5 + 2 * i], _ = _dense(y, f"out {name}", x.dtype, shape, dev)
-        o[name] = y
-        ptrs[i], ptrs[2 + i] = t.data_ptr(), y.data_ptr()
-    for w, name in ((wq, "wq"), (wk, "wk")):
-        if w is not None:
-            _need(w, name, x.dtype, (d,), dev)
-    if not isinstance(cos_sin, torch.Tensor) or cos_sin.dim() != 2:
-        raise ValueError("cos_sin must be [rows, d]")
-    _need(cos_sin, "cos_sin", torch.float32, (cos_sin.shape[0], d), dev)
-    _need(positions, "positions", torch.int32, (T,), dev)
-    with _on(stream):
-        o["status"] = _out(given.get("status"), "status", torch.int32, (T,), dev)
-    s = Heads(T, heads[0], heads[1], d, dtype, cos_sin.shape[0], *strides)
-    st = load().twinkv_qk_norm_rope(ptrs[0], ptrs[1], s, _ptr(wq), _ptr(wk), float(eps),
-                                    cos_sin.data_ptr(), positions.data_ptr(), ptrs[2], ptrs[3],
-                                    o["status"].data_ptr(), _stream(stream))
+    oq = ok = None
+    if q is not None:
+        oq = given.get("q")
+        if oq is None:
+            oq = _made(None, "q", q.dtype, q.shape, dev, stream)
+    if k is not None:
+        ok = given.get("k")
+        if ok is None:
+            ok = _made(None, "k", k.dtype, k.shape, dev, stream)
+    s, dtype, T, d = _rope_plan(q if q is None else _kind(q, "q"), k if k is None else _kind(k, "k"),
+                                oq if q is None else _kind(oq, "out q"),
+                                ok if k is None else _kind(ok, "out k"),
+                                _kind(cos_sin, "cos_sin"))
+    _on(dev, (q, "q"), (k, "k"), (oq, "out q"), (ok, "out k"), (cos_sin, "cos_sin"))
+    if wq is not None:
+        _same(wq, "wq", dtype, (d,), dev)
+    if wk is not None:
+        _same(wk, "wk", dtype, (d,), dev)
+    _same(positions, "positions", torch.int32, (T,), dev)
+    status = _made(given.get("status"), "status", torch.int32, (T,), dev, stream)
+    st = load().twinkv_qk_norm_rope(_ptr(q), _ptr(k), s, _ptr(wq), _ptr(wk), eps,
+                                    cos_sin.data_ptr(), positions.data_ptr(), _ptr(oq), _ptr(ok),
+                                    status.data_ptr(), _stream(stream))
     _check(st, "twinkv_qk_norm_rope")
+    o = {"status": status}
+    if q is not None:
+        o["q"] = oq
+    if k is not None:
+        o["k"] = ok
     return o
 
 
 def _lens_status(out, units, dev, stream):
-    out = out or {}
-    with _on(stream):
-        return {"lens": _out(out.get("lens"), "lens", torch.int32, units, dev),
-                "status": _out(out.get("status"), "status", torch.int32, units, dev)}
+    given = out or {}
+    return (_made(given.get("lens"), "lens", torch.int32, units, dev, stream),
+            _made(given.get("status"), "status", torch.int32, units, dev, stream))
 
 
-def _move_ws(ws, units, N, dev, stream):
-    need = units * N * 4
-    if ws is None:
-        with _on(stream):
-            ws = cache_move_workspace(units, N, dev)
-    if not ws.is_cuda or ws.device != dev or ws.dtype != torch.uint8 or ws.numel() < need:
-        raise ValueError(f"workspace must be a uint8 tensor of {need} bytes on {dev}")
-    return ws
+@functools.lru_cache(maxsize=1024)
+def _move_workspace_size(units, N) -> int:
+    return int(load().twinkv_cache_move_workspace(units, N))
 
 
 def twinkv_cache_pack(keys, values, retained_mask, pool, table, *, out=None, ws=None,
@@ -772,22 +820,34 @@ def twinkv_cache_pack(keys, values, retained_mask, pool, table, *, out=None, ws=
     """
     s = shape_of(keys)
     p, d, dev = _pool(pool)
-    _need(keys, "keys", keys.dtype, keys.shape, dev)
-    _need(values, "values", keys.dtype, keys.shape, dev)
+    shape = keys.shape
+    _same(keys, "keys", keys.dtype, shape, dev)
+    _same(values, "values", keys.dtype, shape, dev)
     if s.d != d:
         raise ValueError(f"the pool's pages hold rows of {d} values, the keys have {s.d}")
-    units = (s.L, s.H)
+    units = shape[:2]
     pages = _table(table, "table", units, dev)
+    wp, wn = None, 0
     if retained_mask is not None:
-        _need(retained_mask, "retained_mask", torch.uint8, (s.L, s.H, s.N), dev)
-        ws = _move_ws(ws, s.L * s.H, s.N, dev, stream)
-    o = _lens_status(out, units, dev, stream)
+        _same(retained_mask, "retained_mask", torch.uint8, shape[:3], dev)
+        ws = _bytes(ws, _move_workspace_size(s.L * s.H, s.N), dev, stream)
+        wp, wn = ws.data_ptr(), ws.numel()
+    lens, status = _lens_status(out, units, dev, stream)
     st = load().twinkv_cache_pack(
         keys.data_ptr(), values.data_ptr(), s, _ptr(retained_mask), p, table.data_ptr(), pages,
-        o["lens"].data_ptr(), o["status"].data_ptr(), _ptr(ws), 0 if ws is None else ws.numel(),
-        _stream(stream))
+        lens.data_ptr(), status.data_ptr(), wp, wn, _stream(stream))
     _check(st, "twinkv_cache_pack")
-    return o
+    return {"lens": lens, "status": status}
+
+
+@functools.lru_cache(maxsize=1024)
+def _append_plan(k, v):
+    code = _rows_dtype(k[0], "k")
+    if len(k[1]) != 4:
+        raise ValueError("k must be [B, n, H, d]")
+    B, n, H, d = k[1]
+    return Rows(B, H, n, code, *_row_strides(k, "k", k[0], k[1]),
+                *_row_strides(v, "v", k[0], k[1])), B, n, H, d
 
 
 def twinkv_cache_append(k, v, positions, pool, table, lens, *, out=None, stream=None) -> dict:
@@ -798,23 +858,20 @@ def twinkv_cache_append(k, v, positions, pool, table, lens, *, out=None, stream=
     lengths (``out`` may hold ``lens`` itself), and status [B,H].
     """
     p, d, dev = _pool(pool)
-    dtype = _rows_dtype(k, "k")
-    if k.dim() != 4:
-        raise ValueError("k must be [B, n, H, d]")
-    B, n, H, _ = k.shape
-    shape = (B, n, H, d)
-    kb, kt, kh, _ = _dense(k, "k", k.dtype, shape, dev)
-    vb, vt, vh, _ = _dense(v, "v", k.dtype, shape, dev)
-    _need(positions, "positions", torch.int32, (B, n), dev)
-    pages = _table(table, "table", (B, H), dev)
-    _need(lens, "lens", torch.int32, (B, H), dev)
-    o = _lens_status(out, (B, H), dev, stream)
+    s, B, n, H, dk = _append_plan(_kind(k, "k"), _kind(v, "v"))
+    if dk != d:
+        raise ValueError(f"the pool's pages hold rows of {d} values, k has {dk}")
+    _on(dev, (k, "k"), (v, "v"))
+    units = (B, H)
+    _same(positions, "positions", torch.int32, (B, n), dev)
+    pages = _table(table, "table", units, dev)
+    _same(lens, "lens", torch.int32, units, dev)
+    new, status = _lens_status(out, units, dev, stream)
     st = load().twinkv_cache_append(
-        k.data_ptr(), v.data_ptr(), Rows(B, H, n, dtype, kb, kt, kh, vb, vt, vh),
-        positions.data_ptr(), p, table.data_ptr(), pages, lens.data_ptr(),
-        o["lens"].data_ptr(), o["status"].data_ptr(), _stream(stream))
+        k.data_ptr(), v.data_ptr(), s, positions.data_ptr(), p, table.data_ptr(), pages,
+        lens.data_ptr(), new.data_ptr(), status.data_ptr(), _stream(stream))
     _check(st, "twinkv_cache_append")
-    return o
+    return {"lens": new, "status": status}
 
 
 def twinkv_cache_compact(pool, table, lens, keep, new_table, *, out=None, ws=None,
@@ -828,24 +885,24 @@ def twinkv_cache_compact(pool, table, lens, keep, new_table, *, out=None, ws=Non
     p, _, dev = _pool(pool)
     if not isinstance(lens, torch.Tensor):
         raise TypeError("lens must be a torch tensor")
-    units = tuple(lens.shape)
-    _need(lens, "lens", torch.int32, units, dev)
+    units = lens.shape
+    _same(lens, "lens", torch.int32, units, dev)
     pages, new_pages = (_table(table, "table", units, dev),
                         _table(new_table, "new_table", units, dev))
-    U, N = lens.numel(), pages * PAGE_SLOTS
+    U, N, wp, wn = lens.numel(), pages * PAGE_SLOTS, None, 0
     if keep is not None:
         if not isinstance(keep, torch.Tensor) or keep.dim() != len(units) + 1:
             raise ValueError("keep must be [units, N]")
         N = keep.shape[-1]
-        _need(keep, "keep", torch.uint8, (*units, N), dev)
-        ws = _move_ws(ws, U, N, dev, stream)
-    o = _lens_status(out, units, dev, stream)
+        _same(keep, "keep", torch.uint8, (*units, N), dev)
+        ws = _bytes(ws, _move_workspace_size(U, N), dev, stream)
+        wp, wn = ws.data_ptr(), ws.numel()
+    new, status = _lens_status(out, units, dev, stream)
     st = load().twinkv_cache_compact(
         p, table.data_ptr(), pages, lens.data_ptr(), U, _ptr(keep), N, new_table.data_ptr(),
-        new_pages, o["lens"].data_ptr(), o["status"].data_ptr(), _ptr(ws),
-        0 if ws is None else ws.numel(), _stream(stream))
+        new_pages, new.data_ptr(), status.data_ptr(), wp, wn, _stream(stream))
     _check(st, "twinkv_cache_compact")
-    return o
+    return {"lens": new, "status": status}
 
 
 def twinkv_cache_read(pool, table, lens, rows: int, *, last=False, out=None,
@@ -859,22 +916,30 @@ def twinkv_cache_read(pool, table, lens, rows: int, *, last=False, out=None,
     p, d, dev = _pool(pool)
     if not isinstance(lens, torch.Tensor):
         raise TypeError("lens must be a torch tensor")
-    units, rows, given = tuple(lens.shape), int(rows), out or {}
-    _need(lens, "lens", torch.int32, units, dev)
+    units, rows, given = lens.shape, int(rows), out or {}
+    _same(lens, "lens", torch.int32, units, dev)
     pages = _table(table, "table", units, dev)
-    with _on(stream):
-        o = {"keys": _out(given.get("keys"), "keys", torch.bfloat16, (*units, rows, d), dev),
-             "values": _out(given.get("values"), "values", torch.bfloat16, (*units, rows, d),
-                            dev),
-             "positions": _out(given.get("positions"), "positions", torch.int32, (*units, rows),
-                               dev),
-             "status": _out(given.get("status"), "status", torch.int32, units, dev)}
+    shape = (*units, rows, d)
+    keys = _made(given.get("keys"), "keys", torch.bfloat16, shape, dev, stream)
+    values = _made(given.get("values"), "values", torch.bfloat16, shape, dev, stream)
+    positions = _made(given.get("positions"), "positions", torch.int32, (*units, rows), dev, stream)
+    status = _made(given.get("status"), "status", torch.int32, units, dev, stream)
     st = load().twinkv_cache_read(
-        p, table.data_ptr(), pages, lens.data_ptr(), lens.numel(), rows, int(bool(last)),
-        o["keys"].data_ptr(), o["values"].data_ptr(), o["positions"].data_ptr(),
-        o["status"].data_ptr(), _stream(stream))
+        p, table.data_ptr(), pages, lens.data_ptr(), lens.numel(), rows, 1 if last else 0,
+        keys.data_ptr(), values.data_ptr(), positions.data_ptr(), status.data_ptr(),
+        _stream(stream))
     _check(st, "twinkv_cache_read")
-    return o
+    return {"keys": keys, "values": values, "positions": positions, "status": status}
+
+
+@functools.lru_cache(maxsize=1024)
+def _attend_plan(q, H, d):
+    if len(q[1]) != 4:
+        raise ValueError("q must be [B, n, Hq, d]")
+    B, n, Hq, _ = q[1]
+    strides = _row_strides(q, "q", torch.bfloat16, (B, n, Hq, d))
+    need = _attend_workspace_size(B, n, Hq, H, d) if H > 0 else 0
+    return Queries(B, H, Hq, n, *strides), B, (B, n, Hq, d), need
 
 
 def twinkv_cache_attend(q, pool, table, lens, *, scale=None, window=0, n_sink=0, want_lse=False,
@@ -887,31 +952,27 @@ def twinkv_cache_attend(q, pool, table, lens, *, scale=None, window=0, n_sink=0,
     [B,n,Hq,d] bf16, status [B,H] int32 and, with want_lse, lse [B,n,Hq] float32.
     """
     p, d, dev = _pool(pool)
-    if not isinstance(q, torch.Tensor) or q.dim() != 4:
-        raise ValueError("q must be [B, n, Hq, d]")
-    B, n, Hq, _ = q.shape
-    qb, qt, qh, _ = _dense(q, "q", torch.bfloat16, (B, n, Hq, d), dev)
     if not isinstance(lens, torch.Tensor) or lens.dim() != 2:
         raise ValueError("lens must be [B, H]")
-    H = lens.shape[1]
-    _need(lens, "lens", torch.int32, (B, H), dev)
-    pages = _table(table, "table", (B, H), dev)
+    units = lens.shape
+    s, B, shape, need = _attend_plan(_kind(q, "q"), units[1], d)
+    _on(dev, (q, "q"))
+    if units[0] != B:
+        raise ValueError(f"lens must be [{B}, H]")
+    _same(lens, "lens", torch.int32, units, dev)
+    pages = _table(table, "table", units, dev)
     given = out or {}
-    need = _attend_workspace_size(B, n, Hq, H, d) if H > 0 else 0
-    with _on(stream):
-        o = {"out": _out(given.get("out"), "out", torch.bfloat16, (B, n, Hq, d), dev),
-             "status": _out(given.get("status"), "status", torch.int32, (B, H), dev)}
-        if want_lse:
-            o["lse"] = _out(given.get("lse"), "lse", torch.float32, (B, n, Hq), dev)
-        if ws is None:
-            ws = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
-    if ws.device != dev or ws.dtype != torch.uint8 or ws.numel() < need:
-        raise ValueError(f"workspace must be a uint8 tensor of {need} bytes on {dev}")
+    o = {"out": _made(given.get("out"), "out", torch.bfloat16, shape, dev, stream),
+         "status": _made(given.get("status"), "status", torch.int32, units, dev, stream)}
+    lse = None
+    if want_lse:
+        o["lse"] = _made(given.get("lse"), "lse", torch.float32, shape[:3], dev, stream)
+        lse = o["lse"].data_ptr()
+    ws = _bytes(ws, need, dev, stream)
     st = load().twinkv_cache_attend(
-        q.data_ptr(), Queries(B, H, Hq, n, qb, qt, qh), d ** -0.5 if scale is None else scale,
-        int(window), int(n_sink), p, table.data_ptr(), pages, lens.data_ptr(),
-        o["out"].data_ptr(), _ptr(o.get("lse")), o["status"].data_ptr(), ws.data_ptr(),
-        ws.numel(), _stream(stream))
+        q.data_ptr(), s, d ** -0.5 if scale is None else scale, window, n_sink, p,
+        table.data_ptr(), pages, lens.data_ptr(), o["out"].data_ptr(), lse,
+        o["status"].data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream))
     _check(st, "twinkv_cache_attend")
     return o
 
