@@ -57,12 +57,13 @@ namespace {
 template <int D, int R>
 struct Config {
     static constexpr int NT = (R + 7) / 8, E = R == 4 ? 1 : 2;   // E: rows of a lane in a group
-    static constexpr int kWarps = NT == 1 ? 12 : 8;
+    // as many as their registers let be, equally many on each quarter of the SM
+    static constexpr int kWarps = R == 16 ? 8 : D == 128 ? 12 : 16;
     static constexpr int kHalf = PageLayout<D>::kValCodes;        // bytes of a page's keys
-    static constexpr int kStages = (NT == 1 ? 2 : 3) * (128 / D); // pages of a warp's ring
+    static constexpr int kStages = 221184 / (2 * kHalf * kWarps); // pages of a warp's ring
     static constexpr int kRing = 2 * kHalf * kStages;
     static_assert(PageLayout<D>::kPos == 2 * kHalf, "values take as many bytes as keys");
-    static_assert(kHalf % 16 == 0);
+    static_assert(kHalf % 16 == 0 && kStages >= 2);
 };
 
 struct AttendParams {
@@ -1038,13 +1039,13 @@ cudaError_t launch(AttendParams& p, int sms, cudaStream_t st)
 
 }  // namespace
 
+constexpr int kMostWarps = 16;
+
 // spans, then windows, then parts
 size_t attend_workspace(int units, int rows, int n, int d)
 {
     const int pr = part_rows(rows), parts = (rows + pr - 1) / pr;
     const int warps = kAttendBlocks * (pr == 8 ? Config<128, 8>::kWarps : Config<128, 16>::kWarps);
-    static_assert(Config<64, 8>::kWarps == Config<128, 4>::kWarps &&
-                  Config<64, 16>::kWarps == Config<128, 16>::kWarps);
     return up256(static_cast<size_t>(units) * parts * sizeof(int2)) +
            up256(static_cast<size_t>(units) * (1 + n) * 4) +
            up256(static_cast<size_t>(2) * warps * (pr * d + 2 * pr) * 4);

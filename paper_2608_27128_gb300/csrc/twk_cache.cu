@@ -102,6 +102,7 @@ __device__ __forceinline__ int mask_count(const uint4& v)
 __global__ void __launch_bounds__(kThreads) index_kernel(const IndexArgs a)
 {
     __shared__ int s_sum[kWarps], s_bad[kWarps], s_scan[kWarps];
+    __shared__ uint16_t s_place[16 * kVecChunk];
     wait_for_previous();
     const int u = blockIdx.y, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     int limit = a.limit ? a.limit[u] : a.N;
@@ -148,18 +149,25 @@ __global__ void __launch_bounds__(kThreads) index_kernel(const IndexArgs a)
         total = 0;
         bad = false;
         for (int i = 0; i < kWarps; ++i) {
-            base += s_sum[i] + (i < warp ? s_scan[i] : 0);
+            base += s_sum[i];
             total += s_sum[i] + s_scan[i];
             bad |= s_bad[i] != 0;
         }
-        int rank = base + scan - own;
-        int* out = a.index + static_cast<int64_t>(u) * a.N;
-        const int p = static_cast<int>(16 * v - mis);
+        // in shared memory by rank, then out in order
+        int rank = scan - own, here = 0;
+        for (int i = 0; i < kWarps; ++i) {
+            rank += i < warp ? s_scan[i] : 0;
+            here += s_scan[i];
+        }
         const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-            if (w[i / 4] >> (8 * (i % 4)) & 1) out[rank++] = p + i;
+            if (w[i / 4] >> (8 * (i % 4)) & 1)
+                s_place[rank++] = static_cast<uint16_t>(16 * threadIdx.x + i);
         __syncthreads();
+        int* out = a.index + static_cast<int64_t>(u) * a.N + base;
+        const int p0 = static_cast<int>(16 * v0 - mis);
+        for (int i = threadIdx.x; i < here; i += kThreads) out[i] = p0 + s_place[i];
     }
     if (static_cast<int>(blockIdx.x) != last) return;
     if (bad) status = kInvalid;
@@ -193,23 +201,27 @@ struct PageImage {
     uint32_t slots[kPage * kSlotWords<D>];   // value codes by slot
 };
 
+// a lane's share of a key row: the codes of chunks j and j + 4, and the group's scale and zero
 template <int D>
-__device__ __forceinline__ void put_key(uint8_t* page, int slot, int j, uint32_t word, float scale,
-                                        int zero)
+__device__ __forceinline__ void put_key(uint8_t* page, int slot, int j, const uint32_t (&w)[2],
+                                        float scale, int zero)
 {
     using P = PageLayout<D>;
-    *reinterpret_cast<uint32_t*>(page + P::key_word(slot, j)) = word;
+    *reinterpret_cast<uint32_t*>(page + P::key_word(slot, j)) = w[0];
+    *reinterpret_cast<uint32_t*>(page + P::key_word(slot, j + 4)) = w[1];
     if (j % 8 == 0)
         *reinterpret_cast<uint32_t*>(page + P::kKeyGroups + (slot * P::kGroups + j / 8) * 4) =
             (__float_as_uint(scale) >> 16) | (0xc3000000u + (static_cast<uint32_t>(zero) << 16));
 }
 
-// the group's part of a value row (its codes go elsewhere)
+// the same of a value row, its codes as words of the slot
 template <int D>
-__device__ __forceinline__ void put_value_group(uint8_t* page, int slot, int j, float scale,
-                                                int zero)
+__device__ __forceinline__ void put_value(uint8_t* page, uint32_t* slot_words, int slot, int j,
+                                          const uint32_t (&w)[2], float scale, int zero)
 {
     using P = PageLayout<D>;
+    slot_words[j] = w[0];
+    slot_words[j + 4] = w[1];
     if (j % 8 == 0) {
         reinterpret_cast<uint16_t*>(page + P::kValScales)[slot * P::kGroups + j / 8] =
             static_cast<uint16_t>(__float_as_uint(scale) >> 16);
@@ -243,82 +255,105 @@ __device__ __forceinline__ void store_page(const PageImage<D>& im, uint8_t* page
         reinterpret_cast<uint4*>(page)[i] = reinterpret_cast<const uint4*>(im.bytes)[i];
 }
 
-// eight values of a row as bf16 pairs, float32 ones rounded
+// A lane's 16 values of a row, as bf16 pairs (float32 ones rounded): the 8 from `p` on and the 8 that
+// lie 32 values further, so that four lanes read whole 64-byte pieces of a group.
 template <typename T>
-struct Values8;
+struct Values16;
 
 template <>
-struct Values8<uint16_t> {
-    uint4 v = {};
-    __device__ void load(const uint16_t* p) { v = __ldg(reinterpret_cast<const uint4*>(p)); }
-    __device__ void get(uint32_t (&x)[4]) const { x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w; }
+struct Values16<uint16_t> {
+    uint4 v[2] = {};
+    __device__ void load(const uint16_t* p)
+    {
+        v[0] = __ldg(reinterpret_cast<const uint4*>(p));
+        v[1] = __ldg(reinterpret_cast<const uint4*>(p + 32));
+    }
+    __device__ void get(uint32_t (&x)[8]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            x[4 * i] = v[i].x, x[4 * i + 1] = v[i].y, x[4 * i + 2] = v[i].z, x[4 * i + 3] = v[i].w;
+    }
 };
 
 template <>
-struct Values8<float> {
-    float4 a = {}, b = {};
+struct Values16<float> {
+    float4 v[4] = {};
     __device__ void load(const float* p)
     {
-        a = __ldg(reinterpret_cast<const float4*>(p));
-        b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            v[i] = __ldg(reinterpret_cast<const float4*>(p + i / 2 * 32) + i % 2);
     }
-    __device__ void get(uint32_t (&x)[4]) const
+    __device__ void get(uint32_t (&x)[8]) const
     {
-        x[0] = bf16_pair(a.x, a.y), x[1] = bf16_pair(a.z, a.w);
-        x[2] = bf16_pair(b.x, b.y), x[3] = bf16_pair(b.z, b.w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = bf16_pair(v[i].x, v[i].y);
+            x[2 * i + 1] = bf16_pair(v[i].z, v[i].w);
+        }
     }
 };
+
+// Lane l of a row has the groups of 8 values (chunks) first() and first() + 4.
+__device__ __forceinline__ int first_chunk(int l) { return l / 4 * 8 + l % 4; }
 
 // ---------------------------------------------------------------- pack
 
-// A block per page to fill.  D / 8 lanes hold a row, eight values each; a thread loads all of its
-// rows before it rounds the first.
+// A block per page to fill.  D / 16 lanes hold a row, 16 values each; a thread loads all of its
+// rows before it rounds the first, and five blocks of an SM do so in turn (two of float32 rows at
+// d = 128, which are twice as large).
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) pack_kernel(const PackArgs a)
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 && D == 128 ? 2 : 5)
+    pack_kernel(const PackArgs a)
 {
     using P = PageLayout<D>;
-    constexpr int kLanes = D / 8, kStep = kThreads / kLanes, kSteps = kPage / kStep;
+    constexpr int kLanes = D / 16, kStep = kThreads / kLanes, kSteps = kPage / kStep;
     __shared__ PageImage<D> im;
     wait_for_previous();
     const int u = blockIdx.y, first = blockIdx.x * kPage;
     const int count = min(kPage, a.lens[u] - first);
     if (count <= 0) return;
-    const int j = threadIdx.x % kLanes, s0 = threadIdx.x / kLanes;
+    const int j = first_chunk(threadIdx.x % kLanes), s0 = threadIdx.x / kLanes;
     const T* keys = static_cast<const T*>(a.keys) + static_cast<int64_t>(u) * a.N * D + 8 * j;
     const T* values = static_cast<const T*>(a.values) + static_cast<int64_t>(u) * a.N * D + 8 * j;
     const int* index = a.index ? a.index + static_cast<int64_t>(u) * a.N + first : nullptr;
+    const int page = a.to.table[static_cast<int64_t>(u) * a.to.max_pages + blockIdx.x];
+    // slots past the last row read that of slot 0 and become zeros
     int row[kSteps];
-    Values8<T> k[kSteps], v[kSteps];
+    Values16<T> k[kSteps], v[kSteps];
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-        const int s = s0 + i * kStep;
-        row[i] = s >= count ? -1 : index ? index[s] : first + s;
+        const int s = s0 + i * kStep < count ? s0 + i * kStep : 0;
+        row[i] = index ? index[s] : first + s;
     }
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i)
-        if (row[i] >= 0) k[i].load(keys + static_cast<int64_t>(row[i]) * D);
+    for (int i = 0; i < kSteps; ++i) k[i].load(keys + static_cast<int64_t>(row[i]) * D);
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) v[i].load(values + static_cast<int64_t>(row[i]) * D);
 #pragma unroll
     for (int i = 0; i < kSteps; ++i)
-        if (row[i] >= 0) v[i].load(values + static_cast<int64_t>(row[i]) * D);
+        if (s0 + i * kStep >= count) {
+            row[i] = -1;
+            k[i] = v[i] = Values16<T>{};
+        }
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
         const int s = s0 + i * kStep;
-        uint32_t x[4];
+        uint32_t x[8], w[2];
         float scale;
         int zero;
         k[i].get(x);
-        uint32_t w = quantize8(x, &scale, &zero);
+        quantize16(x, w, &scale, &zero);
         put_key<D>(im.bytes, s, j, w, scale, zero);
         if (j == 0) reinterpret_cast<int*>(im.bytes + P::kPos)[s] = row[i];
         v[i].get(x);
-        w = quantize8(x, &scale, &zero);
-        im.slots[s * kSlotWords<D> + j] = w;
-        put_value_group<D>(im.bytes, s, j, scale, zero);
+        quantize16(x, w, &scale, &zero);
+        put_value<D>(im.bytes, im.slots + s * kSlotWords<D>, s, j, w, scale, zero);
     }
     __syncthreads();
     slots_to_page<D, kThreads>(im);
     __syncthreads();
-    const int page = a.to.table[static_cast<int64_t>(u) * a.to.max_pages + blockIdx.x];
     store_page<D, kThreads>(im, a.to.base + static_cast<int64_t>(page) * P::kBytes);
 }
 
@@ -332,7 +367,7 @@ template <typename T, int D>
 __global__ void __launch_bounds__(kThreads) append_kernel(const AppendArgs a)
 {
     using P = PageLayout<D>;
-    constexpr int kLanes = D / 8;
+    constexpr int kLanes = D / 16;
     __shared__ uint32_t slots[kAppendMost * kSlotWords<D>];
     const int u = blockIdx.x, b = u / a.H, h = u % a.H;
     const int len = a.lens[u];
@@ -362,22 +397,22 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendArgs a)
     if (status) return;
     const int at = len % kPage;      // the first new row's slot of page[0]
     for (int i0 = 0; i0 < a.n; i0 += kThreads / kLanes) {
-        const int i = i0 + threadIdx.x / kLanes, j = threadIdx.x % kLanes;
+        const int i = i0 + threadIdx.x / kLanes, j = first_chunk(threadIdx.x % kLanes);
         const bool on = i < a.n;
-        Values8<T> k, v;
+        Values16<T> k, v;
         if (on) {
             k.load(static_cast<const T*>(a.keys) + b * a.k_batch + i * a.k_token + h * a.k_head +
                    8 * j);
             v.load(static_cast<const T*>(a.values) + b * a.v_batch + i * a.v_token +
                    h * a.v_head + 8 * j);
         }
-        uint32_t x[4];
-        float scale;
-        int zero;
         uint8_t* to = page[(at + i) / kPage ? 1 : 0];
         const int s = (at + i) % kPage;
+        uint32_t x[8], w[2];
+        float scale;
+        int zero;
         k.get(x);
-        uint32_t w = quantize8(x, &scale, &zero);
+        quantize16(x, w, &scale, &zero);
         if (on) {
             put_key<D>(to, s, j, w, scale, zero);
             if (j == 0)
@@ -385,11 +420,8 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendArgs a)
                     a.positions[static_cast<int64_t>(b) * a.n + i];
         }
         v.get(x);
-        w = quantize8(x, &scale, &zero);
-        if (on) {
-            slots[i * kSlotWords<D> + j] = w;
-            put_value_group<D>(to, s, j, scale, zero);
-        }
+        quantize16(x, w, &scale, &zero);
+        if (on) put_value<D>(to, slots + i * kSlotWords<D>, s, j, w, scale, zero);
     }
     __syncthreads();
     const int blocks = at + a.n > kPage ? 2 * D : D;

@@ -93,8 +93,25 @@ __device__ __forceinline__ float rcp_approx(float x)
     return r;
 }
 
-// 8 values of a group (bf16 pairs) as one word of codes (pairs as above), and the group's scale and
-// zero.  The lanes l, l ^ 1, l ^ 2, l ^ 4 hold the group's other values.
+// (a x + b, a y + b) in one instruction
+__device__ __forceinline__ void fma_pair(float& x, float& y, float a, float b)
+{
+    asm("{.reg .b64 v, m, c;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 m, {%2, %2};\n\t"
+        "mov.b64 c, {%3, %3};\n\tfma.rn.f32x2 v, v, m, c;\n\tmov.b64 {%0, %1}, v;}"
+        : "+f"(x), "+f"(y)
+        : "f"(a), "f"(b));
+}
+__device__ __forceinline__ void add_pair(float& x, float& y, float b)
+{
+    asm("{.reg .b64 v, c;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 c, {%2, %2};\n\t"
+        "add.rn.f32x2 v, v, c;\n\tmov.b64 {%0, %1}, v;}"
+        : "+f"(x), "+f"(y)
+        : "f"(b));
+}
+
+// 16 values of a group (bf16 pairs) as two words of codes (pairs as above), and the group's scale and
+// zero.  The lanes l ^ 1, l ^ 2 and l ^ 3 hold the group's other values (with 8 values in each of 8
+// lanes half of the instructions were the group's own).
 //
 //   lo = min(0, x..), hi = max(0, x..), s = bf16((hi - lo) / 15) (0 below 2^-126),
 //   z = rint(-lo / s), c = min(15, rint(x / s) + z); rint: to nearest, ties to even.
@@ -110,15 +127,20 @@ __device__ __forceinline__ float rcp_approx(float x)
 //            significant bits than hi).  The quotient is correctly rounded: the product with RN(1 / 15) and
 //            one step with its exact remainder (Markstein 1990).
 // Codes need no lower clamp: rint is odd, and -lo is among the values.
-__device__ __forceinline__ uint32_t quantize8(const uint32_t (&x)[4], float* scale, int* zero)
+__device__ __forceinline__ void quantize16(const uint32_t (&x)[8], uint32_t (&w)[2], float* scale,
+                                           int* zero)
 {
-    const uint32_t low = min_pair(min_pair(x[0], x[1]), min_pair(x[2], x[3]));
-    const uint32_t high = max_pair(max_pair(x[0], x[1]), max_pair(x[2], x[3]));
+    uint32_t low = x[0], high = x[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) {
+        low = min_pair(low, x[i]);
+        high = max_pair(high, x[i]);
+    }
     // (largest, -smallest) of the lane's values and 0, then of the group's
     uint32_t ends = max_pair(max_pair(__byte_perm(high, low, 0x5410) ^ 0x80000000u,
                                       __byte_perm(high, low, 0x7632) ^ 0x80000000u), 0u);
-#pragma unroll
-    for (int m = 1; m < 8; m *= 2) ends = max_pair(ends, __shfl_xor_sync(0xffffffffu, ends, m));
+    ends = max_pair(ends, __shfl_xor_sync(0xffffffffu, ends, 1));
+    ends = max_pair(ends, __shfl_xor_sync(0xffffffffu, ends, 2));
     const float up = bf16_lo(ends), down = bf16_hi(ends), range = up + down;
     constexpr float kFifteenth = 1.0f / 15.0f;
     const float q = range * kFifteenth;
@@ -127,23 +149,24 @@ __device__ __forceinline__ uint32_t quantize8(const uint32_t (&x)[4], float* sca
     const bool flat = !(s >= 0x1p-126f);
     s = flat ? 0.0f : s;
     const float r = flat ? 0.0f : rcp_approx(s);
-    constexpr float kFine = 12288.0f, kUnit = 12582912.0f;
-    constexpr uint32_t kBase = 0x4B400000u;   // the bits of kUnit
-    auto rounded = [&](float v) {             // kBase + rint(v / s)
-        return __float_as_int(fmaf(v, r, kFine) + (kUnit - kFine));
-    };
-    const int z = min(static_cast<int>(rounded(down) - kBase), 15) & 15;
-    const int most = static_cast<int>(kBase) + 15 - z;
-    // codes are the sums' last bits less kBase, plus z: taken off all eight at once
-    uint32_t w = (z - kBase) * 0x11111111u;
+    constexpr float kFine = 12288.0f, kUnit = 12582912.0f;   // kUnit's last 16 bits are 0
+    const int z = min(__float_as_int(fmaf(down, r, kFine) + (kUnit - kFine)) & 0xff, 15);
+    const uint32_t zz = z * 0x00010001u;
 #pragma unroll
-    for (int p = 0; p < 4; ++p) {
-        w += static_cast<uint32_t>(min(rounded(bf16_lo(x[p])), most)) << (4 * p);
-        w += static_cast<uint32_t>(min(rounded(bf16_hi(x[p])), most)) << (16 + 4 * p);
+    for (int i = 0; i < 2; ++i) {
+        w[i] = 0;
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            float a = bf16_lo(x[4 * i + p]), b = bf16_hi(x[4 * i + p]);
+            fma_pair(a, b, r, kFine);
+            add_pair(a, b, kUnit - kFine);
+            // both numbers' last 16 bits, plus z, at most 15
+            const uint32_t v = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x5410);
+            w[i] += __viaddmin_s16x2(v, zz, 0x000f000fu) << (4 * p);
+        }
     }
     *scale = s;
     *zero = z;
-    return w;
 }
 
 }  // namespace twk

@@ -810,6 +810,13 @@ def _move_workspace_size(units, N) -> int:
     return int(load().twinkv_cache_move_workspace(units, N))
 
 
+@functools.lru_cache(maxsize=1024)
+def _pack_plan(dtype, shape):
+    if len(shape) != 4:
+        raise ValueError("keys must be [L, H, N, d]")
+    return Shape(*shape, _rows_dtype(dtype, "keys"))
+
+
 def twinkv_cache_pack(keys, values, retained_mask, pool, table, *, out=None, ws=None,
                       stream=None) -> dict:
     """The retained rows of a dense cache into pages, rounded to 4 bits.
@@ -818,9 +825,11 @@ def twinkv_cache_pack(keys, values, retained_mask, pool, table, *, out=None, ws=
     pool as cache_pool makes it; table [L,H,max_pages] int32, the pages of each unit.  Returns a
     dict: lens [L,H] int32 and status [L,H] int32.
     """
-    s = shape_of(keys)
-    p, d, dev = _pool(pool)
+    if not isinstance(keys, torch.Tensor):
+        raise TypeError("keys must be a torch tensor")
     shape = keys.shape
+    s = _pack_plan(keys.dtype, shape)
+    p, d, dev = _pool(pool)
     _same(keys, "keys", keys.dtype, shape, dev)
     _same(values, "values", keys.dtype, shape, dev)
     if s.d != d:
