@@ -42,7 +42,6 @@
 #include <algorithm>
 #include <atomic>
 #include <climits>
-#include <type_traits>
 
 #include "twk_cache.cuh"
 #include "twk_cache_internal.h"
@@ -135,17 +134,6 @@ __device__ __forceinline__ void cp_async_wait()
     asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory");
 }
 
-__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
-                                         uint32_t a3, uint32_t b0, uint32_t b1)
-{
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
-        "{%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-
-// The same with f16 operands.
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
                                         uint32_t a3, uint32_t b0, uint32_t b1)
 {
@@ -218,16 +206,10 @@ __device__ __forceinline__ void load_groups(uint32_t at, uint32_t (&w)[D / 64])
         w[0] = lds32(at);
     }
 }
-template <int D>
-__device__ __forceinline__ void load_scales(uint32_t at, float (&s)[D / 64])
+// 2^e, 0 for e < -126
+__device__ __forceinline__ float power_of_two(int e)
 {
-    if constexpr (D == 128) {
-        const uint32_t v = lds32(at);
-        s[0] = bf16_lo(v);
-        s[1] = bf16_hi(v);
-    } else {
-        s[0] = bf16_lo(lds16(at));
-    }
+    return __uint_as_float(static_cast<uint32_t>(max(e + 127, 0)) << 23);
 }
 
 // The warp's place in the sequence of all pages: (unit, part) pair and page of its visit.
@@ -364,15 +346,6 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
         ++ahead.j;
         return ahead_row[page];
     };
-    // in registers: an instruction takes one constant of its own, the codes' take two
-    uint32_t code_mask, code_one;
-    asm volatile("mov.u32 %0, 0x000f000f;" : "=r"(code_mask));
-    asm volatile("mov.u32 %0, 0x43004300;" : "=r"(code_one));
-    auto pair_of = [&](uint32_t w, int i) {
-        uint32_t r;
-        asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w >> (4 * i)), "r"(code_mask), "r"(code_one));
-        return r;
-    };
     const uint32_t ring = smem_u32(smem + warp * C::kRing);
     auto copy_half = [&](int id, int stage, int half) {
         if (static_cast<unsigned>(id) < static_cast<unsigned>(p.a.from.n_pages)) {
@@ -400,6 +373,9 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
     uint32_t q[NT][G][8];
     float qsum[NT][G][E], unit_of[NT][E];   // sums of q, and what a score's unit is, see below
     float o[NT][M][4], zero_part[NT][G][4], top[NT][E], sum[NT][E];
+    float value_up[G];                // probabilities' scale, see below
+    int value_e[G];
+    uint32_t value_limit;
     int limit[NT][E], from[NT][E];    // row sees slots < limit that are >= from or < sinks
     int sinks = 0, all_limit = 0, all_from = 0;
     int seg_begin = 0;
@@ -481,6 +457,12 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
                 for (int G_ = 0; G_ < G; ++G_) zero_part[nt][G_][i] = 0.0f;
             }
         }
+        value_limit = 0;
+#pragma unroll
+        for (int G_ = 0; G_ < G; ++G_) {
+            value_up[G_] = 0.0f;
+            value_e[G_] = 0;
+        }
         // every row of the part: the first token sees least at the end, the last at the window's
         // begin
         const int first_token = r0 / p.a.G, last_token = (min(r0 + kRows, p.rows) - 1) / p.a.G;
@@ -504,7 +486,9 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
 #pragma unroll
             for (int m = 0; m < M; ++m)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[nt][m][e] += zero_part[nt][m / 4][e % 2];
+                for (int e = 0; e < 4; ++e)
+                    o[nt][m][e] = (o[nt][m][e] - zero_part[nt][m / 4][e % 2]) * 0x1p17f *
+                                  power_of_two(value_e[m / 4]);
         }
     };
     // rows as outputs [kRows][D], maxima and sums [kRows] (rows past the lanes' own: nothing seen)
@@ -698,52 +682,84 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
         // ---- values
         cp_async_wait<2 * C::kStages - 1>();
         __syncwarp();
-        uint32_t prob[NT][4][G][2];      // P s, bf16, slots in the order of the value codes
-        auto weigh = [&](auto masked) {
+        // The slots' scales, bf16 (those of two groups in one word); slots never written count as 0.
+        uint32_t scales[4][2];
+        uint32_t most = 0;
 #pragma unroll
-            for (int tile = 0; tile < 4; ++tile) {
-                float v[2][G];
+        for (int tile = 0; tile < 4; ++tile)
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    load_scales<D>(values + P::kValScales - P::kValCodes +
-                                       (16 * tile + 8 * i + g) * 2 * G, v[i]);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int G_ = 0; G_ < G; ++G_)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            float x[2] = {};        // rows t and t + 4
-#pragma unroll
-                            for (int e = 0; e < E; ++e) {
-                                const float y = s[nt][e][tile][i];
-                                // what an unseen slot holds may be anything
-                                x[e] = decltype(masked)::value && y == 0.0f ? 0.0f : y * v[i][G_];
-                            }
-                            prob[nt][tile][G_][i] = transpose16(bf16_pair(x[0], x[1]));
-                        }
+            for (int i = 0; i < 2; ++i) {
+                const int slot = 16 * tile + 8 * i + g;
+                const uint32_t at_scale = values + P::kValScales - P::kValCodes + slot * 2 * G;
+                uint32_t w;
+                if constexpr (D == 128) w = lds32(at_scale);
+                else w = lds16(at_scale);
+                if (!full && (gone || base + slot >= at.v.len)) w = 0;
+                scales[tile][i] = w;
+                most = __vmaxu2(most, w);
             }
-        };
-        if (full) weigh(std::false_type{});
-        else weigh(std::true_type{});
+        // Probabilities times scales enter as f16, in units of 2^(e - 7), 2^e the power of two below
+        // the largest scale seen.  There is room for scales up to 2^(e + 8); a larger one makes
+        // the unit its own.
+        if (__any_sync(0xffffffffu, __vmaxu2(most, value_limit) != value_limit)) {
+            uint32_t limits = 0;
+#pragma unroll
+            for (int G_ = 0; G_ < G; ++G_) {
+                const uint32_t b = __reduce_max_sync(0xffffffffu, most >> (16 * G_) & 0xffffu);
+                const uint32_t old = value_limit >> (16 * G_) & 0xffffu;
+                uint32_t now = old;
+                if (b > old) {
+                    const int e = max(static_cast<int>(b >> 7) - 127, -110);
+                    const float f = old == 0 ? 1.0f : power_of_two(value_e[G_] - e);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                            for (int m = 4 * G_; m < 4 * G_ + 4; ++m) o[nt][m][i] *= f;
+                            zero_part[nt][G_][i] *= f;
+                        }
+                    value_e[G_] = e;
+                    value_up[G_] = power_of_two(7 - e);
+                    now = static_cast<uint32_t>(min(e + 127 + 8, 255)) << 7;
+                }
+                limits |= now << (16 * G_);
+            }
+            value_limit = limits;
+        }
+        uint32_t prob[NT][4][G][2];      // f16, slots in the order of the value codes
+#pragma unroll
+        for (int tile = 0; tile < 4; ++tile)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int G_ = 0; G_ < G; ++G_) {
+                    // the odd pairs of a word's codes enter times 16
+                    const float f = (G_ ? bf16_hi(scales[tile][i]) : bf16_lo(scales[tile][i])) *
+                                    (i ? value_up[G_] * 0.0625f : value_up[G_]);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        float x[2] = {};        // rows t and t + 4
+#pragma unroll
+                        for (int e = 0; e < E; ++e) x[e] = s[nt][e][tile][i] * f;
+                        prob[nt][tile][G_][i] = transpose16(f16_pair(x[0], x[1]));
+                    }
+                }
 #pragma unroll
         for (int G_ = 0; G_ < G; ++G_)
 #pragma unroll
             for (int a = 0; a < 2; ++a) {
-                uint4 z = lds128(values + P::kValZeros - P::kValCodes + G_ * 2 * kPage + 32 * t +
-                                 16 * a);
-                if (!full) {     // likewise, where it would not be a number
-                    z.x = (z.x & 0x000f000fu) | 0xc300c300u;
-                    z.y = (z.y & 0x000f000fu) | 0xc300c300u;
-                    z.z = (z.z & 0x000f000fu) | 0xc300c300u;
-                    z.w = (z.w & 0x000f000fu) | 0xc300c300u;
-                }
+                // the last bits of -(128 + z) are z
+                const uint4 z = lds128(values + P::kValZeros - P::kValCodes + G_ * 2 * kPage +
+                                       32 * t + 16 * a);
+                const uint32_t z0 = z.x & 0x000f000fu, z1 = z.y << 4 & 0x00f000f0u;
+                const uint32_t z2 = z.z & 0x000f000fu, z3 = z.w << 4 & 0x00f000f0u;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    mma_bf16(zero_part[nt][G_], z.x, z.x, z.y, z.y, prob[nt][2 * a][G_][0],
-                             prob[nt][2 * a][G_][1]);
-                    mma_bf16(zero_part[nt][G_], z.z, z.z, z.w, z.w, prob[nt][2 * a + 1][G_][0],
-                             prob[nt][2 * a + 1][G_][1]);
+                    mma_f16(zero_part[nt][G_], z0, z0, z1, z1, prob[nt][2 * a][G_][0],
+                            prob[nt][2 * a][G_][1]);
+                    mma_f16(zero_part[nt][G_], z2, z2, z3, z3, prob[nt][2 * a + 1][G_][0],
+                            prob[nt][2 * a + 1][G_][1]);
                 }
             }
 #pragma unroll
@@ -754,12 +770,12 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
                 const uint32_t lo = a ? w.y : w.x, hi = a ? w.w : w.z;
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                    const uint32_t r0 = pair_of(lo, 2 * c), r1 = pair_of(hi, 2 * c);
-                    const uint32_t r2 = pair_of(lo, 2 * c + 1), r3 = pair_of(hi, 2 * c + 1);
+                    const uint32_t u = lo >> (8 * c), v = hi >> (8 * c);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
-                        mma_bf16(o[nt][m], r0, r1, r2, r3, prob[nt][2 * a + c][m / 4][0],
-                                 prob[nt][2 * a + c][m / 4][1]);
+                        mma_f16(o[nt][m], u & 0x000f000fu, v & 0x000f000fu, u & 0x00f000f0u,
+                                v & 0x00f000f0u, prob[nt][2 * a + c][m / 4][0],
+                                prob[nt][2 * a + c][m / 4][1]);
                 }
             }
         }
