@@ -1055,16 +1055,21 @@ cudaError_t launch(AttendParams& p, int sms, cudaStream_t st)
 
 }  // namespace
 
-constexpr int kMostWarps = 16;
+// Two parts for each warp of the largest grid; as many warps as any of the kernels of 8 rows, or of 16,
+// has.
+template <int R>
+constexpr size_t kParts = 2 * kAttendBlocks *
+                          std::max(std::max(Config<64, R>::kWarps, Config<128, R>::kWarps),
+                                   R == 8 ? std::max(Config<64, 4>::kWarps, Config<128, 4>::kWarps)
+                                          : 0);
 
 // spans, then windows, then parts
 size_t attend_workspace(int units, int rows, int n, int d)
 {
     const int pr = part_rows(rows), parts = (rows + pr - 1) / pr;
-    const int warps = kAttendBlocks * (pr == 8 ? Config<128, 8>::kWarps : Config<128, 16>::kWarps);
     return up256(static_cast<size_t>(units) * parts * sizeof(int2)) +
            up256(static_cast<size_t>(units) * (1 + n) * 4) +
-           up256(static_cast<size_t>(2) * warps * (pr * d + 2 * pr) * 4);
+           up256((pr == 8 ? kParts<8> : kParts<16>) * (pr * d + 2 * pr) * 4);
 }
 
 cudaError_t launch_attend(const AttendArgs& a, int sms, cudaStream_t st)

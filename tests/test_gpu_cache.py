@@ -439,3 +439,64 @@ def test_calls_on_another_stream_and_in_a_graph():
         torch.cuda.synchronize()
         assert torch.equal(res["out"], ref[i])
     assert torch.equal(lens, ref_lens) and tk.twinkv_get_last_error() == tk.OK
+
+
+# ---------------------------------------------------------------- what lies beyond the arrays
+
+def guarded(n, dtype=torch.uint8):
+    """n elements inside a larger array whose other bytes are 0xA5, and a check that they still are."""
+    size = n * torch.empty(0, dtype=dtype).element_size()
+    store = torch.full((size + 8192,), 0xA5, dtype=torch.uint8, device=device())
+
+    def whole():
+        return bool(store[:4096].eq(0xA5).all() and store[4096 + size:].eq(0xA5).all())
+
+    return store[4096:4096 + size].view(dtype), whole
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G", [1, 4, 5, 8, 9, 16, 33])
+def test_attend_stays_inside_its_workspace(d, G):
+    """Enough pages that every warp of the grid has some, for every kernel."""
+    H, length = 2, 170000
+    pages = -(-length // 64)
+    pool = torch.zeros((100, R.PAGE_BYTES[d]), dtype=torch.uint8, device=device())
+    table = torch.randint(0, 100, (1, H, pages), device=device()).int()
+    lens = torch.full((1, H), length, dtype=torch.int32, device=device())
+    q = torch.randn(1, 1, H * G, d, device=device()).to(torch.bfloat16)
+    ws, whole = guarded(tk._attend_workspace_size(1, 1, H * G, H, d))
+    out, whole_out = guarded(H * G * d, torch.bfloat16)
+    res = tk.twinkv_cache_attend(q, pool, table, lens, ws=ws, window=150000, n_sink=4,
+                                 out={"out": out.view(1, 1, H * G, d)})
+    torch.cuda.synchronize()
+    assert whole() and whole_out() and not res["out"].any()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_moves_stay_inside_their_arrays(d):
+    U, N = 3, 321
+    ids = np.arange(18, dtype=np.int32).reshape(1, U, 6)
+    flat, whole_pool = guarded(18 * R.PAGE_BYTES[d])
+    pool = flat.view(18, R.PAGE_BYTES[d])
+    x = torch.randn(1, U, N, d, device=device()).to(torch.bfloat16)
+    mask = torch.ones(1, U, N, dtype=torch.uint8, device=device())
+    ws, whole_ws = guarded(tk._move_workspace_size(U, N))
+    lens = tk.twinkv_cache_pack(x, x, mask, pool, put(ids), ws=ws)["lens"]
+    mask[0, 1] = 0
+    new, whole_new = guarded(18 * R.PAGE_BYTES[d])
+    both = torch.cat([pool, new.view(18, -1)])
+    out = tk.twinkv_cache_compact(both, put(ids), lens, mask, put(ids + 18), ws=ws)
+    pool.copy_(both[18:])
+    n = 7
+    k, whole_k = guarded(U * n * d, torch.bfloat16)
+    v, whole_v = guarded(U * n * d, torch.bfloat16)
+    pos, whole_pos = guarded(U * n, torch.int32)
+    tk.twinkv_cache_append(x[:, :, :n].transpose(1, 2), x[:, :, :n].transpose(1, 2),
+                           torch.full((1, n), 400, dtype=torch.int32, device=device()), pool,
+                           put(ids), out["lens"], out={"lens": out["lens"]})
+    got = tk.twinkv_cache_read(pool, put(ids), out["lens"], n, last=True,
+                               out={"keys": k.view(1, U, n, d), "values": v.view(1, U, n, d),
+                                    "positions": pos.view(1, U, n)})
+    assert got["positions"].eq(400).all()
+    torch.cuda.synchronize()
+    assert all(w() for w in (whole_pool, whole_ws, whole_new, whole_k, whole_v, whole_pos))
