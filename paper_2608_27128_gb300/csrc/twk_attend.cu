@@ -104,7 +104,7 @@ __device__ __forceinline__ Visit visit_of(const AttendParams& p, int unit)
 
 // floats of a part: outputs, maxima, sums
 template <int D, int R>
-constexpr int kPartSize = Config<D, R>::NT * (8 * D + 16);
+constexpr int kPartSize = R * (D + 2);
 
 // row of out and out_lse
 __device__ __forceinline__ int64_t out_row(const AttendParams& p, int unit, int row)
@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
     using P = PageLayout<D>;
     using C = Config<D, R>;
     constexpr int G = P::kGroups, M = D / 16, NT = C::NT, E = C::E;
-    constexpr int kRows = 8 * NT;
+    constexpr int kRows = R;
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ int s_pair[C::kWarps], s_slot[C::kWarps];
     __shared__ bool s_begins[C::kWarps], s_ends[C::kWarps];
@@ -237,7 +237,7 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
     int64_t total;
     // Pages before each chunk of 32 pairs: up to kFewChunks of them by every warp for itself, without
     // a barrier, more by the block.
-    constexpr int kFewChunks = 8;
+    constexpr int kFewChunks = 1;
     int few[kFewChunks];
     if (p.chunks <= kFewChunks) {
 #pragma unroll
@@ -491,23 +491,21 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
                                   power_of_two(value_e[m / 4]);
         }
     };
-    // rows as outputs [kRows][D], maxima and sums [kRows] (rows past the lanes' own: nothing seen)
+    // rows as outputs [kRows][D], then maxima and sums [kRows]
     auto put_part = [&](float* part) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
+            for (int e = 0; e < E; ++e) {
                 const int r = 8 * nt + 4 * e + t;
-                if (e < E) {
 #pragma unroll
-                    for (int m = 0; m < M; ++m) {
-                        part[r * D + 16 * m + g] = o[nt][m][e];
-                        part[r * D + 16 * m + 8 + g] = o[nt][m][2 + e];
-                    }
+                for (int m = 0; m < M; ++m) {
+                    part[r * D + 16 * m + g] = o[nt][m][e];
+                    part[r * D + 16 * m + 8 + g] = o[nt][m][2 + e];
                 }
                 if (g == 0) {
-                    part[kRows * D + r] = e < E ? top[nt][e % E] : -INFINITY;
-                    part[kRows * D + kRows + r] = e < E ? sum[nt][e % E] : 0.0f;
+                    part[kRows * D + r] = top[nt][e];
+                    part[kRows * D + kRows + r] = sum[nt][e];
                 }
             }
     };
@@ -814,39 +812,46 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
         s_ends[warp] = at.j == at.v.count;
     }
     __syncthreads();
-    for (int w0 = 0, w1; w0 < C::kWarps && s_pair[w0] >= 0; w0 = w1) {
+    // a warp per run of such warps and row
+    for (int w0 = 0, w1, turn = warp; w0 < C::kWarps && s_pair[w0] >= 0; w0 = w1, turn += kRows) {
         const int pair = s_pair[w0], unit = pair / p.parts, r0 = pair % p.parts * kRows;
         for (w1 = w0 + 1; w1 < C::kWarps && s_pair[w1] == pair; ++w1) {}
         const bool begins = s_begins[w0], ends = s_ends[w1 - 1], whole = begins && ends;
         float* part = p.part + static_cast<int64_t>(s_slot[w0]) * kPartSize<D, R>;
-        for (int i = threadIdx.x; i < kRows * D / 4; i += 32 * C::kWarps) {
-            const int r = 4 * i / D, x = 4 * i % D;
-            float m = -INFINITY, l = 0.0f;
-            float4 acc = {};
+        for (int r = turn % C::kWarps; r < kRows; r += C::kWarps) {
+            constexpr int kVec = D / 32;
+            float m = -INFINITY, l = 0.0f, acc[kVec] = {};
             for (int w = w0; w < w1; ++w)
                 m = fmaxf(m, reinterpret_cast<const float*>(smem + w * C::kRing)[kRows * D + r]);
             for (int w = w0; w < w1 && m > -INFINITY; ++w) {
                 const float* from_warp = reinterpret_cast<const float*>(smem + w * C::kRing);
                 const float f = exp2_approx((from_warp[kRows * D + r] - m) * p.c);
-                const float4 y = *reinterpret_cast<const float4*>(from_warp + 4 * i);
                 l = fmaf(from_warp[kRows * D + kRows + r], f, l);
-                acc.x = fmaf(y.x, f, acc.x);
-                acc.y = fmaf(y.y, f, acc.y);
-                acc.z = fmaf(y.z, f, acc.z);
-                acc.w = fmaf(y.w, f, acc.w);
+#pragma unroll
+                for (int v = 0; v < kVec; v += 2) {
+                    const float2 y = *reinterpret_cast<const float2*>(from_warp + r * D + 32 * v +
+                                                                      2 * lane);
+                    acc[v] = fmaf(y.x, f, acc[v]);
+                    acc[v + 1] = fmaf(y.y, f, acc[v + 1]);
+                }
             }
             if (!whole) {
-                *reinterpret_cast<float4*>(part + 4 * i) = acc;
-                if (x == 0) {
+#pragma unroll
+                for (int v = 0; v < kVec; v += 2)
+                    *reinterpret_cast<float2*>(part + r * D + 32 * v + 2 * lane) =
+                        make_float2(acc[v], acc[v + 1]);
+                if (lane == 0) {
                     part[kRows * D + r] = m;
                     part[kRows * D + kRows + r] = l;
                 }
             } else if (r0 + r < p.rows) {
                 const int64_t row = out_row(p, unit, r0 + r);
                 const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-                *reinterpret_cast<uint2*>(p.a.out + row * D + x) = make_uint2(
-                    bf16_pair(acc.x * inv, acc.y * inv), bf16_pair(acc.z * inv, acc.w * inv));
-                if (p.a.out_lse && x == 0) p.a.out_lse[row] = log_sum(p, m, l);
+#pragma unroll
+                for (int v = 0; v < kVec; v += 2)
+                    *reinterpret_cast<uint32_t*>(p.a.out + row * D + 32 * v + 2 * lane) =
+                        bf16_pair(acc[v] * inv, acc[v + 1] * inv);
+                if (p.a.out_lse && lane == 0) p.a.out_lse[row] = log_sum(p, m, l);
             }
         }
         if (threadIdx.x == 0) {
@@ -874,7 +879,7 @@ template <int D, int R>
 __global__ void __launch_bounds__(32 * kMergeWarps)
     merge_kernel(const __grid_constant__ AttendParams p)
 {
-    constexpr int kRows = 8 * Config<D, R>::NT, kWarps = Config<D, R>::kWarps, kVec = D / 32;
+    constexpr int kRows = R, kWarps = Config<D, R>::kWarps, kVec = D / 32;
     __shared__ float s_acc[kMergeWarps][D];
     __shared__ float s_top[kMergeWarps], s_sum[kMergeWarps];
     wait_for_previous();
