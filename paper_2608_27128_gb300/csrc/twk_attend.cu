@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
     using P = PageLayout<D>;
     using C = Config<D, R>;
     constexpr int G = P::kGroups, M = D / 16, NT = C::NT, E = C::E;
-    constexpr int kRows = R;
+    constexpr int kRows = R, kTiles = 2, kDims = 2;
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ int s_pair[C::kWarps], s_slot[C::kWarps];
     __shared__ bool s_begins[C::kWarps], s_ends[C::kWarps];
@@ -562,54 +562,66 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
         __syncwarp();
         float s[NT][E][4][2];               // slots g and g + 8 of each tile
 #pragma unroll
-        for (int tile = 0; tile < 4; ++tile) {
-            const int lo = 16 * tile + g;
-            uint32_t a0[2 * G], a1[2 * G];    // words of slots lo and lo + 8
-            if constexpr (D == 128) {
-                const uint4 u = lds128(keys + lo * P::kRow + 16 * t);
-                const uint4 w = lds128(keys + (lo + 8) * P::kRow + 16 * t);
-                a0[0] = u.x, a0[1] = u.y, a0[2] = u.z, a0[3] = u.w;
-                a1[0] = w.x, a1[1] = w.y, a1[2] = w.z, a1[3] = w.w;
-            } else {
-                const uint2 u = lds64(keys + lo * P::kRow + 8 * t);
-                const uint2 w = lds64(keys + (lo + 8) * P::kRow + 8 * t);
-                a0[0] = u.x, a0[1] = u.y;
-                a1[0] = w.x, a1[1] = w.y;
+        for (int t0 = 0; t0 < 4; t0 += kTiles) {   // tiles side by side: the multiplications' latency
+            uint32_t a0[kTiles][2 * G], a1[kTiles][2 * G];    // words of slots lo and lo + 8
+            uint32_t k0[kTiles][G], k1[kTiles][G];
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i) {
+                const int lo = 16 * (t0 + i) + g;
+                if constexpr (D == 128) {
+                    const uint4 u = lds128(keys + lo * P::kRow + 16 * t);
+                    const uint4 w = lds128(keys + (lo + 8) * P::kRow + 16 * t);
+                    a0[i][0] = u.x, a0[i][1] = u.y, a0[i][2] = u.z, a0[i][3] = u.w;
+                    a1[i][0] = w.x, a1[i][1] = w.y, a1[i][2] = w.z, a1[i][3] = w.w;
+                } else {
+                    const uint2 u = lds64(keys + lo * P::kRow + 8 * t);
+                    const uint2 w = lds64(keys + (lo + 8) * P::kRow + 8 * t);
+                    a0[i][0] = u.x, a0[i][1] = u.y;
+                    a1[i][0] = w.x, a1[i][1] = w.y;
+                }
+                load_groups<D>(keys + P::kKeyGroups + lo * 4 * G, k0[i]);
+                load_groups<D>(keys + P::kKeyGroups + (lo + 8) * 4 * G, k1[i]);
             }
-            uint32_t k0[G], k1[G];
-            load_groups<D>(keys + P::kKeyGroups + lo * 4 * G, k0);
-            load_groups<D>(keys + P::kKeyGroups + (lo + 8) * 4 * G, k1);
 #pragma unroll
             for (int G_ = 0; G_ < G; ++G_) {
-                float acc[NT][4] = {};       // -z Q at first
+                float acc[kTiles][NT][4] = {};       // -z Q at first
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        const float all = 128.0f * qsum[nt][G_][e];
-                        acc[nt][e] = fmaf(bf16_hi(k0[G_]), qsum[nt][G_][e], all);
-                        acc[nt][2 + e] = fmaf(bf16_hi(k1[G_]), qsum[nt][G_][e], all);
-                    }
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < E; ++e) {
+                            const float all = 128.0f * qsum[nt][G_][e];
+                            acc[i][nt][e] = fmaf(bf16_hi(k0[i][G_]), qsum[nt][G_][e], all);
+                            acc[i][nt][2 + e] = fmaf(bf16_hi(k1[i][G_]), qsum[nt][G_][e], all);
+                        }
 #pragma unroll
                 for (int w = 0; w < 2; ++w)
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const uint32_t u = a0[2 * G_ + w] >> (8 * x), v = a1[2 * G_ + w] >> (8 * x);
+                    for (int x = 0; x < 2; ++x)
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-                            mma_f16(acc[nt], u & 0x000f000fu, v & 0x000f000fu, u & 0x00f000f0u,
-                                    v & 0x00f000f0u, q[nt][G_][4 * w + 2 * x],
-                                    q[nt][G_][4 * w + 2 * x + 1]);
-                    }
-                const float s0 = bf16_lo(k0[G_]), s1 = bf16_lo(k1[G_]);
+                        for (int i = 0; i < kTiles; ++i) {
+                            const uint32_t u = a0[i][2 * G_ + w] >> (8 * x);
+                            const uint32_t v = a1[i][2 * G_ + w] >> (8 * x);
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                            for (int nt = 0; nt < NT; ++nt)
+                                mma_f16(acc[i][nt], u & 0x000f000fu, v & 0x000f000fu,
+                                        u & 0x00f000f0u, v & 0x00f000f0u,
+                                        q[nt][G_][4 * w + 2 * x], q[nt][G_][4 * w + 2 * x + 1]);
+                        }
 #pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        float(&y)[2] = s[nt][e][tile];
-                        y[0] = G_ == 0 ? acc[nt][e] * s0 : fmaf(acc[nt][e], s0, y[0]);
-                        y[1] = G_ == 0 ? acc[nt][2 + e] * s1 : fmaf(acc[nt][2 + e], s1, y[1]);
-                    }
+                for (int i = 0; i < kTiles; ++i) {
+                    const float s0 = bf16_lo(k0[i][G_]), s1 = bf16_lo(k1[i][G_]);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < E; ++e) {
+                            float(&y)[2] = s[nt][e][t0 + i];
+                            y[0] = G_ == 0 ? acc[i][nt][e] * s0 : fmaf(acc[i][nt][e], s0, y[0]);
+                            y[1] = G_ == 0 ? acc[i][nt][2 + e] * s1
+                                           : fmaf(acc[i][nt][2 + e], s1, y[1]);
+                        }
+                }
             }
         }
         __syncwarp();
@@ -761,21 +773,26 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
                 }
             }
 #pragma unroll
-        for (int m = 0; m < M; ++m) {
-            const uint4 w = lds128(values + ((m * 8 + g) * 4 + t) * 16);
+        for (int m0 = 0; m0 < M; m0 += kDims) {
+            uint4 w[kDims];
 #pragma unroll
-            for (int a = 0; a < 2; ++a) {
-                const uint32_t lo = a ? w.y : w.x, hi = a ? w.w : w.z;
+            for (int i = 0; i < kDims; ++i)
+                w[i] = lds128(values + (((m0 + i) * 8 + g) * 4 + t) * 16);
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const uint32_t u = lo >> (8 * c), v = hi >> (8 * c);
+            for (int a = 0; a < 2; ++a)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-                        mma_f16(o[nt][m], u & 0x000f000fu, v & 0x000f000fu, u & 0x00f000f0u,
-                                v & 0x00f000f0u, prob[nt][2 * a + c][m / 4][0],
-                                prob[nt][2 * a + c][m / 4][1]);
-                }
-            }
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int i = 0; i < kDims; ++i) {
+                        const int m = m0 + i;
+                        const uint32_t u = (a ? w[i].y : w[i].x) >> (8 * c);
+                        const uint32_t v = (a ? w[i].w : w[i].z) >> (8 * c);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+                            mma_f16(o[nt][m], u & 0x000f000fu, v & 0x000f000fu, u & 0x00f000f0u,
+                                    v & 0x00f000f0u, prob[nt][2 * a + c][m / 4][0],
+                                    prob[nt][2 * a + c][m / 4][1]);
+                    }
         }
         __syncwarp();
         copy_half(id, stage, 1);
