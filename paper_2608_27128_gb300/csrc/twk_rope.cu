@@ -91,48 +91,50 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs a, in
         c.get(cs);
         s.get(sn);
     }
-    for (int h0 = split * kHeads; h0 < heads; h0 += splits * kHeads) {
-        const int h = h0 + lane / kLanes;
-        const bool on = h < heads, is_q = h < a.heads_q;
-        const T* src = nullptr;
-        T* dst = nullptr;
-        const T* w = static_cast<const T*>(is_q ? a.wq : a.wk);
-        if (is_q) {
-            src = static_cast<const T*>(a.q) + token * a.q_token + h * a.q_head;
-            dst = static_cast<T*>(a.out_q) + token * a.oq_token + h * a.oq_head;
-        } else if (on) {
-            const int hk = h - a.heads_q;
-            src = static_cast<const T*>(a.k) + token * a.k_token + hk * a.k_head;
-            dst = static_cast<T*>(a.out_k) + token * a.ok_token + hk * a.ok_head;
-        }
-        float x[8] = {}, y[8] = {};
-        if (on && !bad) {
-            Eight<T> u, v;
-            u.load(src + 8 * l);
-            v.load(src + D / 2 + 8 * l);
-            u.get(x);
-            v.get(y);
-        }
+    // the next heads' values are loaded before the present ones are used
+    auto load = [&](int h, Eight<T>& u, Eight<T>& v) {
+        if (bad || h >= heads) return;
+        const T* src = h < a.heads_q
+                           ? static_cast<const T*>(a.q) + token * a.q_token + h * a.q_head
+                           : static_cast<const T*>(a.k) + token * a.k_token +
+                                 (h - a.heads_q) * a.k_head;
+        u.load(src + 8 * l);
+        v.load(src + D / 2 + 8 * l);
+    };
+    const int step = splits * kHeads;
+    int h = split * kHeads + lane / kLanes;
+    Eight<T> u = {}, v = {};
+    load(h, u, v);
+    for (int h0 = split * kHeads; h0 < heads; h0 += step, h += step) {
+        float x[8], y[8];
+        u.get(x);
+        v.get(y);
+        load(h + step, u, v);
         float sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], fmaf(y[i], y[i], sum));
 #pragma unroll
         for (int m = 1; m < kLanes; m *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, m);
-        if (!on) continue;
+        if (h >= heads) continue;
+        const bool is_q = h < a.heads_q;
+        const T* w = static_cast<const T*>(is_q ? a.wq : a.wk);
         if (w) {
             const float r = rsqrtf(sum * (1.0f / D) + a.eps);
             float wx[8], wy[8];
-            Eight<T> u, v;
-            u.load(w + 8 * l);
-            v.load(w + D / 2 + 8 * l);
-            u.get(wx);
-            v.get(wy);
+            Eight<T> s, c;
+            s.load(w + 8 * l);
+            c.load(w + D / 2 + 8 * l);
+            s.get(wx);
+            c.get(wy);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 x[i] *= r * wx[i];
                 y[i] *= r * wy[i];
             }
         }
+        T* dst = is_q ? static_cast<T*>(a.out_q) + token * a.oq_token + h * a.oq_head
+                      : static_cast<T*>(a.out_k) + token * a.ok_token +
+                            (h - a.heads_q) * a.ok_head;
         float p[8], q[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
