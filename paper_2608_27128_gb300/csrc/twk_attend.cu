@@ -57,7 +57,7 @@ template <int D, int R>
 struct Config {
     static constexpr int NT = (R + 7) / 8, E = R == 4 ? 1 : 2;   // E: rows of a lane in a group
     // as many as their registers let be, equally many on each quarter of the SM
-    static constexpr int kWarps = D == 128 ? (R == 16 ? 8 : 12) : R == 16 ? 12 : 16;
+    static constexpr int kWarps = R == 16 ? 8 : D == 128 ? 12 : 16;
     static constexpr int kHalf = PageLayout<D>::kValCodes;        // bytes of a page's keys
     static constexpr int kStages = 221184 / (2 * kHalf * kWarps); // pages of a warp's ring
     static constexpr int kRing = 2 * kHalf * kStages;
@@ -995,9 +995,8 @@ __global__ void __launch_bounds__(32 * kMergeWarps)
 // ---------------------------------------------------------------- windows
 
 // Positions ascend over a unit's slots, so what a window shows is a run of slots.  A warp per unit
-// and search: the number of slots below n_sink, and per token the first slot inside its window.  The
-// page first, by the first position of up to 128 pages at a time, then the slot in it, two positions a
-// lane: bound by the latency of three or four loads that depend on one another.
+// and search, 32 probes at a time: the number of slots below n_sink, and per token the first slot
+// inside its window.
 template <int D>
 __global__ void __launch_bounds__(128) window_kernel(const AttendArgs a, int units, int* seen)
 {
@@ -1016,7 +1015,7 @@ __global__ void __launch_bounds__(128) window_kernel(const AttendArgs a, int uni
                                             P::kPos)[slot % kPage];
     };
     int64_t wanted = a.n_sink;       // the first slot whose position is not below this
-    int hi = len;                    // is at most this one
+    int hi = len;
     if (which >= 0) {
         const int own = len - a.n + which;
         if (own < 0) {
@@ -1026,37 +1025,17 @@ __global__ void __launch_bounds__(128) window_kernel(const AttendArgs a, int uni
         wanted = position(own) - a.window + 1;
         hi = own;                    // its own slot is inside
     }
-    // pages [lo, last): those that begin below `wanted`; the answer is in the last of them or where
-    // the next one begins
-    int lo = 0, last = (hi + kPage - 1) / kPage;
-    while (lo < last) {
-        const int step = (last - lo + 127) / 128;
-        int n = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int page = lo + (4 * lane + i) * step;
-            n += page < last && position(page * kPage) < wanted;
-        }
-        n = __reduce_add_sync(0xffffffffu, n);     // probes below: the first n of them
-        if (n == 0) {
-            last = lo;
-        } else {
-            last = min(last, lo + n * step);
-            lo += (n - 1) * step + 1;
-        }
+    int lo = 0;                      // the answer is in [lo, hi]
+    while (lo < hi) {
+        const int step = (hi - lo + 31) / 32;
+        const int slot = lo + (lane + 1) * step - 1;
+        const unsigned below = __ballot_sync(0xffffffffu, slot < hi && position(slot) < wanted);
+        const int n = __popc(below);
+        lo += n * step;
+        hi = min(hi, lo + step - 1);
+        lo = min(lo, hi);
     }
-    int answer = 0;
-    if (lo > 0) {
-        const int first = (lo - 1) * kPage;
-        int n = 0;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int slot = first + 2 * lane + i;
-            n += slot < hi && position(slot) < wanted;
-        }
-        answer = first + __reduce_add_sync(0xffffffffu, n);
-    }
-    if (lane == 0) seen[static_cast<int64_t>(unit) * (1 + a.n) + 1 + which] = answer;
+    if (lane == 0) seen[static_cast<int64_t>(unit) * (1 + a.n) + 1 + which] = lo;
 }
 
 size_t up256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }

@@ -29,7 +29,7 @@ def _source(name):
         return f.read()
 
 
-WARPS = {(64, 4): 16, (64, 8): 16, (64, 16): 12, (128, 4): 12, (128, 8): 12, (128, 16): 8}
+WARPS = {(64, 4): 16, (64, 8): 16, (64, 16): 8, (128, 4): 12, (128, 8): 12, (128, 16): 8}
 
 
 def test_warps_are_the_sources():
