@@ -518,7 +518,7 @@ size_t twinkv_cache_attend_workspace(twinkv_queries s, int32_t d);
  * above its own minus `window` or below n_sink (the sinks and the recent region of Sec. 3.2).
  *   o = sum_j softmax_j(scale q . k_j) v_j      float32 sums; a token that sees nothing: 0
  * Precision: codes and queries enter exactly; a probability times its slot's value scale is
- * rounded to bf16, then the result to bf16.
+ * rounded to 11 bits, the result to bf16.
  *   q           [B][n][Hq][d] bf16, 16-byte aligned, strides in s (multiples of 8)
  *   scale       finite, above 0
  *   window      0: none (n_sink is then not used)
@@ -526,7 +526,7 @@ size_t twinkv_cache_attend_workspace(twinkv_queries s, int32_t d);
  *   out         [B][n][Hq][d] bf16, 16-byte aligned
  *   out_lse     [B][n][Hq] float32 log of the softmax's denominator (-inf: nothing seen), or
  *               NULL; attention over several caches is joined with it
- *   out_status  [B*H] int32, or NULL; pages outside the pool count as unseen
+ *   out_status  [B*H] int32, or NULL; slots of a page outside the pool count as unseen
  * Limits (TWINKV_ERR_UNSUPPORTED beyond): n <= 64, Hq / H <= 256, B*H and
  * B*H*ceil(n Hq / H / 16) <= 65535.
  */

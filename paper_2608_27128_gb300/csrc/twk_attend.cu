@@ -7,38 +7,49 @@
 // it sees the slots up to its own and, with a window, of those only the ones whose position is
 // within the window of its own or below n_sink.  A query that sees nothing gives 0.
 //
-// Bound by memory: 144 bytes a slot (d = 128) against 512 operations per query row, and a unit has
-// G n rows, 4 to 16 as a rule.  So what a slot costs in instructions counts, and the design is for
-// few of them:
-//   - Key codes enter the tensor cores as f16 bit patterns as they are: a code c in the last bits of a
+// Bound by memory where it is large: 144 bytes a slot (d = 128) against 512 operations per query row,
+// and a unit has G n rows, 4 to 16 as a rule.  So what a slot costs in instructions counts, and the
+// design is for few of them:
+//   - Codes enter the tensor cores as f16 bit patterns as they are: a code c in the last bits of a
 //     half is the number c 2^-24, and 16 c one place up, so that a word of 8 codes gives 4 operand
-//     registers in 5 instructions; the query values that meet the second kind are divided by 16.
-//     Queries are scaled by a power of two per row, which leaves them exact.  Nothing is subtracted or
-//     scaled per element: with Q_G the sum of q over a group,
-//         q . k = sum_G s_G (sum q c - z_G Q_G):
-//     the second term is the accumulator's start value, the scale one multiplication per group.
-//   - Value codes enter as the bf16 numbers 128 + c (exact; 7 instructions a word), since the
-//     probabilities, which take the slots' scales with them, need bf16's range.  P s is rounded to bf16
-//     (2^-8, the output's own rounding, and independent from slot to slot), and the zeros go
-//     into one more product with the same rounded numbers, so that no rounding is multiplied by 128.
+//     registers in 5 instructions; what meets the second kind is divided by 16.  Nothing is
+//     subtracted or scaled per element.
+//   - Keys: with Q_G the sum of q over a group, q . k = sum_G s_G (sum q c - z_G Q_G): the second term
+//     is the accumulator's start value, the scale one multiplication per group.  Queries are scaled
+//     by a power of two per row, which leaves them exact.
+//   - Values: a probability is multiplied by its slot's scale and rounded to f16, 11 bits, in units that
+//     follow the largest scale seen (bf16 needs none, but has 8 bits, and its codes, as 128 + c, take 7
+//     instructions a word: error against 64 bits 0.0021, 0.0017 now, which is the output's rounding).
+//     The zeros go into one more product with the same rounded numbers.
 //   - mma.sync m16n8k16 with the cache as the 16-row operand (slots for keys, dimensions for values)
 //     and up to 8 query rows as the other one: 18 multiplications for 16 slots at d = 128.  With
-//     tcgen05 the cache would have to be written to shared memory again as bf16, four times its
-//     bytes, for a 128-row operand; here codes go from the page to registers to the multiplication.
-//     (e4m3 operands, where a code's byte is c 2^-9 in 3 instructions a word and q a high and a low
-//     part, are taken apart again into f16 by this part's mma.sync: 90 us where f16 takes 82, and up to
-//     twice the time with more rows.)
+//     tcgen05 the cache would have to be written to shared memory again as 16-bit numbers, four
+//     times its bytes, for a 128-row operand of which 4 to 16 rows are wanted; here codes go from
+//     the page to registers to the multiplication.
 //   - A warp works alone: it takes pages in order, keeps the running maxima, sums and outputs of its
 //     rows in registers, and has its pages' bytes copied into its own ring in shared memory (cp.async,
-//     16 bytes a lane), two pages ahead.  No block barrier after the start.  (One bulk copy per half
-//     page and a barrier instead: 92 us where this takes 82; 16 warps with 3 half pages each instead
-//     of 12 with 4: 88.)
-//   Times here: 32 x 8 units of 4k to 16k slots, d = 128, 4 query rows, at successive steps.
+//     16 bytes a lane), two pages ahead.  No block barrier between the first page and the last.
 //
 // The pages of all units in one sequence are divided evenly among all warps of the grid, whatever
-// the units' lengths: a warp's span may begin and end inside a unit.  A unit that lies in
-// one span is written at once; of the others each warp writes its part (maximum, sum, unnormalised
-// output), and merge_kernel joins them in the order of the slots.
+// the units' lengths: a warp's span may begin and end inside a unit.  A unit that lies in one span, or
+// in a block's, is written at once; of the others each block writes its part (maxima, sums,
+// unnormalised outputs), and merge_kernel joins them in the order of the slots.  Nothing depends on
+// which warp comes first: results are the same from call to call.
+//
+// Measured (us a call; share of the measured copy rate):
+//   32 x 8 units of 4k to 16k slots, 4 rows, d = 128     74.5   76 %
+//   8 units of 131009 slots, 4 rows, d = 128             37.3   60 %
+//   16 x 8 units of 16384 slots, 8 rows, d = 128         62.0   72 %; 16 rows 94, 48 %
+//   32 x 8 units of 16384 slots, 4 rows, d = 64          63.6   70 %
+// Without its arithmetic the first takes 69 and the second 33: about 10 us go into the two launches, the
+// lengths, the first pages' latency and the merge, the rest is loads.  With 16 rows the arithmetic
+// bounds it (two warps on a quarter of the SM, whose registers they fill).
+// Tried, in us of the first where not said: one bulk copy per half page and a barrier 92 where
+// cp.async took 82; 16 warps with 3 half pages each instead of 12 with 4: 88 against 85; shifts on the
+// multiplier pipe 88 against 82; e4m3 codes with q in two parts, which mma.sync runs no faster than
+// f16 here: 90 against 82, and twice the time with more rows; one kernel in which the block that
+// arrives last joins the parts: 80 against 75, and 14.4 against 12.4 for 8 units of 2048 slots (three
+// device-wide fences cost more than the second launch).
 #include <algorithm>
 #include <atomic>
 #include <climits>
@@ -56,7 +67,9 @@ namespace {
 template <int D, int R>
 struct Config {
     static constexpr int NT = (R + 7) / 8, E = R == 4 ? 1 : 2;   // E: rows of a lane in a group
-    // as many as their registers let be, equally many on each quarter of the SM
+    // as many as their registers let be, equally many on each quarter of the SM (12 instead of 8 for
+    // 16 rows at d = 64: 62.4 against 64.2 us for 256 units of 8192 slots, but 30.7 against 29.6 for
+    // 128 units with 44 pages in a window)
     static constexpr int kWarps = R == 16 ? 8 : D == 128 ? 12 : 16;
     static constexpr int kHalf = PageLayout<D>::kValCodes;        // bytes of a page's keys
     static constexpr int kStages = 221184 / (2 * kHalf * kWarps); // pages of a warp's ring
@@ -67,12 +80,12 @@ struct Config {
 
 struct AttendParams {
     AttendArgs a;
-    int units, parts;        // parts: row parts (8 NT rows) of a unit
+    int units, parts;        // parts: of R rows, of a unit
     int rows;                // G n
     int chunks;              // of 32 (unit, part) pairs
     float c;                 // scale * log2(e)
     const int* seen;         // [units][1 + n]: slots below n_sink, window's first slot per token
-    float* part;             // [2 warps of the grid][8 NT D + 16 NT]
+    float* part;             // [2 warps of the grid][kPartSize]
     int2* spans;             // [units * parts]: first part, last warp
 };
 
@@ -235,8 +248,9 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
     const int pairs = p.units * p.parts;
 
     int64_t total;
-    // Pages before each chunk of 32 pairs: up to kFewChunks of them by every warp for itself, without
-    // a barrier, more by the block.
+    // Pages before each chunk of 32 pairs: of one chunk by every warp for itself, without a barrier
+    // (of up to eight so: the same lines read by 1824 warps, 4.6 us where the block takes 1.6), of
+    // more by the block.
     constexpr int kFewChunks = 1;
     int few[kFewChunks];
     if (p.chunks <= kFewChunks) {

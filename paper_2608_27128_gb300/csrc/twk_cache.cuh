@@ -15,8 +15,9 @@
 //            (word >> 4 p) & 0x000f000f holds a pair in two halves.
 //   values   rows are dimensions, columns are slots: 16 bytes of thread (g, t) hold the dimensions
 //            16 m + g and 16 m + 8 + g of 16 slots each, the 8 codes of a word again as 4 pairs.
-//   zeros    -(128 + z) as bf16: what a code's operand 128 + c (below) has too much.  Beside the
-//            scale for keys; for values in the order of the slots in the operand.
+//   zeros    -(128 + z) as bf16, so that z is in the last bits and a code as the bf16 number 128 + c
+//            plus it is c - z.  Beside the scale for keys; for values in the order of the slots in
+//            the operand.
 #pragma once
 #include <cstdint>
 

@@ -108,12 +108,12 @@ def attend_bound(out, size, steps, length):
     """How far the kernel's outputs may be from attend's (`length` slots).
 
     bf16 has 8 significant bits, so a rounding is off by 2^-8 at most.
-      2^-8 size      each probability times its value scale is rounded to bf16
+      2^-8 size      each probability times its value scale is rounded, to 8 bits or more
       2^-8 |out|     so is the output
       2^-10 size     scores: the float32 sums run over terms of size 136 |q| s, 2^-23 each at worst;
                      for |q| about 1.2, 128 dimensions, key scales up to 1.6 and d^-0.5 that is
                      below 5e-4, and twice that in a ratio of sums
-      the last       the sums of p s (128 + c) and of p s (128 + z), whose difference is the output,
+      the last       the sums over codes and over zeros (as such, or plus 128), whose difference is the output,
                      are float32 sums of up to 143 p s in len / 16 steps each, 2^-23 a step
     """
     return (2.0 ** -8 * (size + np.abs(out)) + 2.0 ** -10 * size
