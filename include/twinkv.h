@@ -518,7 +518,8 @@ size_t twinkv_cache_attend_workspace(twinkv_queries s, int32_t d);
  * above its own minus `window` or below n_sink (the sinks and the recent region of Sec. 3.2).
  *   o = sum_j softmax_j(scale q . k_j) v_j      float32 sums; a token that sees nothing: 0
  * Precision: codes and queries enter exactly; a probability times its slot's value scale is
- * rounded to 11 bits, the result to bf16.
+ * rounded to 11 bits (fewer where the scale is below 2^-16 of the largest among the slots of
+ * the pages visited), the result to bf16.
  *   q           [B][n][Hq][d] bf16, 16-byte aligned, strides in s (multiples of 8)
  *   scale       finite, above 0
  *   window      0: none (n_sink is then not used)

@@ -291,6 +291,31 @@ def test_attend_scale_and_strides():
     check_attend(np.random.default_rng(3), [300, 20], 2, 4, 3, 128, strided=True)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("sizes", [[0, 0, 1], [1, 2.0 ** 12, 2.0 ** 24], [2.0 ** 24, 2.0 ** 12, 1],
+                                   [2.0 ** -100, 1, 2.0 ** 100], [2.0 ** -118, 2.0 ** -118, 0],
+                                   [2.0 ** 100, 0, 2.0 ** 100]])
+def test_attend_value_scales_that_change_from_page_to_page(d, sizes):
+    """Values of three pages many powers of two apart, per group another order: the probabilities'
+    units follow the largest.  What is small beside the largest of its group counts as little."""
+    rng = np.random.default_rng(d)
+    n = 64 * len(sizes)
+    k, v = f64(rng_rows(rng, n, d)), f64(rng_rows(rng, n, d, outliers=False))
+    factor = np.repeat(np.array(sizes, np.float64), 64)[:, None]
+    v[:, :64] *= factor
+    v[:, 64:] *= factor[::-1]
+    pos = np.arange(n)
+    raw = np.stack([R.page_of(k[i:i + 64], v[i:i + 64], pos[i:i + 64]) for i in range(0, n, 64)])
+    q = rng_rows(rng, 1, 1, 4, d)
+    table = put(np.arange(len(sizes), dtype=np.int32).reshape(1, 1, -1))
+    out = f64(tk.twinkv_cache_attend(q.to(device()), put(raw), table,
+                                     put(np.array([[n]], np.int32)))["out"])
+    want, _, *sz = R.attend(f64(q)[0], R.round_trip(k), R.round_trip(v), pos, d ** -0.5,
+                            v_scales=R.quantize(v)[1])
+    bound = R.attend_bound(want, *sz, n)
+    assert (np.abs(out[0] - want) <= bound).all(), (np.abs(out[0] - want) / bound).max()
+
+
 def test_attend_many_units_of_few_slots():
     """Spans that hold many units, some of them empty; and more units than a chunk of the grid's
     first step."""
