@@ -677,24 +677,27 @@ def _pool(pool):
     """(Pool, head dimension, CUDA device number) of a pool on the current device."""
     if not isinstance(pool, torch.Tensor):
         raise TypeError("pool must be a torch tensor")
-    shape = pool.shape
-    d = _PAGE_DIM.get(shape[1]) if len(shape) == 2 else None
+    shape, dev = pool.shape, pool.get_device()
+    d = _PAGE_DIM.get(shape[-1]) if len(shape) == 2 else None
     if d is None:
         raise ValueError("pool must be [n_pages, PAGE_BYTES[d]]")
-    dev = torch._C._cuda_getDevice() if pool.is_cuda else -1
-    if pool.get_device() != dev or dev < 0:
+    if dev < 0 or dev != torch._C._cuda_getDevice():
         raise ValueError(f"pool must live on the current CUDA device, not on {pool.device}")
-    _same(pool, "pool", torch.uint8, shape, dev)
+    if pool.dtype is not torch.uint8 or not pool.is_contiguous():
+        raise ValueError("pool must be contiguous uint8")
     return Pool(pool.data_ptr(), shape[0], d), d, dev
 
 
 def _table(table, name, units, dev: int):
     """A page table [*units, max_pages]; its last size."""
-    if not isinstance(table, torch.Tensor) or table.dim() != len(units) + 1:
-        raise ValueError(f"{name} must be [{', '.join(map(str, units))}, max_pages]")
-    pages = table.shape[-1]
-    _same(table, name, torch.int32, (*units, pages), dev)
-    return pages
+    if not isinstance(table, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    shape = table.shape
+    if (shape[:-1] != units or table.dtype is not torch.int32 or table.get_device() != dev
+            or not table.is_contiguous()):
+        raise ValueError(f"{name} must be contiguous int32 [{', '.join(map(str, units))}, "
+                         f"max_pages] on CUDA device {dev}")
+    return shape[-1]
 
 
 def _kind(t, name):
@@ -724,10 +727,8 @@ def _rows_dtype(dtype, name):
     raise ValueError(f"{name} must be bfloat16 or float32")
 
 
-def _on(dev: int, *named):
-    for t, name in named:
-        if t is not None and t.get_device() != dev:
-            raise ValueError(f"{name} must live on CUDA device {dev}, not on {t.device}")
+def _elsewhere(name, t, dev):
+    return ValueError(f"{name} must live on CUDA device {dev}, not on {t.device}")
 
 
 @functools.lru_cache(maxsize=1024)
@@ -763,24 +764,28 @@ def twinkv_qk_norm_rope(q, k, wq, wk, cos_sin, positions, eps=1e-6, *, out=None,
     x = k if q is None else q
     if not isinstance(x, torch.Tensor):
         raise TypeError("q and k must be torch tensors")
-    dev = torch._C._cuda_getDevice() if x.is_cuda else -1
-    if dev < 0:
-        raise ValueError("q and k must be CUDA tensors")
+    dev = x.get_device()
+    if dev < 0 or dev != torch._C._cuda_getDevice():
+        raise _elsewhere("q and k", x, "current")
     given = out or {}
-    oq = ok = None
+    oq = ok = qk = kk = oqk = okk = None
     if q is not None:
         oq = given.get("q")
         if oq is None:
             oq = _made(None, "q", q.dtype, q.shape, dev, stream)
+        qk, oqk = _kind(q, "q"), _kind(oq, "out q")
+        if oq.get_device() != dev:
+            raise _elsewhere("out q", oq, dev)
     if k is not None:
         ok = given.get("k")
         if ok is None:
             ok = _made(None, "k", k.dtype, k.shape, dev, stream)
-    s, dtype, T, d = _rope_plan(q if q is None else _kind(q, "q"), k if k is None else _kind(k, "k"),
-                                oq if q is None else _kind(oq, "out q"),
-                                ok if k is None else _kind(ok, "out k"),
-                                _kind(cos_sin, "cos_sin"))
-    _on(dev, (q, "q"), (k, "k"), (oq, "out q"), (ok, "out k"), (cos_sin, "cos_sin"))
+        kk, okk = _kind(k, "k"), _kind(ok, "out k")
+        if k.get_device() != dev or ok.get_device() != dev:
+            raise _elsewhere("k and out k", k if k.get_device() != dev else ok, dev)
+    s, dtype, T, d = _rope_plan(qk, kk, oqk, okk, _kind(cos_sin, "cos_sin"))
+    if cos_sin.get_device() != dev:
+        raise _elsewhere("cos_sin", cos_sin, dev)
     if wq is not None:
         _same(wq, "wq", dtype, (d,), dev)
     if wk is not None:
@@ -870,7 +875,8 @@ def twinkv_cache_append(k, v, positions, pool, table, lens, *, out=None, stream=
     s, B, n, H, dk = _append_plan(_kind(k, "k"), _kind(v, "v"))
     if dk != d:
         raise ValueError(f"the pool's pages hold rows of {d} values, k has {dk}")
-    _on(dev, (k, "k"), (v, "v"))
+    if k.get_device() != dev or v.get_device() != dev:
+        raise _elsewhere("k and v", k if k.get_device() != dev else v, dev)
     units = (B, H)
     _same(positions, "positions", torch.int32, (B, n), dev)
     pages = _table(table, "table", units, dev)
@@ -965,7 +971,8 @@ def twinkv_cache_attend(q, pool, table, lens, *, scale=None, window=0, n_sink=0,
         raise ValueError("lens must be [B, H]")
     units = lens.shape
     s, B, shape, need = _attend_plan(_kind(q, "q"), units[1], d)
-    _on(dev, (q, "q"))
+    if q.get_device() != dev:
+        raise _elsewhere("q", q, dev)
     if units[0] != B:
         raise ValueError(f"lens must be [{B}, H]")
     _same(lens, "lens", torch.int32, units, dev)
