@@ -247,26 +247,13 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, g = lane / 4, t = lane % 4;
     const int pairs = p.units * p.parts;
 
+    // Pages before each chunk of 32 pairs: a single chunk is summed by every warp for itself, without a
+    // barrier, more by the block (up to eight so by every warp: the same lines read by 1824 warps,
+    // 4.6 us where the block takes 1.6).
     int64_t total;
-    // Pages before each chunk of 32 pairs: of one chunk by every warp for itself, without a barrier
-    // (of up to eight so: the same lines read by 1824 warps, 4.6 us where the block takes 1.6), of
-    // more by the block.
-    constexpr int kFewChunks = 1;
-    int few[kFewChunks];
-    if (p.chunks <= kFewChunks) {
-#pragma unroll
-        for (int c = 0; c < kFewChunks; ++c) {
-            const int pair = 32 * c + lane;
-            few[c] = pair < pairs ? visit_of(p, pair / p.parts).count : 0;
-        }
-        int before = 0;
-#pragma unroll
-        for (int c = 0; c < kFewChunks; ++c) {
-            const int n = __reduce_add_sync(0xffffffffu, few[c]);
-            few[c] = before;
-            before += n;
-        }
-        total = before;
+    if (p.chunks == 1) {
+        total = __reduce_add_sync(0xffffffffu,
+                                  lane < pairs ? visit_of(p, lane / p.parts).count : 0);
     } else {
         for (int c = warp; c < p.chunks; c += C::kWarps) {
             const int pair = 32 * c + lane;
@@ -308,14 +295,7 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
     Place at = {};
     if (has_span) {
         int lo = 0, before = 0;              // last chunk that starts at or before `begin`
-        if (p.chunks <= kFewChunks) {
-#pragma unroll
-            for (int c = 1; c < kFewChunks; ++c)
-                if (c < p.chunks && few[c] <= begin) {
-                    lo = c;
-                    before = few[c];
-                }
-        } else {
+        if (p.chunks > 1) {
             for (int hi = p.chunks - 1; lo < hi;) {
                 const int mid = (lo + hi + 1) / 2;
                 if (chunk_pages[mid] <= begin) lo = mid;
