@@ -239,7 +239,7 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
     using C = Config<D, R>;
     constexpr int G = P::kGroups, M = D / 16, NT = C::NT, E = C::E;
     constexpr int kRows = R, kTiles = 2, kDims = 2;
-    extern __shared__ __align__(16) uint8_t smem[];
+    extern __shared__ __align__(128) uint8_t smem[];   // rows of a copy on whole lines of 128 bytes
     __shared__ int s_pair[C::kWarps], s_slot[C::kWarps];
     __shared__ bool s_begins[C::kWarps], s_ends[C::kWarps];
     int* chunk_pages = reinterpret_cast<int*>(smem + C::kWarps * C::kRing);
