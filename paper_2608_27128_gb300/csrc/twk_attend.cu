@@ -32,7 +32,7 @@
 //
 // The pages of all units in one sequence are divided evenly among all warps of the grid, whatever
 // the units' lengths: a warp's span may begin and end inside a unit.  A unit that lies in one span, or
-// in a block's, is written at once; of the others each block writes its part (maxima, sums,
+// in a block's, is written by the block; of the others each block writes its part (maxima, sums,
 // unnormalised outputs), and merge_kernel joins them in the order of the slots.  Nothing depends on
 // which warp comes first: results are the same from call to call.
 //
@@ -85,8 +85,9 @@ struct AttendParams {
     int chunks;              // of 32 (unit, part) pairs
     float c;                 // scale * log2(e)
     const int* seen;         // [units][1 + n]: slots below n_sink, window's first slot per token
-    float* part;             // [2 warps of the grid][kPartSize]
-    int2* spans;             // [units * parts]: first part, last warp
+    float* part;             // [warps of the grid + its blocks][kPartSize]
+    int2* split;             // [blocks of the grid]: pair that begins in the block and ends in another
+                             // one, or -1; whether one that began in another one ends in it
 };
 
 // What a query row part of a unit visits: the pages of the sinks, then those of the window.
@@ -118,6 +119,19 @@ __device__ __forceinline__ Visit visit_of(const AttendParams& p, int unit)
 // floats of a part: outputs, maxima, sums
 template <int D, int R>
 constexpr int kPartSize = R * (D + 2);
+
+// Parts of units that began before a warp's span and end in it are in the warp's slot; the block's first
+// is its head.  The block's tail: the part of a unit that begins in it and ends in another block.
+template <int D, int R>
+__device__ __forceinline__ int head_slot(int block)
+{
+    return block * Config<D, R>::kWarps;
+}
+template <int D, int R>
+__device__ __forceinline__ int tail_slot(int block)
+{
+    return kAttendBlocks * Config<D, R>::kWarps + block;
+}
 
 // row of out and out_lse
 __device__ __forceinline__ int64_t out_row(const AttendParams& p, int unit, int row)
@@ -240,8 +254,8 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
     constexpr int G = P::kGroups, M = D / 16, NT = C::NT, E = C::E;
     constexpr int kRows = R, kTiles = 2, kDims = 2;
     extern __shared__ __align__(128) uint8_t smem[];   // rows of a copy on whole lines of 128 bytes
-    __shared__ int s_pair[C::kWarps], s_slot[C::kWarps];
-    __shared__ bool s_begins[C::kWarps], s_ends[C::kWarps];
+    __shared__ int s_pair[C::kWarps], s_rest[C::kWarps], s_head[C::kWarps];
+    __shared__ bool s_begins[C::kWarps];
     int* chunk_pages = reinterpret_cast<int*>(smem + C::kWarps * C::kRing);
     wait_for_previous();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, g = lane / 4, t = lane % 4;
@@ -284,7 +298,10 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
     // block's warps follow one another.
     const int64_t blocks = min(total, static_cast<int64_t>(gridDim.x));
     const int64_t workers = min(total, static_cast<int64_t>(gridDim.x) * C::kWarps);
-    if (blockIdx.x >= blocks) return;
+    if (blockIdx.x >= blocks) {
+        if (threadIdx.x == 0) p.split[blockIdx.x] = make_int2(-1, 0);
+        return;
+    }
     const int64_t index = workers * blockIdx.x / blocks + warp;
     const bool has_span = index < workers * (blockIdx.x + 1) / blocks;
     const int worker = blockIdx.x * C::kWarps + warp;
@@ -373,7 +390,7 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
     int limit[NT][E], from[NT][E];    // row sees slots < limit that are >= from or < sinks
     int sinks = 0, all_limit = 0, all_from = 0;
     int seg_begin = 0;
-    bool first_seg = true;
+    if (lane == 0) s_head[warp] = -1;    // the pair that began before the span and ends inside it
 
     auto start_unit = [&]() {
         const int unit = at.pair / p.parts, r0 = at.pair % p.parts * kRows;
@@ -507,11 +524,10 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
     auto finish_unit = [&]() {
         close_rows();
         if (seg_begin > 0) {
-            put_part(p.part + static_cast<int64_t>(2 * worker) * kPartSize<D, R>);
-            if (lane == 0) p.spans[at.pair].y = worker;
+            put_part(p.part + static_cast<int64_t>(worker) * kPartSize<D, R>);
+            if (lane == 0) s_head[warp] = at.pair;
             return;
         }
-        if (lane == 0) p.spans[at.pair] = make_int2(0, -1);
         const int r0 = at.pair % p.parts * kRows;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -799,7 +815,6 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
         --todo;
         if (todo > 0 && at.j == at.v.count) {
             finish_unit();
-            first_seg = false;
             do {
                 ++at.pair;
                 at.v = visit_of(p, at.pair / p.parts);
@@ -818,20 +833,32 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
     }
     if (lane == 0) {
         s_pair[warp] = has_span ? at.pair : -1;
-        s_slot[warp] = 2 * worker + (first_seg ? 0 : 1);
+        s_rest[warp] = at.v.count - at.j;
         s_begins[warp] = seg_begin == 0;
-        s_ends[warp] = at.j == at.v.count;
     }
     __syncthreads();
-    // a warp per run of such warps and row
+    // a warp per run of such warps and row; the next warp may have the rest of the unit as its head
     for (int w0 = 0, w1, turn = warp; w0 < C::kWarps && s_pair[w0] >= 0; w0 = w1, turn += kRows) {
         const int pair = s_pair[w0], unit = pair / p.parts, r0 = pair % p.parts * kRows;
         for (w1 = w0 + 1; w1 < C::kWarps && s_pair[w1] == pair; ++w1) {}
-        const bool begins = s_begins[w0], ends = s_ends[w1 - 1], whole = begins && ends;
-        float* part = p.part + static_cast<int64_t>(s_slot[w0]) * kPartSize<D, R>;
+        const bool with_head = w1 < C::kWarps && s_head[w1] == pair;
+        const bool begins = s_begins[w0], ends = with_head || s_rest[w1 - 1] == 0;
+        const float* rest = p.part + static_cast<int64_t>(worker - warp + w1) * kPartSize<D, R>;
         for (int r = turn % C::kWarps; r < kRows; r += C::kWarps) {
             constexpr int kVec = D / 32;
             float m = -INFINITY, l = 0.0f, acc[kVec] = {};
+            float m_rest = -INFINITY, l_rest = 0.0f, rest_acc[kVec] = {};
+            if (with_head) {
+                m = m_rest = rest[kRows * D + r];
+                l_rest = rest[kRows * D + kRows + r];
+#pragma unroll
+                for (int v = 0; v < kVec; v += 2) {
+                    const float2 y =
+                        *reinterpret_cast<const float2*>(rest + r * D + 32 * v + 2 * lane);
+                    rest_acc[v] = y.x;
+                    rest_acc[v + 1] = y.y;
+                }
+            }
             for (int w = w0; w < w1; ++w)
                 m = fmaxf(m, reinterpret_cast<const float*>(smem + w * C::kRing)[kRows * D + r]);
             for (int w = w0; w < w1 && m > -INFINITY; ++w) {
@@ -846,7 +873,16 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
                     acc[v + 1] = fmaf(y.y, f, acc[v + 1]);
                 }
             }
-            if (!whole) {
+            if (with_head && m > -INFINITY) {
+                const float f = exp2_approx((m_rest - m) * p.c);
+                l = fmaf(l_rest, f, l);
+#pragma unroll
+                for (int v = 0; v < kVec; ++v) acc[v] = fmaf(rest_acc[v], f, acc[v]);
+            }
+            if (!begins || !ends) {
+                float* part = p.part + static_cast<int64_t>(begins ? tail_slot<D, R>(blockIdx.x)
+                                                                   : head_slot<D, R>(blockIdx.x)) *
+                                           kPartSize<D, R>;
 #pragma unroll
                 for (int v = 0; v < kVec; v += 2)
                     *reinterpret_cast<float2*>(part + r * D + 32 * v + 2 * lane) =
@@ -866,40 +902,42 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
             }
         }
         if (threadIdx.x == 0) {
-            if (whole) p.spans[pair] = make_int2(0, -1);
-            if (!whole && begins) p.spans[pair].x = s_slot[w0];
-            if (!whole && ends) p.spans[pair].y = blockIdx.x * C::kWarps + w1 - 1;
+            if (w0 == 0) p.split[blockIdx.x].y = begins ? s_head[0] >= 0 : ends;
+            if (w1 == C::kWarps || s_pair[w1] < 0)
+                p.split[blockIdx.x].x = begins && !ends ? pair : -1;
         }
-        // merge_kernel looks at the unit's last worker, whose part is in the run's first one's
-        if (!whole && ends && w1 - w0 > 1)
-            for (int r = threadIdx.x; r < 2 * kRows; r += 32 * C::kWarps)
-                p.part[static_cast<int64_t>(s_slot[w1 - 1]) * kPartSize<D, R> + kRows * D + r] =
-                    r < kRows ? -INFINITY : 0.0f;
     }
 }
 
-// One block per (unit, part) pair and row: joins the parts of a unit that several blocks took, in
-// the order of its slots, and writes the rows of units without slots.  Its parts are those of the
-// warp it begins in, of the first warp of every block after that, and of the warp it ends in.
-// Bound by latency: lengths and spans are read together, then every warp reads four parts at once,
-// maxima, sums and outputs, and joins them as it would pages; the warps' results are joined in order.
-// The last row of blocks checks lengths and page numbers.
+// Joins the parts of a unit that several blocks took, in the order of its slots: a block per block that
+// such a unit begins in and row.  Its parts are that block's tail and the heads of the blocks after it, up
+// to the one it ends in.  Bound by latency: every warp reads four parts at once, maxima, sums and
+// outputs, and joins them as it would pages; the warps' results are joined in order.  (Blocks for
+// every pair and row, most of which find nothing to do: 37 us for 2048 pairs of 16 rows.)  The
+// blocks past the rows are the units': each checks the length and page numbers of one, and writes
+// the rows of one without slots.
 constexpr int kMergeWarps = 4, kMergeParts = 4;
 
 template <int D, int R>
 __global__ void __launch_bounds__(32 * kMergeWarps)
-    merge_kernel(const __grid_constant__ AttendParams p)
+    merge_kernel(const __grid_constant__ AttendParams p, int rows)
 {
-    constexpr int kRows = R, kWarps = Config<D, R>::kWarps, kVec = D / 32;
+    constexpr int kRows = R, kVec = D / 32;
     __shared__ float s_acc[kMergeWarps][D];
     __shared__ float s_top[kMergeWarps], s_sum[kMergeWarps];
     wait_for_previous();
-    const int pair = blockIdx.x, unit = pair / p.parts, r = blockIdx.y;
-    const int row = pair % p.parts * kRows + r, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    if (blockIdx.y == gridDim.y - 1) {
-        if (pair % p.parts != 0 || !p.a.out_status) return;
+    if (static_cast<int>(blockIdx.y) >= rows) {
+        const int unit = (blockIdx.y - rows) * gridDim.x + blockIdx.x;
+        if (unit >= p.units) return;
         const int len = p.a.lens[unit];
         bool bad = len < 0 || len > static_cast<int64_t>(p.a.from.max_pages) * kPage;
+        if (bad || len == 0)
+            for (int i = threadIdx.x; i < p.rows * (D / 2); i += 32 * kMergeWarps) {
+                const int64_t at = out_row(p, unit, i / (D / 2));
+                reinterpret_cast<uint32_t*>(p.a.out + at * D)[i % (D / 2)] = 0;
+                if (p.a.out_lse && i % (D / 2) == 0) p.a.out_lse[at] = -INFINITY;
+            }
+        if (!p.a.out_status) return;
         if (!bad)
             for (int j = threadIdx.x; j * kPage < len; j += 32 * kMergeWarps)
                 bad |= static_cast<unsigned>(
@@ -909,14 +947,20 @@ __global__ void __launch_bounds__(32 * kMergeWarps)
         if (threadIdx.x == 0) p.a.out_status[unit] = bad ? TWINKV_ERR_INVALID_ARG : TWINKV_OK;
         return;
     }
-    if (row >= p.rows) return;
-    const int2 span = p.spans[pair];   // of a unit with pages
-    int n = 0;
-    if (visit_of(p, unit).count > 0) {
-        if (span.y < 0) return;        // written already
-        n = span.y / kWarps - span.x / 2 / kWarps + 1;
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    int parts = 1;                     // up to the first block after this one that a unit ends in
+    bool open = true;
+#pragma unroll
+    for (int i = 0; i < (kAttendBlocks + 31) / 32; ++i) {
+        const int b = 32 * i + lane;
+        const bool ends = b > blockIdx.x && b < gridDim.x && p.split[b].y;
+        const unsigned at = __ballot_sync(0xffffffffu, ends);
+        if (open && at) parts = 32 * i + __ffs(at) - blockIdx.x;
+        open &= at == 0;
     }
-    const int parts = n + (n > 0 && span.y % kWarps != 0 && span.y != span.x / 2);
+    const int pair = p.split[blockIdx.x].x;
+    const int unit = pair / p.parts, r = blockIdx.y, row = pair % p.parts * kRows + r;
+    if (pair < 0 || row >= p.rows) return;
     float top = -INFINITY, sum = 0.0f, acc[kVec] = {};
     for (int i0 = warp; i0 < parts; i0 += kMergeWarps * kMergeParts) {
         float m[kMergeParts], l[kMergeParts], y[kMergeParts][kVec];
@@ -925,9 +969,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps)
             const int i = i0 + k * kMergeWarps;
             m[k] = -INFINITY;
             if (i >= parts) continue;
-            const int slot = i == 0  ? span.x
-                             : i < n ? 2 * kWarps * (span.x / 2 / kWarps + i)
-                                     : 2 * span.y;
+            const int slot = i == 0 ? tail_slot<D, R>(blockIdx.x) : head_slot<D, R>(blockIdx.x + i);
             const float* x = p.part + static_cast<int64_t>(slot) * kPartSize<D, R>;
             m[k] = x[kRows * D + r];
             l[k] = x[kRows * D + kRows + r];
@@ -1064,26 +1106,27 @@ cudaError_t launch(AttendParams& p, int sms, cudaStream_t st)
         e = cudaGetLastError();
     }
     if (e != cudaSuccess) return e;
+    const int rows = std::min(p.rows, R);
     return launch_dependent(merge_kernel<D, R>,
-                            dim3(p.units * p.parts, std::min(p.rows, 8 * C::NT) + 1), 32 * kMergeWarps, 0,
-                            st, p);
+                            dim3(grid.x, rows + (p.units + grid.x - 1) / grid.x), 32 * kMergeWarps,
+                            0, st, p, rows);
 }
 
 }  // namespace
 
-// Two parts for each warp of the largest grid; as many warps as any of the kernels of 8 rows, or of 16,
-// has.
+// A part for each warp and block of the largest grid; as many warps as any of the kernels of 8 rows, or of
+// 16, has.
 template <int R>
-constexpr size_t kParts = 2 * kAttendBlocks *
-                          std::max(std::max(Config<64, R>::kWarps, Config<128, R>::kWarps),
-                                   R == 8 ? std::max(Config<64, 4>::kWarps, Config<128, 4>::kWarps)
-                                          : 0);
+constexpr size_t kParts =
+    kAttendBlocks * (1 + std::max(std::max(Config<64, R>::kWarps, Config<128, R>::kWarps),
+                                  R == 8 ? std::max(Config<64, 4>::kWarps, Config<128, 4>::kWarps)
+                                         : 0));
 
-// spans, then windows, then parts
+// blocks' split units, then windows, then parts
 size_t attend_workspace(int units, int rows, int n, int d)
 {
-    const int pr = part_rows(rows), parts = (rows + pr - 1) / pr;
-    return up256(static_cast<size_t>(units) * parts * sizeof(int2)) +
+    const int pr = part_rows(rows);
+    return up256(kAttendBlocks * sizeof(int2)) +
            up256(static_cast<size_t>(units) * (1 + n) * 4) +
            up256((pr == 8 ? kParts<8> : kParts<16>) * (pr * d + 2 * pr) * 4);
 }
@@ -1099,8 +1142,8 @@ cudaError_t launch_attend(const AttendArgs& a, int sms, cudaStream_t st)
     p.chunks = (p.units * p.parts + 31) / 32;
     p.c = a.scale * 1.4426950408889634f;
     uint8_t* ws = static_cast<uint8_t*>(a.ws);
-    p.spans = reinterpret_cast<int2*>(ws);
-    ws += up256(static_cast<size_t>(p.units) * p.parts * sizeof(int2));
+    p.split = reinterpret_cast<int2*>(ws);
+    ws += up256(kAttendBlocks * sizeof(int2));
     p.seen = a.window > 0 ? reinterpret_cast<const int*>(ws) : nullptr;
     ws += up256(static_cast<size_t>(p.units) * (1 + a.n) * 4);
     p.part = reinterpret_cast<float*>(ws);
