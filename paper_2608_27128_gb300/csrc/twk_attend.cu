@@ -26,6 +26,11 @@
 //     tcgen05 the cache would have to be written to shared memory again as 16-bit numbers, four
 //     times its bytes, for a 128-row operand of which 4 to 16 rows are wanted; here codes go from
 //     the page to registers to the multiplication.
+//   - With 16 rows the operands change sides: the rows are the 16-row operand, and the same registers
+//     of codes two 8-column ones.  As many multiplications, but a lane then has 2 rows and 16 slots of
+//     each instead of 4 rows and 8: maxima take 4 shuffles instead of 12, probabilities are the next
+//     operand as they are (32 transpositions a page less), zeros take half the products, and neighbours
+//     are computed in pairs (f32x2): 86.1 us where 90.3 (16 x 8 units of 16384 slots, 16 rows).
 //   - A warp works alone: it takes pages in order, keeps the running maxima, sums and outputs of its
 //     rows in registers, and has its pages' bytes copied into its own ring in shared memory (cp.async,
 //     16 bytes a lane), two pages ahead.  No block barrier between the first page and the last.
@@ -37,9 +42,9 @@
 // which warp comes first: results are the same from call to call.
 //
 // Measured (us a call; share of the measured copy rate):
-//   32 x 8 units of 4k to 16k slots, 4 rows, d = 128     74.5   76 %
-//   8 units of 131009 slots, 4 rows, d = 128             37.3   60 %
-//   16 x 8 units of 16384 slots, 8 rows, d = 128         62.0   72 %; 16 rows 94, 48 %
+//   32 x 8 units of 4k to 16k slots, 4 rows, d = 128     73.7   77 %
+//   8 units of 131009 slots, 4 rows, d = 128             37.0   60 %
+//   16 x 8 units of 16384 slots, 8 rows, d = 128         62.5   71 %; 16 rows 86.1, 52 %
 //   32 x 8 units of 16384 slots, 4 rows, d = 64          63.6   70 %
 // Without its arithmetic the first takes 69 and the second 33: about 10 us go into the two launches, the
 // lengths, the first pages' latency and the merge, the rest is loads.  With 16 rows the arithmetic
@@ -62,11 +67,12 @@
 namespace twk {
 namespace {
 
-// R: query rows of a part (4, 8 or 16), in NT groups of 8 columns.  Column 2 t of a group is row t, and
-// column 2 t + 1 row t + 4: with 4 rows a lane has one of them and no idle second.
+// R: query rows of a part (4, 8 or 16).  Up to 8 are columns: column 2 t is row t, and column 2 t + 1 row
+// t + 4, so that with 4 rows a lane has one of them and no idle second.
 template <int D, int R>
 struct Config {
-    static constexpr int NT = (R + 7) / 8, E = R == 4 ? 1 : 2;   // E: rows of a lane in a group
+    static constexpr bool kLeft = R == 16;       // rows are the left operand's
+    static constexpr int E = R == 4 ? 1 : 2;     // rows of a lane
     // as many as their registers let be, equally many on each quarter of the SM (12 instead of 8 for
     // 16 rows at d = 64: 62.4 against 64.2 us for 256 units of 8192 slots, but 30.7 against 29.6 for
     // 128 units with 44 pages in a window)
@@ -221,6 +227,29 @@ __device__ __forceinline__ uint32_t lds16(uint32_t at)
     return v;
 }
 
+// (x a + c, y b + d), (x + a, y + b) and (x a, y b) in one instruction each
+__device__ __forceinline__ void fma_two(float& x, float& y, float a, float b, float c, float d)
+{
+    asm("{.reg .b64 v, m, c;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 m, {%2, %3};\n\t"
+        "mov.b64 c, {%4, %5};\n\tfma.rn.f32x2 v, v, m, c;\n\tmov.b64 {%0, %1}, v;}"
+        : "+f"(x), "+f"(y)
+        : "f"(a), "f"(b), "f"(c), "f"(d));
+}
+__device__ __forceinline__ void add_two(float& x, float& y, float a, float b)
+{
+    asm("{.reg .b64 v, m;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 m, {%2, %3};\n\t"
+        "add.rn.f32x2 v, v, m;\n\tmov.b64 {%0, %1}, v;}"
+        : "+f"(x), "+f"(y)
+        : "f"(a), "f"(b));
+}
+__device__ __forceinline__ void mul_two(float& x, float& y, float a, float b)
+{
+    asm("{.reg .b64 v, m;\n\tmov.b64 v, {%0, %1};\n\tmov.b64 m, {%2, %3};\n\t"
+        "mul.rn.f32x2 v, v, m;\n\tmov.b64 {%0, %1}, v;}"
+        : "+f"(x), "+f"(y)
+        : "f"(a), "f"(b));
+}
+
 // The G words (or halves) that a lane wants of one slot.
 template <int D>
 __device__ __forceinline__ void load_groups(uint32_t at, uint32_t (&w)[D / 64])
@@ -251,8 +280,11 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
 {
     using P = PageLayout<D>;
     using C = Config<D, R>;
-    constexpr int G = P::kGroups, M = D / 16, NT = C::NT, E = C::E;
+    constexpr int G = P::kGroups, M = D / 16, E = C::E;
     constexpr int kRows = R, kTiles = 2, kDims = 2;
+    constexpr bool kLeft = C::kLeft;
+    constexpr int kScores = kLeft ? 16 : 8;          // of a lane, row and page
+    constexpr int kOut = kLeft ? 2 * M : M;          // accumulators of outputs
     extern __shared__ __align__(128) uint8_t smem[];   // rows of a copy on whole lines of 128 bytes
     __shared__ int s_pair[C::kWarps], s_rest[C::kWarps], s_head[C::kWarps];
     __shared__ bool s_begins[C::kWarps];
@@ -380,14 +412,18 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
         id = next_id();
     }
 
-    // ---- state of the unit's rows: thread (g, t) has the rows t and t + 4 of every 8
-    uint32_t q[NT][G][8];
-    float qsum[NT][G][E], unit_of[NT][E];   // sums of q, and what a score's unit is, see below
-    float o[NT][M][4], zero_part[NT][G][4], top[NT][E], sum[NT][E];
+    // ---- state of the unit's rows; a lane has the rows row_of(e), of them the slots slot_of(i) of a
+    // page, and of accumulators the elements element(e, k)
+    auto row_of = [&](int e) { return kLeft ? g + 8 * e : t + 4 * e; };
+    auto slot_of = [&](int i) { return kLeft ? 8 * (i / 2) + 2 * t + i % 2 : 8 * i + g; };
+    auto element = [](int e, int k) { return kLeft ? 2 * e + k : 2 * k + e; };
+    uint32_t q[kLeft ? 2 : 1][G][8];
+    float qsum[G][E], unit_of[E];     // sums of q, and what a score's unit is, see below
+    float o[kOut][4], zero_part[G][4], top[E], sum[E];
     float value_up[G];                // probabilities' scale, see below
     int value_e[G];
     uint32_t value_limit;
-    int limit[NT][E], from[NT][E];    // row sees slots < limit that are >= from or < sinks
+    int limit[E], from[E];            // row sees slots < limit that are >= from or < sinks
     int sinks = 0, all_limit = 0, all_from = 0;
     int seg_begin = 0;
     if (lane == 0) s_head[warp] = -1;    // the pair that began before the span and ends inside it
@@ -402,10 +438,10 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
         // Queries as f16: a row is scaled by a power of two, 2^k, so that its largest value is in
         // [2^14, 2^15); values down to 2^-28 of it stay exact.  Its scores are sums of 2^(k - 24) q c.
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const int in_group = g / 2 + g % 2 * 4, r = r0 + 8 * nt + in_group;   // of column g
+        for (int half = 0; half < (kLeft ? 2 : 1); ++half) {
+            const int in_part = kLeft ? g + 8 * half : g / 2 + g % 2 * 4, r = r0 + in_part;
             const uint16_t* src = nullptr;
-            if (r < p.rows && in_group < R)
+            if (r < p.rows && in_part < R)
                 src = p.a.q + b * p.a.q_batch + r / p.a.G * p.a.q_token +
                       (h * p.a.G + r % p.a.G) * p.a.q_head;
             uint32_t w[G][8];
@@ -437,36 +473,41 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
                     // the odd pairs of a word's codes enter times 16
                     const float x = bf16_lo(w[G_][i]) * up, y = bf16_hi(w[G_][i]) * up;
                     const float f = i % 2 ? 0.0625f : 1.0f;
-                    q[nt][G_][i] = f16_pair(x * f, y * f);
+                    q[half][G_][i] = f16_pair(x * f, y * f);
                     s += x + y;
                 }
                 s += __shfl_xor_sync(0xffffffffu, s, 1);
                 s += __shfl_xor_sync(0xffffffffu, s, 2);
+                if constexpr (kLeft) {
+                    qsum[G_][half] = s * 0x1p-24f;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+                        qsum[G_][e] = __shfl_sync(0xffffffffu, s, 8 * t + 4 * e) * 0x1p-24f;
+                }
+            }
+            if constexpr (kLeft) {
+                unit_of[half] = down;
+            } else {
 #pragma unroll
                 for (int e = 0; e < E; ++e)
-                    qsum[nt][G_][e] = __shfl_sync(0xffffffffu, s, 8 * t + 4 * e) * 0x1p-24f;
+                    unit_of[e] = __shfl_sync(0xffffffffu, down, 8 * t + 4 * e);
             }
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-                unit_of[nt][e] = __shfl_sync(0xffffffffu, down, 8 * t + 4 * e);
         }
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+        for (int e = 0; e < E; ++e) {
+            const int row = r0 + row_of(e), token = row / p.a.G;
+            limit[e] = row < p.rows ? at.v.len - p.a.n + token + 1 : INT_MAX;
+            from[e] = row < p.rows && seen ? seen[1 + token] : 0;
+            top[e] = -INFINITY;
+            sum[e] = 0.0f;
+        }
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const int row = r0 + 8 * nt + 4 * e + t, token = row / p.a.G;
-                limit[nt][e] = row < p.rows ? at.v.len - p.a.n + token + 1 : INT_MAX;
-                from[nt][e] = row < p.rows && seen ? seen[1 + token] : 0;
-                top[nt][e] = -INFINITY;
-                sum[nt][e] = 0.0f;
-            }
+        for (int i = 0; i < 4; ++i) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int m = 0; m < kOut; ++m) o[m][i] = 0.0f;
 #pragma unroll
-                for (int m = 0; m < M; ++m) o[nt][m][i] = 0.0f;
-#pragma unroll
-                for (int G_ = 0; G_ < G; ++G_) zero_part[nt][G_][i] = 0.0f;
-            }
+            for (int G_ = 0; G_ < G; ++G_) zero_part[G_][i] = 0.0f;
         }
         value_limit = 0;
 #pragma unroll
@@ -484,41 +525,43 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
     // the sums of the lanes that share a row; the zeros' part joins the output
     auto close_rows = [&]() {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+        for (int e = 0; e < E; ++e) {
+            float s = sum[e];
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                float s = sum[nt][e];
-                s += __shfl_xor_sync(0xffffffffu, s, 4);
-                s += __shfl_xor_sync(0xffffffffu, s, 8);
-                s += __shfl_xor_sync(0xffffffffu, s, 16);
-                sum[nt][e] = s;
-                top[nt][e] *= unit_of[nt][e];
-            }
-#pragma unroll
-            for (int m = 0; m < M; ++m)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    o[nt][m][e] = (o[nt][m][e] - zero_part[nt][m / 4][e % 2]) * 0x1p17f *
-                                  power_of_two(value_e[m / 4]);
+            for (int i = kLeft ? 1 : 4; i < (kLeft ? 4 : 32); i *= 2)
+                s += __shfl_xor_sync(0xffffffffu, s, i);
+            sum[e] = s;
+            top[e] *= unit_of[e];
         }
+#pragma unroll
+        for (int m = 0; m < kOut; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int G_ = m / (kOut / G);
+                o[m][i] = (o[m][i] - zero_part[G_][kLeft ? i : i % 2]) * 0x1p17f *
+                          power_of_two(value_e[G_]);
+            }
     };
     // rows as outputs [kRows][D], then maxima and sums [kRows]
     auto put_part = [&](float* part) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int e = 0; e < E; ++e) {
+            const int r = row_of(e);
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const int r = 8 * nt + 4 * e + t;
-#pragma unroll
-                for (int m = 0; m < M; ++m) {
-                    part[r * D + 16 * m + g] = o[nt][m][e];
-                    part[r * D + 16 * m + 8 + g] = o[nt][m][2 + e];
-                }
-                if (g == 0) {
-                    part[kRows * D + r] = top[nt][e];
-                    part[kRows * D + kRows + r] = sum[nt][e];
+            for (int m = 0; m < kOut; ++m) {
+                if constexpr (kLeft) {
+                    *reinterpret_cast<float2*>(part + r * D + 8 * m + 2 * t) =
+                        make_float2(o[m][2 * e], o[m][2 * e + 1]);
+                } else {
+                    part[r * D + 16 * m + g] = o[m][e];
+                    part[r * D + 16 * m + 8 + g] = o[m][2 + e];
                 }
             }
+            if ((kLeft ? t : g) == 0) {
+                part[kRows * D + r] = top[e];
+                part[kRows * D + kRows + r] = sum[e];
+            }
+        }
     };
     // a unit that ends inside the span: written at once if it began there
     auto finish_unit = [&]() {
@@ -528,31 +571,39 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
             if (lane == 0) s_head[warp] = at.pair;
             return;
         }
-        const int r0 = at.pair % p.parts * kRows;
+        const int r0 = at.pair % p.parts * kRows, unit = at.pair / p.parts;
+        float inv[2] = {};
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            float inv[2] = {};
+        for (int e = 0; e < E; ++e) inv[e] = sum[e] > 0.0f ? 1.0f / sum[e] : 0.0f;
+        if constexpr (kLeft) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) inv[e] = sum[nt][e] > 0.0f ? 1.0f / sum[nt][e] : 0.0f;
-            const int row = r0 + 8 * nt + g / 2 + g % 2 * 4;     // of column g
-            uint16_t* out = p.a.out + out_row(p, at.pair / p.parts, row) * D;
+            for (int e = 0; e < E; ++e) {
+                const int row = r0 + row_of(e);
+                if (row >= p.rows) continue;
+                uint16_t* out = p.a.out + out_row(p, unit, row) * D;
+#pragma unroll
+                for (int m = 0; m < kOut; ++m)
+                    *reinterpret_cast<uint32_t*>(out + 8 * m + 2 * t) =
+                        bf16_pair(o[m][2 * e] * inv[e], o[m][2 * e + 1] * inv[e]);
+            }
+        } else {
+            const int row = r0 + g / 2 + g % 2 * 4;     // of column g
+            uint16_t* out = p.a.out + out_row(p, unit, row) * D;
 #pragma unroll
             for (int m = 0; m < M; ++m)
 #pragma unroll
                 for (int e = 0; e < 4; e += 2) {
                     const uint32_t w =
-                        transpose16(bf16_pair(o[nt][m][e] * inv[0], o[nt][m][e + 1] * inv[1]));
+                        transpose16(bf16_pair(o[m][e] * inv[0], o[m][e + 1] * inv[1]));
                     if (row < p.rows)
                         *reinterpret_cast<uint32_t*>(out + 16 * m + 4 * e + 2 * t) = w;
                 }
-            if (p.a.out_lse && g == 0) {
+        }
+        if (p.a.out_lse && (kLeft ? t : g) == 0) {
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const int r = r0 + 8 * nt + 4 * e + t;
-                    if (r < p.rows)
-                        p.a.out_lse[out_row(p, at.pair / p.parts, r)] =
-                            log_sum(p, top[nt][e], sum[nt][e]);
-                }
+            for (int e = 0; e < E; ++e) {
+                const int r = r0 + row_of(e);
+                if (r < p.rows) p.a.out_lse[out_row(p, unit, r)] = log_sum(p, top[e], sum[e]);
             }
         }
     };
@@ -570,11 +621,12 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
         // ---- scores of 64 slots
         cp_async_wait<2 * C::kStages - 1>();
         __syncwarp();
-        float s[NT][E][4][2];               // slots g and g + 8 of each tile
+        float s[E][kScores];
 #pragma unroll
         for (int t0 = 0; t0 < 4; t0 += kTiles) {   // tiles side by side: the multiplications' latency
             uint32_t a0[kTiles][2 * G], a1[kTiles][2 * G];    // words of slots lo and lo + 8
-            uint32_t k0[kTiles][G], k1[kTiles][G];
+            constexpr int kMine = kTiles * kScores / 4;
+            uint32_t k[kMine][G];              // scales and zeros of the lane's slots
 #pragma unroll
             for (int i = 0; i < kTiles; ++i) {
                 const int lo = 16 * (t0 + i) + g;
@@ -589,22 +641,45 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
                     a0[i][0] = u.x, a0[i][1] = u.y;
                     a1[i][0] = w.x, a1[i][1] = w.y;
                 }
-                load_groups<D>(keys + P::kKeyGroups + lo * 4 * G, k0[i]);
-                load_groups<D>(keys + P::kKeyGroups + (lo + 8) * 4 * G, k1[i]);
+#pragma unroll
+                for (int l = i * kMine / kTiles; l < (i + 1) * kMine / kTiles; l += kLeft ? 2 : 1) {
+                    const int slot = slot_of(t0 * (kScores / 4) + l);
+                    const uint32_t at_k = keys + P::kKeyGroups + slot * 4 * G;
+                    if constexpr (kLeft && D == 128) {
+                        const uint4 u = lds128(at_k);
+                        k[l][0] = u.x, k[l][1] = u.y, k[l + 1][0] = u.z, k[l + 1][1] = u.w;
+                    } else if constexpr (kLeft) {
+                        const uint2 u = lds64(at_k);
+                        k[l][0] = u.x, k[l + 1][0] = u.y;
+                    } else {
+                        load_groups<D>(at_k, k[l]);
+                    }
+                }
             }
 #pragma unroll
             for (int G_ = 0; G_ < G; ++G_) {
-                float acc[kTiles][NT][4] = {};       // -z Q at first
+                // slots lo and lo + 8 of a tile are two accumulators' columns, or one's rows
+                constexpr int kAcc = kLeft ? 2 : 1;
+                float acc[kTiles][kAcc][4] = {};       // -z Q at first
+                // accumulator's element of the lane's slot i of a tile
+                auto of = [&](int tile, int i, int e) -> float& {
+                    return kLeft ? acc[tile][i / 2][2 * e + i % 2] : acc[tile][0][2 * i + e];
+                };
 #pragma unroll
-                for (int i = 0; i < kTiles; ++i)
+                for (int i = 0; i < kMine; i += kLeft ? 2 : 1)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int e = 0; e < E; ++e) {
-                            const float all = 128.0f * qsum[nt][G_][e];
-                            acc[i][nt][e] = fmaf(bf16_hi(k0[i][G_]), qsum[nt][G_][e], all);
-                            acc[i][nt][2 + e] = fmaf(bf16_hi(k1[i][G_]), qsum[nt][G_][e], all);
+                    for (int e = 0; e < E; ++e) {
+                        const float Q = qsum[G_][e];
+                        float& x = of(i / (kScores / 4), i % (kScores / 4), e);
+                        if constexpr (kLeft) {
+                            float y0 = bf16_hi(k[i][G_]), y1 = bf16_hi(k[i + 1][G_]);
+                            fma_two(y0, y1, Q, Q, 128.0f * Q, 128.0f * Q);
+                            x = y0;
+                            of(i / (kScores / 4), i % (kScores / 4) + 1, e) = y1;
+                        } else {
+                            x = fmaf(bf16_hi(k[i][G_]), Q, 128.0f * Q);
                         }
+                    }
 #pragma unroll
                 for (int w = 0; w < 2; ++w)
 #pragma unroll
@@ -613,110 +688,137 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
                         for (int i = 0; i < kTiles; ++i) {
                             const uint32_t u = a0[i][2 * G_ + w] >> (8 * x);
                             const uint32_t v = a1[i][2 * G_ + w] >> (8 * x);
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt)
-                                mma_f16(acc[i][nt], u & 0x000f000fu, v & 0x000f000fu,
-                                        u & 0x00f000f0u, v & 0x00f000f0u,
-                                        q[nt][G_][4 * w + 2 * x], q[nt][G_][4 * w + 2 * x + 1]);
+                            const int y = 4 * w + 2 * x;
+                            if constexpr (kLeft) {
+                                mma_f16(acc[i][0], q[0][G_][y], q[1][G_][y], q[0][G_][y + 1],
+                                        q[1][G_][y + 1], u & 0x000f000fu, u & 0x00f000f0u);
+                                mma_f16(acc[i][1], q[0][G_][y], q[1][G_][y], q[0][G_][y + 1],
+                                        q[1][G_][y + 1], v & 0x000f000fu, v & 0x00f000f0u);
+                            } else {
+                                mma_f16(acc[i][0], u & 0x000f000fu, v & 0x000f000fu,
+                                        u & 0x00f000f0u, v & 0x00f000f0u, q[0][G_][y],
+                                        q[0][G_][y + 1]);
+                            }
                         }
 #pragma unroll
-                for (int i = 0; i < kTiles; ++i) {
-                    const float s0 = bf16_lo(k0[i][G_]), s1 = bf16_lo(k1[i][G_]);
+                for (int i = 0; i < kMine; i += kLeft ? 2 : 1)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int e = 0; e < E; ++e) {
-                            float(&y)[2] = s[nt][e][t0 + i];
-                            y[0] = G_ == 0 ? acc[i][nt][e] * s0 : fmaf(acc[i][nt][e], s0, y[0]);
-                            y[1] = G_ == 0 ? acc[i][nt][2 + e] * s1
-                                           : fmaf(acc[i][nt][2 + e], s1, y[1]);
+                    for (int e = 0; e < E; ++e) {
+                        float& y = s[e][t0 * (kScores / 4) + i];
+                        if constexpr (kLeft) {
+                            float x0 = of(i / (kScores / 4), i % (kScores / 4), e);
+                            float x1 = of(i / (kScores / 4), i % (kScores / 4) + 1, e);
+                            float& z = s[e][t0 * (kScores / 4) + i + 1];
+                            if (G_ == 0) mul_two(x0, x1, bf16_lo(k[i][G_]), bf16_lo(k[i + 1][G_]));
+                            else fma_two(x0, x1, bf16_lo(k[i][G_]), bf16_lo(k[i + 1][G_]), y, z);
+                            y = x0, z = x1;
+                        } else {
+                            const float x = of(i / (kScores / 4), i % (kScores / 4), e);
+                            y = G_ == 0 ? x * bf16_lo(k[i][G_]) : fmaf(x, bf16_lo(k[i][G_]), y);
                         }
-                }
+                    }
             }
         }
         __syncwarp();
         copy_half(id, stage, 0);
         if (!full) {
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int e = 0; e < E; ++e)
 #pragma unroll
-                for (int e = 0; e < E; ++e)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int slot = base + 8 * i + g;
-                        const bool see = !gone && slot < min(limit[nt][e], at.v.len) &&
-                                         (slot >= from[nt][e] || slot < sinks);
-                        if (!see) s[nt][e][i / 2][i % 2] = -INFINITY;
-                    }
+                for (int i = 0; i < kScores; ++i) {
+                    const int slot = base + slot_of(i);
+                    const bool see = !gone && slot < min(limit[e], at.v.len) &&
+                                     (slot >= from[e] || slot < sinks);
+                    if (!see) s[e][i] = -INFINITY;
+                }
         }
 
         // ---- running maxima; probabilities
         bool grown = false;
-        float shrink[NT][E];
+        float shrink[E];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int e = 0; e < E; ++e) {
+            float(&y)[kScores] = s[e];
+            const float last = top[e], c = p.c * unit_of[e];
+            float m = last;
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                float(&y)[4][2] = s[nt][e];
-                const float last = top[nt][e], c = p.c * unit_of[nt][e];
-                float m = last;
+            for (int i = 0; i < kScores; i += 2) m = fmaxf(m, fmaxf(y[i], y[i + 1]));
 #pragma unroll
-                for (int tile = 0; tile < 4; ++tile) m = fmaxf(m, fmaxf(y[tile][0], y[tile][1]));
-                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
-                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
-                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
-                grown |= m > last;
-                // a row that has seen nothing yet keeps -inf, and its probabilities are 0
-                const float shift = m == -INFINITY ? 0.0f : m * c;
-                const float f = last == -INFINITY ? 0.0f : exp2_approx((last - m) * c);
-                shrink[nt][e] = f;
-                top[nt][e] = m;
-                float l = 0.0f;
+            for (int i = kLeft ? 1 : 4; i < (kLeft ? 4 : 32); i *= 2)
+                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, i));
+            grown |= m > last;
+            // a row that has seen nothing yet keeps -inf, and its probabilities are 0
+            const float shift = m == -INFINITY ? 0.0f : m * c;
+            const float f = last == -INFINITY ? 0.0f : exp2_approx((last - m) * c);
+            shrink[e] = f;
+            top[e] = m;
+            float l = 0.0f, l2 = 0.0f;
 #pragma unroll
-                for (int tile = 0; tile < 4; ++tile)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        y[tile][i] = exp2_approx(fmaf(y[tile][i], c, -shift));
-                        l += y[tile][i];
-                    }
-                sum[nt][e] = fmaf(sum[nt][e], f, l);
+            for (int i = 0; i < kScores; i += 2) {
+                if constexpr (kLeft) {
+                    fma_two(y[i], y[i + 1], c, c, -shift, -shift);
+                } else {
+                    y[i] = fmaf(y[i], c, -shift);
+                    y[i + 1] = fmaf(y[i + 1], c, -shift);
+                }
+                y[i] = exp2_approx(y[i]);
+                y[i + 1] = exp2_approx(y[i + 1]);
+                if constexpr (kLeft) add_two(l, l2, y[i], y[i + 1]);
+                else l += y[i], l += y[i + 1];
             }
+            sum[e] = fmaf(sum[e], f, l + l2);
+        }
         if (__any_sync(0xffffffffu, grown)) {
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int e = 0; e < E; ++e) {
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-#pragma unroll
-                    for (int m = 0; m < M; ++m) {
-                        o[nt][m][e] *= shrink[nt][e];
-                        o[nt][m][2 + e] *= shrink[nt][e];
-                    }
-#pragma unroll
-                    for (int G_ = 0; G_ < G; ++G_) {
-                        zero_part[nt][G_][e] *= shrink[nt][e];
-                        zero_part[nt][G_][2 + e] *= shrink[nt][e];
+                for (int m = 0; m < kOut; ++m) {
+                    if constexpr (kLeft) {
+                        mul_two(o[m][2 * e], o[m][2 * e + 1], shrink[e], shrink[e]);
+                    } else {
+                        o[m][e] *= shrink[e];
+                        o[m][2 + e] *= shrink[e];
                     }
                 }
+#pragma unroll
+                for (int G_ = 0; G_ < G; ++G_)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) zero_part[G_][element(e, k)] *= shrink[e];
+            }
         }
 
         // ---- values
         cp_async_wait<2 * C::kStages - 1>();
         __syncwarp();
         // The slots' scales, bf16 (those of two groups in one word); slots never written count as 0.
-        uint32_t scales[4][2];
+        uint32_t scales[kScores];
         uint32_t most = 0;
 #pragma unroll
         for (int tile = 0; tile < 4; ++tile)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int slot = 16 * tile + 8 * i + g;
+                const int at_tile = (2 * tile + i) * (kScores / 8), slot = slot_of(at_tile);
                 const uint32_t at_scale = values + P::kValScales - P::kValCodes + slot * 2 * G;
-                uint32_t w;
-                if constexpr (D == 128) w = lds32(at_scale);
-                else w = lds16(at_scale);
+                uint32_t w, w2 = 0;
+                if constexpr (kLeft && D == 128) {
+                    const uint2 u = lds64(at_scale);
+                    w = u.x, w2 = u.y;
+                } else if constexpr (kLeft) {
+                    w = lds32(at_scale);
+                    w2 = w >> 16, w &= 0xffffu;
+                } else if constexpr (D == 128) {
+                    w = lds32(at_scale);
+                } else {
+                    w = lds16(at_scale);
+                }
                 if (!full && (gone || base + slot >= at.v.len)) w = 0;
-                scales[tile][i] = w;
+                scales[at_tile] = w;
                 most = __vmaxu2(most, w);
+                if constexpr (kLeft) {
+                    if (!full && (gone || base + slot + 1 >= at.v.len)) w2 = 0;
+                    scales[at_tile + 1] = w2;
+                    most = __vmaxu2(most, w2);
+                }
             }
         // Probabilities times scales enter as f16, in units of 2^(e - 7), 2^e the power of two below
         // the largest scale seen.  There is room for scales up to 2^(e + 8); a larger one makes
@@ -732,13 +834,11 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
                     const int e = max(static_cast<int>(b >> 7) - 127, -110);
                     const float f = old == 0 ? 1.0f : power_of_two(value_e[G_] - e);
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                    for (int i = 0; i < 4; ++i) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-#pragma unroll
-                            for (int m = 4 * G_; m < 4 * G_ + 4; ++m) o[nt][m][i] *= f;
-                            zero_part[nt][G_][i] *= f;
-                        }
+                        for (int m = 0; m < kOut / G; ++m) o[kOut / G * G_ + m][i] *= f;
+                        zero_part[G_][i] *= f;
+                    }
                     value_e[G_] = e;
                     value_up[G_] = power_of_two(7 - e);
                     now = static_cast<uint32_t>(min(e + 127 + 8, 255)) << 7;
@@ -747,22 +847,35 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
             }
             value_limit = limits;
         }
-        uint32_t prob[NT][4][G][2];      // f16, slots in the order of the value codes
+        uint32_t prob[4][G][kLeft ? 4 : 2];      // f16, slots in the order of the value codes
 #pragma unroll
         for (int tile = 0; tile < 4; ++tile)
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int half = 0; half < 2; ++half)       // of the tile's slots
 #pragma unroll
                 for (int G_ = 0; G_ < G; ++G_) {
                     // the odd pairs of a word's codes enter times 16
-                    const float f = (G_ ? bf16_hi(scales[tile][i]) : bf16_lo(scales[tile][i])) *
-                                    (i ? value_up[G_] * 0.0625f : value_up[G_]);
+                    const float up = half ? value_up[G_] * 0.0625f : value_up[G_];
+                    const int i = (2 * tile + half) * (kScores / 8);
+                    auto scale = [&](int j) {
+                        return (G_ ? bf16_hi(scales[j]) : bf16_lo(scales[j])) * up;
+                    };
+                    if constexpr (kLeft) {
+                        float f0 = G_ ? bf16_hi(scales[i]) : bf16_lo(scales[i]);
+                        float f1 = G_ ? bf16_hi(scales[i + 1]) : bf16_lo(scales[i + 1]);
+                        mul_two(f0, f1, up, up);
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
+                        for (int e = 0; e < E; ++e) {
+                            float x0 = s[e][i], x1 = s[e][i + 1];
+                            mul_two(x0, x1, f0, f1);
+                            prob[tile][G_][2 * half + e] = f16_pair(x0, x1);
+                        }
+                    } else {
+                        const float f = scale(i);
                         float x[2] = {};        // rows t and t + 4
 #pragma unroll
-                        for (int e = 0; e < E; ++e) x[e] = s[nt][e][tile][i] * f;
-                        prob[nt][tile][G_][i] = transpose16(f16_pair(x[0], x[1]));
+                        for (int e = 0; e < E; ++e) x[e] = s[e][i] * f;
+                        prob[tile][G_][half] = transpose16(f16_pair(x[0], x[1]));
                     }
                 }
 #pragma unroll
@@ -772,14 +885,16 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
                 // the last bits of -(128 + z) are z
                 const uint4 z = lds128(values + P::kValZeros - P::kValCodes + G_ * 2 * kPage +
                                        32 * t + 16 * a);
-                const uint32_t z0 = z.x & 0x000f000fu, z1 = z.y << 4 & 0x00f000f0u;
-                const uint32_t z2 = z.z & 0x000f000fu, z3 = z.w << 4 & 0x00f000f0u;
+                const uint32_t zeros[2][2] = {{z.x & 0x000f000fu, z.y << 4 & 0x00f000f0u},
+                                              {z.z & 0x000f000fu, z.w << 4 & 0x00f000f0u}};
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    mma_f16(zero_part[nt][G_], z0, z0, z1, z1, prob[nt][2 * a][G_][0],
-                            prob[nt][2 * a][G_][1]);
-                    mma_f16(zero_part[nt][G_], z2, z2, z3, z3, prob[nt][2 * a + 1][G_][0],
-                            prob[nt][2 * a + 1][G_][1]);
+                for (int c = 0; c < 2; ++c) {
+                    const uint32_t(&pr)[kLeft ? 4 : 2] = prob[2 * a + c][G_];
+                    if constexpr (kLeft)
+                        mma_f16(zero_part[G_], pr[0], pr[1], pr[2], pr[3], zeros[c][0], zeros[c][1]);
+                    else
+                        mma_f16(zero_part[G_], zeros[c][0], zeros[c][0], zeros[c][1], zeros[c][1],
+                                pr[0], pr[1]);
                 }
             }
 #pragma unroll
@@ -797,11 +912,16 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
                         const int m = m0 + i;
                         const uint32_t u = (a ? w[i].y : w[i].x) >> (8 * c);
                         const uint32_t v = (a ? w[i].w : w[i].z) >> (8 * c);
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-                            mma_f16(o[nt][m], u & 0x000f000fu, v & 0x000f000fu, u & 0x00f000f0u,
-                                    v & 0x00f000f0u, prob[nt][2 * a + c][m / 4][0],
-                                    prob[nt][2 * a + c][m / 4][1]);
+                        const uint32_t(&pr)[kLeft ? 4 : 2] = prob[2 * a + c][m / 4];
+                        if constexpr (kLeft) {
+                            mma_f16(o[2 * m], pr[0], pr[1], pr[2], pr[3], u & 0x000f000fu,
+                                    u & 0x00f000f0u);
+                            mma_f16(o[2 * m + 1], pr[0], pr[1], pr[2], pr[3], v & 0x000f000fu,
+                                    v & 0x00f000f0u);
+                        } else {
+                            mma_f16(o[m], u & 0x000f000fu, v & 0x000f000fu, u & 0x00f000f0u,
+                                    v & 0x00f000f0u, pr[0], pr[1]);
+                        }
                     }
         }
         __syncwarp();
