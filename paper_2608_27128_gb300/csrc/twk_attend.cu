@@ -1031,12 +1031,13 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
 
 // Joins the parts of a unit that several blocks took, in the order of its slots: a block per block that
 // such a unit begins in and row.  Its parts are that block's tail and the heads of the blocks after it, up
-// to the one it ends in.  Bound by latency: every warp reads four parts at once, maxima, sums and
-// outputs, and joins them as it would pages; the warps' results are joined in order.  (Blocks for
+// to the one it ends in.  Bound by latency: every warp reads five parts at once, maxima, sums and
+// outputs, and joins them as it would pages; the warps' results are joined in order.  (With four, the 19
+// or 20 parts of each of 8 units took a second round: 27.9 us where 26.9, 65536 slots.  Blocks for
 // every pair and row, most of which find nothing to do: 37 us for 2048 pairs of 16 rows.)  The
 // blocks past the rows are the units': each checks the length and page numbers of one, and writes
 // the rows of one without slots.
-constexpr int kMergeWarps = 4, kMergeParts = 4;
+constexpr int kMergeWarps = 4, kMergeParts = 5;
 
 template <int D, int R>
 __global__ void __launch_bounds__(32 * kMergeWarps)
