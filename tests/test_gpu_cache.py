@@ -325,6 +325,34 @@ def test_attend_many_units_of_few_slots():
     check_attend(rng, lens.tolist(), 1, 2, 1, 64)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,n,units,most", [(4, 1, 500, 900), (8, 1, 500, 900), (4, 3, 400, 600),
+                                            (8, 3, 250, 600), (4, 4, 3, 90000)])
+def test_attend_units_that_warps_and_blocks_share(d, G, n, units, most):
+    """More pages than warps in the grid, and units that begin and end anywhere in a warp's span and
+    a block's; with more than 16 rows several parts of each; a few units over all blocks.  The units'
+    pages are drawn from 24."""
+    rng = np.random.default_rng([d, G, n])
+    pool, ids, cache = make_cache(rng, [24 * 64], d)
+    k, v, pos, vs = cache[0]
+    lens = rng.integers(0, most, units)
+    lens[units // 2:units // 2 + units // 20] = 0
+    table = rng.integers(0, 24, (units, -(-most // 64)))
+    q = rng_rows(rng, units, n, G, d, outliers=False)
+    out = tk.twinkv_cache_attend(q.to(device()), pool, ids[0][put(table)].view(units, 1, -1),
+                                 put(lens.astype(np.int32).reshape(units, 1)), want_lse=True)
+    got, lse = f64(out["out"]), f64(out["lse"])
+    for u in range(units):
+        slots = (table[u][:, None] * 64 + np.arange(64)).reshape(-1)[:lens[u]]
+        want, wl, *sizes = R.attend(f64(q)[u], k[slots], v[slots], np.arange(lens[u]), d ** -0.5,
+                                    v_scales=vs[slots])
+        bound = R.attend_bound(want, *sizes, len(slots))
+        assert (np.abs(got[u] - want) <= bound).all(), u
+        assert np.array_equal(np.isneginf(lse[u]), np.isneginf(wl))
+        fine = np.isfinite(wl)
+        assert (np.abs(lse[u][fine] - wl[fine]) <= 5e-4).all()
+
+
 def test_attend_is_the_same_twice():
     rng = np.random.default_rng(6)
     pool, ids, _ = make_cache(rng, [3000, 700], 128)
