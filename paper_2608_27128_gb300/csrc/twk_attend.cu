@@ -284,6 +284,7 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
     constexpr int kRows = R, kTiles = 2, kDims = 2;
     constexpr bool kLeft = C::kLeft;
     constexpr int kScores = kLeft ? 16 : 8;          // of a lane, row and page
+    constexpr int kWritten = -2;
     constexpr int kOut = kLeft ? 2 * M : M;          // accumulators of outputs
     extern __shared__ __align__(128) uint8_t smem[];   // rows of a copy on whole lines of 128 bytes
     __shared__ int s_pair[C::kWarps], s_rest[C::kWarps], s_head[C::kWarps];
@@ -933,8 +934,9 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
         stage = stage + 1 == C::kStages ? 0 : stage + 1;
         ++at.j;
         --todo;
-        if (todo > 0 && at.j == at.v.count) {
+        if (at.j == at.v.count && (todo > 0 || seg_begin == 0)) {
             finish_unit();
+            if (todo == 0) break;
             do {
                 ++at.pair;
                 at.v = visit_of(p, at.pair / p.parts);
@@ -944,27 +946,29 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
         }
     }
 
-    // ---- the spans' last units: the warps of the block that end in the same one join their parts
+    // ---- the spans' last units, if not written: the warps of the block that end in the same one join
+    // their parts
     cp_async_wait<0>();
     __syncwarp();
-    if (has_span) {
+    const bool written = at.j == at.v.count && seg_begin == 0;
+    if (has_span && !written) {
         close_rows();
         put_part(reinterpret_cast<float*>(smem + warp * C::kRing));
     }
     if (lane == 0) {
-        s_pair[warp] = has_span ? at.pair : -1;
+        s_pair[warp] = !has_span ? -1 : written ? kWritten : at.pair;
         s_rest[warp] = at.v.count - at.j;
         s_begins[warp] = seg_begin == 0;
     }
     __syncthreads();
     // a warp per run of such warps and row; the next warp may have the rest of the unit as its head
-    for (int w0 = 0, w1, turn = warp; w0 < C::kWarps && s_pair[w0] >= 0; w0 = w1, turn += kRows) {
+    for (int w0 = 0, w1, turn = warp; w0 < C::kWarps && s_pair[w0] != -1; w0 = w1) {
         const int pair = s_pair[w0], unit = pair / p.parts, r0 = pair % p.parts * kRows;
         for (w1 = w0 + 1; w1 < C::kWarps && s_pair[w1] == pair; ++w1) {}
         const bool with_head = w1 < C::kWarps && s_head[w1] == pair;
         const bool begins = s_begins[w0], ends = with_head || s_rest[w1 - 1] == 0;
         const float* rest = p.part + static_cast<int64_t>(worker - warp + w1) * kPartSize<D, R>;
-        for (int r = turn % C::kWarps; r < kRows; r += C::kWarps) {
+        for (int r = turn % C::kWarps; r < kRows && pair != kWritten; r += C::kWarps) {
             constexpr int kVec = D / 32;
             float m = -INFINITY, l = 0.0f, acc[kVec] = {};
             float m_rest = -INFINITY, l_rest = 0.0f, rest_acc[kVec] = {};
@@ -1021,6 +1025,7 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
                 if (p.a.out_lse && lane == 0) p.a.out_lse[row] = log_sum(p, m, l);
             }
         }
+        turn += pair != kWritten ? kRows : 0;
         if (threadIdx.x == 0) {
             if (w0 == 0) p.split[blockIdx.x].y = begins ? s_head[0] >= 0 : ends;
             if (w1 == C::kWarps || s_pair[w1] < 0)
