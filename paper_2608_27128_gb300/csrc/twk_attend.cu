@@ -42,10 +42,10 @@
 // which warp comes first: results are the same from call to call.
 //
 // Measured (us a call; share of the measured copy rate):
-//   32 x 8 units of 4k to 16k slots, 4 rows, d = 128     73.7   77 %
-//   8 units of 131009 slots, 4 rows, d = 128             37.0   60 %
-//   16 x 8 units of 16384 slots, 8 rows, d = 128         62.5   71 %; 16 rows 86.1, 52 %
-//   32 x 8 units of 16384 slots, 4 rows, d = 64          63.6   70 %
+//   32 x 8 units of 4k to 16k slots, 4 rows, d = 128     73.5   77 %
+//   8 units of 131009 slots, 4 rows, d = 128             36.3   61 %
+//   16 x 8 units of 16384 slots, 8 rows, d = 128         61.4   73 %; 16 rows 85.8, 52 %
+//   32 x 8 units of 16384 slots, 4 rows, d = 64          63.3   70 %
 // Without its arithmetic the first takes 69 and the second 33: about 10 us go into the two launches, the
 // lengths, the first pages' latency and the merge, the rest is loads.  With 16 rows the arithmetic
 // bounds it (two warps on a quarter of the SM, whose registers they fill).
@@ -84,9 +84,30 @@ struct Config {
     static_assert(kHalf % 16 == 0 && kStages >= 2);
 };
 
+// x / d and x % d for x and d below 2^16: with m = ceil(2^32 / d), x m / 2^32 is above x / d by less
+// than x / 2^32 < 1 / d.  (d = 1 has no such m.)  A unit's change has some 25 of them, and a kernel's code is
+// read anew with every launch: 64 x 8 units of 100 slots, 56 rows, 40.7 -> 36.9 us; 8 units of 131009
+// slots, 36.8 -> 36.3.
+struct Divisor {
+    unsigned d, m, one;
+    explicit Divisor(unsigned by = 1)
+        : d(by), m(by > 1 ? 0xffffffffu / by + 1 : 0), one(by > 1 ? 0 : ~0u)
+    {
+    }
+};
+__device__ __forceinline__ int operator/(int x, const Divisor& by)
+{
+    return __umulhi(x, by.m) + (x & by.one);
+}
+__device__ __forceinline__ int operator%(int x, const Divisor& by)
+{
+    return x - x / by * static_cast<int>(by.d);
+}
+
 struct AttendParams {
     AttendArgs a;
-    int units, parts;        // parts: of R rows, of a unit
+    int units;
+    Divisor parts, G, H;     // parts: of R rows, of a unit
     int rows;                // G n
     int chunks;              // of 32 (unit, part) pairs
     float c;                 // scale * log2(e)
@@ -142,9 +163,9 @@ __device__ __forceinline__ int tail_slot(int block)
 // row of out and out_lse
 __device__ __forceinline__ int64_t out_row(const AttendParams& p, int unit, int row)
 {
-    const int b = unit / p.a.H, h = unit % p.a.H;
-    return (static_cast<int64_t>(b) * p.a.n + row / p.a.G) * (p.a.H * p.a.G) + h * p.a.G +
-           row % p.a.G;
+    const int b = unit / p.H, h = unit % p.H;
+    return (static_cast<int64_t>(b) * p.a.n + row / p.G) * (p.H.d * p.G.d) + h * p.G.d +
+           row % p.G;
 }
 
 // log of the softmax's denominator
@@ -292,7 +313,7 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
     int* chunk_pages = reinterpret_cast<int*>(smem + C::kWarps * C::kRing);
     wait_for_previous();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, g = lane / 4, t = lane % 4;
-    const int pairs = p.units * p.parts;
+    const int pairs = p.units * static_cast<int>(p.parts.d);
 
     // Pages before each chunk of 32 pairs: a single chunk is summed by every warp for itself, without a
     // barrier, more by the block (up to eight so by every warp: the same lines read by 1824 warps,
@@ -431,7 +452,7 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
 
     auto start_unit = [&]() {
         const int unit = at.pair / p.parts, r0 = at.pair % p.parts * kRows;
-        const int b = unit / p.a.H, h = unit % p.a.H;
+        const int b = unit / p.H, h = unit % p.H;
         seg_begin = at.j;
         const int* seen =
             p.seen ? p.seen + static_cast<int64_t>(unit) * (1 + p.a.n) : nullptr;
@@ -443,8 +464,8 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
             const int in_part = kLeft ? g + 8 * half : g / 2 + g % 2 * 4, r = r0 + in_part;
             const uint16_t* src = nullptr;
             if (r < p.rows && in_part < R)
-                src = p.a.q + b * p.a.q_batch + r / p.a.G * p.a.q_token +
-                      (h * p.a.G + r % p.a.G) * p.a.q_head;
+                src = p.a.q + b * p.a.q_batch + r / p.G * p.a.q_token +
+                      (h * static_cast<int>(p.G.d) + r % p.G) * p.a.q_head;
             uint32_t w[G][8];
             uint32_t most = 0;
 #pragma unroll
@@ -497,7 +518,7 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
         }
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const int row = r0 + row_of(e), token = row / p.a.G;
+            const int row = r0 + row_of(e), token = row / p.G;
             limit[e] = row < p.rows ? at.v.len - p.a.n + token + 1 : INT_MAX;
             from[e] = row < p.rows && seen ? seen[1 + token] : 0;
             top[e] = -INFINITY;
@@ -518,7 +539,7 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
         }
         // every row of the part: the first token sees least at the end, the last at the window's
         // begin
-        const int first_token = r0 / p.a.G, last_token = (min(r0 + kRows, p.rows) - 1) / p.a.G;
+        const int first_token = r0 / p.G, last_token = (min(r0 + kRows, p.rows) - 1) / p.G;
         all_limit = at.v.len - p.a.n + first_token + 1;
         all_from = seen ? seen[1 + last_token] : 0;
     };
@@ -1264,8 +1285,11 @@ cudaError_t launch_attend(const AttendArgs& a, int sms, cudaStream_t st)
     p.units = a.B * a.H;
     p.rows = a.G * a.n;
     const int pr = part_rows(p.rows);
-    p.parts = (p.rows + pr - 1) / pr;
-    p.chunks = (p.units * p.parts + 31) / 32;
+    const int parts = (p.rows + pr - 1) / pr;
+    p.parts = Divisor(parts);
+    p.G = Divisor(a.G);
+    p.H = Divisor(a.H);
+    p.chunks = (p.units * parts + 31) / 32;
     p.c = a.scale * 1.4426950408889634f;
     uint8_t* ws = static_cast<uint8_t*>(a.ws);
     p.split = reinterpret_cast<int2*>(ws);
