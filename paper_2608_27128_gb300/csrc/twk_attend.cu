@@ -42,10 +42,10 @@
 // which warp comes first: results are the same from call to call.
 //
 // Measured (us a call; share of the measured copy rate):
-//   32 x 8 units of 4k to 16k slots, 4 rows, d = 128     73.5   77 %
-//   8 units of 131009 slots, 4 rows, d = 128             36.3   61 %
-//   16 x 8 units of 16384 slots, 8 rows, d = 128         61.4   73 %; 16 rows 85.8, 52 %
-//   32 x 8 units of 16384 slots, 4 rows, d = 64          63.3   70 %
+//   32 x 8 units of 4k to 16k slots, 4 rows, d = 128     73.4   77 %
+//   8 units of 131009 slots, 4 rows, d = 128             35.2   63 %
+//   16 x 8 units of 16384 slots, 8 rows, d = 128         61.3   73 %; 16 rows 85.2, 52 %
+//   32 x 8 units of 16384 slots, 4 rows, d = 64          62.1   72 %
 // Without its arithmetic the first takes 69 and the second 33: about 10 us go into the two launches, the
 // lengths, the first pages' latency and the merge, the rest is loads.  With 16 rows the arithmetic
 // bounds it (two warps on a quarter of the SM, whose registers they fill).
@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
     // Pages before each chunk of 32 pairs: a single chunk is summed by every warp for itself, without a
     // barrier, more by the block (up to eight so by every warp: the same lines read by 1824 warps,
     // 4.6 us where the block takes 1.6).
-    int64_t total;
+    unsigned total;
     if (p.chunks == 1) {
         total = __reduce_add_sync(0xffffffffu,
                                   lane < pairs ? visit_of(p, lane / p.parts).count : 0);
@@ -350,17 +350,18 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
     }
     // Blocks, and warps within a block, that have a page each, as even as can be; the spans of a
     // block's warps follow one another.
-    const int64_t blocks = min(total, static_cast<int64_t>(gridDim.x));
-    const int64_t workers = min(total, static_cast<int64_t>(gridDim.x) * C::kWarps);
+    const unsigned blocks = min(total, gridDim.x), workers = min(total, gridDim.x * C::kWarps);
     if (blockIdx.x >= blocks) {
         if (threadIdx.x == 0) p.split[blockIdx.x] = make_int2(-1, 0);
         return;
     }
-    const int64_t index = workers * blockIdx.x / blocks + warp;
+    const unsigned index = workers * blockIdx.x / blocks + warp;
     const bool has_span = index < workers * (blockIdx.x + 1) / blocks;
     const int worker = blockIdx.x * C::kWarps + warp;
-    const int64_t begin = has_span ? total * index / workers : 0;
-    int todo = has_span ? static_cast<int>(total * (index + 1) / workers - begin) : 0;
+    // total i / workers, in 32 bits (64-bit divisions here cost 1.1 us of 36 for 8 units of 131009 slots)
+    const unsigned each = total / workers, over = total % workers;
+    const int begin = has_span ? each * index + over * index / workers : 0;
+    int todo = has_span ? each * (index + 1) + over * (index + 1) / workers - begin : 0;
 
     // the span's first page
     Place at = {};
@@ -382,7 +383,7 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
             const int y = __shfl_up_sync(0xffffffffu, scan, m);
             if (lane >= m) scan += y;
         }
-        const int rest = static_cast<int>(begin - before);
+        const int rest = begin - before;
         const unsigned past = __ballot_sync(0xffffffffu, scan > rest);
         const int l = __ffs(past) - 1;
         at.pair = 32 * lo + l;
