@@ -74,8 +74,8 @@ struct Config {
     static constexpr bool kLeft = R == 16;       // rows are the left operand's
     static constexpr int E = R == 4 ? 1 : 2;     // rows of a lane
     // as many as their registers let be, equally many on each quarter of the SM (12 instead of 8 for
-    // 16 rows at d = 64: 62.4 against 64.2 us for 256 units of 8192 slots, but 30.7 against 29.6 for
-    // 128 units with 44 pages in a window)
+    // 16 rows at d = 64: 60.9 against 63.6 us for 256 units of 8192 slots, but 28.8 against 28.0 for
+    // 128 units with a window of 4096, and 20.6 against 18.5 for 32 units of 8192)
     static constexpr int kWarps = R == 16 ? 8 : D == 128 ? 12 : 16;
     static constexpr int kHalf = PageLayout<D>::kValCodes;        // bytes of a page's keys
     static constexpr int kStages = 221184 / (2 * kHalf * kWarps); // pages of a warp's ring
