@@ -3,7 +3,10 @@
 ``PageCache`` holds the pool, the page tables and the lengths of L layers, B sequences and H KV
 heads, and hands out pages on the host: taking, sharing, copying and freeing them.  The repair
 keeps exactly its budget (Sec. 3.4), so the host knows every unit's pages without asking the
-device.  The computation is in ``twinkv``'s calls, which the methods make on the current stream; a
+device.  A unit that does not hold its budget after all (another mask, a data error) gets length -1,
+a data error for every call: none of its pages is read or written until the sequence is packed
+anew or freed.  Only fork, which shares pages by the host's counts, waits for the device and
+compares them.  The computation is in ``twinkv``'s calls, which the methods make on the current stream; a
 page that is free again may be written by the next call on it, so a cache stays on one stream.
 """
 from __future__ import annotations
@@ -79,11 +82,21 @@ class PageCache:
                           device=self.pool.device)
         self.table.view(-1, self.max_pages)[at] = self._rows(lists)
 
+    def _filled(self, b, units, counts, out):
+        """Lengths and statuses of sequence b after the call that filled its pages: -1 and an error
+        where the call failed or a unit has not the slots that the host counts."""
+        want = torch.tensor(counts, dtype=torch.int32).view(self.L, self.H).to(self.pool.device)
+        wrong = (out["lens"] != want) | (out["status"] != 0)
+        self.lens[:, b] = out["lens"].masked_fill(wrong, -1)
+        self._used.update(zip(units, counts))
+        return out["status"].masked_fill(wrong & (out["status"] == 0), tk.ERR_INVALID_ARG)
+
     # ------------------------------------------------------------ one sequence
 
     def pack(self, b: int, keys, values, mask, budget):
         """Sequence b becomes the rows of keys, values [L,H,N,d] that mask [L,H,N] retains;
-        budget: how many that are per unit, as the repair was given it (an int, or L*H)."""
+        budget: how many that are per unit, as the repair was given it (an int, or L*H).  Returns
+        the statuses [L,H]: 1 where the mask retains another number."""
         units = self._sequence(b)
         counts = self._counts(budget, units)
         need = [-(-n // SLOTS) for n in counts]
@@ -98,9 +111,7 @@ class PageCache:
             ids = ids[n:]
         self._set(units, lists)
         out = tk.twinkv_cache_pack(keys, values, mask, self.pool, self.table[:, b].contiguous())
-        self.lens[:, b] = out["lens"]
-        self._used.update(zip(units, counts))
-        return out["status"]
+        return self._filled(b, units, counts, out)
 
     def read(self, b: int, rows: int) -> dict:
         """The first ``rows`` slots of sequence b: keys, values [L,H,rows,d] bf16, positions."""
@@ -108,7 +119,8 @@ class PageCache:
                                     self.lens[:, b].contiguous(), rows)
 
     def compact(self, b: int, keep, budget):
-        """Sequence b keeps the slots that keep [L,H,N] marks, ``budget`` per unit, in new pages."""
+        """Sequence b keeps the slots that keep [L,H,N] marks, ``budget`` per unit, in new pages;
+        statuses as pack's."""
         units = self._sequence(b)
         counts = self._counts(budget, units)
         need = [-(-n // SLOTS) for n in counts]
@@ -123,16 +135,19 @@ class PageCache:
         for u in units:
             self._drop(self._pages[u])
         self._set(units, lists)
-        self.lens[:, b] = out["lens"]
-        self._used.update(zip(units, counts))
-        return out["status"]
+        return self._filled(b, units, counts, out)
 
     def fork(self, b: int, to: int):
         """Sequence ``to`` becomes another end of sequence b: full pages are shared, the last
-        one is copied, so that either may append."""
+        one is copied, so that either may append.  Waits for the device, and raises RuntimeError
+        between a reserve and the last layer's append, or where a pack or compact failed: what the
+        host takes for full pages would be written again."""
         units, others = self._sequence(b), self._sequence(to)
         if b == to:
             raise ValueError("a sequence is no fork of itself")
+        if self.lens[:, b].flatten().tolist() != [self._used[u] for u in units]:
+            raise RuntimeError(f"sequence {b} does not hold the slots counted for it: a step is not "
+                               "over, or a call on it failed")
         part = [u for u in units if self._used[u] % SLOTS]
         own = dict(zip(part, self._take(len(part))))
         self.free(to)
