@@ -11,6 +11,8 @@ page that is free again may be written by the next call on it, so a cache stays 
 """
 from __future__ import annotations
 
+from itertools import islice
+
 import torch
 
 from . import twinkv as tk
@@ -40,13 +42,29 @@ class PageCache:
     def free_pages(self) -> int:
         return len(self._free)
 
-    def _take(self, n: int) -> list:
-        if n > len(self._free):
-            raise MemoryError(f"{n} pages wanted, {len(self._free)} are free")
-        got = [self._free.pop() for _ in range(n)]
-        for i in got:
-            self._users[i] = 1
-        return got
+    def _pick(self, need, back=()) -> list:
+        """Lists of so many pages each, of those that are free and those that the units `back`
+        alone hold.  They are not taken before _hold is called with them."""
+        own = [i for u in back for i in self._pages[u] if self._users[i] == 1]
+        n, free = sum(need), len(self._free) + len(own)
+        if n > free:
+            raise MemoryError(f"{n} pages wanted, {free} are free")
+        own = own[:n]
+        ids = own + self._free[len(self._free) - (n - len(own)):]
+        ids = iter(ids)
+        return [list(islice(ids, n)) for n in need]
+
+    def _hold(self, units, lists):
+        """The units hold these pages from now on, instead of those they held."""
+        before = [i for u in units for i in self._pages[u]]
+        taken = 0
+        for u, x in zip(units, lists):
+            for i in x:
+                taken += self._users[i] == 0
+                self._users[i] += 1
+            self._pages[u] = x
+        del self._free[len(self._free) - taken:]     # where _pick found them
+        self._drop(before)
 
     def _drop(self, pages):
         for i in pages:
@@ -76,8 +94,7 @@ class PageCache:
         return torch.tensor(rows, dtype=torch.int32).to(self.pool.device)
 
     def _set(self, units, lists):
-        for u, x in zip(units, lists):
-            self._pages[u] = x
+        self._hold(units, lists)
         at = torch.tensor([(l * self.B + b) * self.H + h for l, b, h in units],
                           device=self.pool.device)
         self.table.view(-1, self.max_pages)[at] = self._rows(lists)
@@ -99,18 +116,10 @@ class PageCache:
         the statuses [L,H]: 1 where the mask retains another number."""
         units = self._sequence(b)
         counts = self._counts(budget, units)
-        need = [-(-n // SLOTS) for n in counts]
-        own = sum(self._users[i] == 1 for u in units for i in self._pages[u])
-        if sum(need) > len(self._free) + own:
-            raise MemoryError(f"{sum(need)} pages wanted, {len(self._free) + own} are free")
-        self.free(b)
-        ids = self._take(sum(need))
-        lists = []
-        for n in need:
-            lists.append(ids[:n])
-            ids = ids[n:]
+        lists = self._pick([-(-n // SLOTS) for n in counts], units)
+        out = tk.twinkv_cache_pack(keys, values, mask, self.pool,
+                                   self._rows(lists).view(self.L, self.H, -1))
         self._set(units, lists)
-        out = tk.twinkv_cache_pack(keys, values, mask, self.pool, self.table[:, b].contiguous())
         return self._filled(b, units, counts, out)
 
     def read(self, b: int, rows: int) -> dict:
@@ -123,17 +132,10 @@ class PageCache:
         statuses as pack's."""
         units = self._sequence(b)
         counts = self._counts(budget, units)
-        need = [-(-n // SLOTS) for n in counts]
-        ids = self._take(sum(need))
-        lists = []
-        for n in need:
-            lists.append(ids[:n])
-            ids = ids[n:]
-        new = self._rows(lists).view(self.L, self.H, -1)
+        lists = self._pick([-(-n // SLOTS) for n in counts])
         out = tk.twinkv_cache_compact(self.pool, self.table[:, b].contiguous(),
-                                      self.lens[:, b].contiguous(), keep, new)
-        for u in units:
-            self._drop(self._pages[u])
+                                      self.lens[:, b].contiguous(), keep,
+                                      self._rows(lists).view(self.L, self.H, -1))
         self._set(units, lists)
         return self._filled(b, units, counts, out)
 
@@ -149,15 +151,8 @@ class PageCache:
             raise RuntimeError(f"sequence {b} does not hold the slots counted for it: a step is not "
                                "over, or a call on it failed")
         part = [u for u in units if self._used[u] % SLOTS]
-        own = dict(zip(part, self._take(len(part))))
-        self.free(to)
-        lists = []
-        for u in units:
-            pages = list(self._pages[u])
-            full = self._used[u] // SLOTS
-            for i in pages[:full]:
-                self._users[i] += 1
-            lists.append(pages[:full] + ([own[u]] if u in own else []))
+        own = dict(zip(part, self._pick([1] * len(part))))
+        lists = [self._pages[u][:self._used[u] // SLOTS] + own.get(u, []) for u in units]
         self._set(others, lists)
         self.lens[:, to] = self.lens[:, b]
         self._used.update(zip(others, (self._used[u] for u in units)))
@@ -165,7 +160,7 @@ class PageCache:
             dev = self.pool.device
             last = torch.tensor([[self._pages[u][self._used[u] // SLOTS]] for u in part],
                                 dtype=torch.int32).to(dev)
-            new = torch.tensor([[own[u]] for u in part], dtype=torch.int32).to(dev)
+            new = torch.tensor([own[u] for u in part], dtype=torch.int32).to(dev)
             held = torch.tensor([self._used[u] % SLOTS for u in part], dtype=torch.int32).to(dev)
             tk.twinkv_cache_compact(self.pool, last, held, None, new)
 
@@ -185,18 +180,15 @@ class PageCache:
         layers append."""
         if not 1 <= n <= SLOTS:
             raise ValueError(f"n must be in [1, {SLOTS}]")
-        want = {}
+        want, lists = {}, []
         for u, pages in self._pages.items():
             need = -(-(self._used[u] + n) // SLOTS) - len(pages)
             if self._used[u] and need > 0:
                 if len(pages) + need > self.max_pages:
                     raise MemoryError(f"unit {u} has {self.max_pages} pages already")
                 want[u] = need
-        ids = self._take(sum(want.values()))
-        lists = []
-        for u, need in want.items():
-            lists.append(self._pages[u] + ids[:need])
-            ids = ids[need:]
+        for u, new in zip(want, self._pick(want.values())):
+            lists.append(self._pages[u] + new)
         if want:
             self._set(list(want), lists)
         for u, used in self._used.items():

@@ -236,3 +236,47 @@ def test_fork_in_the_middle_of_a_step(model):
     assert cache.lens.eq(128).all()
     for _ in range(3):
         assert all(s.eq(0).all() for s in step(cache))
+
+
+# ---------------------------------------------------------------- calls that raise
+
+def state(cache):
+    return (sorted(cache._free), list(cache._users), {u: list(x) for u, x in cache._pages.items()},
+            dict(cache._used), cache.table.clone(), cache.lens.clone())
+
+
+def same(a, b):
+    return a[:4] == b[:4] and torch.equal(a[4], b[4]) and torch.equal(a[5], b[5])
+
+
+def bad_dense(n):
+    x = torch.zeros(L, H, n, D + 1, dtype=torch.bfloat16)
+    return x, x
+
+
+@pytest.mark.parametrize("full", [False, True])
+def test_a_pack_that_raises_changes_nothing(model, full):
+    """The arguments are refused by the call, after the host has chosen pages."""
+    cache = model.make(L, 2, H, D, 4 * L * H if full else 60, 5)
+    cache.pack(0, *dense(200), ones(200), 200)
+    before, held = state(cache), model.held(0)
+    for args in ((*bad_dense(200), ones(200), 200), (*dense(200), ones(200).float(), 200),
+                 (*dense(200), ones(200)[:1], 100)):
+        with pytest.raises(ValueError):
+            cache.pack(0, *args)
+    if full:
+        with pytest.raises(MemoryError):
+            cache.pack(0, *dense(320), ones(320), 320)
+    assert same(state(cache), before) and model.held(0) == held
+
+
+def test_a_compact_that_raises_loses_no_pages(model):
+    cache = model.make(L, 2, H, D, 60, 5)
+    cache.pack(0, *dense(200), ones(200), 200)
+    before, held = state(cache), model.held(0)
+    for keep in (ones(200).float(), ones(200)[:1]):
+        with pytest.raises(ValueError):
+            cache.compact(0, keep, 100)
+    assert same(state(cache), before) and model.held(0) == held
+    cache.free(0)
+    assert cache.free_pages == 60
