@@ -151,7 +151,7 @@ class PageCache:
             raise RuntimeError(f"sequence {b} does not hold the slots counted for it: a step is not "
                                "over, or a call on it failed")
         part = [u for u in units if self._used[u] % SLOTS]
-        own = dict(zip(part, self._pick([1] * len(part))))
+        own = dict(zip(part, self._pick([1] * len(part), others)))
         lists = [self._pages[u][:self._used[u] // SLOTS] + own.get(u, []) for u in units]
         self._set(others, lists)
         self.lens[:, to] = self.lens[:, b]

@@ -280,3 +280,19 @@ def test_a_compact_that_raises_loses_no_pages(model):
     assert same(state(cache), before) and model.held(0) == held
     cache.free(0)
     assert cache.free_pages == 60
+
+
+def test_fork_onto_a_sequence_uses_its_pages(model):
+    """The target's own pages are free for the copy, as they are for pack."""
+    cache = model.make(L, 2, H, D, 5 * L * H, 5)
+    cache.pack(0, *dense(200), ones(130, 200), 130)
+    cache.pack(1, *dense(200), ones(100, 200), 100)
+    assert cache.free_pages == 0
+    held = model.held(0)
+    cache.fork(0, 1)
+    assert model.held(1) == held and model.held(0) == held
+    assert cache.free_pages == L * H
+    cache.fork(1, 0)                                  # and back, over pages that the two share
+    assert model.held(1) == held and model.held(0) == held
+    cache.free(0), cache.free(1)
+    assert cache.free_pages == 5 * L * H
