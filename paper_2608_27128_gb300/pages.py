@@ -35,6 +35,7 @@ class PageCache:
         self._users = [0] * n_pages
         self._pages = {(l, b, h): [] for l in range(L) for b in range(B) for h in range(H)}
         self._used = dict.fromkeys(self._pages, 0)
+        self._live = [False] * B             # packed or forked, and not freed since
 
     # ------------------------------------------------------------ pages, on the host
 
@@ -106,6 +107,7 @@ class PageCache:
         wrong = (out["lens"] != want) | (out["status"] != 0)
         self.lens[:, b] = out["lens"].masked_fill(wrong, -1)
         self._used.update(zip(units, counts))
+        self._live[b] = True
         return out["status"].masked_fill(wrong & (out["status"] == 0), tk.ERR_INVALID_ARG)
 
     # ------------------------------------------------------------ one sequence
@@ -156,6 +158,7 @@ class PageCache:
         self._set(others, lists)
         self.lens[:, to] = self.lens[:, b]
         self._used.update(zip(others, (self._used[u] for u in units)))
+        self._live[to] = self._live[b]
         if part:
             dev = self.pool.device
             last = torch.tensor([[self._pages[u][self._used[u] // SLOTS]] for u in part],
@@ -170,20 +173,21 @@ class PageCache:
         for u in units:
             self._drop(self._pages[u])
             self._pages[u], self._used[u] = [], 0
+        self._live[b] = False
         self.table[:, b] = -1
         self.lens[:, b] = 0
 
     # ------------------------------------------------------------ one step of every sequence
 
     def reserve(self, n: int = 1):
-        """Pages for n more slots of every sequence that is not empty: once per step, before its
-        layers append."""
+        """Pages for n more slots of every sequence that was packed or forked, and not freed since
+        (of all its units, also those without slots): once per step, before its layers append."""
         if not 1 <= n <= SLOTS:
             raise ValueError(f"n must be in [1, {SLOTS}]")
         want, lists = {}, []
         for u, pages in self._pages.items():
             need = -(-(self._used[u] + n) // SLOTS) - len(pages)
-            if self._used[u] and need > 0:
+            if self._live[u[1]] and need > 0:
                 if len(pages) + need > self.max_pages:
                     raise MemoryError(f"unit {u} has {self.max_pages} pages already")
                 want[u] = need
@@ -192,12 +196,12 @@ class PageCache:
         if want:
             self._set(list(want), lists)
         for u, used in self._used.items():
-            if used:
+            if self._live[u[1]]:
                 self._used[u] = used + n
 
     def append(self, layer: int, k, v, positions):
         """The rows k, v [B,n,H,d] of the step's tokens behind one layer's slots (after reserve(n));
-        a sequence that is empty stays so, with status 1."""
+        a sequence that is not live stays empty, with status 1."""
         lens = self.lens[layer]
         return tk.twinkv_cache_append(k, v, positions, self.pool, self.table[layer], lens,
                                       out={"lens": lens})["status"]

@@ -296,3 +296,36 @@ def test_fork_onto_a_sequence_uses_its_pages(model):
     assert model.held(1) == held and model.held(0) == held
     cache.free(0), cache.free(1)
     assert cache.free_pages == 5 * L * H
+
+
+# ---------------------------------------------------------------- units without slots
+
+def test_a_head_that_keeps_nothing_takes_the_next_tokens(model):
+    """A budget of 0 for one head of a sequence: its new tokens are stored like the others'."""
+    cache = model.make(L, 2, H, D, 60, 5)
+    mask = ones(70, 200)
+    mask[1, 1] = 0
+    assert cache.pack(0, *dense(200), mask, [70, 70, 70, 0]).eq(0).all()
+    cache.fork(0, 1)
+    for _ in range(66):
+        assert all(s.eq(0).all() for s in step(cache))
+    assert cache.lens.tolist() == [[[136, 136]] * 2, [[136, 66]] * 2]
+    a, b = model.held(0), model.held(1)
+    assert not set(a[1, 1]) & set(b[1, 1]) and len(set(a[1, 1])) == 66
+    keep = torch.zeros(L, H, 136, dtype=torch.uint8)
+    assert cache.compact(0, keep, 0).eq(0).all()
+    assert all(s.eq(0).all() for s in step(cache))
+    assert cache.lens[:, 0].eq(1).all() and cache.lens[1, 1].tolist() == [137, 67]
+
+
+def test_a_sequence_that_starts_without_slots(model):
+    cache = model.make(L, 2, H, D, 60, 5)
+    assert cache.pack(0, *dense(5), ones(0, 5), 0).eq(0).all()
+    assert cache.free_pages == 60
+    for _ in range(2):
+        assert [s.tolist() for s in step(cache)] == [[[0, 0], [1, 1]]] * L
+    assert cache.lens[:, 0].eq(2).all() and not cache.lens[:, 1].any()
+    cache.free(0)
+    assert cache.free_pages == 60
+    assert [s.tolist() for s in step(cache)] == [[[1, 1], [1, 1]]] * L
+    assert cache.free_pages == 60
