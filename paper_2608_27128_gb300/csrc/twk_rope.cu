@@ -82,12 +82,15 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs a, in
     const int pos = a.positions[token];
     const bool bad = pos < 0 || pos >= a.rows;
     if (a.out_status && split == 0 && lane == 0) a.out_status[token] = bad ? 1 : 0;
+    // a token without a row of the table: values, cosines and sines are 0, and there is no norm
     float cs[8], sn[8];
     {
-        const float* row = a.cos_sin + static_cast<int64_t>(bad ? 0 : pos) * D + 8 * l;
-        Eight<float> c, s;
-        c.load(row);
-        s.load(row + D / 2);
+        Eight<float> c = {}, s = {};
+        if (!bad) {
+            const float* row = a.cos_sin + static_cast<int64_t>(pos) * D + 8 * l;
+            c.load(row);
+            s.load(row + D / 2);
+        }
         c.get(cs);
         s.get(sn);
     }
@@ -118,7 +121,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs a, in
         if (h >= heads) continue;
         const bool is_q = h < a.heads_q;
         const T* w = static_cast<const T*>(is_q ? a.wq : a.wk);
-        if (w) {
+        if (w && !bad) {
             const float r = rsqrtf(sum * (1.0f / D) + a.eps);
             float wx[8], wy[8];
             Eight<T> s, c;
