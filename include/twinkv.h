@@ -521,7 +521,7 @@ size_t twinkv_cache_attend_workspace(twinkv_queries s, int32_t d);
  * rounded to 11 bits (fewer where the scale is below 2^-16 of the largest among the slots of
  * the pages visited), the result to bf16.
  *   q           [B][n][Hq][d] bf16, 16-byte aligned, strides in s (multiples of 8); values
- *               below 2^100
+ *               below 2^100, and q . k, over each group of 64 and in all, below 2^120
  *   scale       finite, above 0
  *   window      0: none (n_sink is then not used)
  *   table, lens of the B*H units, unit b*H + h; the positions of a unit's slots ascend

@@ -771,18 +771,20 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
                 m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, i));
             grown |= m > last;
             // a row that has seen nothing yet keeps -inf, and its probabilities are 0
-            const float shift = m == -INFINITY ? 0.0f : m * c;
+            const float high = m == -INFINITY ? 0.0f : m;
             const float f = last == -INFINITY ? 0.0f : exp2_approx((last - m) * c);
             shrink[e] = f;
             top[e] = m;
             float l = 0.0f, l2 = 0.0f;
 #pragma unroll
             for (int i = 0; i < kScores; i += 2) {
+                // the difference first: one of products is off by 2^-24 of the scores' size
                 if constexpr (kLeft) {
-                    fma_two(y[i], y[i + 1], c, c, -shift, -shift);
+                    add_two(y[i], y[i + 1], -high, -high);
+                    mul_two(y[i], y[i + 1], c, c);
                 } else {
-                    y[i] = fmaf(y[i], c, -shift);
-                    y[i + 1] = fmaf(y[i + 1], c, -shift);
+                    y[i] = (y[i] - high) * c;
+                    y[i + 1] = (y[i + 1] - high) * c;
                 }
                 y[i] = exp2_approx(y[i]);
                 y[i + 1] = exp2_approx(y[i + 1]);
