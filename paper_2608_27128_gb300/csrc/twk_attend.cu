@@ -762,7 +762,8 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             float(&y)[kScores] = s[e];
-            const float last = top[e], c = p.c * unit_of[e];
+            // not 0, which times an unseen slot's -inf is no number
+            const float last = top[e], c = fmaxf(p.c * unit_of[e], 0x1p-126f);
             float m = last;
 #pragma unroll
             for (int i = 0; i < kScores; i += 2) m = fmaxf(m, fmaxf(y[i], y[i + 1]));

@@ -50,3 +50,27 @@ def test_one_key_far_above_the_others(d, G, length, e):
     score = (R.round_trip(f64(k))[np.where(sign > 0, most, least)] * f64(q)).sum(-1) * d ** -0.5
     lse = f64(got["lse"])[0, 0]
     assert (np.abs(lse - score) <= 2.0 ** -16 * np.abs(score)).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G", [4, 8, 16])
+@pytest.mark.parametrize("scale", [1e-38, 1e-25, 1e-12])
+def test_scores_that_are_all_but_nothing(d, G, scale):
+    """Rows of zeros (a padded head) and of tiny queries with a tiny scale: every slot that a row sees has the
+    same probability, and the others none."""
+    rng = np.random.default_rng([d, G])
+    for length, n in ((3, 1), (200, 3), (5000, 2)):
+        k, v = rng_rows(rng, length, d, outliers=False), rng_rows(rng, length, d)
+        pool, table, lens = pages_of(k, v, d)
+        q = rng_rows(rng, 1, n, G, d)
+        q[:, :, ::2] = 0
+        q[:, :, 1::4] *= 2.0 ** -90
+        kk, vv = R.round_trip(f64(k)), R.round_trip(f64(v))
+        for window in (0, 50):
+            got = tk.twinkv_cache_attend(q.to(device()), pool, table, lens, scale=scale, window=window,
+                                         want_lse=True)
+            want, lse, *sizes = R.attend(f64(q)[0], kk, vv, np.arange(length), scale, window, 0,
+                                         R.quantize(f64(v))[1])
+            bound = R.attend_bound(want, *sizes, length)
+            assert (np.abs(f64(got["out"])[0] - want) <= bound).all()
+            assert (np.abs(f64(got["lse"])[0] - lse) <= 5e-4).all()
