@@ -378,7 +378,8 @@ twinkv_status twinkv_policy(const void* keys, twinkv_shape s, const int32_t* bud
  *     z = min(15, rint(-lo / s)), c = min(15, rint(x / s) + z)
  * (s below 2^-126: s = z = c = 0; rint to nearest, ties to even; the results are those of
  * exact arithmetic).  The group keeps s (bf16), z and the 64 codes c, and stands for the
- * values s (c - z), within about 0.53 s of x.  Values must be finite and below 2^120.
+ * values s (c - z), within about 0.53 s of x.  A group with a value that is not finite, or 2^120 or
+ * more in size, is held as zeros (a data error).
  *
  * Pages.  A page holds TWINKV_PAGE_SLOTS slots of one unit (a sequence or layer, and one
  * KV head): their codes, scales, zeros and positions, twinkv_cache_page_bytes(d) bytes (148
@@ -393,7 +394,9 @@ twinkv_status twinkv_policy(const void* keys, twinkv_shape s, const int32_t* bud
  * Data errors, in out_status[u]: TWINKV_ERR_INVALID_ARG for a length outside
  * [0, 64 max_pages], a mask byte above 1 or a page number outside the pool;
  * TWINKV_ERR_TOO_LARGE for more slots than the unit's row of `table` has pages.  No
- * such unit makes a kernel read or write outside the caller's arrays.
+ * such unit makes a kernel read or write outside the caller's arrays.  A unit with a value that
+ * its pages cannot hold (Rounding) is stored otherwise, length included, and gets
+ * TWINKV_ERR_INVALID_ARG from the call that writes it.
  */
 #define TWINKV_PAGE_SLOTS 64
 
@@ -443,7 +446,7 @@ size_t twinkv_cache_move_workspace(int32_t units, int32_t N);
  *   keys, values   [L][H][N][d] device, s.dtype, 16-byte aligned; only retained rows are read
  *   retained_mask  [L][H][N] uint8, or NULL: every row is kept (no workspace then)
  *   table          [L*H][max_pages]; the pages a unit fills must be in no other row
- *   out_lens       [L*H] int32: rows kept (0 for a unit with a data error)
+ *   out_lens       [L*H] int32: rows kept (0 for a unit with a data error in its mask or pages)
  *   out_status     [L*H] int32, or NULL
  */
 twinkv_status twinkv_cache_pack(const void* keys, const void* values, twinkv_shape s,
@@ -463,8 +466,8 @@ typedef struct {
  *   keys, values  [B][n][H][d] of s.dtype, 16-byte aligned, strides in s
  *   positions     [B][n] int32, at least 0, ascending and above those already stored
  *   table, lens   of the B*H units; the pages from slot lens[u] on must be in no other row
- *   out_lens      [B*H] int32: lens + n, or lens for a unit with a data error (nothing is
- *                 written to its pages); may be `lens` itself
+ *   out_lens      [B*H] int32: lens + n, or lens for a unit with a data error in its length or
+ *                 pages (nothing is written to them); may be `lens` itself
  *   out_status    [B*H] int32, or NULL
  * More than 64 tokens: TWINKV_ERR_UNSUPPORTED.
  */

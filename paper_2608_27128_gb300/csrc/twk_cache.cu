@@ -337,6 +337,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 && D == 128 ? 2 : 5)
             row[i] = -1;
             k[i] = v[i] = Values16<T>{};
         }
+    bool beyond = false;
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
         const int s = s0 + i * kStep;
@@ -344,13 +345,14 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 && D == 128 ? 2 : 5)
         float scale;
         int zero;
         k[i].get(x);
-        quantize16(x, w, &scale, &zero);
+        beyond |= quantize16(x, w, &scale, &zero);
         put_key<D>(im.bytes, s, j, w, scale, zero);
         if (j == 0) reinterpret_cast<int*>(im.bytes + P::kPos)[s] = row[i];
         v[i].get(x);
-        quantize16(x, w, &scale, &zero);
+        beyond |= quantize16(x, w, &scale, &zero);
         put_value<D>(im.bytes, im.slots + s * kSlotWords<D>, s, j, w, scale, zero);
     }
+    if (beyond && a.out_status) a.out_status[u] = kInvalid;     // the index kernel has written it
     __syncthreads();
     slots_to_page<D, kThreads>(im);
     __syncthreads();
@@ -396,6 +398,7 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendArgs a)
     }
     if (status) return;
     const int at = len % kPage;      // the first new row's slot of page[0]
+    bool beyond = false;
     for (int i0 = 0; i0 < a.n; i0 += kThreads / kLanes) {
         const int i = i0 + threadIdx.x / kLanes, j = first_chunk(threadIdx.x % kLanes);
         const bool on = i < a.n;
@@ -412,7 +415,7 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendArgs a)
         float scale;
         int zero;
         k.get(x);
-        quantize16(x, w, &scale, &zero);
+        beyond |= quantize16(x, w, &scale, &zero);
         if (on) {
             put_key<D>(to, s, j, w, scale, zero);
             if (j == 0)
@@ -420,10 +423,11 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendArgs a)
                     a.positions[static_cast<int64_t>(b) * a.n + i];
         }
         v.get(x);
-        quantize16(x, w, &scale, &zero);
+        beyond |= quantize16(x, w, &scale, &zero);
         if (on) put_value<D>(to, slots + i * kSlotWords<D>, s, j, w, scale, zero);
     }
     __syncthreads();
+    if (beyond && a.out_status) a.out_status[u] = kInvalid;     // the first thread has written it
     const int blocks = at + a.n > kPage ? 2 * D : D;
     for (int i = threadIdx.x; i < blocks; i += kThreads) {
         const Block8 blk(i % D);

@@ -74,17 +74,17 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi)
     return r;
 }
 
-// two bf16 numbers at a time; a NaN gives way to a number
+// two bf16 numbers at a time; a NaN stays one
 __device__ __forceinline__ uint32_t min_pair(uint32_t a, uint32_t b)
 {
     uint32_t r;
-    asm("min.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
 __device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b)
 {
     uint32_t r;
-    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
 __device__ __forceinline__ float rcp_approx(float x)
@@ -128,7 +128,11 @@ __device__ __forceinline__ void add_pair(float& x, float& y, float b)
 //            significant bits than hi).  The quotient is correctly rounded: the product with RN(1 / 15) and
 //            one step with its exact remainder (Markstein 1990).
 // Codes need no lower clamp: rint is odd, and -lo is among the values.
-__device__ __forceinline__ void quantize16(const uint32_t (&x)[8], uint32_t (&w)[2], float* scale,
+//
+// A group with a value that is not finite, or 2^120 or more in size, becomes s = z = c = 0; returns
+// whether this is one.
+constexpr float kMostValue = 0x1p120f;
+__device__ __forceinline__ bool quantize16(const uint32_t (&x)[8], uint32_t (&w)[2], float* scale,
                                            int* zero)
 {
     uint32_t low = x[0], high = x[0];
@@ -143,11 +147,12 @@ __device__ __forceinline__ void quantize16(const uint32_t (&x)[8], uint32_t (&w)
     ends = max_pair(ends, __shfl_xor_sync(0xffffffffu, ends, 1));
     ends = max_pair(ends, __shfl_xor_sync(0xffffffffu, ends, 2));
     const float up = bf16_lo(ends), down = bf16_hi(ends), range = up + down;
+    const bool beyond = !(up < kMostValue && down < kMostValue);
     constexpr float kFifteenth = 1.0f / 15.0f;
     const float q = range * kFifteenth;
     float s = fmaf(fmaf(-15.0f, q, range), kFifteenth, q);
     s = bf16_hi(bf16_pair(0.0f, s));
-    const bool flat = !(s >= 0x1p-126f);
+    const bool flat = !(s >= 0x1p-126f) || beyond;
     s = flat ? 0.0f : s;
     const float r = flat ? 0.0f : rcp_approx(s);
     constexpr float kFine = 12288.0f, kUnit = 12582912.0f;   // kUnit's last 16 bits are 0
@@ -166,8 +171,10 @@ __device__ __forceinline__ void quantize16(const uint32_t (&x)[8], uint32_t (&w)
             w[i] += __viaddmin_s16x2(v, zz, 0x000f000fu) << (4 * p);
         }
     }
+    if (beyond) w[0] = w[1] = 0;      // 0 times such a value is no number
     *scale = s;
-    *zero = z;
+    *zero = beyond ? 0 : z;
+    return beyond;
 }
 
 }  // namespace twk

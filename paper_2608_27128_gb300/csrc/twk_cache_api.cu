@@ -178,6 +178,7 @@ twinkv_status twinkv_cache_pack(const void* keys, const void* values, twinkv_sha
     a.index = retained_mask ? x.index : nullptr;
     a.lens = out_lens;
     a.to = pages_of(pool, table, max_pages);
+    a.out_status = out_status;
     return cuda_result(launch_pack(a, s.d, s.dtype == TWINKV_F32, st));
 }
 

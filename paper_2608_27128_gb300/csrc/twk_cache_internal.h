@@ -58,6 +58,7 @@ struct PackArgs {
     const int* index;            // [units][N] or null
     const int* lens;             // [units] slots to fill
     Pages to;
+    int* out_status;             // written by the index; or null
 };
 cudaError_t launch_pack(const PackArgs& a, int d, bool f32, cudaStream_t st);
 
