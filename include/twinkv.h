@@ -531,7 +531,8 @@ size_t twinkv_cache_attend_workspace(twinkv_queries s, int32_t d);
  *   out         [B][n][Hq][d] bf16, 16-byte aligned
  *   out_lse     [B][n][Hq] float32 log of the softmax's denominator (-inf: nothing seen), or
  *               NULL; attention over several caches is joined with it
- *   out_status  [B*H] int32, or NULL; slots of a page outside the pool count as unseen
+ *   out_status  [B*H] int32, or NULL; slots of a page outside the pool count as unseen, and a token
+ *               whose own slot is one has the position of the last slot before it on a page inside
  * Limits (TWINKV_ERR_UNSUPPORTED beyond): n <= 64, Hq / H <= 256, B*H and
  * B*H*ceil(n Hq / H / 16) <= 65535.
  */

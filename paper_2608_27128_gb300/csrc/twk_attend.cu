@@ -1195,11 +1195,17 @@ __global__ void __launch_bounds__(128) window_kernel(const AttendArgs a, int uni
     int len = a.lens[unit];
     if (len < 0 || len > static_cast<int64_t>(a.from.max_pages) * kPage) len = 0;
     const int* table = a.from.table + static_cast<int64_t>(unit) * a.from.max_pages;
+    // Slots of a page outside the pool are unseen and have no position: with that of the last slot before
+    // them that has one, positions ascend all the same.
     auto position = [&](int slot) -> int64_t {
-        const int id = table[slot / kPage];
-        if (static_cast<unsigned>(id) >= static_cast<unsigned>(a.from.n_pages)) return 0;
+        int page = slot / kPage, at = slot % kPage, id = table[page];
+        while (static_cast<unsigned>(id) >= static_cast<unsigned>(a.from.n_pages)) {
+            if (page == 0) return -1;
+            id = table[--page];
+            at = kPage - 1;
+        }
         return reinterpret_cast<const int*>(a.from.base + static_cast<int64_t>(id) * P::kBytes +
-                                            P::kPos)[slot % kPage];
+                                            P::kPos)[at];
     };
     int64_t wanted = a.n_sink;       // the first slot whose position is not below this
     int hi = len;
