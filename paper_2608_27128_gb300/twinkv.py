@@ -267,6 +267,8 @@ def _ws(ws, shape, op, device):
         ws = workspace(shape, op, device)
     if ws.numel() < need:
         raise ValueError(f"workspace needs {need} bytes, got {ws.numel()}")
+    if ws.device != device or not ws.is_contiguous():
+        raise ValueError(f"workspace must be contiguous and live on {device}")
     return ws
 
 
@@ -668,8 +670,10 @@ def _bytes(ws, need, dev: int, stream):
     """A workspace: the caller's, or a new one, allocated on the stream the call runs on."""
     if ws is None:
         return _made(None, "workspace", torch.uint8, (max(need, 1),), dev, stream)
-    if ws.get_device() != dev or ws.dtype is not torch.uint8 or ws.numel() < need:
-        raise ValueError(f"workspace must be a uint8 tensor of {need} bytes on CUDA device {dev}")
+    if (ws.get_device() != dev or ws.dtype is not torch.uint8 or ws.numel() < need
+            or not ws.is_contiguous()):
+        raise ValueError(f"workspace must be a contiguous uint8 tensor of {need} bytes on CUDA "
+                         f"device {dev}")
     return ws
 
 

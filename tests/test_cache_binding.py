@@ -1,0 +1,52 @@
+"""What the binding of the operators around the pass refuses or falls back to, without a GPU."""
+import pytest
+import torch
+
+from paper_2608_27128_gb300 import twinkv as tk
+
+
+class OnDevice(torch.Tensor):
+    """A tensor of the CPU that says it is on a CUDA device: the checks read no memory."""
+
+    def get_device(self):
+        return 0
+
+    @property
+    def device(self):
+        return torch.device("cuda", 0)
+
+
+def on_device(t):
+    return t.as_subclass(OnDevice)
+
+
+def workspaces(n):
+    one = torch.zeros(1, dtype=torch.uint8)
+    wide = torch.zeros(2 * n, dtype=torch.uint8)
+    return [one.expand(n), wide[::2], wide.view(2, n)[:, :n // 2].expand(2, n // 2)]
+
+
+def test_a_workspace_that_is_not_contiguous_is_refused():
+    """It has as many elements as are asked for, and not that many bytes from its address on."""
+    n = 4096
+    assert tk._bytes(on_device(torch.zeros(n, dtype=torch.uint8)), n, 0, None).numel() == n
+    for ws in workspaces(n):
+        if ws.is_contiguous():
+            continue
+        assert ws.numel() >= n
+        with pytest.raises(ValueError):
+            tk._bytes(on_device(ws), n, 0, None)
+
+
+def test_a_workspace_of_the_pass_has_to_be_contiguous_and_on_the_device():
+    s = tk.Shape(1, 2, 600, 128, tk.BF16)
+    n = tk.twinkv_workspace_size(s, tk.OP_REPAIR)
+    dev = torch.device("cuda", 0)
+    assert tk._ws(on_device(torch.zeros(n, dtype=torch.uint8)), s, tk.OP_REPAIR, dev).numel() == n
+    for ws in workspaces(n):
+        if ws.is_contiguous():
+            continue
+        with pytest.raises(ValueError):
+            tk._ws(on_device(ws), s, tk.OP_REPAIR, dev)
+    with pytest.raises(ValueError):
+        tk._ws(torch.zeros(n, dtype=torch.uint8), s, tk.OP_REPAIR, dev)
