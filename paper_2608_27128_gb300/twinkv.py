@@ -13,6 +13,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import math
+import operator
 import os
 import threading
 
@@ -731,6 +732,14 @@ def _rows_dtype(dtype, name):
     raise ValueError(f"{name} must be bfloat16 or float32")
 
 
+def _int32(x, name):
+    """An int that int32 holds: ctypes takes others modulo 2^32 without a word."""
+    i = operator.index(x)
+    if not -0x80000000 <= i <= 0x7fffffff:
+        raise ValueError(f"{name} must fit 32 bits, got {i}")
+    return i
+
+
 def _elsewhere(name, t, dev):
     return ValueError(f"{name} must live on CUDA device {dev}, not on {t.device}")
 
@@ -990,7 +999,8 @@ def twinkv_cache_attend(q, pool, table, lens, *, scale=None, window=0, n_sink=0,
         lse = o["lse"].data_ptr()
     ws = _bytes(ws, need, dev, stream)
     st = load().twinkv_cache_attend(
-        q.data_ptr(), s, d ** -0.5 if scale is None else scale, window, n_sink, p,
+        q.data_ptr(), s, d ** -0.5 if scale is None else scale, _int32(window, "window"),
+        _int32(n_sink, "n_sink"), p,
         table.data_ptr(), pages, lens.data_ptr(), o["out"].data_ptr(), lse,
         o["status"].data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream))
     _check(st, "twinkv_cache_attend")

@@ -50,3 +50,16 @@ def test_a_workspace_of_the_pass_has_to_be_contiguous_and_on_the_device():
             tk._ws(on_device(ws), s, tk.OP_REPAIR, dev)
     with pytest.raises(ValueError):
         tk._ws(torch.zeros(n, dtype=torch.uint8), s, tk.OP_REPAIR, dev)
+
+
+@pytest.mark.parametrize("value", [2 ** 31, 2 ** 32, 2 ** 32 + 5, -2 ** 31 - 1, -2 ** 32 + 1, 2.5, "7"])
+def test_windows_and_sinks_beyond_32_bits_are_refused(value):
+    """ctypes would take them modulo 2^32: a window of 2^32 + 5 as one of 5."""
+    with pytest.raises((ValueError, TypeError)):
+        tk._int32(value, "window")
+
+
+def test_windows_and_sinks_of_32_bits():
+    import numpy as np
+    for value in (0, 4, 2 ** 31 - 1, -1, np.int64(300), True):
+        assert tk._int32(value, "window") == value

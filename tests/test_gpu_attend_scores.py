@@ -74,3 +74,13 @@ def test_scores_that_are_all_but_nothing(d, G, scale):
             bound = R.attend_bound(want, *sizes, length)
             assert (np.abs(f64(got["out"])[0] - want) <= bound).all()
             assert (np.abs(f64(got["lse"])[0] - lse) <= 5e-4).all()
+
+
+@pytest.mark.parametrize("kw", [{"window": 2 ** 32 + 5}, {"window": 5, "n_sink": 2 ** 32},
+                                {"window": 2 ** 31}])
+def test_a_window_beyond_32_bits_is_refused(kw):
+    x = torch.randn(100, 64).to(torch.bfloat16)
+    pool, table, lens = pages_of(x, x, 64)
+    q = torch.randn(1, 1, 4, 64, device=device()).to(torch.bfloat16)
+    with pytest.raises(ValueError):
+        tk.twinkv_cache_attend(q, pool, table, lens, **kw)
