@@ -195,11 +195,20 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _current_calls():
+    """Functions for the current device's number and for the handle of a device's current stream."""
+    # torch.cuda's own make objects on the way (1.5 us a call); what lies beneath them is not public,
+    # so a torch that lacks it gets the public ones
+    device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return device, raw or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
+
+_current_device, _current_stream = _current_calls()
+
+
 def _stream(stream):
-    if stream is None:
-        # torch.cuda.current_stream().cuda_stream without the Stream object (1.5 us less a call)
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
-    return stream.cuda_stream
+    return _current_stream(_current_device()) if stream is None else stream.cuda_stream
 
 
 def _need(t, name, dtype, shape, device):
@@ -686,7 +695,7 @@ def _pool(pool):
     d = _PAGE_DIM.get(shape[-1]) if len(shape) == 2 else None
     if d is None:
         raise ValueError("pool must be [n_pages, PAGE_BYTES[d]]")
-    if dev < 0 or dev != torch._C._cuda_getDevice():
+    if dev < 0 or dev != _current_device():
         raise ValueError(f"pool must live on the current CUDA device, not on {pool.device}")
     if pool.dtype is not torch.uint8 or not pool.is_contiguous():
         raise ValueError("pool must be contiguous uint8")
@@ -778,7 +787,7 @@ def twinkv_qk_norm_rope(q, k, wq, wk, cos_sin, positions, eps=1e-6, *, out=None,
     if not isinstance(x, torch.Tensor):
         raise TypeError("q and k must be torch tensors")
     dev = x.get_device()
-    if dev < 0 or dev != torch._C._cuda_getDevice():
+    if dev < 0 or dev != _current_device():
         raise _elsewhere("q and k", x, "current")
     given = out or {}
     oq = ok = qk = kk = oqk = okk = None

@@ -63,3 +63,18 @@ def test_windows_and_sinks_of_32_bits():
     import numpy as np
     for value in (0, 4, 2 ** 31 - 1, -1, np.int64(300), True):
         assert tk._int32(value, "window") == value
+
+
+def test_current_stream_without_torchs_private_calls(monkeypatch):
+    """A torch that lacks the calls beneath torch.cuda's gets the public ones."""
+    class Bare:
+        pass
+
+    class Stream:
+        cuda_stream = 4711
+
+    monkeypatch.setattr(torch, "_C", Bare())
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda dev=None: Stream())
+    device, raw = tk._current_calls()
+    assert device() == 3 and raw(3) == 4711
