@@ -393,7 +393,8 @@ twinkv_status twinkv_policy(const void* keys, twinkv_shape s, const int32_t* bud
  *
  * Data errors, in out_status[u]: TWINKV_ERR_INVALID_ARG for a length outside
  * [0, 64 max_pages], a mask byte above 1 or a page number outside the pool;
- * TWINKV_ERR_TOO_LARGE for more slots than the unit's row of `table` has pages.  No
+ * TWINKV_ERR_TOO_LARGE for more slots than the unit's row of `table` has pages, which in
+ * twinkv_cache_append a length above 64 max_pages is too.  No
  * such unit makes a kernel read or write outside the caller's arrays.  A unit with a value that
  * its pages cannot hold (Rounding) is stored otherwise, length included, and gets
  * TWINKV_ERR_INVALID_ARG from the call that writes it.
