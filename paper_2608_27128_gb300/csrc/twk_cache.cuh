@@ -41,15 +41,6 @@ struct PageLayout {
     {
         return slot * kRow + (j % 8 / 2) * (8 * kGroups) + (j / 8) * 8 + (j & 1) * 4;
     }
-    // word (of kValCodes) and nibble of a value
-    __host__ __device__ static constexpr int val_word(int dim, int slot)
-    {
-        return (((dim / 16) * 8 + dim % 8) * 4 + slot % 8 / 2) * 4 + dim % 16 / 8 * 2 + slot / 32;
-    }
-    __host__ __device__ static constexpr int val_nibble(int slot)
-    {
-        return 4 * (slot & 1) + 2 * (slot % 32 / 16) + slot % 16 / 8;
-    }
     // element of kValZeros
     __host__ __device__ static constexpr int val_zero(int group, int slot)
     {
