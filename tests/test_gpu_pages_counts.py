@@ -1,4 +1,5 @@
 """PageCache (GPU): sequences whose lengths are not what the host counted, and heads without slots."""
+import numpy as np
 import pytest
 import torch
 
