@@ -521,9 +521,10 @@ size_t twinkv_cache_attend_workspace(twinkv_queries s, int32_t d);
  * the slots up to its own and, with window > 0, of those only the ones whose position is
  * above its own minus `window` or below n_sink (the sinks and the recent region of Sec. 3.2).
  *   o = sum_j softmax_j(scale q . k_j) v_j      float32 sums; a token that sees nothing: 0
- * Precision: codes and queries enter exactly; a probability times its slot's value scale is
- * rounded to 11 bits (fewer where the scale is below 2^-16 of the largest among the slots of
- * the pages visited), the result to bf16.
+ * Precision: codes enter exactly, and so do query values down to 2^-27 of their row's largest (or
+ * of 2^-100).  The product of a probability, exp(score - largest so far), and its slot's value
+ * scale is rounded to 11 bits, or by up to 2^-28 of the largest value scale among the slots of the
+ * pages visited (or of 2^-110) where that is more.  The result is rounded to bf16.
  *   q           [B][n][Hq][d] bf16, 16-byte aligned, strides in s (multiples of 8); values
  *               below 2^100, and q . k, over each group of 64 and in all, below 2^120
  *   scale       finite, above 0

@@ -16,11 +16,12 @@
 //     subtracted or scaled per element.
 //   - Keys: with Q_G the sum of q over a group, q . k = sum_G s_G (sum q c - z_G Q_G): the second term
 //     is the accumulator's start value, the scale one multiplication per group.  Queries are scaled
-//     by a power of two per row, which leaves them exact.
-//   - Values: a probability is multiplied by its slot's scale and rounded to f16, 11 bits, in units that
-//     follow the largest scale seen (bf16 needs none, but has 8 bits, and its codes, as 128 + c, take 7
-//     instructions a word: error against 64 bits 0.0021, 0.0017 now, which is the output's rounding).
-//     The zeros go into one more product with the same rounded numbers.
+//     by a power of two per row, which leaves them exact down to 2^-27 of the row's largest.
+//   - Values: a probability is multiplied by its slot's scale and rounded to f16, in units that follow
+//     the largest scale seen: to 11 bits, or by up to 2^-28 of that scale where the product is below
+//     2^-17 of it (bf16 needs no units, but has 8 bits, and its codes, as 128 + c, take 7 instructions
+//     a word: error against 64 bits 0.0021, 0.0017 now, which is the output's rounding).  The zeros go
+//     into one more product with the same rounded numbers.
 //   - mma.sync m16n8k16 with the cache as the 16-row operand (slots for keys, dimensions for values)
 //     and up to 8 query rows as the other one: 18 multiplications for 16 slots at d = 128.  With
 //     tcgen05 the cache would have to be written to shared memory again as 16-bit numbers, four
@@ -459,7 +460,7 @@ __global__ void __launch_bounds__(32 * Config<D, R>::kWarps, 1)
             p.seen ? p.seen + static_cast<int64_t>(unit) * (1 + p.a.n) : nullptr;
         sinks = seen ? seen[0] : 0;
         // Queries as f16: a row is scaled by a power of two, 2^k, so that its largest value is in
-        // [2^14, 2^15); values down to 2^-28 of it stay exact.  Its scores are sums of 2^(k - 24) q c.
+        // [2^14, 2^15); values down to 2^-27 of it stay exact.  Its scores are sums of 2^(k - 24) q c.
 #pragma unroll
         for (int half = 0; half < (kLeft ? 2 : 1); ++half) {
             const int in_part = kLeft ? g + 8 * half : g / 2 + g % 2 * 4, r = r0 + in_part;

@@ -72,3 +72,31 @@ def test_a_slot_seen_that_must_not_be(d, window, n_sink):
     everything, *_ = J.definition(q, k, v, np.ones_like(see), scale, ks, vs, 80)
     for g in (3, 7):
         assert (np.abs(everything - out)[:, g] > bound[:, g]).mean() > 0.3
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_probabilities_of_8_bits(d):
+    """Products of probabilities and value scales rounded to bf16 instead of f16."""
+    rng = np.random.default_rng(d)
+    beyond = 0
+    for n in (2, 4, 8) * 20:
+        half = rng.standard_normal((n // 2, d))
+        v0 = R.to_bf16(np.stack([half, -half], 1).reshape(n, d))
+        k0 = R.to_bf16(rng.standard_normal((n, d)) * 0.3)
+        k, v, ks, vs = R.round_trip(k0), R.round_trip(v0), R.quantize(k0)[1], R.quantize(v0)[1]
+        q = R.to_bf16(rng.standard_normal((1, 4, d)) * 0.3)
+        see = np.ones((1, n), bool)
+        out, bound, *_ = J.definition(q, k, v, see, d ** -0.5, ks, vs, 1)
+        x = q[0] @ k.T * d ** -0.5
+        p = np.exp(x - x.max(-1, keepdims=True))
+        for bits, least in ((R.to_bf16, True), (lambda y: y.astype(np.float16).astype(float), False)):
+            got = np.zeros((4, d))
+            for e in range(d):
+                s = vs[:, e // 64]
+                got[:, e] = bits(p * s) @ (v[:, e] / np.where(s > 0, s, 1)) / p.sum(-1)
+            wrong = (np.abs(R.to_bf16(got) - out[0]) > bound[0]).any()
+            if least:
+                beyond += wrong
+            else:
+                assert not wrong
+    assert beyond > 30

@@ -212,3 +212,38 @@ def test_windows_over_the_grid(d, G, n, units, least, most, window, n_sink):
 def test_windows_over_gaps_between_positions(gap, window):
     c = Units(gap, [1, 64, 65, 700, 1300], 64, gap=gap)
     check(c, pointing_queries(window, c, 5, 4, window, 4), 5, window, 4)
+
+
+# ---------------------------------------------------------------- roundings
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G", [4, 8, 16])
+@pytest.mark.parametrize("length", [500, 20000])
+@pytest.mark.parametrize("above", [8, 12, 14, 16])
+def test_one_key_with_a_value_of_0_above_all_others(d, G, length, above):
+    """As a sink often is: the output is what the small probabilities of the others come to."""
+    rng = np.random.default_rng([d, G, length, above])
+    u = rng.choice([-1.0, 1.0], d)
+    k = rng.standard_normal((length, d)) * 0.05
+    v = 1.0 + 0.2 * rng.standard_normal((length, d))
+    first = int(rng.integers(length))
+    k[first], v[first] = u, 0.0
+    c = Units(above, [length], d, gap=1, k=[k], v=[v])
+    q = np.broadcast_to(u * above * d ** -0.5, (1, 1, G, d)) * rng.uniform(0.9, 1.1, (1, 1, G, 1))
+    check(c, q, 1)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G", [4, 8, 16])
+def test_probabilities_have_11_bits(d, G):
+    """Pairs of opposite values under nearly equal scores: outputs are near 0, and what the
+    probabilities lose stays visible beside the output's own rounding."""
+    rng = np.random.default_rng([d, G])
+    lens = [2, 4, 8] * 40
+    k = [rng.standard_normal((n, d)) * 0.3 for n in lens]
+    v = []
+    for n in lens:
+        half = rng.standard_normal((n // 2, d))
+        v.append(np.stack([half, -half], 1).reshape(n, d))
+    c = Units(d + G, lens, d, gap=1, k=k, v=v)
+    check(c, rng.standard_normal((len(lens), 1, G, d)) * 0.3, 1)
