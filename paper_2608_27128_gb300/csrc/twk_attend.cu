@@ -42,15 +42,18 @@
 // unnormalised outputs), and merge_kernel joins them in the order of the slots.  Nothing depends on
 // which warp comes first: results are the same from call to call.
 //
-// Measured (us a call; share of the measured copy rate):
-//   32 x 8 units of 4k to 16k slots, 4 rows, d = 128     73.4   77 %
-//   8 units of 131009 slots, 4 rows, d = 128             35.2   63 %
-//   16 x 8 units of 16384 slots, 8 rows, d = 128         61.3   73 %; 16 rows 85.2, 52 %
-//   32 x 8 units of 16384 slots, 4 rows, d = 64          62.1   72 %
-// Without its arithmetic the first takes 69 and the second 33: about 10 us go into the two launches, the
-// lengths, the first pages' latency and the merge, the rest is loads.  With 16 rows the arithmetic
-// bounds it (two warps on a quarter of the SM, whose registers they fill).
-// Tried, in us of the first where not said: one bulk copy per half page and a barrier 92 where
+// Measured (us a call in a graph, over caches taken in turn; share of the measured copy rate):
+//   32 x 8 units of 4k to 16k slots, 4 rows, d = 128     71.7   79 %
+//   32 x 8 units of 8192, 16384, 32768 slots, the same   57.4, 100.4, 188.3   78, 89, 95 %
+//   8 units of 131009 slots, 4 rows, d = 128             32.8   68 %
+//   16 x 8 units of 16384 slots, 8 rows, d = 128         58.9   76 %; 16 rows 83.6, 53 %
+//   32 x 8 units of 16384 slots, 4 rows, d = 64          60.3   74 %
+//   32 x 8 units of 8192 slots, 16 rows, d = 64          57.8   39 %
+// By the differences of the second line loads run at 6.9 TB/s, and about 15 us go into the launches,
+// the lengths, the first pages' latency, the last warps and the merge.  With 16 rows two warps on a
+// quarter of the SM bound it, which do not cover each other's latencies: at d = 128 their registers fill
+// it, at d = 64 (186 registers) more warps gained 4 % at best (Config).
+// Tried, in us of a call on the first where not said (then 75 to 85): one bulk copy per half page and a barrier 92 where
 // cp.async took 82; 16 warps with 3 half pages each instead of 12 with 4: 88 against 85; shifts on the
 // multiplier pipe 88 against 82; e4m3 codes with q in two parts, which mma.sync runs no faster than
 // f16 here: 90 against 82, and twice the time with more rows; one kernel in which the block that
