@@ -423,7 +423,8 @@ typedef struct {
  * turns a layer's projections into queries and into the post-RoPE keys of Sec. 3.2.
  *   y = x / sqrt(mean(x^2) + eps) * w         (w NULL: y = x)
  *   out[j] = y[j] cos - y[j + d/2] sin,  out[j + d/2] = y[j] sin + y[j + d/2] cos
- * in float32, rounded once.
+ * in float32, rounded once; with norms, values have to be below 2^60 (float32 sums of squares), and
+ * heads not all 0 or below 2^-60 if eps is 0.
  *   q, k        [tokens][heads][d] of s.dtype, 16-byte aligned, strides in s (views into a
  *               fused projection, or a dense cache [H][N][d]); heads_q or heads_k may be 0
  *   wq, wk      [d] of s.dtype, 16-byte aligned, or NULL (no norm)
