@@ -545,6 +545,124 @@ twinkv_status twinkv_cache_attend(const void* q, twinkv_queries s, float scale, 
                                   float* out_lse, int32_t* out_status, void* workspace,
                                   size_t workspace_bytes, void* stream);
 
+/* ==== The retained set by attention weight ============================================
+ *
+ * The calls below make the set S0 that the pass repairs, from what the layers' attention pays
+ * to each key: attention over a prompt (twinkv_prompt_attend), the sum of its weights at each
+ * key (twinkv_prompt_weights; for tokens decoded over pages twinkv_cache_weights adds theirs),
+ * and the positions that a budget keeps by that sum (twinkv_weight_policy), a mask for
+ * twinkv_repair, twinkv_cache_pack or twinkv_cache_compact.  Streams, workspaces, CUDA graphs
+ * and errors are as above.
+ *
+ * Sequences.  Queries [tokens][Hq][d] and keys [keys][H][d] hold B sequences one after another.
+ * Sequence b has the rows [offsets[b], offsets[b + 1]) of q, of which the first lens[b] are its
+ * tokens, and rows of k likewise from k_offsets and k_lens.  With n tokens and m keys, token i is at
+ * the key m - n + i: a prompt has n = m, a chunk of one n < m, and with n > m the first n - m
+ * tokens see nothing.  Token i sees the keys up to its own and, with window > 0, of those only the ones
+ * less than `window` behind it and the first n_sink of the sequence.  Rows that are no sequence's
+ * tokens (or keys) are not computed: their outputs are left as they were.
+ */
+typedef struct {
+    const int32_t* offsets;     /* [B + 1] device, ascending, or NULL (B = 1): every row */
+    const int32_t* lens;        /* [B], or NULL: offsets[b + 1] - offsets[b] */
+    const int32_t* k_offsets;   /* [B + 1], or NULL: offsets (if that is NULL: every row of k) */
+    const int32_t* k_lens;      /* [B], or NULL: with k_offsets their differences, else lens */
+} twinkv_sequences;
+
+/* Sizes, and strides in elements: multiples of 8, above 0 (of a dimension of 1: any). */
+typedef struct {
+    int32_t B, H, Hq, d;        /* d 64 or 128 */
+    int32_t tokens, keys;       /* rows of q, and of k and v */
+    int64_t q_token, q_head, k_token, k_head, v_token, v_head;
+} twinkv_prompt;
+
+size_t twinkv_prompt_attend_workspace(twinkv_prompt s);
+
+/*
+ * Attention over prompts, query head h reading KV head h / (Hq / H):
+ *   o = sum_j softmax_j(scale q . k_j) v_j over the keys j that the token sees; 0 if there are none
+ * Precision: products of bf16 values in float32 sums; exp(score - m), m within 6 of the largest score
+ * so far, is rounded to bf16 for its product with the values, not for the denominator.  The
+ * result is rounded to bf16.
+ *   q, k, v     bf16, 16-byte aligned, strides in s; q . k below 2^120; what a sequence's keys and
+ *               values hold has to be finite, other rows may hold anything
+ *   scale       finite, above 0
+ *   window      0: none (n_sink is then not used)
+ *   out         [tokens][Hq][d] bf16, 16-byte aligned
+ *   out_lse     [tokens][Hq] float32 log of the softmax's denominator (-inf: nothing seen), or NULL
+ *   out_status  [B] int32, or NULL: TWINKV_ERR_INVALID_ARG for a sequence whose offsets descend or
+ *               are outside q or k, or whose length is below 0 or beyond its rows (it is not computed)
+ * Limits (TWINKV_ERR_UNSUPPORTED beyond): tokens and keys <= 2^24, B <= 65535, Hq / H <= 128.
+ */
+twinkv_status twinkv_prompt_attend(const void* q, const void* k, const void* v, twinkv_prompt s,
+                                   twinkv_sequences seqs, float scale, int32_t window,
+                                   int32_t n_sink, void* out, float* out_lse, int32_t* out_status,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+
+size_t twinkv_prompt_weights_workspace(twinkv_prompt s);
+
+/*
+ * What the attention over prompts pays to each key: per KV head h and key j the sum
+ *   [score +] sum over tokens i that see j, query heads g of h:  exp(scale q_ig . k_j - lse_ig)
+ * in float32, in an order that the sizes alone decide.
+ *   q, k, s, seqs, scale, window, n_sink   as in twinkv_prompt_attend (the strides of v are not used)
+ *   lse         [tokens][Hq] float32, as twinkv_prompt_attend gives it
+ *   last        > 0: only the last `last` tokens of each sequence count (the observation window of
+ *               a policy); 0: all
+ *   score       [H][keys] float32: sums so far (of earlier chunks), or NULL
+ *   out_score   [H][keys] float32; may be `score` itself
+ *   out_status  [B] int32, or NULL, as in twinkv_prompt_attend
+ * Limits as there.
+ */
+twinkv_status twinkv_prompt_weights(const void* q, const void* k, const float* lse,
+                                    twinkv_prompt s, twinkv_sequences seqs, float scale,
+                                    int32_t window, int32_t n_sink, int32_t last,
+                                    const float* score, float* out_score, int32_t* out_status,
+                                    void* workspace, size_t workspace_bytes, void* stream);
+
+size_t twinkv_cache_weights_workspace(twinkv_queries s, int32_t d);
+
+/*
+ * The same for the newest n <= 64 tokens of each sequence over its pages (Token i is the one in slot
+ * lens[u] - n + i, and sees what it sees in twinkv_cache_attend): per unit u and slot j
+ *   out_score = score + sum over the tokens i and query heads g that see j of
+ *               exp(scale q_ig . k_j - lse_ig)
+ *   q, s, scale, window, n_sink, pool, table, lens   as in twinkv_cache_attend
+ *   lse         [B][n][Hq] float32, as twinkv_cache_attend gives it
+ *   score       [B*H][N] float32: the slots' sums so far
+ *   out_score   [B*H][N] float32; may be `score` itself.  Entries from lens[u] on are left as they were
+ *   out_status  [B*H] int32, or NULL: TWINKV_ERR_INVALID_ARG as in twinkv_cache_attend (slots of a page
+ *               outside the pool keep their sums), TWINKV_ERR_TOO_LARGE for lens[u] > N (that unit is
+ *               not computed)
+ * Limits as there, and N <= 2^20.  The workspace (256-byte aligned) is only needed with a window.
+ */
+twinkv_status twinkv_cache_weights(const void* q, const float* lse, twinkv_queries s, float scale,
+                                   int32_t window, int32_t n_sink, twinkv_pool pool,
+                                   const int32_t* table, int32_t max_pages, const int32_t* lens,
+                                   const float* score, float* out_score, int32_t N,
+                                   int32_t* out_status, void* workspace, size_t workspace_bytes,
+                                   void* stream);
+
+/*
+ * Eviction by accumulated weight: per unit the budget[u] positions with the highest score, sink and
+ * recent positions first (Sec. 3.1; they tie among themselves), equal scores in position order (lower
+ * first), -0 equal to 0, NaN below every number.
+ *   score       [units][N] float32 device, N <= 2^20, units <= 65535
+ *   lens        [units] int32: positions (slots) of each unit, or NULL: N.  Entries from lens[u] on are
+ *               not looked at
+ *   budget      [units] int32; more than lens[u]: every position is kept
+ *   n_sink, n_recent   protected positions: the first n_sink, and the last n_recent of lens[u]
+ *   out_mask    [units][N] uint8: 1 for a kept position, 0 for others
+ *   out_score   [units][N] float32: the kept positions' scores in order, then 0: the sums of a cache
+ *               that is compacted by out_mask; or NULL.  Not `score`
+ *   out_status  [units] int32, or NULL: TWINKV_ERR_INVALID_ARG where budget[u] or lens[u] is outside
+ *               [0, N] (that unit's mask and scores are all 0)
+ */
+twinkv_status twinkv_weight_policy(const float* score, int32_t units, int32_t N,
+                                   const int32_t* lens, const int32_t* budget, int32_t n_sink,
+                                   int32_t n_recent, uint8_t* out_mask, float* out_score,
+                                   int32_t* out_status, void* stream);
+
 /* Static description of a status code. */
 const char* twinkv_status_string(twinkv_status st);
 

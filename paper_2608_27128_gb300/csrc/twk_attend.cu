@@ -66,6 +66,7 @@
 #include "twk_cache.cuh"
 #include "twk_cache_internal.h"
 #include "twk_internal.h"
+#include "twk_prompt_internal.h"
 #include "twk_ptx.cuh"
 
 namespace twk {
@@ -1235,6 +1236,18 @@ __global__ void __launch_bounds__(128) window_kernel(const AttendArgs a, int uni
     if (lane == 0) seen[static_cast<int64_t>(unit) * (1 + a.n) + 1 + which] = lo;
 }
 
+}  // namespace
+
+cudaError_t launch_windows(const AttendArgs& a, int units, int* seen, cudaStream_t st)
+{
+    const int warps = units * (1 + a.n);
+    if (a.d == 128) window_kernel<128><<<(warps + 3) / 4, 128, 0, st>>>(a, units, seen);
+    else window_kernel<64><<<(warps + 3) / 4, 128, 0, st>>>(a, units, seen);
+    return cudaGetLastError();
+}
+
+namespace {
+
 size_t up256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
 int part_rows(int rows) { return rows <= 8 ? 8 : 16; }
@@ -1257,10 +1270,8 @@ cudaError_t launch(AttendParams& p, int sms, cudaStream_t st)
     const size_t smem = kRings + (p.chunks + 1) * 4;
     const dim3 grid(std::min(sms, kAttendBlocks));
     if (p.seen) {
-        const int warps = p.units * (1 + p.a.n);
-        window_kernel<D><<<(warps + 3) / 4, 128, 0, st>>>(p.a, p.units,
-                                                          const_cast<int*>(p.seen));
-        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+        if ((e = launch_windows(p.a, p.units, const_cast<int*>(p.seen), st)) != cudaSuccess)
+            return e;
         e = launch_dependent(attend_kernel<D, R>, grid, 32 * C::kWarps, smem, st, p);
     } else {
         attend_kernel<D, R><<<grid, 32 * C::kWarps, smem, st>>>(p);

@@ -42,6 +42,9 @@ EXPORTED = (
     "twinkv_cache_page_bytes", "twinkv_cache_move_workspace", "twinkv_cache_attend_workspace",
     "twinkv_qk_norm_rope", "twinkv_cache_pack", "twinkv_cache_append", "twinkv_cache_compact",
     "twinkv_cache_read", "twinkv_cache_attend",
+    "twinkv_prompt_attend_workspace", "twinkv_prompt_weights_workspace",
+    "twinkv_cache_weights_workspace", "twinkv_prompt_attend", "twinkv_prompt_weights",
+    "twinkv_cache_weights", "twinkv_weight_policy",
 )
 PAGE_SLOTS = 64                                 # slots of a page (TWINKV_PAGE_SLOTS)
 PAGE_BYTES = {64: 4864, 128: 9472}              # twinkv_cache_page_bytes by head dimension
@@ -79,6 +82,16 @@ class Rows(ctypes.Structure):
 class Queries(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("B", "H", "Hq", "n")] + \
                [(n, ctypes.c_int64) for n in ("q_batch", "q_token", "q_head")]
+
+
+class Sequences(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("offsets", "lens", "k_offsets", "k_lens")]
+
+
+class Prompt(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "H", "Hq", "d", "tokens", "keys")] + \
+               [(n, ctypes.c_int64) for n in ("q_token", "q_head", "k_token", "k_head",
+                                              "v_token", "v_head")]
 
 
 class TwinKVError(RuntimeError):
@@ -159,8 +172,22 @@ def load(build_if_missing: bool = True):
         lib.twinkv_cache_read.argtypes = [Pool, _P, i32, _P, i32, i32, i32, _P, _P, _P, _P, _P]
         lib.twinkv_cache_attend.argtypes = [_P, Queries, ctypes.c_float, i32, i32, Pool, _P, i32,
                                             _P, _P, _P, _P, _P, ctypes.c_size_t, _P]
+        for name in ("twinkv_prompt_attend_workspace", "twinkv_prompt_weights_workspace"):
+            getattr(lib, name).argtypes = [Prompt]
+            getattr(lib, name).restype = ctypes.c_size_t
+        lib.twinkv_cache_weights_workspace.argtypes = [Queries, i32]
+        lib.twinkv_cache_weights_workspace.restype = ctypes.c_size_t
+        lib.twinkv_prompt_attend.argtypes = [_P, _P, _P, Prompt, Sequences, ctypes.c_float, i32,
+                                             i32, _P, _P, _P, _P, ctypes.c_size_t, _P]
+        lib.twinkv_prompt_weights.argtypes = [_P, _P, _P, Prompt, Sequences, ctypes.c_float, i32,
+                                              i32, i32, _P, _P, _P, _P, ctypes.c_size_t, _P]
+        lib.twinkv_cache_weights.argtypes = [_P, _P, Queries, ctypes.c_float, i32, i32, Pool, _P,
+                                             i32, _P, _P, _P, i32, _P, _P, ctypes.c_size_t, _P]
+        lib.twinkv_weight_policy.argtypes = [_P, i32, i32, _P, _P, i32, i32, _P, _P, _P, _P]
         for name in ("twinkv_qk_norm_rope", "twinkv_cache_pack", "twinkv_cache_append",
-                     "twinkv_cache_compact", "twinkv_cache_read", "twinkv_cache_attend"):
+                     "twinkv_cache_compact", "twinkv_cache_read", "twinkv_cache_attend",
+                     "twinkv_prompt_attend", "twinkv_prompt_weights", "twinkv_cache_weights",
+                     "twinkv_weight_policy"):
             getattr(lib, name).restype = ctypes.c_int
         lib.twinkv_status_string.argtypes = [ctypes.c_int]
         lib.twinkv_status_string.restype = ctypes.c_char_p
@@ -1013,6 +1040,219 @@ def twinkv_cache_attend(q, pool, table, lens, *, scale=None, window=0, n_sink=0,
         table.data_ptr(), pages, lens.data_ptr(), o["out"].data_ptr(), lse,
         o["status"].data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream))
     _check(st, "twinkv_cache_attend")
+    return o
+
+
+# ---- the retained set by attention weight
+
+@functools.lru_cache(maxsize=1024)
+def _prompt_workspace_size(what, *sizes) -> int:
+    return int(getattr(load(), f"twinkv_prompt_{what}_workspace")(Prompt(*sizes)))
+
+
+def _prompt_workspace(what, q_shape, k_shape, B, device):
+    T, Hq, d = (int(x) for x in q_shape)
+    Tk, H, dk = (int(x) for x in k_shape)
+    size = _prompt_workspace_size(what, int(B), H, Hq, d, T, Tk) if d == dk else 0
+    if size == 0:
+        raise ValueError("unsupported queries and keys")
+    return torch.empty(size, dtype=torch.uint8, device=device)
+
+
+def prompt_attend_workspace(q_shape, k_shape, B: int, device) -> torch.Tensor:
+    """A workspace for twinkv_prompt_attend with queries of q_shape [T, Hq, d], keys of k_shape
+    [Tk, H, d] and B sequences."""
+    return _prompt_workspace("attend", q_shape, k_shape, B, device)
+
+
+def prompt_weights_workspace(q_shape, k_shape, B: int, device) -> torch.Tensor:
+    """A workspace for twinkv_prompt_weights, likewise."""
+    return _prompt_workspace("weights", q_shape, k_shape, B, device)
+
+
+@functools.lru_cache(maxsize=1024)
+def _prompt_plan(what, B, q, k, v):
+    if len(q[1]) != 3 or len(k[1]) != 3:
+        raise ValueError("q must be [T, Hq, d], k and v [Tk, H, d]")
+    (T, Hq, d), (Tk, H, _) = q[1], k[1]
+    if T < 1 or Tk < 1 or H < 1 or Hq < 1 or Hq % H:
+        raise ValueError("q and k need rows, and as many query heads as a multiple of the KV heads")
+    strides = []
+    for x, name, shape in ((q, "q", (T, Hq, d)), (k, "k", (Tk, H, d)), (v, "v", (Tk, H, d))):
+        at = _row_strides(x, name, torch.bfloat16, shape) if x is not None else [0, 0]
+        if x is not None and any(n > 1 and y <= 0 for n, y in zip(shape, at)):
+            raise ValueError(f"{name}'s rows must be apart from each other")
+        strides += at
+    sizes = (B, H, Hq, d, T, Tk)
+    return Prompt(*sizes, *strides), _prompt_workspace_size(what, *sizes)
+
+
+def _prompt(what, q, k, v, offsets, lens, k_offsets, k_lens):
+    """(Prompt, Sequences, sizes B, T, Tk, Hq, H, d, device number, workspace bytes) of a call."""
+    kinds = _kind(q, "q"), _kind(k, "k"), _kind(v, "v") if what == "attend" else None
+    dev = q.get_device()
+    if dev < 0 or dev != _current_device():
+        raise _elsewhere("q", q, "current")
+    for x, name in ((k, "k"), (v, "v")):
+        if x is not None and x.get_device() != dev:
+            raise _elsewhere(name, x, dev)
+    B = 1
+    if offsets is not None:
+        if not isinstance(offsets, torch.Tensor) or offsets.dim() != 1 or len(offsets) < 2:
+            raise ValueError("offsets must be a tensor [B + 1]")
+        B = offsets.shape[0] - 1
+    at = []
+    for x, name, n in ((offsets, "offsets", B + 1), (lens, "lens", B),
+                       (k_offsets, "k_offsets", B + 1), (k_lens, "k_lens", B)):
+        at.append(None if x is None else _same(x, name, torch.int32, (n,), dev).data_ptr())
+    s, need = _prompt_plan(what, B, *kinds)
+    if need == 0:
+        raise TwinKVError(ERR_UNSUPPORTED, f"twinkv_prompt_{what}")
+    return s, Sequences(*at), B, dev, need
+
+
+def twinkv_prompt_attend(q, k, v, offsets=None, *, lens=None, k_offsets=None, k_lens=None,
+                         scale=None, window=0, n_sink=0, want_lse=False, out=None, ws=None,
+                         stream=None) -> dict:
+    """Causal attention over whole prompts, or chunks of them, packed one after another.
+
+    q [T,Hq,d], k and v [Tk,H,d] bf16, any strides that keep rows on 16-byte boundaries (views into
+    a fused projection, or a dense cache [H,N,d]).  offsets [B+1] int32: sequence b has the rows
+    offsets[b] to offsets[b+1] of q, the first lens[b] ([B] int32; None: all) being its tokens; its
+    keys likewise by k_offsets and k_lens (None: as the tokens); no offsets: one sequence.  Token i
+    of n with m keys is at key m - n + i and sees the keys up to it; window > 0: of those only the
+    ones less than ``window`` behind it, and the first ``n_sink``.  Returns a dict: out [T,Hq,d]
+    bf16, status [B] int32 and, with want_lse, lse [T,Hq] float32; rows that are no token's are
+    left as they were.
+    """
+    s, seqs, B, dev, need = _prompt("attend", q, k, v, offsets, lens, k_offsets, k_lens)
+    given, shape = out or {}, tuple(q.shape)
+    o = {"out": _made(given.get("out"), "out", torch.bfloat16, shape, dev, stream),
+         "status": _made(given.get("status"), "status", torch.int32, (B,), dev, stream)}
+    if want_lse:
+        o["lse"] = _made(given.get("lse"), "lse", torch.float32, shape[:2], dev, stream)
+    ws = _bytes(ws, need, dev, stream)
+    st = load().twinkv_prompt_attend(
+        q.data_ptr(), k.data_ptr(), v.data_ptr(), s, seqs, s.d ** -0.5 if scale is None else scale,
+        _int32(window, "window"), _int32(n_sink, "n_sink"), o["out"].data_ptr(),
+        _ptr(o.get("lse")), o["status"].data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream))
+    _check(st, "twinkv_prompt_attend")
+    return o
+
+
+def twinkv_prompt_weights(q, k, lse, offsets=None, *, lens=None, k_offsets=None, k_lens=None,
+                          scale=None, window=0, n_sink=0, last=0, score=None, out=None, ws=None,
+                          stream=None) -> dict:
+    """What the attention of twinkv_prompt_attend pays to each key, summed over tokens and the query
+    heads of a KV head.
+
+    q, k, offsets and so on as there; lse [T,Hq] float32 as it gave it; last > 0: only so many last
+    tokens of each sequence count; score [H,Tk] float32: sums so far to add to.  Returns a dict:
+    score [H,Tk] float32 (``out`` may hold ``score`` itself) and status [B] int32; entries that are no
+    key's are left as they were.
+    """
+    s, seqs, B, dev, need = _prompt("weights", q, k, None, offsets, lens, k_offsets, k_lens)
+    given, shape = out or {}, (s.H, s.keys)
+    _same(lse, "lse", torch.float32, (s.tokens, s.Hq), dev)
+    if score is not None:
+        _same(score, "score", torch.float32, shape, dev)
+    o = {"score": _made(given.get("score"), "score", torch.float32, shape, dev, stream),
+         "status": _made(given.get("status"), "status", torch.int32, (B,), dev, stream)}
+    ws = _bytes(ws, need, dev, stream)
+    st = load().twinkv_prompt_weights(
+        q.data_ptr(), k.data_ptr(), lse.data_ptr(), s, seqs,
+        s.d ** -0.5 if scale is None else scale, _int32(window, "window"),
+        _int32(n_sink, "n_sink"), _int32(last, "last"), _ptr(score), o["score"].data_ptr(),
+        o["status"].data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream))
+    _check(st, "twinkv_prompt_weights")
+    return o
+
+
+@functools.lru_cache(maxsize=1024)
+def _cache_weights_workspace_size(B, n, Hq, H, d) -> int:
+    return int(load().twinkv_cache_weights_workspace(Queries(B, H, Hq, n, 0, 0, 0), d))
+
+
+def cache_weights_workspace(q_shape, H: int, device) -> torch.Tensor:
+    """A workspace for twinkv_cache_weights with a window, queries [B, n, Hq, d], H KV heads."""
+    B, n, Hq, d = (int(x) for x in q_shape)
+    size = _cache_weights_workspace_size(B, n, Hq, int(H), d)
+    if size == 0:
+        raise ValueError("unsupported queries")
+    return torch.empty(size, dtype=torch.uint8, device=device)
+
+
+def twinkv_cache_weights(q, lse, pool, table, lens, score, *, scale=None, window=0, n_sink=0,
+                         out=None, ws=None, stream=None) -> dict:
+    """What the newest n tokens' attention over pages pays to each slot, added to the sums so far.
+
+    q, pool, table, lens, scale, window and n_sink as in twinkv_cache_attend, lse [B,n,Hq] float32
+    as it gave it; score [B,H,N] float32, N at least the longest unit.  Returns a dict: score [B,H,N]
+    (``out`` may hold ``score`` itself; entries from lens on are left as they were) and status [B,H].
+    """
+    p, d, dev = _pool(pool)
+    if not isinstance(lens, torch.Tensor) or lens.dim() != 2:
+        raise ValueError("lens must be [B, H]")
+    units = lens.shape
+    s, B, shape, _ = _attend_plan(_kind(q, "q"), units[1], d)
+    if q.get_device() != dev:
+        raise _elsewhere("q", q, dev)
+    if units[0] != B:
+        raise ValueError(f"lens must be [{B}, H]")
+    _same(lens, "lens", torch.int32, units, dev)
+    _same(lse, "lse", torch.float32, shape[:3], dev)
+    pages = _table(table, "table", units, dev)
+    if not isinstance(score, torch.Tensor) or score.dim() != 3:
+        raise ValueError("score must be [B, H, N]")
+    N, given = score.shape[-1], out or {}
+    _same(score, "score", torch.float32, (*units, N), dev)
+    o = {"score": _made(given.get("score"), "score", torch.float32, (*units, N), dev, stream),
+         "status": _made(given.get("status"), "status", torch.int32, units, dev, stream)}
+    wp, wn = None, 0
+    if window > 0:
+        ws = _bytes(ws, _cache_weights_workspace_size(B, shape[1], shape[2], units[1], d), dev, stream)
+        wp, wn = ws.data_ptr(), ws.numel()
+    st = load().twinkv_cache_weights(
+        q.data_ptr(), lse.data_ptr(), s, d ** -0.5 if scale is None else scale,
+        _int32(window, "window"), _int32(n_sink, "n_sink"), p, table.data_ptr(), pages,
+        lens.data_ptr(), score.data_ptr(), o["score"].data_ptr(), N, o["status"].data_ptr(), wp, wn,
+        _stream(stream))
+    _check(st, "twinkv_cache_weights")
+    return o
+
+
+def twinkv_weight_policy(score, budget, *, lens=None, n_sink=None, n_recent=None,
+                         want_score=False, out=None, stream=None) -> dict:
+    """Eviction by accumulated weight: the budget's worth of positions with the highest score.
+
+    score [...,N] float32; budget [...] int32, or an int for every unit; lens [...] int32: positions
+    of each unit (None: N).  The first n_sink and the last n_recent come first (4 and 64 by default),
+    equal scores in position order.  Returns a dict: mask [...,N] uint8, status [...] int32 and, with
+    want_score, score [...,N] float32: the kept scores in order, then 0.
+    """
+    if not isinstance(score, torch.Tensor) or score.dim() < 1:
+        raise TypeError("score must be a torch tensor [..., N]")
+    dev, shape = score.get_device(), score.shape
+    if dev < 0 or dev != _current_device():
+        raise _elsewhere("score", score, "current")
+    _same(score, "score", torch.float32, shape, dev)
+    units, N, given = shape[:-1], shape[-1], out or {}
+    if not isinstance(budget, torch.Tensor):
+        with torch.cuda.stream(stream):
+            budget = torch.full(units, _int32(budget, "budget"), dtype=torch.int32, device=dev)
+    _same(budget, "budget", torch.int32, units, dev)
+    if lens is not None:
+        _same(lens, "lens", torch.int32, units, dev)
+    n_sink = _defaults()[2] if n_sink is None else _int32(n_sink, "n_sink")
+    n_recent = _defaults()[3] if n_recent is None else _int32(n_recent, "n_recent")
+    o = {"mask": _made(given.get("mask"), "mask", torch.uint8, shape, dev, stream),
+         "status": _made(given.get("status"), "status", torch.int32, units, dev, stream)}
+    if want_score:
+        o["score"] = _made(given.get("score"), "score", torch.float32, shape, dev, stream)
+    st = load().twinkv_weight_policy(
+        score.data_ptr(), budget.numel(), N, _ptr(lens), budget.data_ptr(), n_sink, n_recent,
+        o["mask"].data_ptr(), _ptr(o.get("score")), o["status"].data_ptr(), _stream(stream))
+    _check(st, "twinkv_weight_policy")
     return o
 
 
