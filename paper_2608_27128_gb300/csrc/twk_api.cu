@@ -12,6 +12,7 @@
 #include "twinkv.h"
 #include "twk_cache_internal.h"
 #include "twk_internal.h"
+#include "twk_prompt_internal.h"
 
 namespace twk {
 namespace {
@@ -438,6 +439,31 @@ twinkv_status device_facts(int* sms)
 }
 
 twinkv_status cuda_result(cudaError_t e) { return cuda_status(e); }
+
+twinkv_status wait_facts(WaitFacts* w)
+{
+    DeviceInfo* dev = nullptr;
+    const twinkv_status r = device_info(&dev);
+    if (r == TWINKV_OK) *w = {dev->err, g_timeout_ns};
+    return r;
+}
+
+bool encode_rows(CUtensorMap* map, const void* base, int d, int heads, int rows, int64_t head,
+                 int64_t row, int box_heads, int box_rows)
+{
+    // a dimension of one has no stride: any will do
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(heads),
+                                static_cast<cuuint64_t>(rows)};
+    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(heads > 1 ? head : d) * 2,
+                                   static_cast<cuuint64_t>(rows > 1 ? row : d) * 2};
+    const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box_heads),
+                               static_cast<cuuint32_t>(box_rows)};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides,
+                    box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 
 }  // namespace twk
 

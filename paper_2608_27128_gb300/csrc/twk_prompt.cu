@@ -1,76 +1,753 @@
 // twk_prompt.cu -- attention over prompts.
 //
 // Per token at position p = m - n + i of its sequence and query head:
-//     o = sum_j exp(scale q . k_j - lse) v_j,   lse = log sum_j exp(scale q . k_j)
+//     o = sum_j exp(x_j - lse) v_j,   x_j = scale q . k_j,   lse = log sum_j exp(x_j)
 // over the keys j <= p and, with a window W, of those p - j < W or j < n_sink.
 //
-// One warp per token and query head, over the keys one by one: right for every case, and the measure for
-// what follows.
+// One pass over the keys, a tile of 128 at a time, with a running maximum and sum per row: with
+// c = scale log2(e) and t the row's top, about the largest c q . k so far,
+//     p_j = 2^(c q . k_j - t),   l = sum p_j,   O = sum p_j v_j,   o = O / l,   lse = ln2 t + ln l.
+// The top follows the maximum only where that has risen by more than 8 (a factor of 256, which
+// bf16's exponent does not notice): O is then scaled in tensor memory, a rare event.
+//
+// Bound by the tensor cores: 4 d operations for each pair of a row and a key, of which a prompt of n tokens
+// has n^2 / 2 per head; exponentials (a row and key each) take about half their time at d = 128 and as
+// long at d = 64.  Design (persistent, one block of 384 threads per SM):
+//   - An item is 256 query rows of one KV head: (token, head) pairs, the heads of a token side by side,
+//     so that every head of the group reads the same keys, and short sequences fill a tile.  Two
+//     tiles of 128 rows take turns: one's softmax runs beside the other's products.
+//   - S = Q K^T by tcgen05.mma from shared memory, both K-major; P (bf16, written over S in tensor memory)
+//     times V, whose rows run along the keys: operand A from tensor memory, B as TMA left it.
+//   - Warps 0 to 3 and 4 to 7: softmax, a thread per row.  Warp 8: TMA (queries once per item, then keys
+//     and values in one ring).  Warp 9: one thread issues every product.  Warp 10 hands out items.
+//   - Work is divided evenly whatever the lengths (twk_prompt.cuh): a block's span may begin and end inside
+//     an item, whose parts (unnormalised O, top, l in float32) merge_kernel joins in order.
+#include <atomic>
+
 #include "twk_cache.cuh"
+#include "twk_internal.h"
 #include "twk_prompt.cuh"
 #include "twk_ptx.cuh"
 
 namespace twk {
 namespace {
 
+constexpr int kThreads = 384;
+constexpr int kLaunchRegs = 168, kHelperRegs = 56, kSoftmaxRegs = 224;
+static_assert(4 * kHelperRegs + 8 * kSoftmaxRegs <= 12 * kLaunchRegs,
+              "the split draws on the registers of the launch");
+constexpr int kPairRows = 2 * kTileRows;
+constexpr float kLazy = 8.0f;            // what a maximum may rise, in powers of two, before O follows
+
+// tokens of a tile
+__device__ __forceinline__ int tile_tokens(const PromptArgs& a) { return kTileRows / a.G; }
+
+// Items of attention: pairs of row tiles; as long as their list of key tiles.
+struct RowPairs {
+    __device__ static __forceinline__ int items(const PromptArgs& a, const Sequence& s)
+    {
+        const int tokens = 2 * tile_tokens(a);
+        return (s.n + tokens - 1) / tokens;
+    }
+    __device__ static __forceinline__ KeyTiles tiles(const PromptArgs& a, const Sequence& s, int i)
+    {
+        const int tokens = 2 * tile_tokens(a), first = s.m - s.n + i * tokens;
+        return key_tiles(a, first, min(first + tokens, s.m) - 1);
+    }
+    // 1 where nothing is seen: the rows are written all the same
+    __device__ static __forceinline__ int length(const PromptArgs& a, const Sequence& s, int i)
+    {
+        return max(1, tiles(a, s, i).count);
+    }
+};
+
 template <int D>
-__global__ void __launch_bounds__(128) prompt_attend_kernel(const __grid_constant__ PromptArgs a)
+struct Cfg {
+    static constexpr int KC = D / 64;                     // chunks of 128 bytes of a row
+    static constexpr int CHUNK = kTileRows * 128;
+    static constexpr int Q_BYTES = KC * CHUNK;            // a tile of queries
+    static constexpr int STAGE = KC * CHUNK;              // a tile of keys or values
+    static constexpr int STAGES = D == 128 ? 5 : 8;
+    static constexpr int OFF_KV = 2 * Q_BYTES;
+    static constexpr int OFF_MISC = OFF_KV + STAGES * STAGE;
+    static constexpr int BYTES = OFF_MISC + 1024 + 1024;  // + 1024 for alignment
+    static constexpr int T_S = 0, T_O = 256;              // columns of tensor memory: S, O of tile 0
+    static_assert(BYTES <= 232448, "shared memory per block");
+    static_assert(STAGES * STAGE >= 2 * (kChunks + 1) * 8, "the chunks' sums lie there at first");
+};
+
+constexpr int kItemSlots = 4;
+
+// What the roles have to know of an item's part.
+struct Item {
+    int t0, tokens;          // first row of q, tokens from there to the sequence's end (for both tiles)
+    int pos;                 // position of the first token
+    int j0, m, head;         // keys; KV head, -1: no more items
+    int s0, s1;              // units of the list that this part takes
+    int count[2];            // length of each tile's list
+    int sinks, from;         // see KeyTiles
+    int slot;                // part's slot, or -1: the whole item
+    int pad[3];
+};
+static_assert(sizeof(Item) == 64);
+
+struct Misc {
+    uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2], drain;
+    uint64_t kv_full[8], kv_empty[8], item_full[kItemSlots], item_empty[kItemSlots];
+    Item items[kItemSlots];
+    uint32_t tmem;
+    int abort_flag;
+};
+static_assert(sizeof(Misc) <= 1024);
+
+struct AttendKernelArgs {
+    PromptArgs a;
+    float c;                 // scale * log2(e)
+    float* part;             // [2 per block] parts, null: no item is shared
+    int4* join;              // [2 per block]: parts of the item that begins in the block and ends in
+                             // another one (0: none), t0, tokens, KV head; first slot in the second
+    int* err;
+    unsigned long long timeout_ns;
+};
+
+// A part: outputs [D / 4][256 rows][4], tops [256], sums [256].
+template <int D>
+constexpr int kPartFloats = kPairRows * (D + 2);
+
+__device__ __forceinline__ float exp2_approx(float x)
 {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float as_f(uint32_t x) { return __uint_as_float(x); }
+
+// Orders every later use of x after the preceding tcgen05.wait::ld.
+__device__ __forceinline__ void reg_fence(uint32_t (&x)[32])
+{
+#pragma unroll
+    for (int i = 0; i < 32; i += 8)
+        asm volatile(""
+                     : "+r"(x[i]), "+r"(x[i + 1]), "+r"(x[i + 2]), "+r"(x[i + 3]), "+r"(x[i + 4]),
+                       "+r"(x[i + 5]), "+r"(x[i + 6]), "+r"(x[i + 7]));
+}
+
+__device__ __forceinline__ bool all_wait(uint64_t* bar, uint32_t parity, const WaitCtl& w, int where)
+{
+    const bool ok = mbar_wait(bar, parity, w, where);
+    return __all_sync(0xffffffffu, ok);
+}
+
+__device__ __forceinline__ void drain_wait(uint64_t* bar, uint32_t parity, uint64_t limit_ns)
+{
+    const uint64_t limit = limit_ns > kDrainFloorNs ? limit_ns : kDrainFloorNs;
+    const uint32_t a = smem_u32(bar);
+    const uint64_t t0 = globaltimer_ns();
+    while (!mbar_try_wait_sleep(a, parity, 1000000u))
+        if (globaltimer_ns() - t0 > limit) return;
+}
+
+// A ring's slot and the parity of its phase.
+template <int kN>
+struct Ring {
+    uint32_t slot = 0, phase = 0;
+    __device__ __forceinline__ void next()
+    {
+        if (++slot == kN) {
+            slot = 0;
+            phase ^= 1u;
+        }
+    }
+};
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+    prompt_attend_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                         const __grid_constant__ CUtensorMap tmV,
+                         const __grid_constant__ AttendKernelArgs p)
+{
+    using C = Cfg<D>;
+    const PromptArgs& a = p.a;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    Misc& M = *reinterpret_cast<Misc*>(smem + C::OFF_MISC);
+    const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0);
+    const int lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&M.q_full[i], 1);
+            mbar_init(&M.q_empty[i], 1);
+            mbar_init(&M.s_full[i], 1);
+            mbar_init(&M.p_full[i], 4);
+            mbar_init(&M.o_full[i], 1);
+        }
+        mbar_init(&M.drain, 1);
+        for (int i = 0; i < C::STAGES; ++i) {
+            mbar_init(&M.kv_full[i], 1);
+            mbar_init(&M.kv_empty[i], 1);
+        }
+        for (int i = 0; i < kItemSlots; ++i) {
+            mbar_init(&M.item_full[i], 1);
+            mbar_init(&M.item_empty[i], 10);      // TMA, products, eight of softmax
+        }
+        M.abort_flag = 0;
+        fence_mbarrier_init();
+    }
+    if (warp == 8 && lane == 0) {
+        prefetch_tensormap(&tmQ);
+        prefetch_tensormap(&tmK);
+        prefetch_tensormap(&tmV);
+    }
+    if (warp == 9) tmem_alloc<1>(&M.tmem, 512);
+    wait_for_previous();
+    // the chunks' sums lie where keys and values come later
+    long long* sums = reinterpret_cast<long long*>(smem + C::OFF_KV);
+    const Totals total = sum_chunks<RowPairs>(a, sums, sums + kChunks + 1);
+    const int blocks = span_blocks(total);
+    Place at{}, end_at{};
+    long long begin = 0, end = 0;
+    const bool mine = static_cast<int>(blockIdx.x) < blocks;
+    if (warp == 10 && mine) {
+        begin = cut<RowPairs>(a, sums, total.units, blocks, blockIdx.x, at);
+        end = cut<RowPairs>(a, sums, total.units, blocks, blockIdx.x + 1, end_at);
+    }
+    fence_async_shared();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = M.tmem;
+
+    WaitCtl wc;
+    wc.limit_ns = p.timeout_ns;
+    wc.abort_flag = &M.abort_flag;
+    wc.err = p.err;
+    wc.where = 0;
+    const int tpt = tile_tokens(a);
+
+    if (warp >= 8) {
+        setmaxnreg_dec<kHelperRegs>();
+        if (warp == 8) {
+            // ------------------------------------------------------------ TMA
+            if (lane == 0) {
+                Ring<kItemSlots> ri;
+                Ring<C::STAGES> rs;
+                uint32_t q_uses[2] = {}, stages = 0;
+                const uint32_t q_bytes = static_cast<uint32_t>(tpt * a.G) * 128u * C::KC;
+                bool ok = true;
+                auto load = [&](const CUtensorMap* map, const Item& it, int tile) {
+                    if (!(ok = mbar_wait(&M.kv_empty[rs.slot], rs.phase ^ 1u, wc, 21))) return;
+                    mbar_arrive_expect_tx(&M.kv_full[rs.slot], C::STAGE);
+                    uint8_t* dst = smem + C::OFF_KV + rs.slot * C::STAGE;
+#pragma unroll
+                    for (int kc = 0; kc < C::KC; ++kc)
+                        tma_load_3d(dst + kc * C::CHUNK, map, &M.kv_full[rs.slot], kc * 64, it.head,
+                                    it.j0 + tile * kTileKeys);
+                    rs.next();
+                    ++stages;
+                };
+                for (;;) {
+                    if (!(ok = mbar_wait(&M.item_full[ri.slot], ri.phase, wc, 22))) break;
+                    const Item it = M.items[ri.slot];
+                    mbar_arrive(&M.item_empty[ri.slot]);
+                    ri.next();
+                    if (it.head < 0) break;
+                    const KeyTiles kt{it.sinks, it.from, 0};
+                    // the queries of a tile that has products, then the first keys
+                    for (int x = 0; x < 2 && ok; ++x) {
+                        if (min(it.s1, it.count[x]) <= it.s0) continue;
+                        ok = mbar_wait(&M.q_empty[x], (q_uses[x] & 1u) ^ 1u, wc, 23);
+                        if (!ok) break;
+                        ++q_uses[x];
+                        mbar_arrive_expect_tx(&M.q_full[x], q_bytes);
+#pragma unroll
+                        for (int kc = 0; kc < C::KC; ++kc)
+                            tma_load_3d(smem + x * C::Q_BYTES + kc * C::CHUNK, &tmQ, &M.q_full[x],
+                                        kc * 64, it.head * a.G, it.t0 + x * tpt);
+                    }
+                    const int n = min(it.s1, max(it.count[0], it.count[1]));
+                    for (int j = it.s0; j < n && ok; ++j) {
+                        load(&tmK, it, kt.tile(j));
+                        if (ok) load(&tmV, it, kt.tile(j));
+                    }
+                    if (!ok) break;
+                }
+                // after a give-up: no copy of this thread is in flight when the block ends
+                if (!ok) {
+                    for (int x = 0; x < 2; ++x)
+                        if (q_uses[x]) drain_wait(&M.q_full[x], (q_uses[x] - 1) & 1u, p.timeout_ns);
+                    const uint32_t used = min(stages, static_cast<uint32_t>(C::STAGES));
+                    for (uint32_t k = 1; k <= used; ++k) {
+                        const uint32_t i = stages - k;
+                        drain_wait(&M.kv_full[i % C::STAGES], i / C::STAGES & 1u, p.timeout_ns);
+                    }
+                }
+            }
+        } else if (warp == 9) {
+            // ------------------------------------------------------------ products
+            // every lane follows, lane 0 issues
+            constexpr uint32_t id_s = umma_idesc_bf16_f32(kTileRows, kTileKeys);
+            constexpr uint32_t id_o = umma_idesc_bf16_f32(kTileRows, D) | kIdescBRows;
+            Ring<kItemSlots> ri;
+            Ring<C::STAGES> rs;
+            uint32_t q_uses[2] = {}, p_uses[2] = {};
+            bool ok = true;
+            auto commit = [&](uint64_t* bar) {
+                if (lane == 0) umma_commit(bar);
+            };
+            auto scores = [&](int x, uint32_t stage, bool last) {
+                if (lane != 0) return;
+                const uint64_t q = umma_desc_sw128(smem_u32(smem + x * C::Q_BYTES));
+                const uint64_t k = umma_desc_sw128(smem_u32(smem + C::OFF_KV + stage * C::STAGE));
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                    const uint32_t at_i = (i / 4) * (C::CHUNK >> 4) + 2 * (i % 4);
+                    umma_bf16(tmem + C::T_S + x * kTileKeys, q + at_i, k + at_i, id_s, i != 0);
+                }
+                umma_commit(&M.s_full[x]);
+                if (last) umma_commit(&M.q_empty[x]);
+            };
+            auto outputs = [&](int x, uint32_t stage, bool first, bool last) {
+                if (lane != 0) return;
+                const uint64_t v =
+                    umma_desc_sw128_rows(smem_u32(smem + C::OFF_KV + stage * C::STAGE), C::CHUNK);
+#pragma unroll
+                for (int i = 0; i < kTileKeys / 16; ++i)
+                    umma_bf16_tmem(tmem + C::T_O + x * D, tmem + C::T_S + x * kTileKeys + 8 * i,
+                                   v + i * (16 * 128 >> 4), id_o, !first || i != 0);
+                if (last) umma_commit(&M.o_full[x]);
+            };
+            while (ok) {
+                if (!(ok = all_wait(&M.item_full[ri.slot], ri.phase, wc, 24))) break;
+                const Item it = M.items[ri.slot];
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&M.item_empty[ri.slot]);
+                ri.next();
+                if (it.head < 0) break;
+                int n[2];
+                for (int x = 0; x < 2; ++x) n[x] = min(it.s1, it.count[x]);
+                const int all = max(n[0], n[1]);
+                if (all <= it.s0) continue;
+                const KeyTiles kt{it.sinks, it.from, 0};
+                ok = all_wait(&M.kv_full[rs.slot], rs.phase, wc, 25);
+                for (int x = 0; x < 2 && ok; ++x) {
+                    if (n[x] <= it.s0) continue;
+                    if (!(ok = all_wait(&M.q_full[x], q_uses[x]++ & 1u, wc, 26))) break;
+                    tc_fence_after();
+                    scores(x, rs.slot, it.s0 + 1 == n[x]);
+                }
+                if (!ok) break;
+                commit(&M.kv_empty[rs.slot]);
+                rs.next();
+                for (int j = it.s0; j < all && ok; ++j) {
+                    const Ring<C::STAGES> rv = rs;
+                    rs.next();
+                    if (!(ok = all_wait(&M.kv_full[rv.slot], rv.phase, wc, 27))) break;
+                    const int held = it.m - kt.tile(j) * kTileKeys;
+                    if (held < kTileKeys) {
+                        // the sequence ends inside the tile: its probabilities are 0 from there on,
+                        // and so are the values, whatever lies behind it
+                        uint8_t* v = smem + C::OFF_KV + rv.slot * C::STAGE;
+                        for (int y = held * 128 + lane * 16; y < C::CHUNK; y += 512)
+#pragma unroll
+                            for (int kc = 0; kc < C::KC; ++kc)
+                                *reinterpret_cast<uint4*>(v + kc * C::CHUNK + y) =
+                                    make_uint4(0, 0, 0, 0);
+                        fence_async_shared();
+                        __syncwarp();
+                    }
+                    bool keys = false;
+                    for (int x = 0; x < 2 && ok; ++x) {
+                        if (j < n[x]) {
+                            if (!(ok = all_wait(&M.p_full[x], p_uses[x]++ & 1u, wc, 29))) break;
+                            tc_fence_after();
+                            outputs(x, rv.slot, j == it.s0, j + 1 == n[x]);
+                        }
+                        if (x == 1 || j >= n[1]) commit(&M.kv_empty[rv.slot]);
+                        if (j + 1 < n[x]) {
+                            if (!keys) ok = all_wait(&M.kv_full[rs.slot], rs.phase, wc, 30);
+                            if (!ok) break;
+                            keys = true;
+                            tc_fence_after();
+                            scores(x, rs.slot, j + 2 == n[x]);
+                        }
+                        if (j >= n[1]) break;
+                    }
+                    if (!ok) break;
+                    if (j + 1 < all) {
+                        commit(&M.kv_empty[rs.slot]);
+                        rs.next();
+                    }
+                }
+            }
+            // every product has ended before tensor memory is freed
+            if (lane == 0) {
+                umma_commit(&M.drain);
+                drain_wait(&M.drain, 0, p.timeout_ns);
+            }
+        } else if (warp == 10) {
+            // ------------------------------------------------------------ items
+            Ring<kItemSlots> ri;
+            bool ok = true;
+            if (lane == 0) {
+                if (p.join) p.join[2 * blockIdx.x] = make_int4(0, 0, 0, 0);
+                const int tokens = 2 * tpt;
+                long long g = begin;
+                while (ok && g < end) {
+                    const int take = static_cast<int>(
+                        end - g < at.length - at.off ? end - g : at.length - at.off);
+                    Item it{};
+                    const int i0 = at.item * tokens;
+                    it.t0 = at.s.t0 + i0;
+                    it.tokens = at.s.n - i0;
+                    it.pos = at.s.m - at.s.n + i0;
+                    it.j0 = at.s.j0;
+                    it.m = at.s.m;
+                    it.head = at.head;
+                    it.s0 = at.off;
+                    it.s1 = at.off + take;
+                    const KeyTiles kt = RowPairs::tiles(a, at.s, at.item);
+                    it.sinks = kt.sinks;
+                    it.from = kt.from;
+                    for (int x = 0; x < 2; ++x) {
+                        // the same list, as far as the tile's last token sees
+                        const int last = min(it.pos + (x + 1) * tpt, it.m) - 1;
+                        const bool any = it.tokens > x * tpt && last >= 0;
+                        it.count[x] = any ? kt.sinks + last / kTileKeys + 1 - kt.from : 0;
+                    }
+                    const bool whole = at.off == 0 && take == at.length;
+                    // heads and middles in slot 2 c, the item that begins in the block in 2 c + 1
+                    it.slot = whole ? -1 : 2 * static_cast<int>(blockIdx.x) + (at.off == 0 ? 1 : 0);
+                    if (!whole && at.off == 0) {
+                        const int parts = parts_of(total.units, blocks, blockIdx.x, g, at.length);
+                        p.join[2 * blockIdx.x] = make_int4(parts, it.t0, it.tokens, it.head);
+                    }
+                    ok = mbar_wait(&M.item_empty[ri.slot], ri.phase ^ 1u, wc, 31);
+                    if (!ok) break;
+                    M.items[ri.slot] = it;
+                    mbar_arrive(&M.item_full[ri.slot]);
+                    ri.next();
+                    g += take;
+                    if (at.off + take < at.length || !next_item<RowPairs>(a, at)) break;
+                }
+                if (ok) ok = mbar_wait(&M.item_empty[ri.slot], ri.phase ^ 1u, wc, 31);
+                if (ok) {
+                    M.items[ri.slot].head = -1;
+                    mbar_arrive(&M.item_full[ri.slot]);
+                }
+                // no one waits on the slots after this but what has been published
+            }
+        } else {
+            if (blockIdx.x == 0 && a.out_status)
+                for (int b = lane; b < a.s.B; b += 32)
+                    a.out_status[b] = sequence_of(a, b).ok ? TWINKV_OK : TWINKV_ERR_INVALID_ARG;
+        }
+        __syncwarp();
+        tc_fence_before();
+        __syncthreads();
+        tc_fence_after();
+        if (warp == 9) tmem_dealloc<1>(tmem, 512);
+    } else {
+        // ------------------------------------------------------------ softmax
+        setmaxnreg_inc<kSoftmaxRegs>();
+        const int x = warp >> 2, q = warp & 3;
+        const int row = q * 32 + lane;
+        const uint32_t base = tmem + (static_cast<uint32_t>(q * 32) << 16);
+        const uint32_t t_s = base + C::T_S + x * kTileKeys, t_o = base + C::T_O + x * D;
+        const int token = row / a.G, sub = row - token * a.G;        // of the tile
+        const int first_token = q * 32 / a.G, last_token = (q * 32 + 31) / a.G;
+        Ring<kItemSlots> ri;
+        uint32_t s_uses = 0, o_uses = 0;
+        bool ok = true;
+        while (ok) {
+            if (!(ok = all_wait(&M.item_full[ri.slot], ri.phase, wc, 34))) break;
+            const Item it = M.items[ri.slot];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&M.item_empty[ri.slot]);
+            ri.next();
+            if (it.head < 0) break;
+            const KeyTiles kt{it.sinks, it.from, 0};
+            const int n = min(it.s1, x ? it.count[1] : it.count[0]);
+            const int p0 = it.pos + x * tpt;                         // position of the tile's first token
+            const int pos = p0 + token;
+            const int low = a.window > 0 ? pos - a.window + 1 : INT_MIN;
+            float top = -INFINITY, sum = 0.0f;
+            for (int j = it.s0; j < n; ++j) {
+                const int k0 = kt.tile(j) * kTileKeys;
+                if (!(ok = all_wait(&M.s_full[x], s_uses++ & 1u, wc, 35))) break;
+                tc_fence_after();
+                uint32_t s[4][32];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) tmem_ld_32x32b_x32(t_s + 32 * i, s[i]);
+                tmem_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 4; ++i) reg_fence(s[i]);
+                const bool edge = k0 + kTileKeys - 1 > p0 + first_token ||
+                                  (a.window > 0 && k0 < p0 + last_token - a.window + 1 &&
+                                   k0 + kTileKeys > a.n_sink);
+                if (edge) {
+                    const int hi = pos - k0, lo = low - k0, sinks = a.n_sink - k0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            const int k = 32 * i + e;
+                            const bool see = k <= hi && (a.window == 0 || k >= lo || k < sinks);
+                            if (!see) s[i][e] = 0xff800000u;
+                        }
+                }
+                float m[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float y[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        y[e] = max3(as_f(s[i][4 * e]), as_f(s[i][4 * e + 1]),
+                                    fmaxf(as_f(s[i][4 * e + 2]), as_f(s[i][4 * e + 3])));
+                    m[i] = max3(max3(y[0], y[1], y[2]), max3(y[3], y[4], y[5]), fmaxf(y[6], y[7]));
+                }
+                const float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * p.c;
+                if (j == it.s0) {
+                    top = most;
+                } else {
+                    const bool rise = most > top + kLazy;
+                    if (__any_sync(0xffffffffu, rise)) {
+                        const float f = rise ? exp2_approx(top - most) : 1.0f;   // top -inf: 0
+                        if (rise) top = most;
+                        sum *= f;
+#pragma unroll
+                        for (int i = 0; i < D / 32; ++i) {
+                            uint32_t o[32];
+                            tmem_ld_32x32b_x32(t_o + 32 * i, o);
+                            tmem_wait_ld();
+                            reg_fence(o);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(as_f(o[e]) * f);
+                            tmem_st_32x32b_x32(t_o + 32 * i, o);
+                        }
+                    }
+                }
+                const float t = top == -INFINITY ? 0.0f : top;
+                const float2 c2 = make_float2(p.c, p.c), t2 = make_float2(-t, -t);
+                float2 l[4] = {};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t w[32];
+#pragma unroll
+                    for (int e = 0; e < 64; e += 2) {
+                        const int i = 2 * h + e / 32;
+                        const float2 y = __ffma2_rn(
+                            make_float2(as_f(s[i][e % 32]), as_f(s[i][e % 32 + 1])), c2, t2);
+                        const float u = exp2_approx(y.x), v = exp2_approx(y.y);
+                        l[e / 2 % 4] = __fadd2_rn(l[e / 2 % 4], make_float2(u, v));
+                        w[e / 2] = bf16_pair(u, v);
+                    }
+                    tmem_st_32x32b_x32(t_s + 32 * h, w);
+                }
+                const float2 l2 = __fadd2_rn(__fadd2_rn(l[0], l[1]), __fadd2_rn(l[2], l[3]));
+                sum += l2.x + l2.y;
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&M.p_full[x]);
+            }
+            if (!ok) break;
+            // ---- the item's rows: outputs, or a part
+            const bool any = n > it.s0;
+            if (any) {
+                if (!(ok = all_wait(&M.o_full[x], o_uses++ & 1u, wc, 36))) break;
+                tc_fence_after();
+            }
+            const bool held = token < tpt && x * tpt + token < it.tokens;
+            const int64_t at_row = static_cast<int64_t>(it.t0 + x * tpt + token) * a.s.Hq +
+                                   it.head * a.G + sub;
+            if (it.slot < 0) {
+                const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;      // O is 0 where sum is
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) {
+                    uint32_t o[32] = {};
+                    if (any) {
+                        tmem_ld_32x32b_x32(t_o + 32 * i, o);
+                        tmem_wait_ld();
+                        reg_fence(o);
+                    }
+                    if (held) {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 8) {
+                            uint4 w;
+                            w.x = bf16_pair(as_f(o[e]) * inv, as_f(o[e + 1]) * inv);
+                            w.y = bf16_pair(as_f(o[e + 2]) * inv, as_f(o[e + 3]) * inv);
+                            w.z = bf16_pair(as_f(o[e + 4]) * inv, as_f(o[e + 5]) * inv);
+                            w.w = bf16_pair(as_f(o[e + 6]) * inv, as_f(o[e + 7]) * inv);
+                            *reinterpret_cast<uint4*>(a.out + at_row * D + 32 * i + e) = w;
+                        }
+                    }
+                }
+                if (held && a.out_lse)
+                    a.out_lse[at_row] = sum > 0.0f ? fmaf(top, 0.6931471805599453f, logf(sum))
+                                                   : -INFINITY;
+            } else {
+                float* part = p.part + static_cast<int64_t>(it.slot) * kPartFloats<D>;
+                const int r = x * kTileRows + row;
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) {
+                    uint32_t o[32] = {};
+                    if (any) {
+                        tmem_ld_32x32b_x32(t_o + 32 * i, o);
+                        tmem_wait_ld();
+                        reg_fence(o);
+                    }
+                    if (!any) continue;
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4)
+                        *reinterpret_cast<uint4*>(part + ((8 * i + e / 4) * kPairRows + r) * 4) =
+                            make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                }
+                part[kPairRows * D + r] = sum > 0.0f ? top : -INFINITY;
+                part[kPairRows * (D + 1) + r] = sum;
+            }
+            tc_fence_before();
+        }
+        tc_fence_before();
+        __syncthreads();
+    }
+}
+
+// Joins the parts of an item that several blocks took, in order: a block per block that such an item
+// begins in and 32 rows of it, a warp for every eighth group of four values.
+constexpr int kMergeWarps = 8;
+
+template <int D>
+__global__ void __launch_bounds__(32 * kMergeWarps)
+    merge_kernel(const __grid_constant__ AttendKernelArgs p)
+{
+    constexpr int kVec = D / 4 / kMergeWarps;
+    wait_for_previous();
+    const PromptArgs& a = p.a;
+    const int4 join = p.join[2 * blockIdx.x];
+    if (join.x == 0) return;
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    if (blockIdx.x == 0 && a.out_status)
-        for (int b = threadIdx.x; b < a.s.B; b += 128)
-            a.out_status[b] = sequence_of(a, b).ok ? TWINKV_OK : TWINKV_ERR_INVALID_ARG;
-    const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + warp;
-    const int t = static_cast<int>(item / a.s.Hq), head = static_cast<int>(item % a.s.Hq);
-    if (t >= a.s.tokens) return;
-    Sequence s{};
-    int b = 0;
-    for (; b < a.s.B; ++b) {
-        s = sequence_of(a, b);
-        if (s.ok && t >= s.t0 && t - s.t0 < s.n) break;
-    }
-    if (b == a.s.B) return;
-    constexpr int V = D / 32;
-    float q[V], o[V] = {};
-    const uint16_t* src = a.q + t * a.s.q_token + head * a.s.q_head + V * lane;
+    const int r = blockIdx.y * 32 + lane;
+    const int x = r / kTileRows, row = r % kTileRows, tpt = tile_tokens(a);
+    const int token = row / a.G;
+    if (token >= tpt || x * tpt + token >= join.z) return;
+    float top = -INFINITY, sum = 0.0f, acc[kVec][4] = {};
+    constexpr int kAhead = 4;
+    for (int k0 = 0; k0 < join.x; k0 += kAhead) {
+        float m[kAhead], l[kAhead];
+        float4 y[kAhead][kVec];
 #pragma unroll
-    for (int v = 0; v < V; ++v) q[v] = bf16_lo(src[v]);
-    const int p = s.m - s.n + t - s.t0, h = head / a.G;
-    float top = -INFINITY, sum = 0.0f;
-    for (int j = 0; j <= p; ++j) {
-        if (a.window > 0 && p - j >= a.window && j >= a.n_sink) continue;
-        const int64_t row = s.j0 + j;
-        const uint16_t* k = a.k + row * a.s.k_token + h * a.s.k_head + V * lane;
-        const uint16_t* w = a.v + row * a.s.v_token + h * a.s.v_head + V * lane;
-        float x = 0.0f;
+        for (int k = 0; k < kAhead; ++k) {
+            m[k] = -INFINITY;
+            l[k] = 0.0f;
+            if (k0 + k >= join.x) continue;
+            const int slot = 2 * (blockIdx.x + k0 + k) + (k0 + k == 0 ? 1 : 0);
+            const float* part = p.part + static_cast<int64_t>(slot) * kPartFloats<D>;
+            m[k] = part[kPairRows * D + r];
+            l[k] = part[kPairRows * (D + 1) + r];
 #pragma unroll
-        for (int v = 0; v < V; ++v) x = fmaf(q[v], bf16_lo(k[v]), x);
+            for (int v = 0; v < kVec; ++v)
+                y[k][v] = *reinterpret_cast<const float4*>(
+                    part + ((warp + kMergeWarps * v) * kPairRows + r) * 4);
+        }
+        float most = top;
 #pragma unroll
-        for (int i = 16; i > 0; i /= 2) x += __shfl_xor_sync(0xffffffffu, x, i);
-        x *= a.scale;
-        const float most = fmaxf(top, x), f = expf(top - most), y = expf(x - most);
-        sum = fmaf(sum, f, y);
+        for (int k = 0; k < kAhead; ++k) most = fmaxf(most, m[k]);
+        if (most == -INFINITY) continue;
+        const float f = exp2_approx(top - most);
+        sum *= f;
 #pragma unroll
-        for (int v = 0; v < V; ++v) o[v] = fmaf(o[v], f, y * bf16_lo(w[v]));
+        for (int v = 0; v < kVec; ++v)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[v][e] *= f;
         top = most;
-    }
-    const int64_t at = static_cast<int64_t>(t) * a.s.Hq + head;
 #pragma unroll
-    for (int v = 0; v < V; v += 2)
-        *reinterpret_cast<uint32_t*>(a.out + at * D + V * lane + v) =
-            sum > 0.0f ? bf16_pair(o[v] / sum, o[v + 1] / sum) : 0u;
-    if (a.out_lse && lane == 0) a.out_lse[at] = sum > 0.0f ? top + logf(sum) : -INFINITY;
+        for (int k = 0; k < kAhead; ++k) {
+            if (m[k] == -INFINITY) continue;          // what it holds is no number
+            const float w = exp2_approx(m[k] - top);
+            sum = fmaf(l[k], w, sum);
+#pragma unroll
+            for (int v = 0; v < kVec; ++v) {
+                acc[v][0] = fmaf(y[k][v].x, w, acc[v][0]);
+                acc[v][1] = fmaf(y[k][v].y, w, acc[v][1]);
+                acc[v][2] = fmaf(y[k][v].z, w, acc[v][2]);
+                acc[v][3] = fmaf(y[k][v].w, w, acc[v][3]);
+            }
+        }
+    }
+    const int64_t at = static_cast<int64_t>(join.y + x * tpt + token) * a.s.Hq + join.w * a.G +
+                       row - token * a.G;
+    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+#pragma unroll
+    for (int v = 0; v < kVec; ++v)
+        *reinterpret_cast<uint2*>(a.out + at * D + 4 * (warp + kMergeWarps * v)) =
+            make_uint2(bf16_pair(acc[v][0] * inv, acc[v][1] * inv),
+                       bf16_pair(acc[v][2] * inv, acc[v][3] * inv));
+    if (warp == 0 && a.out_lse)
+        a.out_lse[at] = sum > 0.0f ? fmaf(top, 0.6931471805599453f, logf(sum)) : -INFINITY;
+}
+
+// An item that reads this many keys or fewer is never cut.
+constexpr int kWholeKeys = (2 * kSnap + 1) * kTileKeys;
+
+template <int D>
+cudaError_t launch(const PromptArgs& a, int sms, const WaitFacts& w, cudaStream_t st)
+{
+    using C = Cfg<D>;
+    static std::atomic<bool> allowed[64];     // by device
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 64 || !allowed[dev].load(std::memory_order_relaxed)) {
+        // the warpgroups' shares add up to the launch's registers: with fewer, waits for them have no end
+        cudaFuncAttributes f;
+        if ((e = cudaFuncGetAttributes(&f, prompt_attend_kernel<D>)) != cudaSuccess) return e;
+        if (f.numRegs < kLaunchRegs) return cudaErrorInvalidConfiguration;
+        e = cudaFuncSetAttribute(prompt_attend_kernel<D>,
+                                 cudaFuncAttributeMaxDynamicSharedMemorySize, C::BYTES);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) allowed[dev].store(true, std::memory_order_relaxed);
+    }
+    CUtensorMap q, k, v;
+    const int tpt = kTileRows / a.G;
+    if (!encode_rows(&q, a.q, D, a.s.Hq, a.s.tokens, a.s.q_head, a.s.q_token, a.G, tpt) ||
+        !encode_rows(&k, a.k, D, a.s.H, a.s.keys, a.s.k_head, a.s.k_token, 1, kTileKeys) ||
+        !encode_rows(&v, a.v, D, a.s.H, a.s.keys, a.s.v_head, a.s.v_token, 1, kTileKeys))
+        return cudaErrorInvalidValue;
+    AttendKernelArgs p{};
+    p.a = a;
+    p.c = a.scale * 1.4426950408889634f;
+    const bool shared = a.s.keys > kWholeKeys;
+    if (shared) {
+        p.join = static_cast<int4*>(a.ws);
+        p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(a.ws) + 32 * kPromptBlocks);
+    }
+    p.err = w.err;
+    p.timeout_ns = w.timeout_ns;
+    const int grid = std::min(sms, kPromptBlocks);
+    prompt_attend_kernel<D><<<grid, kThreads, C::BYTES, st>>>(q, k, v, p);
+    if ((e = cudaGetLastError()) != cudaSuccess || !shared) return e;
+    return launch_dependent(merge_kernel<D>, dim3(grid, kPairRows / 32), 32 * kMergeWarps, 0, st, p);
 }
 
 }  // namespace
 
-cudaError_t launch_prompt_attend(const PromptArgs& a, int sms, cudaStream_t st)
+size_t prompt_attend_workspace(const twinkv_prompt& s)
 {
-    const int64_t items = static_cast<int64_t>(a.s.tokens) * a.s.Hq;
-    const unsigned grid = static_cast<unsigned>((items + 3) / 4);
-    if (a.s.d == 128) prompt_attend_kernel<128><<<grid, 128, 0, st>>>(a);
-    else prompt_attend_kernel<64><<<grid, 128, 0, st>>>(a);
-    return cudaGetLastError();
+    if (s.keys <= kWholeKeys) return 256;
+    return 32 * kPromptBlocks +
+           2 * kPromptBlocks * static_cast<size_t>(kPairRows) * (s.d + 2) * sizeof(float);
+}
+
+cudaError_t launch_prompt_attend(const PromptArgs& a, int sms, const WaitFacts& w, cudaStream_t st)
+{
+    return a.s.d == 128 ? launch<128>(a, sms, w, st) : launch<64>(a, sms, w, st);
 }
 
 }  // namespace twk

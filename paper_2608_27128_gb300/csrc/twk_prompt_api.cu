@@ -18,6 +18,8 @@ constexpr int kMaxGroup = 128;         // query heads per KV head over prompts
 
 bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
+size_t up256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
+
 // of a dimension of n: rows on 16-byte boundaries, apart from each other, within a copy's reach
 bool stride_ok(int64_t stride, int n)
 {
@@ -84,7 +86,7 @@ extern "C" {
 
 size_t twinkv_prompt_attend_workspace(twinkv_prompt s)
 {
-    return sizes_ok(s) == TWINKV_OK ? 256 : 0;
+    return sizes_ok(s) == TWINKV_OK ? up256(prompt_attend_workspace(s)) : 0;
 }
 
 size_t twinkv_prompt_weights_workspace(twinkv_prompt s)
@@ -95,8 +97,7 @@ size_t twinkv_prompt_weights_workspace(twinkv_prompt s)
 size_t twinkv_cache_weights_workspace(twinkv_queries s, int32_t d)
 {
     if (twinkv_cache_attend_workspace(s, d) == 0) return 0;
-    const size_t seen = static_cast<size_t>(s.B) * s.H * (1 + s.n) * 4;
-    return (seen + 255) & ~static_cast<size_t>(255);
+    return up256(static_cast<size_t>(s.B) * s.H * (1 + s.n) * 4);
 }
 
 twinkv_status twinkv_prompt_attend(const void* q, const void* k, const void* v, twinkv_prompt s,
@@ -112,12 +113,13 @@ twinkv_status twinkv_prompt_attend(const void* q, const void* k, const void* v, 
     r = check_ws(workspace, workspace_bytes, twinkv_prompt_attend_workspace(s));
     if (r != TWINKV_OK) return r;
     int sms = 0;
-    if ((r = device_facts(&sms)) != TWINKV_OK) return r;
+    WaitFacts w;
+    if ((r = device_facts(&sms)) != TWINKV_OK || (r = wait_facts(&w)) != TWINKV_OK) return r;
     PromptArgs a = args_of(q, k, s, seqs, scale, window, n_sink, out_status, workspace);
     a.v = static_cast<const uint16_t*>(v);
     a.out = static_cast<uint16_t*>(out);
     a.out_lse = out_lse;
-    return cuda_result(launch_prompt_attend(a, sms, static_cast<cudaStream_t>(stream)));
+    return cuda_result(launch_prompt_attend(a, sms, w, static_cast<cudaStream_t>(stream)));
 }
 
 twinkv_status twinkv_prompt_weights(const void* q, const void* k, const float* lse,

@@ -3,6 +3,7 @@
 // declarations only).
 #pragma once
 #include <cstdint>
+#include <cuda.h>
 #include <cuda_runtime.h>
 
 #include "twinkv.h"
@@ -28,7 +29,21 @@ struct PromptArgs {
     float* out_score;
     void* ws;
 };
-cudaError_t launch_prompt_attend(const PromptArgs& a, int sms, cudaStream_t st);
+
+// What a kernel with bounded waits needs: the device's error word and the limit of a wait.
+struct WaitFacts {
+    int* err;
+    unsigned long long timeout_ns;
+};
+twinkv_status wait_facts(WaitFacts* w);
+
+// A tensor map over bf16 rows [rows][heads][d] (strides in elements): boxes of 64 elements x box_heads x
+// box_rows, 128-byte swizzle, zeros beyond the ends.
+bool encode_rows(CUtensorMap* map, const void* base, int d, int heads, int rows, int64_t head,
+                 int64_t row, int box_heads, int box_rows);
+
+size_t prompt_attend_workspace(const twinkv_prompt& s);
+cudaError_t launch_prompt_attend(const PromptArgs& a, int sms, const WaitFacts& w, cudaStream_t st);
 cudaError_t launch_prompt_weights(const PromptArgs& a, int sms, cudaStream_t st);
 
 struct CacheWeightsArgs {
