@@ -126,6 +126,11 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
+// the lowest n bits (none for n <= 0, all for n >= 32)
+__device__ __forceinline__ uint32_t bits_below(int n)
+{
+    return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
+}
 __device__ __forceinline__ float as_f(uint32_t x) { return __uint_as_float(x); }
 
 // Orders every later use of x after the preceding tcgen05.wait::ld.
@@ -138,8 +143,10 @@ __device__ __forceinline__ void reg_fence(uint32_t (&x)[32])
                        "+r"(x[i + 5]), "+r"(x[i + 6]), "+r"(x[i + 7]));
 }
 
+// Every lane waits (each needs the acquire), the warp agrees on the verdict.
 __device__ __forceinline__ bool all_wait(uint64_t* bar, uint32_t parity, const WaitCtl& w, int where)
 {
+    if (__all_sync(0xffffffffu, mbar_try_wait(smem_u32(bar), parity))) return true;
     const bool ok = mbar_wait(bar, parity, w, where);
     return __all_sync(0xffffffffu, ok);
 }
@@ -291,65 +298,74 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
         } else if (warp == 9) {
             // ------------------------------------------------------------ products
-            // every lane follows, lane 0 issues
+            // Every lane follows, an elected one issues.  What the descriptors and the loops depend on comes
+            // from shuffles and votes, so that the compiler knows it to be the same in all lanes and keeps it
+            // in uniform registers: an instruction took 80 cycles to issue where it did not.
             constexpr uint32_t id_s = umma_idesc_bf16_f32(kTileRows, kTileKeys);
             constexpr uint32_t id_o = umma_idesc_bf16_f32(kTileRows, D) | kIdescBRows;
             Ring<kItemSlots> ri;
             Ring<C::STAGES> rs;
             uint32_t q_uses[2] = {}, p_uses[2] = {};
-            bool ok = true;
-            auto commit = [&](uint64_t* bar) {
-                if (lane == 0) umma_commit(bar);
-            };
-            auto scores = [&](int x, uint32_t stage, bool last) {
-                if (lane != 0) return;
-                const uint64_t q = umma_desc_sw128(smem_u32(smem + x * C::Q_BYTES));
-                const uint64_t k = umma_desc_sw128(smem_u32(smem + C::OFF_KV + stage * C::STAGE));
+            const uint64_t q_desc = umma_desc_sw128(smem_u32(smem));
+            const uint64_t k_desc = umma_desc_sw128(smem_u32(smem + C::OFF_KV));
+            const uint64_t v_desc = umma_desc_sw128_rows(smem_u32(smem + C::OFF_KV), C::CHUNK);
+            auto scores = [&](int x, uint32_t stage) {
+                const uint64_t k = k_desc + stage * (C::STAGE >> 4);
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i) {
                     const uint32_t at_i = (i / 4) * (C::CHUNK >> 4) + 2 * (i % 4);
-                    umma_bf16(tmem + C::T_S + x * kTileKeys, q + at_i, k + at_i, id_s, i != 0);
+                    umma_bf16(tmem + C::T_S + x * kTileKeys, q_desc + x * (C::Q_BYTES >> 4) + at_i,
+                              k + at_i, id_s, i != 0);
                 }
                 umma_commit(&M.s_full[x]);
-                if (last) umma_commit(&M.q_empty[x]);
             };
-            auto outputs = [&](int x, uint32_t stage, bool first, bool last) {
-                if (lane != 0) return;
-                const uint64_t v =
-                    umma_desc_sw128_rows(smem_u32(smem + C::OFF_KV + stage * C::STAGE), C::CHUNK);
+            auto outputs = [&](int x, uint32_t stage, uint32_t add) {
+                const uint64_t v = v_desc + stage * (C::STAGE >> 4);
 #pragma unroll
                 for (int i = 0; i < kTileKeys / 16; ++i)
                     umma_bf16_tmem(tmem + C::T_O + x * D, tmem + C::T_S + x * kTileKeys + 8 * i,
-                                   v + i * (16 * 128 >> 4), id_o, !first || i != 0);
-                if (last) umma_commit(&M.o_full[x]);
+                                   v + i * (16 * 128 >> 4), id_o, i != 0 ? 1u : add);
             };
+            bool ok = true;
             while (ok) {
                 if (!(ok = all_wait(&M.item_full[ri.slot], ri.phase, wc, 24))) break;
-                const Item it = M.items[ri.slot];
-                __syncwarp();
+                const Item& it = M.items[ri.slot];
+                const int head = __shfl_sync(0xffffffffu, it.head, 0);
+                const int s0 = __shfl_sync(0xffffffffu, it.s0, 0);
+                const int s1 = __shfl_sync(0xffffffffu, it.s1, 0);
+                const int n0 = min(s1, __shfl_sync(0xffffffffu, it.count[0], 0));
+                const int n1 = min(s1, __shfl_sync(0xffffffffu, it.count[1], 0));
+                const KeyTiles kt{__shfl_sync(0xffffffffu, it.sinks, 0),
+                                  __shfl_sync(0xffffffffu, it.from, 0), 0};
+                const int m = __shfl_sync(0xffffffffu, it.m, 0);
                 if (lane == 0) mbar_arrive(&M.item_empty[ri.slot]);
                 ri.next();
-                if (it.head < 0) break;
-                int n[2];
-                for (int x = 0; x < 2; ++x) n[x] = min(it.s1, it.count[x]);
-                const int all = max(n[0], n[1]);
-                if (all <= it.s0) continue;
-                const KeyTiles kt{it.sinks, it.from, 0};
+                if (head < 0) break;
+                const int all = max(n0, n1);
+                if (all <= s0) continue;
+                const bool both = n1 > s0;       // else the second tile has no tokens
                 ok = all_wait(&M.kv_full[rs.slot], rs.phase, wc, 25);
-                for (int x = 0; x < 2 && ok; ++x) {
-                    if (n[x] <= it.s0) continue;
-                    if (!(ok = all_wait(&M.q_full[x], q_uses[x]++ & 1u, wc, 26))) break;
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const int n = x ? n1 : n0;
+                    if (!ok || n <= s0) continue;
+                    if (!(ok = all_wait(&M.q_full[x], q_uses[x]++ & 1u, wc, 26))) continue;
                     tc_fence_after();
-                    scores(x, rs.slot, it.s0 + 1 == n[x]);
+                    if (elect_one()) {
+                        scores(x, rs.slot);
+                        if (s0 + 1 == n) umma_commit(&M.q_empty[x]);
+                        if (x == (both ? 1 : 0)) umma_commit(&M.kv_empty[rs.slot]);
+                    }
                 }
                 if (!ok) break;
-                commit(&M.kv_empty[rs.slot]);
                 rs.next();
-                for (int j = it.s0; j < all && ok; ++j) {
+                for (int j = s0; j < all; ++j) {
                     const Ring<C::STAGES> rv = rs;
                     rs.next();
                     if (!(ok = all_wait(&M.kv_full[rv.slot], rv.phase, wc, 27))) break;
-                    const int held = it.m - kt.tile(j) * kTileKeys;
+                    if (j + 1 < all)
+                        if (!(ok = all_wait(&M.kv_full[rs.slot], rs.phase, wc, 30))) break;
+                    const int held = m - kt.tile(j) * kTileKeys;
                     if (held < kTileKeys) {
                         // the sequence ends inside the tile: its probabilities are 0 from there on,
                         // and so are the values, whatever lies behind it
@@ -362,32 +378,33 @@ __global__ void __launch_bounds__(kThreads, 1)
                         fence_async_shared();
                         __syncwarp();
                     }
-                    bool keys = false;
-                    for (int x = 0; x < 2 && ok; ++x) {
-                        if (j < n[x]) {
-                            if (!(ok = all_wait(&M.p_full[x], p_uses[x]++ & 1u, wc, 29))) break;
-                            tc_fence_after();
-                            outputs(x, rv.slot, j == it.s0, j + 1 == n[x]);
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const int n = x ? n1 : n0;
+                        if (!ok || j >= n) continue;
+                        if (!(ok = all_wait(&M.p_full[x], p_uses[x]++ & 1u, wc, 29))) continue;
+                        tc_fence_after();
+                        if (elect_one()) {
+                            outputs(x, rv.slot, j != s0);
+                            if (j + 1 < n) {
+                                scores(x, rs.slot);
+                                if (j + 2 == n) umma_commit(&M.q_empty[x]);
+                            } else {
+                                umma_commit(&M.o_full[x]);
+                            }
+                            if (x == (both ? 1 : 0)) {
+                                umma_commit(&M.kv_empty[rv.slot]);
+                                if (j + 1 < all) umma_commit(&M.kv_empty[rs.slot]);
+                            }
                         }
-                        if (x == 1 || j >= n[1]) commit(&M.kv_empty[rv.slot]);
-                        if (j + 1 < n[x]) {
-                            if (!keys) ok = all_wait(&M.kv_full[rs.slot], rs.phase, wc, 30);
-                            if (!ok) break;
-                            keys = true;
-                            tc_fence_after();
-                            scores(x, rs.slot, j + 2 == n[x]);
-                        }
-                        if (j >= n[1]) break;
                     }
                     if (!ok) break;
-                    if (j + 1 < all) {
-                        commit(&M.kv_empty[rs.slot]);
-                        rs.next();
-                    }
+                    if (j + 1 < all) rs.next();
                 }
             }
             // every product has ended before tensor memory is freed
-            if (lane == 0) {
+            __syncwarp();
+            if (elect_one()) {
                 umma_commit(&M.drain);
                 drain_wait(&M.drain, 0, p.timeout_ns);
             }
@@ -494,13 +511,14 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (edge) {
                     const int hi = pos - k0, lo = low - k0, sinks = a.n_sink - k0;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t see = bits_below(hi + 1 - 32 * i);
+                        if (a.window > 0)
+                            see &= ~bits_below(lo - 32 * i) | bits_below(sinks - 32 * i);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            const int k = 32 * i + e;
-                            const bool see = k <= hi && (a.window == 0 || k >= lo || k < sinks);
-                            if (!see) s[i][e] = 0xff800000u;
-                        }
+                        for (int e = 0; e < 32; ++e)
+                            s[i][e] = see >> e & 1u ? s[i][e] : 0xff800000u;
+                    }
                 }
                 float m[4];
 #pragma unroll
