@@ -33,25 +33,22 @@ namespace twk {
 namespace {
 
 constexpr int kThreads = 384;
-constexpr int kLaunchRegs = 168, kHelperRegs = 56, kSoftmaxRegs = 224;
+constexpr int kLaunchRegs = 168, kHelperRegs = 88, kSoftmaxRegs = 208;
 static_assert(4 * kHelperRegs + 8 * kSoftmaxRegs <= 12 * kLaunchRegs,
               "the split draws on the registers of the launch");
 constexpr int kPairRows = 2 * kTileRows;
 constexpr float kLazy = 8.0f;            // what a maximum may rise, in powers of two, before O follows
 
-// tokens of a tile
-__device__ __forceinline__ int tile_tokens(const PromptArgs& a) { return kTileRows / a.G; }
-
 // Items of attention: pairs of row tiles; as long as their list of key tiles.
 struct RowPairs {
     __device__ static __forceinline__ int items(const PromptArgs& a, const Sequence& s)
     {
-        const int tokens = 2 * tile_tokens(a);
+        const int tokens = 2 * a.tile_tokens;
         return (s.n + tokens - 1) / tokens;
     }
     __device__ static __forceinline__ KeyTiles tiles(const PromptArgs& a, const Sequence& s, int i)
     {
-        const int tokens = 2 * tile_tokens(a), first = s.m - s.n + i * tokens;
+        const int tokens = 2 * a.tile_tokens, first = s.m - s.n + i * tokens;
         return key_tiles(a, first, min(first + tokens, s.m) - 1);
     }
     // 1 where nothing is seen: the rows are written all the same
@@ -67,13 +64,14 @@ struct Cfg {
     static constexpr int CHUNK = kTileRows * 128;
     static constexpr int Q_BYTES = KC * CHUNK;            // a tile of queries
     static constexpr int STAGE = KC * CHUNK;              // a tile of keys or values
-    static constexpr int STAGES = D == 128 ? 5 : 8;
+    static constexpr int STAGES = D == 128 ? 4 : 8;
     static constexpr int OFF_KV = 2 * Q_BYTES;
-    static constexpr int OFF_MISC = OFF_KV + STAGES * STAGE;
+    static constexpr int OFF_OUT = OFF_KV + STAGES * STAGE;     // a warp's rows, 128 bytes of each
+    static constexpr int OFF_MISC = OFF_OUT + 8 * 32 * 128;
     static constexpr int BYTES = OFF_MISC + 1024 + 1024;  // + 1024 for alignment
     static constexpr int T_S = 0, T_O = 256;              // columns of tensor memory: S, O of tile 0
     static_assert(BYTES <= 232448, "shared memory per block");
-    static_assert(STAGES * STAGE >= 2 * (kChunks + 1) * 8, "the chunks' sums lie there at first");
+    static_assert(STAGES * STAGE >= kSumsBytes, "the chunks' sums lie there at first");
 };
 
 constexpr int kItemSlots = 4;
@@ -104,8 +102,8 @@ struct AttendKernelArgs {
     PromptArgs a;
     float c;                 // scale * log2(e)
     float* part;             // [2 per block] parts, null: no item is shared
-    int4* join;              // [2 per block]: parts of the item that begins in the block and ends in
-                             // another one (0: none), t0, tokens, KV head; first slot in the second
+    int4* join;              // [per block]: parts of the item that begins in the block and ends in
+                             // another one (0: none), its t0, tokens and KV head
     int* err;
     unsigned long long timeout_ns;
 };
@@ -216,16 +214,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     wait_for_previous();
     // the chunks' sums lie where keys and values come later
     long long* sums = reinterpret_cast<long long*>(smem + C::OFF_KV);
-    const Totals total = sum_chunks<RowPairs>(a, sums, sums + kChunks + 1);
-    const int blocks = span_blocks(total);
-    Place at{}, end_at{};
-    long long begin = 0, end = 0;
-    const bool mine = static_cast<int>(blockIdx.x) < blocks;
-    if (warp == 10 && mine) {
-        begin = cut<RowPairs>(a, sums, total.units, blocks, blockIdx.x, at);
-        end = cut<RowPairs>(a, sums, total.units, blocks, blockIdx.x + 1, end_at);
-    }
-    fence_async_shared();
+    if (a.s.B > 32) sum_chunks<RowPairs>(a, sums);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -236,7 +225,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     wc.abort_flag = &M.abort_flag;
     wc.err = p.err;
     wc.where = 0;
-    const int tpt = tile_tokens(a);
+    const int tpt = a.tile_tokens;
 
     if (warp >= 8) {
         setmaxnreg_dec<kHelperRegs>();
@@ -306,66 +295,74 @@ __global__ void __launch_bounds__(kThreads, 1)
             Ring<kItemSlots> ri;
             Ring<C::STAGES> rs;
             uint32_t q_uses[2] = {}, p_uses[2] = {};
-            const uint64_t q_desc = umma_desc_sw128(smem_u32(smem));
-            const uint64_t k_desc = umma_desc_sw128(smem_u32(smem + C::OFF_KV));
-            const uint64_t v_desc = umma_desc_sw128_rows(smem_u32(smem + C::OFF_KV), C::CHUNK);
+            const uint32_t q_low = static_cast<uint32_t>(umma_desc_sw128(smem_u32(smem)));
+            const uint32_t k_low = static_cast<uint32_t>(umma_desc_sw128(smem_u32(smem + C::OFF_KV)));
+            const uint32_t v_low =
+                static_cast<uint32_t>(umma_desc_sw128_rows(smem_u32(smem + C::OFF_KV), C::CHUNK));
             auto scores = [&](int x, uint32_t stage) {
-                const uint64_t k = k_desc + stage * (C::STAGE >> 4);
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i) {
-                    const uint32_t at_i = (i / 4) * (C::CHUNK >> 4) + 2 * (i % 4);
-                    umma_bf16(tmem + C::T_S + x * kTileKeys, q_desc + x * (C::Q_BYTES >> 4) + at_i,
-                              k + at_i, id_s, i != 0);
-                }
+                umma_rows<C::KC>(tmem + C::T_S + x * kTileKeys, q_low + x * (C::Q_BYTES >> 4),
+                                 k_low + stage * (C::STAGE >> 4), id_s);
                 umma_commit(&M.s_full[x]);
             };
             auto outputs = [&](int x, uint32_t stage, uint32_t add) {
-                const uint64_t v = v_desc + stage * (C::STAGE >> 4);
-#pragma unroll
-                for (int i = 0; i < kTileKeys / 16; ++i)
-                    umma_bf16_tmem(tmem + C::T_O + x * D, tmem + C::T_S + x * kTileKeys + 8 * i,
-                                   v + i * (16 * 128 >> 4), id_o, i != 0 ? 1u : add);
+                umma_tmem_128(tmem + C::T_O + x * D, tmem + C::T_S + x * kTileKeys,
+                              v_low + stage * (C::STAGE >> 4), id_o, add);
             };
             bool ok = true;
-            while (ok) {
-                if (!(ok = all_wait(&M.item_full[ri.slot], ri.phase, wc, 24))) break;
-                const Item& it = M.items[ri.slot];
-                const int head = __shfl_sync(0xffffffffu, it.head, 0);
-                const int s0 = __shfl_sync(0xffffffffu, it.s0, 0);
-                const int s1 = __shfl_sync(0xffffffffu, it.s1, 0);
-                const int n0 = min(s1, __shfl_sync(0xffffffffu, it.count[0], 0));
-                const int n1 = min(s1, __shfl_sync(0xffffffffu, it.count[1], 0));
-                const KeyTiles kt{__shfl_sync(0xffffffffu, it.sinks, 0),
-                                  __shfl_sync(0xffffffffu, it.from, 0), 0};
-                const int m = __shfl_sync(0xffffffffu, it.m, 0);
-                if (lane == 0) mbar_arrive(&M.item_empty[ri.slot]);
-                ri.next();
-                if (head < 0) break;
-                const int all = max(n0, n1);
-                if (all <= s0) continue;
-                const bool both = n1 > s0;       // else the second tile has no tokens
-                ok = all_wait(&M.kv_full[rs.slot], rs.phase, wc, 25);
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const int n = x ? n1 : n0;
-                    if (!ok || n <= s0) continue;
-                    if (!(ok = all_wait(&M.q_full[x], q_uses[x]++ & 1u, wc, 26))) continue;
-                    tc_fence_after();
-                    if (elect_one()) {
-                        scores(x, rs.slot);
-                        if (s0 + 1 == n) umma_commit(&M.q_empty[x]);
-                        if (x == (both ? 1 : 0)) umma_commit(&M.kv_empty[rs.slot]);
-                    }
+            // an item with products: its list's units [s0, all), of which tile x takes those below n[x]
+            struct Part {
+                int s0, n[2], all, last;        // last: the last tile that has any
+                int m;
+                KeyTiles kt;
+            };
+            auto fetch = [&](Part& f) {         // all = s0: there are no more
+                for (;;) {
+                    f.s0 = f.all = 0;
+                    if (!(ok = all_wait(&M.item_full[ri.slot], ri.phase, wc, 24))) return;
+                    const Item& it = M.items[ri.slot];
+                    const int head = __shfl_sync(0xffffffffu, it.head, 0);
+                    const int s1 = __shfl_sync(0xffffffffu, it.s1, 0);
+                    f.s0 = __shfl_sync(0xffffffffu, it.s0, 0);
+                    f.n[0] = min(s1, __shfl_sync(0xffffffffu, it.count[0], 0));
+                    f.n[1] = min(s1, __shfl_sync(0xffffffffu, it.count[1], 0));
+                    f.kt = KeyTiles{__shfl_sync(0xffffffffu, it.sinks, 0),
+                                    __shfl_sync(0xffffffffu, it.from, 0), 0};
+                    f.m = __shfl_sync(0xffffffffu, it.m, 0);
+                    if (lane == 0) mbar_arrive(&M.item_empty[ri.slot]);
+                    ri.next();
+                    f.last = f.n[1] > f.s0 ? 1 : 0;
+                    f.all = head < 0 ? f.s0 : max(f.s0, max(f.n[0], f.n[1]));
+                    if (head < 0 || f.all > f.s0) return;
                 }
-                if (!ok) break;
+            };
+            // the scores of the item's first unit by tile x
+            auto first_scores = [&](const Part& f, int x) {
+                if (!ok || f.n[x] <= f.s0) return;
+                ok = all_wait(&M.kv_full[rs.slot], rs.phase, wc, 25) &&
+                     all_wait(&M.q_full[x], q_uses[x]++ & 1u, wc, 26);
+                if (!ok) return;
+                tc_fence_after();
+                if (elect_one()) {
+                    scores(x, rs.slot);
+                    if (f.s0 + 1 == f.n[x]) umma_commit(&M.q_empty[x]);
+                    if (x == f.last) umma_commit(&M.kv_empty[rs.slot]);
+                }
+            };
+            Part f, g;
+            fetch(f);
+            if (ok && f.all > f.s0) {
+                first_scores(f, 0);
+                first_scores(f, 1);
                 rs.next();
-                for (int j = s0; j < all; ++j) {
+            }
+            while (ok && f.all > f.s0) {
+                for (int j = f.s0; j < f.all; ++j) {
                     const Ring<C::STAGES> rv = rs;
                     rs.next();
+                    const bool end = j + 1 == f.all;
                     if (!(ok = all_wait(&M.kv_full[rv.slot], rv.phase, wc, 27))) break;
-                    if (j + 1 < all)
-                        if (!(ok = all_wait(&M.kv_full[rs.slot], rs.phase, wc, 30))) break;
-                    const int held = m - kt.tile(j) * kTileKeys;
+                    if (!end && !(ok = all_wait(&M.kv_full[rs.slot], rs.phase, wc, 30))) break;
+                    const int held = f.m - f.kt.tile(j) * kTileKeys;
                     if (held < kTileKeys) {
                         // the sequence ends inside the tile: its probabilities are 0 from there on,
                         // and so are the values, whatever lies behind it
@@ -378,29 +375,37 @@ __global__ void __launch_bounds__(kThreads, 1)
                         fence_async_shared();
                         __syncwarp();
                     }
+                    if (end) {
+                        fetch(g);
+                        if (!ok) break;
+                    }
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        const int n = x ? n1 : n0;
-                        if (!ok || j >= n) continue;
-                        if (!(ok = all_wait(&M.p_full[x], p_uses[x]++ & 1u, wc, 29))) continue;
-                        tc_fence_after();
-                        if (elect_one()) {
-                            outputs(x, rv.slot, j != s0);
-                            if (j + 1 < n) {
-                                scores(x, rs.slot);
-                                if (j + 2 == n) umma_commit(&M.q_empty[x]);
-                            } else {
-                                umma_commit(&M.o_full[x]);
+                        if (ok && j < f.n[x]) {
+                            ok = all_wait(&M.p_full[x], p_uses[x]++ & 1u, wc, 29);
+                            if (ok) tc_fence_after();
+                            if (ok && elect_one()) {
+                                outputs(x, rv.slot, j != f.s0);
+                                if (j + 1 < f.n[x]) {
+                                    scores(x, rs.slot);
+                                    if (j + 2 == f.n[x]) umma_commit(&M.q_empty[x]);
+                                } else {
+                                    umma_commit(&M.o_full[x]);
+                                }
+                                if (x == f.last) {
+                                    umma_commit(&M.kv_empty[rv.slot]);
+                                    if (!end) umma_commit(&M.kv_empty[rs.slot]);
+                                }
                             }
-                            if (x == (both ? 1 : 0)) {
-                                umma_commit(&M.kv_empty[rv.slot]);
-                                if (j + 1 < all) umma_commit(&M.kv_empty[rs.slot]);
-                            }
+                            __syncwarp();
                         }
+                        // the next item's first scores, while the softmax of this one's last unit runs
+                        if (end && g.all > g.s0) first_scores(g, x);
                     }
                     if (!ok) break;
-                    if (j + 1 < all) rs.next();
+                    if (!end || g.all > g.s0) rs.next();
                 }
+                f = g;
             }
             // every product has ended before tensor memory is freed
             __syncwarp();
@@ -410,17 +415,17 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
         } else if (warp == 10) {
             // ------------------------------------------------------------ items
-            Ring<kItemSlots> ri;
-            bool ok = true;
+            Walk<RowPairs> at;
+            at.start(a, sums);
+            fence_async_shared();       // the sums have been read
+            __syncwarp();
             if (lane == 0) {
-                if (p.join) p.join[2 * blockIdx.x] = make_int4(0, 0, 0, 0);
-                const int tokens = 2 * tpt;
-                long long g = begin;
-                while (ok && g < end) {
-                    const int take = static_cast<int>(
-                        end - g < at.length - at.off ? end - g : at.length - at.off);
+                Ring<kItemSlots> ri;
+                bool ok = true;
+                int4 join = make_int4(0, 0, 0, 0);
+                for (; ok && at.more; at.next(a)) {
                     Item it{};
-                    const int i0 = at.item * tokens;
+                    const int i0 = at.item * 2 * tpt;
                     it.t0 = at.s.t0 + i0;
                     it.tokens = at.s.n - i0;
                     it.pos = at.s.m - at.s.n + i0;
@@ -428,7 +433,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     it.m = at.s.m;
                     it.head = at.head;
                     it.s0 = at.off;
-                    it.s1 = at.off + take;
+                    it.s1 = at.off + at.take;
                     const KeyTiles kt = RowPairs::tiles(a, at.s, at.item);
                     it.sinks = kt.sinks;
                     it.from = kt.from;
@@ -438,27 +443,24 @@ __global__ void __launch_bounds__(kThreads, 1)
                         const bool any = it.tokens > x * tpt && last >= 0;
                         it.count[x] = any ? kt.sinks + last / kTileKeys + 1 - kt.from : 0;
                     }
-                    const bool whole = at.off == 0 && take == at.length;
-                    // heads and middles in slot 2 c, the item that begins in the block in 2 c + 1
-                    it.slot = whole ? -1 : 2 * static_cast<int>(blockIdx.x) + (at.off == 0 ? 1 : 0);
-                    if (!whole && at.off == 0) {
-                        const int parts = parts_of(total.units, blocks, blockIdx.x, g, at.length);
-                        p.join[2 * blockIdx.x] = make_int4(parts, it.t0, it.tokens, it.head);
+                    it.slot = -1;
+                    if (at.take < at.length) {
+                        // heads and middles in slot 2 c, the item that begins in the block in 2 c + 1
+                        it.slot = 2 * static_cast<int>(blockIdx.x) + (at.off == 0 ? 1 : 0);
+                        if (at.off == 0) join = make_int4(at.parts(), it.t0, it.tokens, it.head);
                     }
                     ok = mbar_wait(&M.item_empty[ri.slot], ri.phase ^ 1u, wc, 31);
                     if (!ok) break;
                     M.items[ri.slot] = it;
                     mbar_arrive(&M.item_full[ri.slot]);
                     ri.next();
-                    g += take;
-                    if (at.off + take < at.length || !next_item<RowPairs>(a, at)) break;
                 }
+                if (p.join) p.join[blockIdx.x] = join;
                 if (ok) ok = mbar_wait(&M.item_empty[ri.slot], ri.phase ^ 1u, wc, 31);
                 if (ok) {
                     M.items[ri.slot].head = -1;
                     mbar_arrive(&M.item_full[ri.slot]);
                 }
-                // no one waits on the slots after this but what has been published
             }
         } else {
             if (blockIdx.x == 0 && a.out_status)
@@ -587,15 +589,21 @@ __global__ void __launch_bounds__(kThreads, 1)
                                    it.head * a.G + sub;
             if (it.slot < 0) {
                 const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;      // O is 0 where sum is
+                // through shared memory, 128 bytes of every row at a time, so that eight lanes write a
+                // row's (a row to a lane: 6700 cycles for 256 rows of 128, now 2000)
+                uint8_t* mine = smem + C::OFF_OUT + warp * 32 * 128;
+                const int to = held ? (x * tpt + token) * a.s.Hq + sub : -1;
+                uint16_t* out = a.out + (static_cast<int64_t>(it.t0) * a.s.Hq + it.head * a.G) * D;
 #pragma unroll
-                for (int i = 0; i < D / 32; ++i) {
-                    uint32_t o[32] = {};
-                    if (any) {
-                        tmem_ld_32x32b_x32(t_o + 32 * i, o);
-                        tmem_wait_ld();
-                        reg_fence(o);
-                    }
-                    if (held) {
+                for (int h = 0; h < C::KC; ++h) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t o[32] = {};
+                        if (any) {
+                            tmem_ld_32x32b_x32(t_o + 64 * h + 32 * i, o);
+                            tmem_wait_ld();
+                            reg_fence(o);
+                        }
 #pragma unroll
                         for (int e = 0; e < 32; e += 8) {
                             uint4 w;
@@ -603,9 +611,22 @@ __global__ void __launch_bounds__(kThreads, 1)
                             w.y = bf16_pair(as_f(o[e + 2]) * inv, as_f(o[e + 3]) * inv);
                             w.z = bf16_pair(as_f(o[e + 4]) * inv, as_f(o[e + 5]) * inv);
                             w.w = bf16_pair(as_f(o[e + 6]) * inv, as_f(o[e + 7]) * inv);
-                            *reinterpret_cast<uint4*>(a.out + at_row * D + 32 * i + e) = w;
+                            *reinterpret_cast<uint4*>(mine + lane * 128 +
+                                                      ((4 * i + e / 8) ^ (lane & 7)) * 16) = w;
                         }
                     }
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int r = 4 * i + lane / 8;
+                        const uint4 w = *reinterpret_cast<const uint4*>(
+                            mine + r * 128 + ((lane & 7) ^ (r & 7)) * 16);
+                        const int at_r = __shfl_sync(0xffffffffu, to, r);
+                        if (at_r >= 0)
+                            *reinterpret_cast<uint4*>(out + static_cast<int64_t>(at_r) * D + 64 * h +
+                                                      8 * (lane & 7)) = w;
+                    }
+                    __syncwarp();
                 }
                 if (held && a.out_lse)
                     a.out_lse[at_row] = sum > 0.0f ? fmaf(top, 0.6931471805599453f, logf(sum))
@@ -648,11 +669,11 @@ __global__ void __launch_bounds__(32 * kMergeWarps)
     constexpr int kVec = D / 4 / kMergeWarps;
     wait_for_previous();
     const PromptArgs& a = p.a;
-    const int4 join = p.join[2 * blockIdx.x];
+    const int4 join = p.join[blockIdx.x];
     if (join.x == 0) return;
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int r = blockIdx.y * 32 + lane;
-    const int x = r / kTileRows, row = r % kTileRows, tpt = tile_tokens(a);
+    const int x = r / kTileRows, row = r % kTileRows, tpt = a.tile_tokens;
     const int token = row / a.G;
     if (token >= tpt || x * tpt + token >= join.z) return;
     float top = -INFINITY, sum = 0.0f, acc[kVec][4] = {};
@@ -733,7 +754,7 @@ cudaError_t launch(const PromptArgs& a, int sms, const WaitFacts& w, cudaStream_
         if (dev < 64) allowed[dev].store(true, std::memory_order_relaxed);
     }
     CUtensorMap q, k, v;
-    const int tpt = kTileRows / a.G;
+    const int tpt = a.tile_tokens;
     if (!encode_rows(&q, a.q, D, a.s.Hq, a.s.tokens, a.s.q_head, a.s.q_token, a.G, tpt) ||
         !encode_rows(&k, a.k, D, a.s.H, a.s.keys, a.s.k_head, a.s.k_token, 1, kTileKeys) ||
         !encode_rows(&v, a.v, D, a.s.H, a.s.keys, a.s.v_head, a.s.v_token, 1, kTileKeys))
@@ -744,7 +765,7 @@ cudaError_t launch(const PromptArgs& a, int sms, const WaitFacts& w, cudaStream_
     const bool shared = a.s.keys > kWholeKeys;
     if (shared) {
         p.join = static_cast<int4*>(a.ws);
-        p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(a.ws) + 32 * kPromptBlocks);
+        p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(a.ws) + 16 * kPromptBlocks);
     }
     p.err = w.err;
     p.timeout_ns = w.timeout_ns;
@@ -759,7 +780,7 @@ cudaError_t launch(const PromptArgs& a, int sms, const WaitFacts& w, cudaStream_
 size_t prompt_attend_workspace(const twinkv_prompt& s)
 {
     if (s.keys <= kWholeKeys) return 256;
-    return 32 * kPromptBlocks +
+    return 16 * kPromptBlocks +
            2 * kPromptBlocks * static_cast<size_t>(kPairRows) * (s.d + 2) * sizeof(float);
 }
 

@@ -68,74 +68,89 @@ __device__ __forceinline__ KeyTiles key_tiles(const PromptArgs& a, int first, in
 // ---- work among blocks
 //
 // A call's items (of a sequence and KV head) follow one another, each as long as W::length says (1
-// or more units), and all units are cut into equal spans, one for each block.  An item that spans share
-// is done in parts, which a second kernel joins in order: what is cut where depends on the sizes alone.
-// A cut within kSnap units of an item's end moves there, since a part costs about as much as so many
-// units.
+// or more units), and all units are cut into even spans, one for each block.  An item that spans
+// share is done in parts, which a second kernel joins in order: what is cut where depends on the sizes
+// alone.  A cut within kSnap units of an item's end moves there, since a part costs about as much as so
+// many units.
 
 constexpr int kSnap = 3;
 constexpr int kChunks = 256;        // groups of sequences with their sums in shared memory
 
-// lengths of the sequence's items of one head, added up by a warp
-template <class W>
-__device__ __forceinline__ long long warp_length(const PromptArgs& a, const Sequence& s, int items)
+// x / y, both above 0
+__device__ __forceinline__ long long quotient(long long x, long long y)
 {
-    int sum = 0;                    // at most 2^18 items a lane, of 2^17 + 2 units: in 64 bits below
-    long long all = 0;
-    for (int i = threadIdx.x % 32; i < items; i += 32) {
-        sum += W::length(a, s, i);
-        if (sum > (1 << 29)) all += sum, sum = 0;
-    }
-    all += sum;
+    if (((x | y) >> 31) == 0) return static_cast<unsigned>(x) / static_cast<unsigned>(y);
+    return x / y;
+}
+
+__device__ __forceinline__ long long shfl64(long long x, int lane)
+{
+    return __shfl_sync(0xffffffffu, x, lane);
+}
+
+__device__ __forceinline__ long long inclusive_scan(long long x)
+{
 #pragma unroll
-    for (int o = 16; o > 0; o /= 2) all += __shfl_xor_sync(0xffffffffu, all, o);
-    return all;
-}
-
-// The lanes' sequences b0 + lane below `end`: units of all their heads (0 where there is none), and items.
-template <class W>
-__device__ __forceinline__ long long lane_units(const PromptArgs& a, int b, int end, long long& items_all)
-{
-    Sequence s{};
-    if (b < end) s = sequence_of(a, b);
-    const int items = W::items(a, s);
-    long long units = 0;
-    if (items <= 8)
-        for (int i = 0; i < items; ++i) units += W::length(a, s, i);
-    for (unsigned big = __ballot_sync(0xffffffffu, items > 8); big; big &= big - 1) {
-        const int l = __ffs(big) - 1;
-        Sequence t;
-        t.t0 = __shfl_sync(0xffffffffu, s.t0, l);
-        t.n = __shfl_sync(0xffffffffu, s.n, l);
-        t.j0 = __shfl_sync(0xffffffffu, s.j0, l);
-        t.m = __shfl_sync(0xffffffffu, s.m, l);
-        t.ok = true;
-        const long long x = warp_length<W>(a, t, __shfl_sync(0xffffffffu, items, l));
-        if (threadIdx.x % 32 == l) units = x;
+    for (int o = 1; o < 32; o *= 2) {
+        const long long y = __shfl_up_sync(0xffffffffu, x, o);
+        if (threadIdx.x % 32 >= o) x += y;
     }
-    items_all = static_cast<long long>(items) * a.s.H;
-    return units * a.s.H;
+    return x;
 }
 
-__device__ __forceinline__ int chunk_size(int B) { return (B + 32 * kChunks - 1) / (32 * kChunks) * 32; }
-
-struct Totals {
-    long long units, items;
+// The sequence of a lane, its items of a head and their units.
+struct LaneUnits {
+    Sequence s;
+    int items;
+    long long units;
 };
 
-// Units before each chunk, by all warps of the block, to sums[kChunks + 1] in shared memory, and the totals.
-// Ends with a barrier.
+// The lanes' sequences b0 + lane (0 items from B on), by a converged warp.
 template <class W>
-__device__ __forceinline__ Totals sum_chunks(const PromptArgs& a, long long* sums, long long* counts)
+__device__ __forceinline__ LaneUnits lane_units(const PromptArgs& a, int b0)
+{
+    const int lane = threadIdx.x % 32;
+    LaneUnits u{};
+    if (b0 + lane < a.s.B) u.s = sequence_of(a, b0 + lane);
+    u.items = W::items(a, u.s);
+    if (u.items <= 4)
+        for (int i = 0; i < u.items; ++i) u.units += W::length(a, u.s, i);
+    // the long ones by all lanes
+    for (unsigned big = __ballot_sync(0xffffffffu, u.items > 4); big; big &= big - 1) {
+        const int l = __ffs(big) - 1, items = __shfl_sync(0xffffffffu, u.items, l);
+        Sequence t;
+        t.t0 = t.j0 = 0;
+        t.ok = true;
+        t.n = __shfl_sync(0xffffffffu, u.s.n, l);
+        t.m = __shfl_sync(0xffffffffu, u.s.m, l);
+        long long all = 0;
+        for (int i = lane; i < items; i += 32) all += W::length(a, t, i);
+#pragma unroll
+        for (int o = 16; o > 0; o /= 2) all += __shfl_xor_sync(0xffffffffu, all, o);
+        if (lane == l) u.units = all;
+    }
+    return u;
+}
+
+__device__ __forceinline__ int chunk_size(int B)
+{
+    return (B + 32 * kChunks - 1) / (32 * kChunks) * 32;
+}
+
+// More than 32 sequences: units (of all heads) before each chunk, by all warps of the block, to
+// sums[kChunks + 1] in shared memory, and all items in sums[kChunks + 1].  Ends with a barrier.
+template <class W>
+__device__ __forceinline__ void sum_chunks(const PromptArgs& a, long long* sums)
 {
     const int lane = threadIdx.x % 32, size = chunk_size(a.s.B);
     const int chunks = (a.s.B + size - 1) / size;
+    long long* counts = sums + kChunks + 1;
     for (int c = threadIdx.x / 32; c < chunks; c += blockDim.x / 32) {
         long long units = 0, items = 0;
         for (int b = c * size; b < min((c + 1) * size, a.s.B); b += 32) {
-            long long n;
-            units += lane_units<W>(a, b + lane, a.s.B, n);
-            items += n;
+            const LaneUnits u = lane_units<W>(a, b);
+            units += u.units;
+            items += u.items;
         }
 #pragma unroll
         for (int o = 16; o > 0; o /= 2) {
@@ -143,8 +158,8 @@ __device__ __forceinline__ Totals sum_chunks(const PromptArgs& a, long long* sum
             items += __shfl_xor_sync(0xffffffffu, items, o);
         }
         if (lane == 0) {
-            sums[c] = units;
-            counts[c] = items;
+            sums[c] = units * a.s.H;
+            counts[c] = items * a.s.H;
         }
     }
     __syncthreads();
@@ -153,15 +168,9 @@ __device__ __forceinline__ Totals sum_chunks(const PromptArgs& a, long long* sum
         for (int c0 = 0; c0 < chunks; c0 += 32) {
             const long long n = c0 + lane < chunks ? sums[c0 + lane] : 0;
             items += c0 + lane < chunks ? counts[c0 + lane] : 0;
-            long long scan = n;
-#pragma unroll
-            for (int o = 1; o < 32; o *= 2) {
-                const long long y = __shfl_up_sync(0xffffffffu, scan, o);
-                if (lane >= o) scan += y;
-            }
-            __syncwarp();
+            const long long scan = inclusive_scan(n);
             if (c0 + lane < chunks) sums[c0 + lane] = before + scan - n;
-            before += __shfl_sync(0xffffffffu, scan, 31);
+            before += shfl64(scan, 31);
         }
 #pragma unroll
         for (int o = 16; o > 0; o /= 2) items += __shfl_xor_sync(0xffffffffu, items, o);
@@ -171,136 +180,168 @@ __device__ __forceinline__ Totals sum_chunks(const PromptArgs& a, long long* sum
         }
     }
     __syncthreads();
-    return {sums[chunks], counts[0]};
 }
+constexpr int kSumsBytes = (2 * kChunks + 1) * 8;
 
-// Blocks that get a span: no more than there are items where those are short, and at least four
-// units to a block where they are long.
-__device__ __forceinline__ int span_blocks(const Totals& t)
-{
-    long long n = t.units / 4 > t.items ? t.units / 4 : t.items;
-    return static_cast<int>(n < gridDim.x ? n : gridDim.x);
-}
+// A block's walk over the items of its span: next() gives one part after another.
+template <class W>
+struct Walk {
+    int b = 0, head = 0, item = 0, length = 0;   // where it is; length of the item
+    int items = 0;                               // of the sequence and head
+    int off = 0, take = 0;                       // the part: its first unit and units
+    Sequence s{};
+    long long begin = 0, end = 0;                // the item's first unit; where the span ends, before it snaps
+    long long each = 0;                          // units of a block, and how many blocks have one more
+    unsigned over = 0;
+    int blocks = 0;
+    bool more = false;                           // the part at hand is one
 
-// A place in the sequence of all units.
-struct Place {
-    int b, head, item, length;      // length: of the item
-    int items;                      // of the sequence and head
-    int off;                        // unit of the item
-    Sequence s;
+    // By one converged warp; sums as sum_chunks left them, not looked at for up to 32 sequences.
+    __device__ __forceinline__ void start(const PromptArgs& a, const long long* sums)
+    {
+        const int lane = threadIdx.x % 32;
+        long long units, count;
+        LaneUnits u{};
+        if (a.s.B <= 32) {
+            u = lane_units<W>(a, 0);
+            units = u.units;
+            count = u.items;
+#pragma unroll
+            for (int o = 16; o > 0; o /= 2) {
+                units += __shfl_xor_sync(0xffffffffu, units, o);
+                count += __shfl_xor_sync(0xffffffffu, count, o);
+            }
+            units *= a.s.H;
+            count *= a.s.H;
+        } else {
+            const int size = chunk_size(a.s.B);
+            units = sums[(a.s.B + size - 1) / size];
+            count = sums[kChunks + 1];
+        }
+        if (units == 0) return;
+        // at least four units to a block, or half an item where those are short
+        long long want = units / 4 > 2 * count ? units / 4 : 2 * count;
+        if (want > units) want = units;          // every span has units
+        blocks = static_cast<int>(want < gridDim.x ? want : gridDim.x);
+        if (static_cast<int>(blockIdx.x) >= blocks) return;
+        each = quotient(units, blocks);
+        over = static_cast<unsigned>(units - each * blocks);
+        const long long g = cut(blockIdx.x);
+        if (g >= units) return;
+        end = cut(blockIdx.x + 1);
+
+        // the sequence, then the head, then the item with unit g
+        long long rest = g;
+        int b0 = 0;
+        if (a.s.B > 32) {
+            const int size = chunk_size(a.s.B);
+            int lo = 0;
+            for (int hi = (a.s.B + size - 1) / size - 1; lo < hi;) {
+                const int mid = (lo + hi + 1) / 2;
+                if (sums[mid] <= g) lo = mid;
+                else hi = mid - 1;
+            }
+            rest -= sums[lo];
+            b0 = lo * size;
+            u = lane_units<W>(a, b0);
+        }
+        long long per_head = 0;
+        for (;;) {
+            const long long scan = inclusive_scan(u.units * a.s.H);
+            const unsigned past = __ballot_sync(0xffffffffu, scan > rest);
+            if (past) {
+                const int l = __ffs(past) - 1;
+                per_head = shfl64(u.units, l);
+                rest -= shfl64(scan, l) - per_head * a.s.H;
+                b = b0 + l;
+                items = __shfl_sync(0xffffffffu, u.items, l);
+                s.t0 = __shfl_sync(0xffffffffu, u.s.t0, l);
+                s.n = __shfl_sync(0xffffffffu, u.s.n, l);
+                s.j0 = __shfl_sync(0xffffffffu, u.s.j0, l);
+                s.m = __shfl_sync(0xffffffffu, u.s.m, l);
+                s.ok = true;
+                break;
+            }
+            rest -= shfl64(scan, 31);
+            b0 += 32;
+            if (b0 >= a.s.B) return;
+            u = lane_units<W>(a, b0);
+        }
+        head = static_cast<int>(quotient(rest, per_head));
+        rest -= per_head * head;
+        for (int i = 0;; i += 32) {
+            if (i >= items) return;
+            const long long mine = i + lane < items ? W::length(a, s, i + lane) : 0;
+            const long long scan = inclusive_scan(mine);
+            const unsigned past = __ballot_sync(0xffffffffu, scan > rest);
+            if (past) {
+                const int l = __ffs(past) - 1;
+                length = static_cast<int>(shfl64(mine, l));
+                off = static_cast<int>(rest - (shfl64(scan, l) - length));
+                item = i + l;
+                break;
+            }
+            rest -= shfl64(scan, 31);
+        }
+        begin = g - off;
+        more = true;
+        if (off <= kSnap) off = 0;
+        else if (length - off <= kSnap) advance(a);
+        part();
+    }
+
+    // The part after this one, by any one lane.
+    __device__ __forceinline__ void next(const PromptArgs& a)
+    {
+        if (off + take < length) more = false;
+        else advance(a);
+        part();
+    }
+
+    // Blocks that share the item, this one being the first.
+    __device__ __forceinline__ int parts() const
+    {
+        int n = 1;
+        while (cut(blockIdx.x + n) + kSnap < begin + length) ++n;
+        return n;
+    }
+
+private:
+    // where the span of block c begins, before it snaps
+    __device__ __forceinline__ long long cut(unsigned c) const
+    {
+        return each * c + over * c / static_cast<unsigned>(blocks);
+    }
+    __device__ __forceinline__ void advance(const PromptArgs& a)
+    {
+        begin += length;
+        off = 0;
+        if (++item == items) {
+            item = 0;
+            if (++head == a.s.H) {
+                head = 0;
+                do {
+                    if (++b == a.s.B) {
+                        more = false;
+                        return;
+                    }
+                    s = sequence_of(a, b);
+                    items = W::items(a, s);
+                } while (items == 0);
+            }
+        }
+        length = W::length(a, s, item);
+    }
+    // how far the span takes the item
+    __device__ __forceinline__ void part()
+    {
+        if (!more) return;
+        take = length - off;
+        if (end < begin + length) {
+            if (end - begin <= kSnap) more = false;
+            else if (begin + length - end > kSnap) take = static_cast<int>(end - begin) - off;
+        }
+    }
 };
-
-// The place of unit g < total, by one warp.
-template <class W>
-__device__ __forceinline__ Place locate(const PromptArgs& a, const long long* sums, long long g)
-{
-    const int lane = threadIdx.x % 32, size = chunk_size(a.s.B);
-    int lo = 0;
-    for (int hi = (a.s.B + size - 1) / size - 1; lo < hi;) {
-        const int mid = (lo + hi + 1) / 2;
-        if (sums[mid] <= g) lo = mid;
-        else hi = mid - 1;
-    }
-    long long rest = g - sums[lo];
-    Place p{};
-    long long units = 0;
-    for (int b = lo * size; b < a.s.B; b += 32) {
-        long long n, mine = lane_units<W>(a, b + lane, a.s.B, n), scan = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o *= 2) {
-            const long long y = __shfl_up_sync(0xffffffffu, scan, o);
-            if (lane >= o) scan += y;
-        }
-        const unsigned past = __ballot_sync(0xffffffffu, scan > rest);
-        if (past) {
-            const int l = __ffs(past) - 1;
-            units = __shfl_sync(0xffffffffu, mine, l);
-            rest -= __shfl_sync(0xffffffffu, scan, l) - units;
-            p.b = b + l;
-            break;
-        }
-        rest -= __shfl_sync(0xffffffffu, scan, 31);
-    }
-    p.s = sequence_of(a, p.b);
-    p.items = W::items(a, p.s);
-    units /= a.s.H;
-    if (units > 0) {
-        p.head = static_cast<int>(rest / units);
-        rest -= units * p.head;
-    }
-    for (int i = 0; i < p.items; i += 32) {
-        const int mine = i + lane < p.items ? W::length(a, p.s, i + lane) : 0;
-        int scan = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o *= 2) {
-            const int y = __shfl_up_sync(0xffffffffu, scan, o);
-            if (lane >= o) scan += y;
-        }
-        const unsigned past = __ballot_sync(0xffffffffu, scan > rest);
-        if (past) {
-            const int l = __ffs(past) - 1;
-            p.length = __shfl_sync(0xffffffffu, mine, l);
-            p.off = static_cast<int>(rest - (__shfl_sync(0xffffffffu, scan, l) - p.length));
-            p.item = i + l;
-            break;
-        }
-        rest -= __shfl_sync(0xffffffffu, scan, 31);
-    }
-    return p;
-}
-
-// The next item; false past the last one.
-template <class W>
-__device__ __forceinline__ bool next_item(const PromptArgs& a, Place& p)
-{
-    p.off = 0;
-    if (++p.item == p.items) {
-        p.item = 0;
-        if (++p.head == a.s.H) {
-            p.head = 0;
-            do {
-                if (++p.b == a.s.B) return false;
-                p.s = sequence_of(a, p.b);
-                p.items = W::items(a, p.s);
-            } while (p.items == 0);
-        }
-    }
-    p.length = W::length(a, p.s, p.item);
-    return true;
-}
-
-// Where the span of block c begins, and its place; the end of a block's span is the next one's begin.
-__device__ __forceinline__ long long raw_cut(long long units, int blocks, int c)
-{
-    return units / blocks * c + units % blocks * c / blocks;
-}
-
-template <class W>
-__device__ __forceinline__ long long cut(const PromptArgs& a, const long long* sums, long long units,
-                                         int blocks, int c, Place& p)
-{
-    const long long g = raw_cut(units, blocks, c);
-    if (g >= units) return units;
-    p = locate<W>(a, sums, g);
-    if (p.off <= kSnap) {
-        const int off = p.off;
-        p.off = 0;
-        return g - off;
-    }
-    if (p.length - p.off <= kSnap) {
-        const int more = p.length - p.off;
-        next_item<W>(a, p);
-        return g + more;
-    }
-    return g;
-}
-
-// Blocks that share the item, from the one that has its unit `off` (the item begins at unit `begin`) on.
-__device__ __forceinline__ int parts_of(long long units, int blocks, int c, long long begin, int length)
-{
-    int parts = 1;
-    while (c + parts < blocks && raw_cut(units, blocks, c + parts) + kSnap < begin + length) ++parts;
-    return parts;
-}
 
 }  // namespace twk

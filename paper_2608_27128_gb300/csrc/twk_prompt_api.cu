@@ -72,6 +72,7 @@ PromptArgs args_of(const void* q, const void* k, const twinkv_prompt& s,
     a.s = s;
     a.seqs = seqs;
     a.G = s.Hq / s.H;
+    a.tile_tokens = 128 / a.G;
     a.scale = scale;
     a.window = window;
     a.n_sink = n_sink;

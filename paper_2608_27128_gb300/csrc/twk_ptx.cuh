@@ -309,28 +309,53 @@ __device__ __forceinline__ void umma_commit_own(uint64_t* bar)
         : "memory");
 }
 
-// The forms of one CTA: D[tmem] (+)= A B^T, A and B in shared memory, or A in tensor memory (a
-// 32-bit column holds two neighbours along K); one instruction of shape M x N x 16, bf16 -> f32.
-__device__ __forceinline__ void umma_bf16(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc,
-                                          uint32_t idesc, uint32_t accumulate)
+// The forms of one CTA, for operands as umma_desc_sw128 and umma_desc_sw128_rows describe them (low words
+// of the descriptors, the high word being the same): D[tmem] (+)= A B, bf16 -> f32, in steps of 16 along
+// K.  The steps' descriptors are made inside: as C++ values the compiler keeps them all in registers.
+constexpr uint32_t kDescHigh = 0x40004040u;
+
+// A and B K-major in shared memory, K = 64 kChunks: rows of 64 values, chunks of 64 of them 16 KB apart.
+template <int kChunks>
+__device__ __forceinline__ void umma_rows(uint32_t d_tmem, uint32_t a_low, uint32_t b_low,
+                                          uint32_t idesc)
 {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
-        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
-        : "memory");
+#define TWK_STEP(offset, sum)                                                              \
+    "add.u32 a, %1, " #offset ";\n\tadd.u32 b, %2, " #offset ";\n\t"                       \
+    "mov.b64 x, {a, h};\n\tmov.b64 y, {b, h};\n\t"                                        \
+    "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, " #sum ";\n\t"
+#define TWK_BEGIN                                                                          \
+    "{\n\t.reg .pred p, q;\n\t.reg .b32 a, b, h;\n\t.reg .b64 x, y;\n\t"                   \
+    "mov.b32 h, 0x40004040;\n\tsetp.ne.b32 p, h, 0;\n\t"
+    if constexpr (kChunks == 2)
+        asm volatile(TWK_BEGIN "setp.eq.b32 q, h, 0;\n\t" TWK_STEP(0, q) TWK_STEP(2, p)
+                         TWK_STEP(4, p) TWK_STEP(6, p) TWK_STEP(1024, p) TWK_STEP(1026, p)
+                             TWK_STEP(1028, p) TWK_STEP(1030, p) "}" ::"r"(d_tmem),
+                     "r"(a_low), "r"(b_low), "r"(idesc)
+                     : "memory");
+    else
+        asm volatile(TWK_BEGIN "setp.eq.b32 q, h, 0;\n\t" TWK_STEP(0, q) TWK_STEP(2, p)
+                         TWK_STEP(4, p) TWK_STEP(6, p) "}" ::"r"(d_tmem),
+                     "r"(a_low), "r"(b_low), "r"(idesc)
+                     : "memory");
+#undef TWK_STEP
 }
 
-__device__ __forceinline__ void umma_bf16_tmem(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc,
-                                               uint32_t idesc, uint32_t accumulate)
+// A [128][128] in tensor memory (a 32-bit column holds two neighbours along K), B's rows along K; the
+// first step adds to D where `add`.
+__device__ __forceinline__ void umma_tmem_128(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_low,
+                                              uint32_t idesc, uint32_t add)
 {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
-        "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
-        : "memory");
+#define TWK_STEP(i, column, offset, sum)                                                   \
+    "add.u32 a, %1, " #column ";\n\tadd.u32 b, %2, " #offset ";\n\tmov.b64 y, {b, h};\n\t" \
+    "tcgen05.mma.cta_group::1.kind::f16 [%0], [a], y, %3, " #sum ";\n\t"
+    asm volatile(TWK_BEGIN "setp.ne.b32 q, %4, 0;\n\t" TWK_STEP(0, 0, 0, q) TWK_STEP(1, 8, 128, p)
+                     TWK_STEP(2, 16, 256, p) TWK_STEP(3, 24, 384, p) TWK_STEP(4, 32, 512, p)
+                         TWK_STEP(5, 40, 640, p) TWK_STEP(6, 48, 768, p)
+                             TWK_STEP(7, 56, 896, p) "}" ::"r"(d_tmem),
+                 "r"(a_tmem), "r"(b_low), "r"(idesc), "r"(add)
+                 : "memory");
+#undef TWK_STEP
+#undef TWK_BEGIN
 }
 
 // Arrive on the barrier once every tcgen05 operation this thread issued so far has completed.
@@ -414,13 +439,7 @@ __device__ __forceinline__ uint64_t umma_desc_sw128(uint32_t saddr)
 // the next 8 rows are.
 __device__ __forceinline__ uint64_t umma_desc_sw128_rows(uint32_t saddr, uint32_t next64)
 {
-    uint64_t d = 0;
-    d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
-    d |= static_cast<uint64_t>(next64 >> 4) << 16;
-    d |= static_cast<uint64_t>(1024u >> 4) << 32;
-    d |= static_cast<uint64_t>(1u) << 46;
-    d |= static_cast<uint64_t>(2u) << 61;
-    return d;
+    return (umma_desc_sw128(saddr) & ~0xffff0000ull) | static_cast<uint64_t>(next64 >> 4) << 16;
 }
 constexpr uint32_t kIdescBRows = 1u << 16;   // of the instruction: B is such an operand
 
