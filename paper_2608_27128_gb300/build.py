@@ -22,7 +22,8 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libtwinkv.so")
 SOURCES = ["twk_api.cu", "twk_audit.cu", "twk_prep.cu", "twk_refine.cu", "twk_repair.cu",
            "twk_policy.cu", "twk_rope.cu", "twk_cache.cu", "twk_attend.cu", "twk_cache_api.cu",
-           "twk_prompt.cu", "twk_weights.cu", "twk_weight_policy.cu", "twk_prompt_api.cu"]
+           "twk_prompt.cu", "twk_weights.cu", "twk_cache_weights.cu",
+           "twk_weight_policy.cu", "twk_prompt_api.cu"]
 HEADERS = ["twk_internal.h", "twk_ptx.cuh", "twk_df.cuh", "twk_bound.cuh", "twk_cache.cuh",
            "twk_cache_internal.h", "twk_prompt_internal.h", "twk_prompt.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]

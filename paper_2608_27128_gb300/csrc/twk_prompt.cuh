@@ -3,7 +3,9 @@
 #pragma once
 #include <cstdint>
 
+#include "twk_internal.h"
 #include "twk_prompt_internal.h"
+#include "twk_ptx.cuh"
 
 namespace twk {
 
@@ -64,6 +66,61 @@ __device__ __forceinline__ KeyTiles key_tiles(const PromptArgs& a, int first, in
     t.count = t.sinks + end - t.from;
     return t;
 }
+
+// ---- small things
+
+__device__ __forceinline__ float exp2_approx(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// the lowest n bits (none for n <= 0, all for n >= 32)
+__device__ __forceinline__ uint32_t bits_below(int n)
+{
+    return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
+}
+__device__ __forceinline__ float as_f(uint32_t x) { return __uint_as_float(x); }
+
+// Orders every later use of x after the preceding tcgen05.wait::ld.
+__device__ __forceinline__ void reg_fence(uint32_t (&x)[32])
+{
+#pragma unroll
+    for (int i = 0; i < 32; i += 8)
+        asm volatile(""
+                     : "+r"(x[i]), "+r"(x[i + 1]), "+r"(x[i + 2]), "+r"(x[i + 3]), "+r"(x[i + 4]),
+                       "+r"(x[i + 5]), "+r"(x[i + 6]), "+r"(x[i + 7]));
+}
+
+// Every lane waits (each needs the acquire), the warp agrees on the verdict.
+__device__ __forceinline__ bool all_wait(uint64_t* bar, uint32_t parity, const WaitCtl& w, int where)
+{
+    if (__all_sync(0xffffffffu, mbar_try_wait(smem_u32(bar), parity))) return true;
+    const bool ok = mbar_wait(bar, parity, w, where);
+    return __all_sync(0xffffffffu, ok);
+}
+
+__device__ __forceinline__ void drain_wait(uint64_t* bar, uint32_t parity, uint64_t limit_ns)
+{
+    const uint64_t limit = limit_ns > kDrainFloorNs ? limit_ns : kDrainFloorNs;
+    const uint32_t a = smem_u32(bar);
+    const uint64_t t0 = globaltimer_ns();
+    while (!mbar_try_wait_sleep(a, parity, 1000000u))
+        if (globaltimer_ns() - t0 > limit) return;
+}
+
+// A ring's slot and the parity of its phase.
+template <int kN>
+struct Ring {
+    uint32_t slot = 0, phase = 0;
+    __device__ __forceinline__ void next()
+    {
+        if (++slot == kN) {
+            slot = 0;
+            phase ^= 1u;
+        }
+    }
+};
 
 // ---- work among blocks
 //

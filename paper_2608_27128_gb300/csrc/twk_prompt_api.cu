@@ -74,8 +74,9 @@ PromptArgs args_of(const void* q, const void* k, const twinkv_prompt& s,
     a.G = s.Hq / s.H;
     a.tile_tokens = 128 / a.G;
     a.scale = scale;
-    a.window = window;
-    a.n_sink = n_sink;
+    // beyond every position they are alike, and sums with positions stay in 32 bits
+    a.window = window < 2 * kMaxPacked ? window : 2 * kMaxPacked;
+    a.n_sink = n_sink < 2 * kMaxPacked ? n_sink : 2 * kMaxPacked;
     a.out_status = out_status;
     a.ws = ws;
     return a;
@@ -92,7 +93,7 @@ size_t twinkv_prompt_attend_workspace(twinkv_prompt s)
 
 size_t twinkv_prompt_weights_workspace(twinkv_prompt s)
 {
-    return sizes_ok(s) == TWINKV_OK ? 256 : 0;
+    return sizes_ok(s) == TWINKV_OK ? up256(prompt_weights_workspace(s)) : 0;
 }
 
 size_t twinkv_cache_weights_workspace(twinkv_queries s, int32_t d)
@@ -137,13 +138,14 @@ twinkv_status twinkv_prompt_weights(const void* q, const void* k, const float* l
     r = check_ws(workspace, workspace_bytes, twinkv_prompt_weights_workspace(s));
     if (r != TWINKV_OK) return r;
     int sms = 0;
-    if ((r = device_facts(&sms)) != TWINKV_OK) return r;
+    WaitFacts w;
+    if ((r = device_facts(&sms)) != TWINKV_OK || (r = wait_facts(&w)) != TWINKV_OK) return r;
     PromptArgs a = args_of(q, k, s, seqs, scale, window, n_sink, out_status, workspace);
     a.lse = lse;
     a.last = last;
     a.score = score;
     a.out_score = out_score;
-    return cuda_result(launch_prompt_weights(a, sms, static_cast<cudaStream_t>(stream)));
+    return cuda_result(launch_prompt_weights(a, sms, w, static_cast<cudaStream_t>(stream)));
 }
 
 twinkv_status twinkv_cache_weights(const void* q, const float* lse, twinkv_queries s, float scale,

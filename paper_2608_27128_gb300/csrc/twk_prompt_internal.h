@@ -45,7 +45,8 @@ bool encode_rows(CUtensorMap* map, const void* base, int d, int heads, int rows,
 
 size_t prompt_attend_workspace(const twinkv_prompt& s);
 cudaError_t launch_prompt_attend(const PromptArgs& a, int sms, const WaitFacts& w, cudaStream_t st);
-cudaError_t launch_prompt_weights(const PromptArgs& a, int sms, cudaStream_t st);
+size_t prompt_weights_workspace(const twinkv_prompt& s);
+cudaError_t launch_prompt_weights(const PromptArgs& a, int sms, const WaitFacts& w, cudaStream_t st);
 
 struct CacheWeightsArgs {
     AttendArgs a;                  // as for the attention; its outputs are not used, but the statuses

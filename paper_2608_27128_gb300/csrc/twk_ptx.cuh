@@ -355,6 +355,29 @@ __device__ __forceinline__ void umma_tmem_128(uint32_t d_tmem, uint32_t a_tmem, 
                  "r"(a_tmem), "r"(b_low), "r"(idesc), "r"(add)
                  : "memory");
 #undef TWK_STEP
+}
+
+// A [128][64 kChunks] in tensor memory, B K-major in shared memory as in umma_rows.
+template <int kChunks>
+__device__ __forceinline__ void umma_tmem_rows(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_low,
+                                               uint32_t idesc)
+{
+#define TWK_STEP(column, offset, sum)                                                      \
+    "add.u32 a, %1, " #column ";\n\tadd.u32 b, %2, " #offset ";\n\tmov.b64 y, {b, h};\n\t" \
+    "tcgen05.mma.cta_group::1.kind::f16 [%0], [a], y, %3, " #sum ";\n\t"
+    if constexpr (kChunks == 2)
+        asm volatile(TWK_BEGIN "setp.eq.b32 q, h, 0;\n\t" TWK_STEP(0, 0, q) TWK_STEP(8, 2, p)
+                         TWK_STEP(16, 4, p) TWK_STEP(24, 6, p) TWK_STEP(32, 1024, p)
+                             TWK_STEP(40, 1026, p) TWK_STEP(48, 1028, p)
+                                 TWK_STEP(56, 1030, p) "}" ::"r"(d_tmem),
+                     "r"(a_tmem), "r"(b_low), "r"(idesc)
+                     : "memory");
+    else
+        asm volatile(TWK_BEGIN "setp.eq.b32 q, h, 0;\n\t" TWK_STEP(0, 0, q) TWK_STEP(8, 2, p)
+                         TWK_STEP(16, 4, p) TWK_STEP(24, 6, p) "}" ::"r"(d_tmem),
+                     "r"(a_tmem), "r"(b_low), "r"(idesc)
+                     : "memory");
+#undef TWK_STEP
 #undef TWK_BEGIN
 }
 

@@ -1,139 +1,615 @@
-// twk_weights.cu -- what attention pays to each key: over prompts, and over pages of 4-bit codes.
+// twk_weights.cu -- what attention over prompts pays to each key.
 //
 //     A(j) = [score(j) +] sum over tokens i that see j, and query heads of the KV head:
 //            exp(scale q_i . k_j - lse_i)
 //
-// One warp per key (or slot) and KV head: right for every case, and the measure for what follows.
-#include "twk_cache.cuh"
+// The scores are computed again, a tile of 128 keys x 128 (token, head) columns at a time, with the keys
+// as the rows of the product: a key's sum is then a thread's, over the columns of its row of the
+// accumulator, in one order whatever the grid.  With c = scale log2(e), a weight is
+// 2^(c q . k - log2(e) lse): one multiply-add, one exponential and one addition each.
+//
+// Bound by the tensor cores (2 d operations a pair of key and column) and the exponentials, about alike at
+// d = 128; with few tokens (an observation window) by the keys' bytes.  Design (persistent, one block of
+// 384 threads per SM):
+//   - An item is 256 keys of one KV head, and runs over the columns that see any of them.  The keys stay:
+//     they go from TMA's tile through registers to tensor memory, as the products' operand A, so that
+//     only the queries are read from shared memory (A from there as well would ask for all of its
+//     bandwidth).  Three accumulators of 128 columns take turns.
+//   - Warps 0 to 3 and 4 to 7: a thread per key of the item's halves.  Warp 8: TMA.  Warp 9: products.
+//     Warp 10: items.  Warp 11: the columns' lse, +inf where a column does not count, which makes its
+//     weight 0.  A column's place in shared memory is zero where the tile has none (G does not
+//     divide 128).
+//   - Work is divided evenly whatever the lengths (twk_prompt.cuh); merge_kernel adds the parts of an item
+//     that blocks share, in order.
+#include <atomic>
+
 #include "twk_prompt.cuh"
-#include "twk_ptx.cuh"
 
 namespace twk {
 namespace {
 
-template <int D>
-__global__ void __launch_bounds__(128) prompt_weights_kernel(const __grid_constant__ PromptArgs a)
+constexpr int kThreads = 384;
+constexpr int kLaunchRegs = 168, kHelperRegs = 88, kSumRegs = 208;
+static_assert(4 * kHelperRegs + 8 * kSumRegs <= 12 * kLaunchRegs,
+              "the split draws on the registers of the launch");
+constexpr int kPairKeys = 2 * kTileKeys;
+constexpr int kAccs = 3, kItemSlots = 4, kLogSlots = 4;
+
+// The tokens that see some key of [j, last]: the first, and the end; of those that count.
+__device__ __forceinline__ int2 tokens_of(const PromptArgs& a, const Sequence& s, int j, int last)
 {
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    if (blockIdx.x == 0 && blockIdx.y == 0 && a.out_status)
-        for (int b = threadIdx.x; b < a.s.B; b += 128)
-            a.out_status[b] = sequence_of(a, b).ok ? TWINKV_OK : TWINKV_ERR_INVALID_ARG;
-    const int row = blockIdx.x * 4 + warp, h = blockIdx.y;
-    if (row >= a.s.keys) return;
-    Sequence s{};
-    int b = 0;
-    for (; b < a.s.B; ++b) {
-        s = sequence_of(a, b);
-        if (s.ok && row >= s.j0 && row - s.j0 < s.m) break;
-    }
-    if (b == a.s.B) return;
-    constexpr int V = D / 32;
-    float k[V], sum = 0.0f;
-    const uint16_t* src = a.k + row * a.s.k_token + h * a.s.k_head + V * lane;
-#pragma unroll
-    for (int v = 0; v < V; ++v) k[v] = bf16_lo(src[v]);
-    const int j = row - s.j0;
-    int first = max(0, j - (s.m - s.n));
+    int first = max(0, j - (s.m - s.n)), end = s.n;
     if (a.last > 0) first = max(first, s.n - a.last);
-    for (int i = first; i < s.n; ++i) {
-        if (a.window > 0 && s.m - s.n + i - j >= a.window && j >= a.n_sink) continue;
-        for (int g = 0; g < a.G; ++g) {
-            const int head = h * a.G + g;
-            const uint16_t* q =
-                a.q + (s.t0 + i) * a.s.q_token + head * a.s.q_head + V * lane;
-            float x = 0.0f;
-#pragma unroll
-            for (int v = 0; v < V; ++v) x = fmaf(k[v], bf16_lo(q[v]), x);
-#pragma unroll
-            for (int e = 16; e > 0; e /= 2) x += __shfl_xor_sync(0xffffffffu, x, e);
-            sum += expf(x * a.scale - a.lse[static_cast<int64_t>(s.t0 + i) * a.s.Hq + head]);
-        }
-    }
-    const int64_t at = static_cast<int64_t>(h) * a.s.keys + row;
-    if (lane == 0) a.out_score[at] = (a.score ? a.score[at] : 0.0f) + sum;
+    if (a.window > 0 && j >= a.n_sink) end = min(end, last + a.window - (s.m - s.n));
+    return make_int2(first, max(first, end));
 }
 
-template <int D>
-__global__ void __launch_bounds__(64)
-    cache_weights_kernel(const __grid_constant__ CacheWeightsArgs p, const int* seen)
-{
-    using P = PageLayout<D>;
-    const AttendArgs& a = p.a;
-    wait_for_previous();
-    const int unit = blockIdx.y, page = blockIdx.x, slot = page * kPage + threadIdx.x;
-    const int len = a.lens[unit];
-    const bool bad = len < 0 || len > static_cast<int64_t>(a.from.max_pages) * kPage;
-    const bool large = !bad && len > p.N;
-    const int* table = a.from.table + static_cast<int64_t>(unit) * a.from.max_pages;
-    if (page == 0 && a.out_status) {
-        bool wrong = false;
-        if (!bad)
-            for (int j = threadIdx.x; j * kPage < len; j += 64)
-                wrong |= static_cast<unsigned>(table[j]) >= static_cast<unsigned>(a.from.n_pages);
-        wrong = __syncthreads_or(wrong);
-        if (threadIdx.x == 0)
-            a.out_status[unit] = large ? TWINKV_ERR_TOO_LARGE
-                                       : bad || wrong ? TWINKV_ERR_INVALID_ARG : TWINKV_OK;
+// Items: pairs of key tiles; as long as there are tiles of columns that see them.
+struct KeyPairs {
+    __device__ static __forceinline__ int items(const PromptArgs&, const Sequence& s)
+    {
+        return (s.m + kPairKeys - 1) / kPairKeys;
     }
-    if (bad || large || slot >= len) return;
-    const int id = table[page];
-    const int64_t at = static_cast<int64_t>(unit) * p.N + slot;
-    float sum = p.score[at];
-    if (static_cast<unsigned>(id) < static_cast<unsigned>(a.from.n_pages)) {
-        const uint8_t* base = a.from.base + static_cast<int64_t>(id) * P::kBytes;
-        const int b = unit / a.H, h = unit % a.H;
-        const int* see = seen ? seen + static_cast<int64_t>(unit) * (1 + a.n) : nullptr;
-        for (int i = 0; i < a.n; ++i) {
-            if (slot > len - a.n + i || (see && slot < see[1 + i] && slot >= see[0])) continue;
-            for (int g = 0; g < a.G; ++g) {
-                const int head = h * a.G + g;
-                const uint16_t* q = a.q + b * a.q_batch + i * a.q_token + head * a.q_head;
-                float x = 0.0f;
-                for (int G = 0; G < P::kGroups; ++G) {
-                    const uint32_t m = *reinterpret_cast<const uint32_t*>(
-                        base + P::kKeyGroups + (threadIdx.x * P::kGroups + G) * 4);
-                    const float zero = bf16_hi(m) + 128.0f;
-                    float y = 0.0f;
-                    for (int e = 0; e < 64; ++e) {
-                        const int at_e = 64 * G + e;
-                        const uint32_t w = *reinterpret_cast<const uint32_t*>(
-                            base + P::key_word(threadIdx.x, at_e / 8));
-                        const int nibble = 4 * (e % 2) + e % 8 / 2;
-                        y = fmaf(bf16_lo(q[at_e]), (w >> (4 * nibble) & 15u) + zero, y);
+    __device__ static __forceinline__ int2 tokens(const PromptArgs& a, const Sequence& s, int i)
+    {
+        return tokens_of(a, s, i * kPairKeys, min(i * kPairKeys + kPairKeys, s.m) - 1);
+    }
+    // 1 where no token sees them: their sums are written all the same
+    __device__ static __forceinline__ int length(const PromptArgs& a, const Sequence& s, int i)
+    {
+        const int2 t = tokens(a, s, i);
+        return max(1, (t.y - t.x + a.tile_tokens - 1) / a.tile_tokens);
+    }
+};
+
+template <int D>
+struct Cfg {
+    static constexpr int KC = D / 64;
+    static constexpr int CHUNK = 128 * 128;
+    static constexpr int TILE = KC * CHUNK;
+    static constexpr int STAGES = D == 128 ? 4 : 8;       // tiles of queries
+    static constexpr int OFF_Q = 2 * TILE;                // behind two tiles of keys
+    static constexpr int OFF_LOG = OFF_Q + STAGES * TILE;
+    static constexpr int OFF_MISC = OFF_LOG + kLogSlots * 512;
+    static constexpr int BYTES = OFF_MISC + 1024 + 1024;  // + 1024 for alignment
+    static constexpr int T_K = 0, T_ACC = 128;            // columns of tensor memory
+    static_assert(BYTES <= 232448, "shared memory per block");
+    static_assert(T_K + D <= T_ACC && T_ACC + kAccs * 128 <= 512);
+    static_assert(STAGES * TILE >= kSumsBytes, "the chunks' sums lie there at first");
+};
+
+struct Item {
+    int t0, i0;              // first row of q of the sequence; first token of the list
+    int n, back;             // tokens; m - n, what a token's position is beyond its number
+    int j0, j, m;            // first row of k, first key of the item, keys
+    int head;                // KV head, -1: no more items
+    int u0, u1;              // units of the list that this part takes
+    int b[2], e[2];          // those that each half has a part in
+    int slot;                // of a part, or -1: the whole item
+    int pad;
+};
+static_assert(sizeof(Item) == 64);
+
+struct Misc {
+    uint64_t k_full[2], k_empty[2], kt_full[2], drain;
+    // acc_full: by half and its own count, since a half that skips another's phases would lose track
+    uint64_t acc_full[2][kAccs], acc_empty[kAccs], log_full[kLogSlots], log_empty[kLogSlots];
+    uint64_t q_full[8], q_empty[8], item_full[kItemSlots], item_empty[kItemSlots];
+    Item items[kItemSlots];
+    uint32_t tmem;
+    int abort_flag;
+};
+static_assert(sizeof(Misc) <= 1024);
+
+struct WeightsKernelArgs {
+    PromptArgs a;
+    float c;                 // scale * log2(e)
+    float* part;             // [2 per block][256], null: no item is shared
+    int4* join;              // [per block]: parts of the item that begins in the block and ends in
+                             // another one (0: none), its first row of k, keys and KV head
+    int* err;
+    unsigned long long timeout_ns;
+};
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+    prompt_weights_kernel(const __grid_constant__ CUtensorMap tmQ,
+                          const __grid_constant__ CUtensorMap tmK,
+                          const __grid_constant__ WeightsKernelArgs p)
+{
+    using C = Cfg<D>;
+    const PromptArgs& a = p.a;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    Misc& M = *reinterpret_cast<Misc*>(smem + C::OFF_MISC);
+    const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0);
+    const int lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&M.k_full[i], 1);
+            mbar_init(&M.k_empty[i], 4);
+            mbar_init(&M.kt_full[i], 4);
+        }
+        mbar_init(&M.drain, 1);
+        for (int i = 0; i < kAccs; ++i) {
+            mbar_init(&M.acc_full[0][i], 1);
+            mbar_init(&M.acc_full[1][i], 1);
+            mbar_init(&M.acc_empty[i], 4);
+        }
+        for (int i = 0; i < kLogSlots; ++i) {
+            mbar_init(&M.log_full[i], 1);
+            mbar_init(&M.log_empty[i], 8);
+        }
+        for (int i = 0; i < C::STAGES; ++i) {
+            mbar_init(&M.q_full[i], 1);
+            mbar_init(&M.q_empty[i], 1);
+        }
+        for (int i = 0; i < kItemSlots; ++i) {
+            mbar_init(&M.item_full[i], 1);
+            mbar_init(&M.item_empty[i], 11);      // TMA, products, lse, eight that sum
+        }
+        M.abort_flag = 0;
+        fence_mbarrier_init();
+    }
+    if (warp == 8 && lane == 0) {
+        prefetch_tensormap(&tmQ);
+        prefetch_tensormap(&tmK);
+    }
+    if (warp == 9) tmem_alloc<1>(&M.tmem, 512);
+    wait_for_previous();
+    // the chunks' sums lie where queries come later
+    long long* sums = reinterpret_cast<long long*>(smem + C::OFF_Q);
+    if (a.s.B > 32) sum_chunks<KeyPairs>(a, sums);
+    const int tpt = a.tile_tokens, columns = tpt * a.G;
+    // columns that no copy writes
+    for (int i = threadIdx.x; i < C::STAGES * C::KC * (128 - columns) * 8; i += kThreads) {
+        const int chunk = i / ((128 - columns) * 8), r = i - chunk * ((128 - columns) * 8);
+        *reinterpret_cast<uint4*>(smem + C::OFF_Q + chunk * C::CHUNK + columns * 128 + r * 16) =
+            make_uint4(0, 0, 0, 0);
+    }
+    fence_async_shared();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = M.tmem;
+
+    WaitCtl wc;
+    wc.limit_ns = p.timeout_ns;
+    wc.abort_flag = &M.abort_flag;
+    wc.err = p.err;
+    wc.where = 0;
+
+    if (warp >= 8) {
+        setmaxnreg_dec<kHelperRegs>();
+        if (warp == 8) {
+            // ------------------------------------------------------------ TMA
+            if (lane == 0) {
+                Ring<kItemSlots> ri;
+                Ring<C::STAGES> rs;
+                uint32_t k_uses[2] = {}, stages = 0;
+                const uint32_t q_bytes = static_cast<uint32_t>(columns) * 128u * C::KC;
+                bool ok = true;
+                while (ok) {
+                    if (!(ok = mbar_wait(&M.item_full[ri.slot], ri.phase, wc, 41))) break;
+                    const Item it = M.items[ri.slot];
+                    mbar_arrive(&M.item_empty[ri.slot]);
+                    ri.next();
+                    if (it.head < 0) break;
+                    int u = it.u1, end = it.u0;
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const int b = max(it.b[x], it.u0), e = min(it.e[x], it.u1);
+                        if (!ok || b >= e) continue;
+                        u = min(u, b);
+                        end = max(end, e);
+                        ok = mbar_wait(&M.k_empty[x], (k_uses[x] & 1u) ^ 1u, wc, 42);
+                        if (!ok) continue;
+                        ++k_uses[x];
+                        mbar_arrive_expect_tx(&M.k_full[x], C::TILE);
+#pragma unroll
+                        for (int kc = 0; kc < C::KC; ++kc)
+                            tma_load_3d(smem + x * C::TILE + kc * C::CHUNK, &tmK, &M.k_full[x],
+                                        kc * 64, it.head, it.j0 + it.j + x * kTileKeys);
                     }
-                    x = fmaf(bf16_lo(m), y, x);
+                    for (; ok && u < end; ++u) {
+                        if (!(ok = mbar_wait(&M.q_empty[rs.slot], rs.phase ^ 1u, wc, 43))) break;
+                        mbar_arrive_expect_tx(&M.q_full[rs.slot], q_bytes);
+                        uint8_t* dst = smem + C::OFF_Q + rs.slot * C::TILE;
+#pragma unroll
+                        for (int kc = 0; kc < C::KC; ++kc)
+                            tma_load_3d(dst + kc * C::CHUNK, &tmQ, &M.q_full[rs.slot], kc * 64,
+                                        it.head * a.G, it.t0 + it.i0 + u * tpt);
+                        rs.next();
+                        ++stages;
+                    }
                 }
-                sum += expf(x * a.scale -
-                            p.lse[(static_cast<int64_t>(b) * a.n + i) * (a.H * a.G) + head]);
+                // after a give-up: no copy of this thread is in flight when the block ends
+                if (!ok) {
+                    for (int x = 0; x < 2; ++x)
+                        if (k_uses[x]) drain_wait(&M.k_full[x], (k_uses[x] - 1) & 1u, p.timeout_ns);
+                    const uint32_t used = min(stages, static_cast<uint32_t>(C::STAGES));
+                    for (uint32_t k = 1; k <= used; ++k) {
+                        const uint32_t i = stages - k;
+                        drain_wait(&M.q_full[i % C::STAGES], i / C::STAGES & 1u, p.timeout_ns);
+                    }
+                }
+            }
+        } else if (warp == 9) {
+            // ------------------------------------------------------------ products
+            // every lane follows, an elected one issues; what it issues comes from uniform registers
+            constexpr uint32_t idesc = umma_idesc_bf16_f32(kTileKeys, 128);
+            Ring<kItemSlots> ri;
+            Ring<C::STAGES> rs;
+            Ring<kAccs> ra, rx[2];
+            uint32_t k_uses[2] = {};
+            const uint32_t q_low = static_cast<uint32_t>(umma_desc_sw128(smem_u32(smem + C::OFF_Q)));
+            bool ok = true;
+            while (ok) {
+                if (!(ok = all_wait(&M.item_full[ri.slot], ri.phase, wc, 44))) break;
+                const Item& it = M.items[ri.slot];
+                const int head = __shfl_sync(0xffffffffu, it.head, 0);
+                const int u0 = __shfl_sync(0xffffffffu, it.u0, 0);
+                const int u1 = __shfl_sync(0xffffffffu, it.u1, 0);
+                const int b0 = max(u0, __shfl_sync(0xffffffffu, it.b[0], 0));
+                const int b1 = max(u0, __shfl_sync(0xffffffffu, it.b[1], 0));
+                const int e0 = min(u1, __shfl_sync(0xffffffffu, it.e[0], 0));
+                const int e1 = min(u1, __shfl_sync(0xffffffffu, it.e[1], 0));
+                if (lane == 0) mbar_arrive(&M.item_empty[ri.slot]);
+                ri.next();
+                if (head < 0) break;
+                if (b0 < e0) ok = all_wait(&M.kt_full[0], k_uses[0]++ & 1u, wc, 45);
+                bool second = false;            // the second half's keys are waited for at their first use
+                const int begin = b0 < e0 ? (b1 < e1 ? min(b0, b1) : b0) : b1;
+                const int end = b0 < e0 ? (b1 < e1 ? max(e0, e1) : e0) : e1;
+                for (int u = begin; ok && u < end; ++u) {
+                    if (!(ok = all_wait(&M.q_full[rs.slot], rs.phase, wc, 46))) break;
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const int b = x ? b1 : b0, e = x ? e1 : e0;
+                        if (!ok || u < b || u >= e) continue;
+                        if (x == 1 && !second) {
+                            if (!(ok = all_wait(&M.kt_full[1], k_uses[1]++ & 1u, wc, 45))) continue;
+                            second = true;
+                        }
+                        if (!(ok = all_wait(&M.acc_empty[ra.slot], ra.phase ^ 1u, wc, 47))) continue;
+                        tc_fence_after();
+                        if (elect_one()) {
+                            umma_tmem_rows<C::KC>(tmem + C::T_ACC + ra.slot * 128,
+                                                  tmem + C::T_K + x * (D / 2),
+                                                  q_low + rs.slot * (C::TILE >> 4), idesc);
+                            umma_commit(&M.acc_full[x][rx[x].slot]);
+                        }
+                        __syncwarp();
+                        ra.next();
+                        rx[x].next();
+                    }
+                    if (!ok) break;
+                    if (elect_one()) umma_commit(&M.q_empty[rs.slot]);
+                    __syncwarp();
+                    rs.next();
+                }
+            }
+            // every product has ended before tensor memory is freed
+            __syncwarp();
+            if (elect_one()) {
+                umma_commit(&M.drain);
+                drain_wait(&M.drain, 0, p.timeout_ns);
+            }
+        } else if (warp == 10) {
+            // ------------------------------------------------------------ items
+            Walk<KeyPairs> at;
+            at.start(a, sums);
+            fence_async_shared();       // the sums have been read
+            __syncwarp();
+            if (lane == 0) {
+                Ring<kItemSlots> ri;
+                bool ok = true;
+                int4 join = make_int4(0, 0, 0, 0);
+                for (; ok && at.more; at.next(a)) {
+                    Item it{};
+                    const int2 t = KeyPairs::tokens(a, at.s, at.item);
+                    it.t0 = at.s.t0;
+                    it.i0 = t.x;
+                    it.n = at.s.n;
+                    it.back = at.s.m - at.s.n;
+                    it.j0 = at.s.j0;
+                    it.j = at.item * kPairKeys;
+                    it.m = at.s.m;
+                    it.head = at.head;
+                    it.u0 = at.off;
+                    it.u1 = at.off + at.take;
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const int j = it.j + x * kTileKeys;
+                        if (j >= it.m) continue;
+                        const int2 w = tokens_of(a, at.s, j, min(j + kTileKeys, it.m) - 1);
+                        if (w.x >= w.y) continue;
+                        it.b[x] = (w.x - t.x) / tpt;
+                        it.e[x] = (w.y - t.x + tpt - 1) / tpt;
+                    }
+                    it.slot = -1;
+                    if (at.take < at.length) {
+                        // heads and middles in slot 2 c, the item that begins in the block in 2 c + 1
+                        it.slot = 2 * static_cast<int>(blockIdx.x) + (at.off == 0 ? 1 : 0);
+                        if (at.off == 0)
+                            join = make_int4(at.parts(), it.j0 + it.j, min(kPairKeys, it.m - it.j),
+                                             it.head);
+                    }
+                    ok = mbar_wait(&M.item_empty[ri.slot], ri.phase ^ 1u, wc, 48);
+                    if (!ok) break;
+                    M.items[ri.slot] = it;
+                    mbar_arrive(&M.item_full[ri.slot]);
+                    ri.next();
+                }
+                if (p.join) p.join[blockIdx.x] = join;
+                if (ok) ok = mbar_wait(&M.item_empty[ri.slot], ri.phase ^ 1u, wc, 48);
+                if (ok) {
+                    M.items[ri.slot].head = -1;
+                    mbar_arrive(&M.item_full[ri.slot]);
+                }
+            }
+        } else {
+            // ------------------------------------------------------------ lse
+            if (blockIdx.x == 0 && a.out_status)
+                for (int b = lane; b < a.s.B; b += 32)
+                    a.out_status[b] = sequence_of(a, b).ok ? TWINKV_OK : TWINKV_ERR_INVALID_ARG;
+            Ring<kItemSlots> ri;
+            Ring<kLogSlots> rl;
+            bool ok = true;
+            int token[4], sub[4];                    // of the lane's columns
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                token[k] = (4 * lane + k) / a.G;
+                sub[k] = 4 * lane + k - token[k] * a.G;
+                if (token[k] >= tpt) token[k] = INT_MAX / 2;
+            }
+            while (ok) {
+                if (!(ok = all_wait(&M.item_full[ri.slot], ri.phase, wc, 49))) break;
+                const Item it = M.items[ri.slot];
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&M.item_empty[ri.slot]);
+                ri.next();
+                if (it.head < 0) break;
+                int u = it.u1, end = it.u0;
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const int b = max(it.b[x], it.u0), e = min(it.e[x], it.u1);
+                    if (b < e) {
+                        u = min(u, b);
+                        end = max(end, e);
+                    }
+                }
+                auto load = [&](int unit, float (&y)[4]) {
+                    const int i = it.i0 + unit * tpt;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        y[k] = token[k] < it.n - i
+                                   ? a.lse[static_cast<int64_t>(it.t0 + i + token[k]) * a.s.Hq +
+                                           it.head * a.G + sub[k]]
+                                   : INFINITY;
+                };
+                float y[4], next[4];
+                if (u < end) load(u, y);
+                for (; u < end; ++u) {
+                    if (u + 1 < end) load(u + 1, next);
+                    if (!(ok = all_wait(&M.log_empty[rl.slot], rl.phase ^ 1u, wc, 50))) break;
+                    constexpr float kLog2e = 1.4426950408889634f;
+                    *reinterpret_cast<float4*>(smem + C::OFF_LOG + rl.slot * 512 + lane * 16) =
+                        make_float4(-kLog2e * y[0], -kLog2e * y[1], -kLog2e * y[2], -kLog2e * y[3]);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&M.log_full[rl.slot]);
+                    rl.next();
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) y[k] = next[k];
+                }
             }
         }
+        __syncwarp();
+        tc_fence_before();
+        __syncthreads();
+        tc_fence_after();
+        if (warp == 9) tmem_dealloc<1>(tmem, 512);
+    } else {
+        // ------------------------------------------------------------ sums
+        setmaxnreg_inc<kSumRegs>();
+        const int x = warp >> 2, q = warp & 3;
+        const int row = q * 32 + lane;
+        const uint32_t base = tmem + (static_cast<uint32_t>(q * 32) << 16);
+        Ring<kItemSlots> ri;
+        Ring<kLogSlots> rl;
+        Ring<kAccs> ra, rx;
+        uint32_t k_uses = 0;
+        bool ok = true;
+        while (ok) {
+            if (!(ok = all_wait(&M.item_full[ri.slot], ri.phase, wc, 51))) break;
+            const Item& its = M.items[ri.slot];
+            const int head = its.head, j0 = its.j0 + its.j, slot = its.slot;
+            const int u0 = its.u0, u1 = its.u1;
+            const int b = max(u0, x ? its.b[1] : its.b[0]), e = min(u1, x ? its.e[1] : its.e[0]);
+            const int ob = max(u0, x ? its.b[0] : its.b[1]), oe = min(u1, x ? its.e[0] : its.e[1]);
+            const int held = min(kTileKeys, its.m - its.j - x * kTileKeys);
+            // position of the item's first token less the warp's first key, and tokens from it on
+            const int gap = its.back + its.i0 - its.j - x * kTileKeys - q * 32;
+            const int left = its.n - its.i0;
+            const int key = its.j + x * kTileKeys + row;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&M.item_empty[ri.slot]);
+            ri.next();
+            if (head < 0) break;
+            const bool mine = b < e, other = ob < oe;
+            if (mine) {
+                // the half's keys: from TMA's tile to operand A, a key to a thread.  The products that
+                // read the last ones have ended: their sums are done.
+                if (!(ok = all_wait(&M.k_full[x], k_uses++ & 1u, wc, 52))) break;
+#pragma unroll
+                for (int kc = 0; kc < C::KC; ++kc) {
+                    uint32_t w[32];
+                    const uint8_t* src = smem + x * C::TILE + kc * C::CHUNK + row * 128;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const uint4 y = *reinterpret_cast<const uint4*>(src + ((i ^ (row & 7)) * 16));
+                        w[4 * i] = y.x, w[4 * i + 1] = y.y, w[4 * i + 2] = y.z, w[4 * i + 3] = y.w;
+                    }
+                    tmem_st_32x32b_x32(base + C::T_K + x * (D / 2) + 32 * kc, w);
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(&M.kt_full[x]);
+                    mbar_arrive(&M.k_empty[x]);
+                }
+            }
+            float sum = 0.0f;
+            const int begin = mine ? (other ? min(b, ob) : b) : ob;
+            const int end = mine ? (other ? max(e, oe) : e) : oe;
+            for (int u = begin; u < end; ++u) {
+                // accumulators go to the halves in order
+                const bool on = mine && u >= b && u < e, also = other && u >= ob && u < oe;
+                if (x == 1 && also) ra.next();
+                if (on) {
+                    if (!(ok = all_wait(&M.acc_full[x][rx.slot], rx.phase, wc, 53))) break;
+                    rx.next();
+                    tc_fence_after();
+                    uint32_t s[4][32];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        tmem_ld_32x32b_x32(base + C::T_ACC + ra.slot * 128 + 32 * i, s[i]);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) reg_fence(s[i]);
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&M.acc_empty[ra.slot]);
+                    ra.next();
+                    const int p0 = gap + u * tpt;         // first token's position less the warp's first key
+                    const int rest = left - u * tpt;      // tokens from it on
+                    if (p0 < 31 || rest < tpt ||
+                        (a.window > 0 && p0 + tpt - 1 >= a.window)) {
+                        // columns [lo, hi) see the thread's key: those of the tokens from its own on, as far
+                        // as the window reaches
+                        const int lo = min(max(lane - p0, 0), 128) * a.G;
+                        int hi = min(rest, tpt);
+                        if (a.window > 0 && key >= a.n_sink) hi = min(hi, lane + a.window - p0);
+                        hi = max(hi, 0) * a.G;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t see = bits_below(hi - 32 * i) & ~bits_below(lo - 32 * i);
+#pragma unroll
+                            for (int y = 0; y < 32; ++y)
+                                s[i][y] = see >> y & 1u ? s[i][y] : 0xff800000u;
+                        }
+                    }
+                    if (!(ok = all_wait(&M.log_full[rl.slot], rl.phase, wc, 54))) break;
+                    const float4* log = reinterpret_cast<const float4*>(smem + C::OFF_LOG +
+                                                                        rl.slot * 512);
+                    const float2 c2 = make_float2(p.c, p.c);
+                    float2 l[4] = {};
+#pragma unroll
+                    for (int y = 0; y < 128; y += 4) {
+                        const float4 t = log[y / 4];
+                        const float2 v = __ffma2_rn(
+                            make_float2(as_f(s[y / 32][y % 32]), as_f(s[y / 32][y % 32 + 1])), c2,
+                            make_float2(t.x, t.y));
+                        const float2 w = __ffma2_rn(
+                            make_float2(as_f(s[y / 32][y % 32 + 2]), as_f(s[y / 32][y % 32 + 3])), c2,
+                            make_float2(t.z, t.w));
+                        l[y / 4 % 2] = __fadd2_rn(l[y / 4 % 2],
+                                                  make_float2(exp2_approx(v.x), exp2_approx(v.y)));
+                        l[2 + y / 4 % 2] = __fadd2_rn(
+                            l[2 + y / 4 % 2], make_float2(exp2_approx(w.x), exp2_approx(w.y)));
+                    }
+                    const float2 l2 = __fadd2_rn(__fadd2_rn(l[0], l[1]), __fadd2_rn(l[2], l[3]));
+                    sum += l2.x + l2.y;
+                }
+                // also where it has no part in the unit: its arrivals must not run ahead of the slot
+                if (!on && !(ok = all_wait(&M.log_full[rl.slot], rl.phase, wc, 54))) break;
+                if (x == 0 && also) ra.next();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&M.log_empty[rl.slot]);
+                rl.next();
+            }
+            if (!ok) break;
+            if (slot >= 0) {
+                p.part[slot * kPairKeys + x * kTileKeys + row] = sum;
+            } else if (row < held) {
+                const int64_t at = static_cast<int64_t>(head) * a.s.keys + j0 + x * kTileKeys + row;
+                a.out_score[at] = a.score ? a.score[at] + sum : sum;
+            }
+        }
+        tc_fence_before();
+        __syncthreads();
     }
-    p.out_score[at] = sum;
+}
+
+// Adds the parts of an item that several blocks took, in order: a block per block that one begins in.
+__global__ void __launch_bounds__(kPairKeys)
+    merge_weights_kernel(const __grid_constant__ WeightsKernelArgs p)
+{
+    wait_for_previous();
+    const int4 join = p.join[blockIdx.x];
+    if (static_cast<int>(threadIdx.x) >= join.z || join.x == 0) return;
+    float sum = p.part[(2 * blockIdx.x + 1) * kPairKeys + threadIdx.x];
+#pragma unroll 8
+    for (int k = 1; k < join.x; ++k)
+        sum += p.part[2 * (blockIdx.x + k) * kPairKeys + threadIdx.x];
+    const int64_t at = static_cast<int64_t>(join.w) * p.a.s.keys + join.y + threadIdx.x;
+    p.a.out_score[at] = p.a.score ? p.a.score[at] + sum : sum;
+}
+
+// An item that no more tokens than this look at is never cut.
+int whole_tokens(const PromptArgs& a) { return (2 * kSnap + 1) * a.tile_tokens; }
+
+template <int D>
+cudaError_t launch(const PromptArgs& a, int sms, const WaitFacts& w, cudaStream_t st)
+{
+    using C = Cfg<D>;
+    static std::atomic<bool> allowed[64];     // by device
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev >= 64 || !allowed[dev].load(std::memory_order_relaxed)) {
+        // the warpgroups' shares add up to the launch's registers: with fewer, waits for them have no end
+        cudaFuncAttributes f;
+        if ((e = cudaFuncGetAttributes(&f, prompt_weights_kernel<D>)) != cudaSuccess) return e;
+        if (f.numRegs < kLaunchRegs) return cudaErrorInvalidConfiguration;
+        e = cudaFuncSetAttribute(prompt_weights_kernel<D>,
+                                 cudaFuncAttributeMaxDynamicSharedMemorySize, C::BYTES);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) allowed[dev].store(true, std::memory_order_relaxed);
+    }
+    CUtensorMap q, k;
+    if (!encode_rows(&q, a.q, D, a.s.Hq, a.s.tokens, a.s.q_head, a.s.q_token, a.G, a.tile_tokens) ||
+        !encode_rows(&k, a.k, D, a.s.H, a.s.keys, a.s.k_head, a.s.k_token, 1, kTileKeys))
+        return cudaErrorInvalidValue;
+    WeightsKernelArgs p{};
+    p.a = a;
+    p.c = a.scale * 1.4426950408889634f;
+    const int tokens = a.last > 0 ? std::min(a.last, a.s.tokens) : a.s.tokens;
+    const bool shared = tokens > whole_tokens(a);
+    if (shared) {
+        p.join = static_cast<int4*>(a.ws);
+        p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(a.ws) + 16 * kPromptBlocks);
+    }
+    p.err = w.err;
+    p.timeout_ns = w.timeout_ns;
+    const int grid = std::min(sms, kPromptBlocks);
+    prompt_weights_kernel<D><<<grid, kThreads, C::BYTES, st>>>(q, k, p);
+    if ((e = cudaGetLastError()) != cudaSuccess || !shared) return e;
+    return launch_dependent(merge_weights_kernel, dim3(grid), kPairKeys, 0, st, p);
 }
 
 }  // namespace
 
-cudaError_t launch_prompt_weights(const PromptArgs& a, int sms, cudaStream_t st)
+size_t prompt_weights_workspace(const twinkv_prompt&)
 {
-    const dim3 grid((a.s.keys + 3) / 4, a.s.H);
-    if (a.s.d == 128) prompt_weights_kernel<128><<<grid, 128, 0, st>>>(a);
-    else prompt_weights_kernel<64><<<grid, 128, 0, st>>>(a);
-    return cudaGetLastError();
+    return 16 * kPromptBlocks + 2 * kPromptBlocks * kPairKeys * sizeof(float);
 }
 
-cudaError_t launch_cache_weights(const CacheWeightsArgs& p, int sms, cudaStream_t st)
+cudaError_t launch_prompt_weights(const PromptArgs& a, int sms, const WaitFacts& w, cudaStream_t st)
 {
-    const int units = p.a.B * p.a.H;
-    int* seen = nullptr;
-    if (p.a.window > 0) {
-        seen = static_cast<int*>(p.a.ws);
-        const cudaError_t e = launch_windows(p.a, units, seen, st);
-        if (e != cudaSuccess) return e;
-    }
-    const dim3 grid((p.N + kPage - 1) / kPage, units);
-    if (p.a.d == 128) cache_weights_kernel<128><<<grid, 64, 0, st>>>(p, seen);
-    else cache_weights_kernel<64><<<grid, 64, 0, st>>>(p, seen);
-    return cudaGetLastError();
+    return a.s.d == 128 ? launch<128>(a, sms, w, st) : launch<64>(a, sms, w, st);
 }
 
 }  // namespace twk
