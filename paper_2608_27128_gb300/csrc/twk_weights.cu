@@ -10,14 +10,14 @@
 //
 // Bound by the tensor cores (2 d operations a pair of key and column) and the exponentials, about alike at
 // d = 128; with few tokens (an observation window) by the keys' bytes.  Design (persistent, one block of
-// 384 threads per SM):
+// 640 threads per SM):
 //   - An item is 256 keys of one KV head, and runs over the columns that see any of them.  The keys stay:
 //     they go from TMA's tile through registers to tensor memory, as the products' operand A, so that
 //     only the queries are read from shared memory (A from there as well would ask for all of its
 //     bandwidth).  Three accumulators of 128 columns take turns.
-//   - Warps 0 to 3 and 4 to 7: a thread per key of the item's halves.  Warp 8: TMA.  Warp 9: products.
-//     Warp 10: items.  Warp 11: the columns' lse, +inf where a column does not count, which makes its
-//     weight 0.  A column's place in shared memory is zero where the tile has none (G does not
+//   - Warps 0 to 15: a thread per key of the item's halves and half a tile's columns.  Warp 16: TMA.
+//     Warp 17: products.  Warp 18: items.  Warp 19: the columns' lse, +inf where a column does not
+//     count, which makes its weight 0.  A column's place in shared memory is zero where the tile has none (G does not
 //     divide 128).
 //   - Work is divided evenly whatever the lengths (twk_prompt.cuh); merge_kernel adds the parts of an item
 //     that blocks share, in order.
@@ -28,12 +28,18 @@
 namespace twk {
 namespace {
 
-constexpr int kThreads = 384;
-constexpr int kLaunchRegs = 168, kHelperRegs = 88, kSumRegs = 208;
-static_assert(4 * kHelperRegs + 8 * kSumRegs <= 12 * kLaunchRegs,
+// Sixteen warps sum, four to a quarter of the SM, half a tile's columns each: eight with whole tiles do not
+// cover each other's latencies (235 us for every token of 8192 where these take XXX).
+constexpr int kSumWarps = 16, kThreads = 32 * (kSumWarps + 4);
+constexpr int kLaunchRegs = 96, kHelperRegs = 64, kSumRegs = 104;
+static_assert(4 * kHelperRegs + kSumWarps * kSumRegs <= (kSumWarps + 4) * kLaunchRegs,
               "the split draws on the registers of the launch");
 constexpr int kPairKeys = 2 * kTileKeys;
-constexpr int kAccs = 3, kItemSlots = 4, kLogSlots = 4;
+constexpr int kAccs = 3, kItemSlots = 4;
+// Tiles' lse, a ring for each half.  A tile's lse is written when its accumulator is free, as its products
+// start: every tile three and more before it, of either half, is then released.  So the half's tile
+// kAccs before it, at least as far back, is released, and the one before that, whose slot is taken, is done.
+constexpr int kLogSlots = kAccs + 1;
 
 // The tokens that see some key of [j, last]: the first, and the end; of those that count.
 __device__ __forceinline__ int2 tokens_of(const PromptArgs& a, const Sequence& s, int j, int last)
@@ -70,7 +76,8 @@ struct Cfg {
     static constexpr int STAGES = D == 128 ? 4 : 8;       // tiles of queries
     static constexpr int OFF_Q = 2 * TILE;                // behind two tiles of keys
     static constexpr int OFF_LOG = OFF_Q + STAGES * TILE;
-    static constexpr int OFF_MISC = OFF_LOG + kLogSlots * 512;
+    static constexpr int OFF_HALF = OFF_LOG + 2 * kLogSlots * 512;
+    static constexpr int OFF_MISC = OFF_HALF + 2 * kTileKeys * 4;
     static constexpr int BYTES = OFF_MISC + 1024 + 1024;  // + 1024 for alignment
     static constexpr int T_K = 0, T_ACC = 128;            // columns of tensor memory
     static_assert(BYTES <= 232448, "shared memory per block");
@@ -91,9 +98,9 @@ struct Item {
 static_assert(sizeof(Item) == 64);
 
 struct Misc {
-    uint64_t k_full[2], k_empty[2], kt_full[2], drain;
+    uint64_t k_full[2], k_empty[2], kt_full[2], half_full[2], half_empty[2], drain;
     // acc_full: by half and its own count, since a half that skips another's phases would lose track
-    uint64_t acc_full[2][kAccs], acc_empty[kAccs], log_full[kLogSlots], log_empty[kLogSlots];
+    uint64_t acc_full[2][kAccs], acc_empty[kAccs], log_full[2][kLogSlots];
     uint64_t q_full[8], q_empty[8], item_full[kItemSlots], item_empty[kItemSlots];
     Item items[kItemSlots];
     uint32_t tmem;
@@ -110,6 +117,15 @@ struct WeightsKernelArgs {
     int* err;
     unsigned long long timeout_ns;
 };
+
+// Both barriers' phases, as all_wait.
+__device__ __forceinline__ bool both_wait(uint64_t& a, uint32_t a_parity, uint64_t& b, uint32_t b_parity,
+                                          const WaitCtl& w, int where)
+{
+    if (__all_sync(0xffffffffu, mbar_test2(smem_u32(&a), a_parity, smem_u32(&b), b_parity) != 0))
+        return true;
+    return all_wait(&b, b_parity, w, where + 1) && all_wait(&a, a_parity, w, where);
+}
 
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -130,16 +146,18 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_init(&M.k_full[i], 1);
             mbar_init(&M.k_empty[i], 4);
             mbar_init(&M.kt_full[i], 4);
+            mbar_init(&M.half_full[i], 4);
+            mbar_init(&M.half_empty[i], 4);
         }
         mbar_init(&M.drain, 1);
         for (int i = 0; i < kAccs; ++i) {
             mbar_init(&M.acc_full[0][i], 1);
             mbar_init(&M.acc_full[1][i], 1);
-            mbar_init(&M.acc_empty[i], 4);
+            mbar_init(&M.acc_empty[i], 8);
         }
         for (int i = 0; i < kLogSlots; ++i) {
-            mbar_init(&M.log_full[i], 1);
-            mbar_init(&M.log_empty[i], 8);
+            mbar_init(&M.log_full[0][i], 1);
+            mbar_init(&M.log_full[1][i], 1);
         }
         for (int i = 0; i < C::STAGES; ++i) {
             mbar_init(&M.q_full[i], 1);
@@ -147,16 +165,16 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         for (int i = 0; i < kItemSlots; ++i) {
             mbar_init(&M.item_full[i], 1);
-            mbar_init(&M.item_empty[i], 11);      // TMA, products, lse, eight that sum
+            mbar_init(&M.item_empty[i], 3 + kSumWarps);      // TMA, products, lse
         }
         M.abort_flag = 0;
         fence_mbarrier_init();
     }
-    if (warp == 8 && lane == 0) {
+    if (warp == kSumWarps && lane == 0) {
         prefetch_tensormap(&tmQ);
         prefetch_tensormap(&tmK);
     }
-    if (warp == 9) tmem_alloc<1>(&M.tmem, 512);
+    if (warp == kSumWarps + 1) tmem_alloc<1>(&M.tmem, 512);
     wait_for_previous();
     // the chunks' sums lie where queries come later
     long long* sums = reinterpret_cast<long long*>(smem + C::OFF_Q);
@@ -180,9 +198,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     wc.err = p.err;
     wc.where = 0;
 
-    if (warp >= 8) {
+    if (warp >= kSumWarps) {
         setmaxnreg_dec<kHelperRegs>();
-        if (warp == 8) {
+        if (warp == kSumWarps) {
             // ------------------------------------------------------------ TMA
             if (lane == 0) {
                 Ring<kItemSlots> ri;
@@ -235,7 +253,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                 }
             }
-        } else if (warp == 9) {
+        } else if (warp == kSumWarps + 1) {
             // ------------------------------------------------------------ products
             // every lane follows, an elected one issues; what it issues comes from uniform registers
             constexpr uint32_t idesc = umma_idesc_bf16_f32(kTileKeys, 128);
@@ -296,7 +314,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 umma_commit(&M.drain);
                 drain_wait(&M.drain, 0, p.timeout_ns);
             }
-        } else if (warp == 10) {
+        } else if (warp == kSumWarps + 2) {
             // ------------------------------------------------------------ items
             Walk<KeyPairs> at;
             at.start(a, sums);
@@ -355,7 +373,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int b = lane; b < a.s.B; b += 32)
                     a.out_status[b] = sequence_of(a, b).ok ? TWINKV_OK : TWINKV_ERR_INVALID_ARG;
             Ring<kItemSlots> ri;
-            Ring<kLogSlots> rl;
+            Ring<kLogSlots> rl[2];
+            Ring<kAccs> ra;
             bool ok = true;
             int token[4], sub[4];                    // of the lane's columns
 #pragma unroll
@@ -391,15 +410,23 @@ __global__ void __launch_bounds__(kThreads, 1)
                 };
                 float y[4], next[4];
                 if (u < end) load(u, y);
-                for (; u < end; ++u) {
+                for (; ok && u < end; ++u) {
                     if (u + 1 < end) load(u + 1, next);
-                    if (!(ok = all_wait(&M.log_empty[rl.slot], rl.phase ^ 1u, wc, 50))) break;
                     constexpr float kLog2e = 1.4426950408889634f;
-                    *reinterpret_cast<float4*>(smem + C::OFF_LOG + rl.slot * 512 + lane * 16) =
+                    const float4 w =
                         make_float4(-kLog2e * y[0], -kLog2e * y[1], -kLog2e * y[2], -kLog2e * y[3]);
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&M.log_full[rl.slot]);
-                    rl.next();
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        if (!ok || u < max(it.b[x], it.u0) || u >= min(it.e[x], it.u1)) continue;
+                        // as the products wait
+                        if (!(ok = all_wait(&M.acc_empty[ra.slot], ra.phase ^ 1u, wc, 50))) continue;
+                        ra.next();
+                        *reinterpret_cast<float4*>(smem + C::OFF_LOG +
+                                                   (x * kLogSlots + rl[x].slot) * 512 + lane * 16) = w;
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&M.log_full[x][rl[x].slot]);
+                        rl[x].next();
+                    }
 #pragma unroll
                     for (int k = 0; k < 4; ++k) y[k] = next[k];
                 }
@@ -409,17 +436,19 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc_fence_before();
         __syncthreads();
         tc_fence_after();
-        if (warp == 9) tmem_dealloc<1>(tmem, 512);
+        if (warp == kSumWarps + 1) tmem_dealloc<1>(tmem, 512);
     } else {
         // ------------------------------------------------------------ sums
         setmaxnreg_inc<kSumRegs>();
-        const int x = warp >> 2, q = warp & 3;
+        // half of the item's keys, half of a tile's columns, quarter of tensor memory
+        const int x = warp >> 3, half = warp >> 2 & 1, q = warp & 3;
         const int row = q * 32 + lane;
         const uint32_t base = tmem + (static_cast<uint32_t>(q * 32) << 16);
         Ring<kItemSlots> ri;
         Ring<kLogSlots> rl;
         Ring<kAccs> ra, rx;
-        uint32_t k_uses = 0;
+        float* halves = reinterpret_cast<float*>(smem + C::OFF_HALF) + x * kTileKeys + row;
+        uint32_t k_uses = 0, joins = 0;
         bool ok = true;
         while (ok) {
             if (!(ok = all_wait(&M.item_full[ri.slot], ri.phase, wc, 51))) break;
@@ -438,7 +467,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             ri.next();
             if (head < 0) break;
             const bool mine = b < e, other = ob < oe;
-            if (mine) {
+            if (mine && half == 0) {
                 // the half's keys: from TMA's tile to operand A, a key to a thread.  The products that
                 // read the last ones have ended: their sums are done.
                 if (!(ok = all_wait(&M.k_full[x], k_uses++ & 1u, wc, 52))) break;
@@ -462,75 +491,93 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
             }
             float sum = 0.0f;
-            const int begin = mine ? (other ? min(b, ob) : b) : ob;
-            const int end = mine ? (other ? max(e, oe) : e) : oe;
-            for (int u = begin; u < end; ++u) {
-                // accumulators go to the halves in order
-                const bool on = mine && u >= b && u < e, also = other && u >= ob && u < oe;
+            // accumulators go to the halves in order
+            for (int u = other ? min(b, ob) : b; mine && u < e; ++u) {
+                const bool on = u >= b, also = other && u >= ob && u < oe;
                 if (x == 1 && also) ra.next();
                 if (on) {
-                    if (!(ok = all_wait(&M.acc_full[x][rx.slot], rx.phase, wc, 53))) break;
+                    if (!(ok = both_wait(M.acc_full[x][rx.slot], rx.phase, M.log_full[x][rl.slot],
+                                         rl.phase, wc, 53)))
+                        break;
                     rx.next();
                     tc_fence_after();
-                    uint32_t s[4][32];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        tmem_ld_32x32b_x32(base + C::T_ACC + ra.slot * 128 + 32 * i, s[i]);
+                    const uint32_t acc = base + C::T_ACC + ra.slot * 128 + half * 64;
+                    uint32_t s[2][32];
+                    tmem_ld_32x32b_x32(acc, s[0]);
+                    tmem_ld_32x32b_x32(acc + 32, s[1]);
+                    const int p0 = gap + u * tpt;         // first token's position less the warp's first key
+                    const int rest = left - u * tpt;      // tokens from it on
+                    const bool edge = p0 < 31 || rest < tpt ||
+                                      (a.window > 0 && p0 + tpt - 1 >= a.window);
+                    // columns [lo, hi) see the thread's key: those of the tokens from its own on, as far
+                    // as the window reaches
+                    int lo = 0, hi = 128;
+                    if (edge) {
+                        lo = min(max(lane - p0, 0), 128) * a.G;
+                        hi = min(rest, tpt);
+                        if (a.window > 0 && key >= a.n_sink) hi = min(hi, lane + a.window - p0);
+                        hi = max(hi, 0) * a.G;
+                    }
+                    const float4* log = reinterpret_cast<const float4*>(smem + C::OFF_LOG +
+                                                                        (x * kLogSlots + rl.slot) * 512 +
+                                                                        half * 256);
+                    const float2 c2 = make_float2(p.c, p.c);
+                    float2 l[4] = {};
                     tmem_wait_ld();
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) reg_fence(s[i]);
+                    reg_fence(s[0]);
+                    reg_fence(s[1]);
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&M.acc_empty[ra.slot]);
                     ra.next();
-                    const int p0 = gap + u * tpt;         // first token's position less the warp's first key
-                    const int rest = left - u * tpt;      // tokens from it on
-                    if (p0 < 31 || rest < tpt ||
-                        (a.window > 0 && p0 + tpt - 1 >= a.window)) {
-                        // columns [lo, hi) see the thread's key: those of the tokens from its own on, as far
-                        // as the window reaches
-                        const int lo = min(max(lane - p0, 0), 128) * a.G;
-                        int hi = min(rest, tpt);
-                        if (a.window > 0 && key >= a.n_sink) hi = min(hi, lane + a.window - p0);
-                        hi = max(hi, 0) * a.G;
+                    if (edge) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint32_t see = bits_below(hi - 32 * i) & ~bits_below(lo - 32 * i);
+                        for (int i = 0; i < 2; ++i) {
+                            const int first = 64 * half + 32 * i;
+                            const uint32_t see = bits_below(hi - first) & ~bits_below(lo - first);
 #pragma unroll
                             for (int y = 0; y < 32; ++y)
                                 s[i][y] = see >> y & 1u ? s[i][y] : 0xff800000u;
                         }
                     }
-                    if (!(ok = all_wait(&M.log_full[rl.slot], rl.phase, wc, 54))) break;
-                    const float4* log = reinterpret_cast<const float4*>(smem + C::OFF_LOG +
-                                                                        rl.slot * 512);
-                    const float2 c2 = make_float2(p.c, p.c);
-                    float2 l[4] = {};
 #pragma unroll
-                    for (int y = 0; y < 128; y += 4) {
+                    for (int y = 0; y < 64; y += 4) {
+                        const uint32_t(&v)[32] = s[y / 32];
                         const float4 t = log[y / 4];
-                        const float2 v = __ffma2_rn(
-                            make_float2(as_f(s[y / 32][y % 32]), as_f(s[y / 32][y % 32 + 1])), c2,
+                        const float2 w0 = __ffma2_rn(
+                            make_float2(as_f(v[y % 32]), as_f(v[y % 32 + 1])), c2,
                             make_float2(t.x, t.y));
-                        const float2 w = __ffma2_rn(
-                            make_float2(as_f(s[y / 32][y % 32 + 2]), as_f(s[y / 32][y % 32 + 3])), c2,
+                        const float2 w1 = __ffma2_rn(
+                            make_float2(as_f(v[y % 32 + 2]), as_f(v[y % 32 + 3])), c2,
                             make_float2(t.z, t.w));
                         l[y / 4 % 2] = __fadd2_rn(l[y / 4 % 2],
-                                                  make_float2(exp2_approx(v.x), exp2_approx(v.y)));
+                                                  make_float2(exp2_approx(w0.x), exp2_approx(w0.y)));
                         l[2 + y / 4 % 2] = __fadd2_rn(
-                            l[2 + y / 4 % 2], make_float2(exp2_approx(w.x), exp2_approx(w.y)));
+                            l[2 + y / 4 % 2], make_float2(exp2_approx(w1.x), exp2_approx(w1.y)));
                     }
                     const float2 l2 = __fadd2_rn(__fadd2_rn(l[0], l[1]), __fadd2_rn(l[2], l[3]));
                     sum += l2.x + l2.y;
+                    rl.next();
                 }
-                // also where it has no part in the unit: its arrivals must not run ahead of the slot
-                if (!on && !(ok = all_wait(&M.log_full[rl.slot], rl.phase, wc, 54))) break;
                 if (x == 0 && also) ra.next();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&M.log_empty[rl.slot]);
-                rl.next();
             }
             if (!ok) break;
+            if (other) {
+                // what the other half takes after this one's last unit
+                for (int u = max(ob, mine ? e : ob); u < oe; ++u) ra.next();
+            }
+            // the two halves of the columns, in order
+            if (half == 1) {
+                if (!(ok = all_wait(&M.half_empty[x], (joins++ & 1u) ^ 1u, wc, 55))) break;
+                *halves = sum;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&M.half_full[x]);
+                continue;
+            }
+            if (!(ok = all_wait(&M.half_full[x], joins++ & 1u, wc, 56))) break;
+            sum += *halves;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&M.half_empty[x]);
             if (slot >= 0) {
                 p.part[slot * kPairKeys + x * kTileKeys + row] = sum;
             } else if (row < held) {
