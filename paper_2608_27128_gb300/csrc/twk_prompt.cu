@@ -7,8 +7,10 @@
 // One pass over the keys, a tile of 128 at a time, with a running maximum and sum per row: with
 // c = scale log2(e) and t the row's top, about the largest c q . k so far,
 //     p_j = 2^(c q . k_j - t),   l = sum p_j,   O = sum p_j v_j,   o = O / l,   lse = ln2 t + ln l.
-// The top follows the maximum only where that has risen by more than 8 (a factor of 256, which
-// bf16's exponent does not notice): O is then scaled in tensor memory, a rare event.
+// The top is the maximum of the row's first tile, and follows later ones only where a tile's sum of
+// probabilities shows that it is far behind them (2^15: floats and bf16 do not notice such factors, and
+// the sum of 128 probabilities stays below it else): the tile's maximum is found, O scaled in tensor
+// memory and the tile done again, a rare event.  So a tile costs no maximum (XXX).
 //
 // Bound by the tensor cores: 4 d operations for each pair of a row and a key, of which a prompt of n tokens
 // has n^2 / 2 per head; exponentials (a row and key each) take about half their time at d = 128 and as
@@ -37,7 +39,7 @@ constexpr int kLaunchRegs = 168, kHelperRegs = 88, kSoftmaxRegs = 208;
 static_assert(4 * kHelperRegs + 8 * kSoftmaxRegs <= 12 * kLaunchRegs,
               "the split draws on the registers of the launch");
 constexpr int kPairRows = 2 * kTileRows;
-constexpr float kLazy = 8.0f;            // what a maximum may rise, in powers of two, before O follows
+constexpr float kFar = 0x1p15f;          // sum of a tile's probabilities from which the top follows
 
 // Items of attention: pairs of row tiles; as long as their list of key tiles.
 struct RowPairs {
@@ -69,7 +71,16 @@ struct Cfg {
     static constexpr int OFF_OUT = OFF_KV + STAGES * STAGE;     // a warp's rows, 128 bytes of each
     static constexpr int OFF_MISC = OFF_OUT + 8 * 32 * 128;
     static constexpr int BYTES = OFF_MISC + 1024 + 1024;  // + 1024 for alignment
-    static constexpr int T_S = 0, T_O = 256;              // columns of tensor memory: S, O of tile 0
+    // Columns of tensor memory, of tile 0.  At d = 128 the probabilities take the scores' place, and the next
+    // scores come after their products.  At d = 64 there is room beside them: the next scores come as soon
+    // as the softmax has the last ones in registers, and are there when it is done.  Scores and outputs are
+    // then issued by a warp each: what a warp does around its products takes longer than they do
+    // (16384 tokens, one warp and one place: 1075 us; two places: 1232; XXX).
+    static constexpr bool EARLY = D == 64;
+    static constexpr int T_S = 0, T_P = EARLY ? 256 : 0, P_STRIDE = EARLY ? 64 : kTileKeys;
+    static constexpr int T_O = EARLY ? 384 : 256;
+    static_assert(T_O + 2 * D <= 512);
+    static_assert(STAGES % 2 == 0, "keys in even stages, values in odd ones");
     static_assert(BYTES <= 232448, "shared memory per block");
     static_assert(STAGES * STAGE >= kSumsBytes, "the chunks' sums lie there at first");
 };
@@ -90,7 +101,7 @@ struct Item {
 static_assert(sizeof(Item) == 64);
 
 struct Misc {
-    uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2], drain;
+    uint64_t q_full[2], q_empty[2], s_full[2], s_free[2], p_full[2], o_full[2], drain[2];
     uint64_t kv_full[8], kv_empty[8], item_full[kItemSlots], item_empty[kItemSlots];
     Item items[kItemSlots];
     uint32_t tmem;
@@ -137,17 +148,18 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_init(&M.q_full[i], 1);
             mbar_init(&M.q_empty[i], 1);
             mbar_init(&M.s_full[i], 1);
+            mbar_init(&M.s_free[i], 4);
             mbar_init(&M.p_full[i], 4);
+            mbar_init(&M.drain[i], 1);
             mbar_init(&M.o_full[i], 1);
         }
-        mbar_init(&M.drain, 1);
         for (int i = 0; i < C::STAGES; ++i) {
             mbar_init(&M.kv_full[i], 1);
             mbar_init(&M.kv_empty[i], 1);
         }
         for (int i = 0; i < kItemSlots; ++i) {
             mbar_init(&M.item_full[i], 1);
-            mbar_init(&M.item_empty[i], 10);      // TMA, products, eight of softmax
+            mbar_init(&M.item_empty[i], C::EARLY ? 11 : 10);      // TMA, products, eight of softmax
         }
         M.abort_flag = 0;
         fence_mbarrier_init();
@@ -232,7 +244,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                 }
             }
-        } else if (warp == 9) {
+        } else if (warp == 9 || (C::EARLY && warp == 11)) {
             // ------------------------------------------------------------ products
             // Every lane follows, an elected one issues.  What the descriptors and the loops depend on comes
             // from shuffles and votes, so that the compiler knows it to be the same in all lanes and keeps it
@@ -240,8 +252,6 @@ __global__ void __launch_bounds__(kThreads, 1)
             constexpr uint32_t id_s = umma_idesc_bf16_f32(kTileRows, kTileKeys);
             constexpr uint32_t id_o = umma_idesc_bf16_f32(kTileRows, D) | kIdescBRows;
             Ring<kItemSlots> ri;
-            Ring<C::STAGES> rs;
-            uint32_t q_uses[2] = {}, p_uses[2] = {};
             const uint32_t q_low = static_cast<uint32_t>(umma_desc_sw128(smem_u32(smem)));
             const uint32_t k_low = static_cast<uint32_t>(umma_desc_sw128(smem_u32(smem + C::OFF_KV)));
             const uint32_t v_low =
@@ -252,7 +262,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 umma_commit(&M.s_full[x]);
             };
             auto outputs = [&](int x, uint32_t stage, uint32_t add) {
-                umma_tmem_128(tmem + C::T_O + x * D, tmem + C::T_S + x * kTileKeys,
+                umma_tmem_128(tmem + C::T_O + x * D, tmem + C::T_P + x * C::P_STRIDE,
                               v_low + stage * (C::STAGE >> 4), id_o, add);
             };
             bool ok = true;
@@ -282,83 +292,138 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (head < 0 || f.all > f.s0) return;
                 }
             };
-            // the scores of the item's first unit by tile x
-            auto first_scores = [&](const Part& f, int x) {
-                if (!ok || f.n[x] <= f.s0) return;
-                ok = all_wait(&M.kv_full[rs.slot], rs.phase, wc, 25) &&
-                     all_wait(&M.q_full[x], q_uses[x]++ & 1u, wc, 26);
-                if (!ok) return;
-                tc_fence_after();
-                if (elect_one()) {
-                    scores(x, rs.slot);
-                    if (f.s0 + 1 == f.n[x]) umma_commit(&M.q_empty[x]);
-                    if (x == f.last) umma_commit(&M.kv_empty[rs.slot]);
-                }
-            };
-            Part f, g;
-            fetch(f);
-            if (ok && f.all > f.s0) {
-                first_scores(f, 0);
-                first_scores(f, 1);
-                rs.next();
-            }
-            while (ok && f.all > f.s0) {
-                for (int j = f.s0; j < f.all; ++j) {
-                    const Ring<C::STAGES> rv = rs;
-                    rs.next();
-                    const bool end = j + 1 == f.all;
-                    if (!(ok = all_wait(&M.kv_full[rv.slot], rv.phase, wc, 27))) break;
-                    if (!end && !(ok = all_wait(&M.kv_full[rs.slot], rs.phase, wc, 30))) break;
-                    const int held = f.m - f.kt.tile(j) * kTileKeys;
-                    if (held < kTileKeys) {
-                        // the sequence ends inside the tile: its probabilities are 0 from there on,
-                        // and so are the values, whatever lies behind it
-                        uint8_t* v = smem + C::OFF_KV + rv.slot * C::STAGE;
-                        for (int y = held * 128 + lane * 16; y < C::CHUNK; y += 512)
+            // where the sequence ends inside the tile its probabilities are 0 from there on, and so are the
+            // values, whatever lies behind it
+            auto end_values = [&](int held, uint32_t stage) {
+                if (held >= kTileKeys) return;
+                uint8_t* v = smem + C::OFF_KV + stage * C::STAGE;
+                for (int y = held * 128 + lane * 16; y < C::CHUNK; y += 512)
 #pragma unroll
-                            for (int kc = 0; kc < C::KC; ++kc)
-                                *reinterpret_cast<uint4*>(v + kc * C::CHUNK + y) =
-                                    make_uint4(0, 0, 0, 0);
-                        fence_async_shared();
-                        __syncwarp();
-                    }
-                    if (end) {
-                        fetch(g);
+                    for (int kc = 0; kc < C::KC; ++kc)
+                        *reinterpret_cast<uint4*>(v + kc * C::CHUNK + y) = make_uint4(0, 0, 0, 0);
+                fence_async_shared();
+                __syncwarp();
+            };
+            Part f;
+            if constexpr (C::EARLY) {
+                Ring<C::STAGES / 2> rs;          // even stages for scores, odd ones for outputs
+                uint32_t uses[2] = {}, q_uses[2] = {};
+                if (warp == 9) {
+                    for (fetch(f); ok && f.all > f.s0; fetch(f)) {
+                        for (int j = f.s0; ok && j < f.all; ++j) {
+                            const uint32_t stage = 2 * rs.slot;
+                            if (!(ok = all_wait(&M.kv_full[stage], rs.phase, wc, 25))) break;
+#pragma unroll
+                            for (int x = 0; x < 2; ++x) {
+                                if (!ok || j >= f.n[x]) continue;
+                                if (j == f.s0) ok = all_wait(&M.q_full[x], q_uses[x]++ & 1u, wc, 26);
+                                if (ok) ok = all_wait(&M.s_free[x], (uses[x]++ & 1u) ^ 1u, wc, 37);
+                                if (!ok) continue;
+                                tc_fence_after();
+                                if (elect_one()) {
+                                    scores(x, stage);
+                                    if (j + 1 == f.n[x]) umma_commit(&M.q_empty[x]);
+                                    if (x == f.last) umma_commit(&M.kv_empty[stage]);
+                                }
+                                __syncwarp();
+                            }
+                            // the second tile's last unit may be past the first's, not the other way round
+                            rs.next();
+                        }
                         if (!ok) break;
                     }
+                } else {
+                    for (fetch(f); ok && f.all > f.s0; fetch(f)) {
+                        for (int j = f.s0; ok && j < f.all; ++j) {
+                            const uint32_t stage = 2 * rs.slot + 1;
+                            if (!(ok = all_wait(&M.kv_full[stage], rs.phase, wc, 27))) break;
+                            end_values(f.m - f.kt.tile(j) * kTileKeys, stage);
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        if (ok && j < f.n[x]) {
-                            ok = all_wait(&M.p_full[x], p_uses[x]++ & 1u, wc, 29);
-                            if (ok) tc_fence_after();
-                            if (ok && elect_one()) {
-                                outputs(x, rv.slot, j != f.s0);
-                                if (j + 1 < f.n[x]) {
-                                    scores(x, rs.slot);
-                                    if (j + 2 == f.n[x]) umma_commit(&M.q_empty[x]);
-                                } else {
+                            for (int x = 0; x < 2; ++x) {
+                                if (!ok || j >= f.n[x]) continue;
+                                if (!(ok = all_wait(&M.p_full[x], uses[x]++ & 1u, wc, 29))) continue;
+                                tc_fence_after();
+                                if (elect_one()) {
+                                    outputs(x, stage, j != f.s0);
                                     umma_commit(&M.o_full[x]);
+                                    if (x == f.last) umma_commit(&M.kv_empty[stage]);
                                 }
-                                if (x == f.last) {
-                                    umma_commit(&M.kv_empty[rv.slot]);
-                                    if (!end) umma_commit(&M.kv_empty[rs.slot]);
-                                }
+                                __syncwarp();
                             }
-                            __syncwarp();
+                            rs.next();
                         }
-                        // the next item's first scores, while the softmax of this one's last unit runs
-                        if (end && g.all > g.s0) first_scores(g, x);
+                        if (!ok) break;
                     }
-                    if (!ok) break;
-                    if (!end || g.all > g.s0) rs.next();
                 }
-                f = g;
+            } else {
+                Ring<C::STAGES> rs;
+                uint32_t q_uses[2] = {}, p_uses[2] = {};
+                // the scores of the item's first unit by tile x
+                auto first_scores = [&](const Part& f, int x) {
+                    if (!ok || f.n[x] <= f.s0) return;
+                    ok = all_wait(&M.kv_full[rs.slot], rs.phase, wc, 25) &&
+                         all_wait(&M.q_full[x], q_uses[x]++ & 1u, wc, 26);
+                    if (!ok) return;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        scores(x, rs.slot);
+                        if (f.s0 + 1 == f.n[x]) umma_commit(&M.q_empty[x]);
+                        if (x == f.last) umma_commit(&M.kv_empty[rs.slot]);
+                    }
+                };
+                Part g;
+                fetch(f);
+                if (ok && f.all > f.s0) {
+                    first_scores(f, 0);
+                    first_scores(f, 1);
+                    rs.next();
+                }
+                while (ok && f.all > f.s0) {
+                    for (int j = f.s0; j < f.all; ++j) {
+                        const Ring<C::STAGES> rv = rs;
+                        rs.next();
+                        const bool end = j + 1 == f.all;
+                        if (!(ok = all_wait(&M.kv_full[rv.slot], rv.phase, wc, 27))) break;
+                        if (!end && !(ok = all_wait(&M.kv_full[rs.slot], rs.phase, wc, 30))) break;
+                        end_values(f.m - f.kt.tile(j) * kTileKeys, rv.slot);
+                        if (end) {
+                            fetch(g);
+                            if (!ok) break;
+                        }
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            if (ok && j < f.n[x]) {
+                                ok = all_wait(&M.p_full[x], p_uses[x]++ & 1u, wc, 29);
+                                if (ok) tc_fence_after();
+                                if (ok && elect_one()) {
+                                    outputs(x, rv.slot, j != f.s0);
+                                    if (j + 1 < f.n[x]) {
+                                        scores(x, rs.slot);
+                                        if (j + 2 == f.n[x]) umma_commit(&M.q_empty[x]);
+                                    } else {
+                                        umma_commit(&M.o_full[x]);
+                                    }
+                                    if (x == f.last) {
+                                        umma_commit(&M.kv_empty[rv.slot]);
+                                        if (!end) umma_commit(&M.kv_empty[rs.slot]);
+                                    }
+                                }
+                                __syncwarp();
+                            }
+                            // the next item's first scores, while the softmax of this one's last unit runs
+                            if (end && g.all > g.s0) first_scores(g, x);
+                        }
+                        if (!ok) break;
+                        if (!end || g.all > g.s0) rs.next();
+                    }
+                    f = g;
+                }
             }
             // every product has ended before tensor memory is freed
             __syncwarp();
             if (elect_one()) {
-                umma_commit(&M.drain);
-                drain_wait(&M.drain, 0, p.timeout_ns);
+                umma_commit(&M.drain[warp == 9 ? 0 : 1]);
+                drain_wait(&M.drain[warp == 9 ? 0 : 1], 0, p.timeout_ns);
             }
         } else if (warp == 10) {
             // ------------------------------------------------------------ items
@@ -409,7 +474,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     mbar_arrive(&M.item_full[ri.slot]);
                 }
             }
-        } else {
+            __syncwarp();
             if (blockIdx.x == 0 && a.out_status)
                 for (int b = lane; b < a.s.B; b += 32)
                     a.out_status[b] = sequence_of(a, b).ok ? TWINKV_OK : TWINKV_ERR_INVALID_ARG;
@@ -426,6 +491,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int row = q * 32 + lane;
         const uint32_t base = tmem + (static_cast<uint32_t>(q * 32) << 16);
         const uint32_t t_s = base + C::T_S + x * kTileKeys, t_o = base + C::T_O + x * D;
+        const uint32_t t_p = base + C::T_P + x * C::P_STRIDE;
         const int token = row / a.G, sub = row - token * a.G;        // of the tile
         const int first_token = q * 32 / a.G, last_token = (q * 32 + 31) / a.G;
         Ring<kItemSlots> ri;
@@ -454,6 +520,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                 tmem_wait_ld();
 #pragma unroll
                 for (int i = 0; i < 4; ++i) reg_fence(s[i]);
+                if constexpr (C::EARLY) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&M.s_free[x]);
+                }
                 const bool edge = k0 + kTileKeys - 1 > p0 + first_token ||
                                   (a.window > 0 && k0 < p0 + last_token - a.window + 1 &&
                                    k0 + kTileKeys > a.n_sink);
@@ -469,56 +540,68 @@ __global__ void __launch_bounds__(kThreads, 1)
                             s[i][e] = see >> e & 1u ? s[i][e] : 0xff800000u;
                     }
                 }
-                float m[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float y[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        y[e] = max3(as_f(s[i][4 * e]), as_f(s[i][4 * e + 1]),
-                                    fmaxf(as_f(s[i][4 * e + 2]), as_f(s[i][4 * e + 3])));
-                    m[i] = max3(max3(y[0], y[1], y[2]), max3(y[3], y[4], y[5]), fmaxf(y[6], y[7]));
+                // With the top so far; again with the true one where a row has none, or its sum shows that
+                // the scores have left it far behind.
+                bool exact = __any_sync(0xffffffffu, top == -INFINITY);
+                // the products with the tile's last probabilities, whose place the next ones take
+                if (C::EARLY && j > it.s0) {
+                    if (!(ok = all_wait(&M.o_full[x], o_uses++ & 1u, wc, 36))) break;
+                    tc_fence_after();
                 }
-                const float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * p.c;
-                if (j == it.s0) {
-                    top = most;
-                } else {
-                    const bool rise = most > top + kLazy;
-                    if (__any_sync(0xffffffffu, rise)) {
-                        const float f = rise ? exp2_approx(top - most) : 1.0f;   // top -inf: 0
+                for (;;) {
+                    if (exact) {
+                        float m[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            m[i] = as_f(s[i][0]);
+#pragma unroll
+                            for (int e = 1; e < 31; e += 2)
+                                m[i] = max3(m[i], as_f(s[i][e]), as_f(s[i][e + 1]));
+                            m[i] = fmaxf(m[i], as_f(s[i][31]));
+                        }
+                        const float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * p.c;
+                        const bool rise = most > top;
+                        const float f = rise ? exp2_approx(top - most) : 1.0f;    // top -inf: 0
                         if (rise) top = most;
-                        sum *= f;
+                        if (j > it.s0) {
+                            sum *= f;
 #pragma unroll
-                        for (int i = 0; i < D / 32; ++i) {
-                            uint32_t o[32];
-                            tmem_ld_32x32b_x32(t_o + 32 * i, o);
-                            tmem_wait_ld();
-                            reg_fence(o);
+                            for (int i = 0; i < D / 32; ++i) {
+                                uint32_t o[32];
+                                tmem_ld_32x32b_x32(t_o + 32 * i, o);
+                                tmem_wait_ld();
+                                reg_fence(o);
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(as_f(o[e]) * f);
-                            tmem_st_32x32b_x32(t_o + 32 * i, o);
+                                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(as_f(o[e]) * f);
+                                tmem_st_32x32b_x32(t_o + 32 * i, o);
+                            }
                         }
                     }
-                }
-                const float t = top == -INFINITY ? 0.0f : top;
-                const float2 c2 = make_float2(p.c, p.c), t2 = make_float2(-t, -t);
-                float2 l[4] = {};
+                    const float t = top == -INFINITY ? 0.0f : top;
+                    const float2 c2 = make_float2(p.c, p.c), t2 = make_float2(-t, -t);
+                    float2 l[4] = {};
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t w[32];
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t w[32];
 #pragma unroll
-                    for (int e = 0; e < 64; e += 2) {
-                        const int i = 2 * h + e / 32;
-                        const float2 y = __ffma2_rn(
-                            make_float2(as_f(s[i][e % 32]), as_f(s[i][e % 32 + 1])), c2, t2);
-                        const float u = exp2_approx(y.x), v = exp2_approx(y.y);
-                        l[e / 2 % 4] = __fadd2_rn(l[e / 2 % 4], make_float2(u, v));
-                        w[e / 2] = bf16_pair(u, v);
+                        for (int e = 0; e < 64; e += 2) {
+                            const int i = 2 * h + e / 32;
+                            const float2 y = __ffma2_rn(
+                                make_float2(as_f(s[i][e % 32]), as_f(s[i][e % 32 + 1])), c2, t2);
+                            const float u = exp2_approx(y.x), v = exp2_approx(y.y);
+                            l[e / 2 % 4] = __fadd2_rn(l[e / 2 % 4], make_float2(u, v));
+                            w[e / 2] = bf16_pair(u, v);
+                        }
+                        tmem_st_32x32b_x32(t_p + 32 * h, w);
                     }
-                    tmem_st_32x32b_x32(t_s + 32 * h, w);
+                    const float2 l2 = __fadd2_rn(__fadd2_rn(l[0], l[1]), __fadd2_rn(l[2], l[3]));
+                    const float add = l2.x + l2.y;
+                    if (exact || !__any_sync(0xffffffffu, add > kFar)) {
+                        sum += add;
+                        break;
+                    }
+                    exact = true;
                 }
-                const float2 l2 = __fadd2_rn(__fadd2_rn(l[0], l[1]), __fadd2_rn(l[2], l[3]));
-                sum += l2.x + l2.y;
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
