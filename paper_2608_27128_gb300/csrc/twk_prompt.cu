@@ -53,10 +53,12 @@ struct RowPairs {
         const int tokens = 2 * a.tile_tokens, first = s.m - s.n + i * tokens;
         return key_tiles(a, first, min(first + tokens, s.m) - 1);
     }
-    // 1 where nothing is seen: the rows are written all the same
+    // beside them an item takes as long as so many tiles (its start, masks and rows: 2.3 to 3 us, a tile 0.9 at
+    // d = 64; 1.4 and 1.5 at d = 128)
+    __device__ __host__ static constexpr int more(int d) { return d == 64 ? 3 : 1; }
     __device__ static __forceinline__ int length(const PromptArgs& a, const Sequence& s, int i)
     {
-        return max(1, tiles(a, s, i).count);
+        return tiles(a, s, i).count + more(a.s.d);
     }
 };
 
@@ -763,7 +765,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps)
 }
 
 // An item that reads this many keys or fewer is never cut.
-constexpr int kWholeKeys = (2 * kSnap + 1) * kTileKeys;
+constexpr int whole_keys(int d) { return (2 * kSnap + 1 - RowPairs::more(d)) * kTileKeys; }
 
 template <int D>
 cudaError_t launch(const PromptArgs& a, int sms, const WaitFacts& w, cudaStream_t st)
@@ -792,7 +794,7 @@ cudaError_t launch(const PromptArgs& a, int sms, const WaitFacts& w, cudaStream_
     AttendKernelArgs p{};
     p.a = a;
     p.c = a.scale * 1.4426950408889634f;
-    const bool shared = a.s.keys > kWholeKeys;
+    const bool shared = a.s.keys > whole_keys(D);
     if (shared) {
         p.join = static_cast<int4*>(a.ws);
         p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(a.ws) + 16 * kPromptBlocks);
@@ -809,7 +811,7 @@ cudaError_t launch(const PromptArgs& a, int sms, const WaitFacts& w, cudaStream_
 
 size_t prompt_attend_workspace(const twinkv_prompt& s)
 {
-    if (s.keys <= kWholeKeys) return 256;
+    if (s.keys <= whole_keys(s.d)) return 256;
     return 16 * kPromptBlocks +
            2 * kPromptBlocks * static_cast<size_t>(kPairRows) * (s.d + 2) * sizeof(float);
 }

@@ -124,13 +124,13 @@ struct Ring {
 
 // ---- work among blocks
 //
-// A call's items (of a sequence and KV head) follow one another, each as long as W::length says (1
-// or more units), and all units are cut into even spans, one for each block.  An item that spans
+// A call's items (of a sequence and KV head) follow one another, each as long as W::length says: its tiles,
+// and up to kSnap more for what it takes beside them, at least 1.  All units are cut into even spans, one for each block.  An item that spans
 // share is done in parts, which a second kernel joins in order: what is cut where depends on the sizes
 // alone.  A cut within kSnap units of an item's end moves there, since a part costs about as much as so
 // many units.
 
-constexpr int kSnap = 3;
+constexpr int kSnap = 3;           // so a cut that stays inside an item is at one of its tiles
 constexpr int kChunks = 256;        // groups of sequences with their sums in shared memory
 
 // x / y, both above 0

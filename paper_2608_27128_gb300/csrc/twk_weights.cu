@@ -60,11 +60,12 @@ struct KeyPairs {
     {
         return tokens_of(a, s, i * kPairKeys, min(i * kPairKeys + kPairKeys, s.m) - 1);
     }
-    // 1 where no token sees them: their sums are written all the same
+    // beside them an item takes as long as so many tiles
+    static constexpr int kMore = 2;
     __device__ static __forceinline__ int length(const PromptArgs& a, const Sequence& s, int i)
     {
         const int2 t = tokens(a, s, i);
-        return max(1, (t.y - t.x + a.tile_tokens - 1) / a.tile_tokens);
+        return (t.y - t.x + a.tile_tokens - 1) / a.tile_tokens + kMore;
     }
 };
 
@@ -606,7 +607,7 @@ __global__ void __launch_bounds__(kPairKeys)
 }
 
 // An item that no more tokens than this look at is never cut.
-int whole_tokens(const PromptArgs& a) { return (2 * kSnap + 1) * a.tile_tokens; }
+int whole_tokens(const PromptArgs& a) { return (2 * kSnap + 1 - KeyPairs::kMore) * a.tile_tokens; }
 
 template <int D>
 cudaError_t launch(const PromptArgs& a, int sms, const WaitFacts& w, cudaStream_t st)
