@@ -1087,28 +1087,32 @@ def _prompt_plan(what, B, q, k, v):
     return Prompt(*sizes, *strides), _prompt_workspace_size(what, *sizes)
 
 
+def _ints(t, name, n, dev: int):
+    """The address of an int32 tensor [n], None for None."""
+    return None if t is None else _same(t, name, torch.int32, (n,), dev).data_ptr()
+
+
 def _prompt(what, q, k, v, offsets, lens, k_offsets, k_lens):
-    """(Prompt, Sequences, sizes B, T, Tk, Hq, H, d, device number, workspace bytes) of a call."""
-    kinds = _kind(q, "q"), _kind(k, "k"), _kind(v, "v") if what == "attend" else None
+    """(Prompt, Sequences, number of sequences, device number, workspace bytes) of a call."""
+    kq, kk, kv = _kind(q, "q"), _kind(k, "k"), _kind(v, "v") if what == "attend" else None
     dev = q.get_device()
     if dev < 0 or dev != _current_device():
         raise _elsewhere("q", q, "current")
-    for x, name in ((k, "k"), (v, "v")):
-        if x is not None and x.get_device() != dev:
-            raise _elsewhere(name, x, dev)
+    if k.get_device() != dev:
+        raise _elsewhere("k", k, dev)
+    if kv is not None and v.get_device() != dev:
+        raise _elsewhere("v", v, dev)
     B = 1
     if offsets is not None:
-        if not isinstance(offsets, torch.Tensor) or offsets.dim() != 1 or len(offsets) < 2:
+        if not isinstance(offsets, torch.Tensor) or offsets.dim() != 1 or offsets.shape[0] < 2:
             raise ValueError("offsets must be a tensor [B + 1]")
         B = offsets.shape[0] - 1
-    at = []
-    for x, name, n in ((offsets, "offsets", B + 1), (lens, "lens", B),
-                       (k_offsets, "k_offsets", B + 1), (k_lens, "k_lens", B)):
-        at.append(None if x is None else _same(x, name, torch.int32, (n,), dev).data_ptr())
-    s, need = _prompt_plan(what, B, *kinds)
+    seqs = Sequences(_ints(offsets, "offsets", B + 1, dev), _ints(lens, "lens", B, dev),
+                     _ints(k_offsets, "k_offsets", B + 1, dev), _ints(k_lens, "k_lens", B, dev))
+    s, need = _prompt_plan(what, B, kq, kk, kv)
     if need == 0:
         raise TwinKVError(ERR_UNSUPPORTED, f"twinkv_prompt_{what}")
-    return s, Sequences(*at), B, dev, need
+    return s, seqs, B, dev, need
 
 
 def twinkv_prompt_attend(q, k, v, offsets=None, *, lens=None, k_offsets=None, k_lens=None,
@@ -1126,7 +1130,7 @@ def twinkv_prompt_attend(q, k, v, offsets=None, *, lens=None, k_offsets=None, k_
     left as they were.
     """
     s, seqs, B, dev, need = _prompt("attend", q, k, v, offsets, lens, k_offsets, k_lens)
-    given, shape = out or {}, tuple(q.shape)
+    given, shape = out or {}, q.shape
     o = {"out": _made(given.get("out"), "out", torch.bfloat16, shape, dev, stream),
          "status": _made(given.get("status"), "status", torch.int32, (B,), dev, stream)}
     if want_lse:
