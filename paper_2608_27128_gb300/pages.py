@@ -141,6 +141,19 @@ class PageCache:
         self._set(units, lists)
         return self._filled(b, units, counts, out)
 
+    def evict(self, b: int, score, budget, *, n_sink=None, n_recent=None) -> dict:
+        """Sequence b keeps, per unit, the budget's worth of slots with the highest score
+        [L,H,N] float32 (N at least the longest unit), sinks and recent ones first
+        (twinkv_weight_policy), in new pages; a unit with fewer slots keeps all of them.  Returns a
+        dict: status [L,H] as pack's, mask [L,H,N], and score [L,H,N], the kept slots' in order."""
+        units = self._sequence(b)
+        counts = [min(n, self._used[u]) for n, u in zip(self._counts(budget, units), units)]
+        want = torch.tensor(counts, dtype=torch.int32).view(self.L, self.H).to(self.pool.device)
+        out = tk.twinkv_weight_policy(score, want, lens=self.lens[:, b].contiguous(), n_sink=n_sink,
+                                      n_recent=n_recent, want_score=True)
+        out["status"] = self.compact(b, out["mask"], counts)
+        return out
+
     def fork(self, b: int, to: int):
         """Sequence ``to`` becomes another end of sequence b: full pages are shared, the last
         one is copied, so that either may append.  Waits for the device, and raises RuntimeError
@@ -209,3 +222,10 @@ class PageCache:
     def attend(self, layer: int, q, **kw) -> dict:
         """Attention of the step's queries q [B,n,Hq,d] over one layer (twinkv_cache_attend)."""
         return tk.twinkv_cache_attend(q, self.pool, self.table[layer], self.lens[layer], **kw)
+
+    def weigh(self, layer: int, q, lse, score, **kw):
+        """Adds what the attention of the step's queries pays to each slot of one layer to score
+        [B,H,N] float32, in place (twinkv_cache_weights); lse as attend gave it.  Returns the
+        statuses."""
+        return tk.twinkv_cache_weights(q, lse, self.pool, self.table[layer], self.lens[layer], score,
+                                       out={"score": score}, **kw)["status"]
