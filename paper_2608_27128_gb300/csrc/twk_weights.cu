@@ -491,82 +491,102 @@ __global__ void __launch_bounds__(kThreads, 1)
                     mbar_arrive(&M.k_empty[x]);
                 }
             }
-            float sum = 0.0f;
-            // accumulators go to the halves in order
-            for (int u = other ? min(b, ob) : b; mine && u < e; ++u) {
-                const bool on = u >= b, also = other && u >= ob && u < oe;
-                if (x == 1 && also) ra.next();
-                if (on) {
-                    if (!(ok = both_wait(M.acc_full[x][rx.slot], rx.phase, M.log_full[x][rl.slot],
-                                         rl.phase, wc, 53)))
-                        break;
-                    rx.next();
-                    tc_fence_after();
-                    const uint32_t acc = base + C::T_ACC + ra.slot * 128 + half * 64;
-                    uint32_t s[2][32];
-                    tmem_ld_32x32b_x32(acc, s[0]);
-                    tmem_ld_32x32b_x32(acc + 32, s[1]);
+            // Accumulators go to the halves in order.  A tile's columns come in two steps of 32: the second one's
+            // are on their way while the first is worked on, the next tile's first while the second is.
+            float2 l[4] = {};
+            float sum = 0.0f;            // what l had every 32 units: short sums of sums
+            auto wait_tile = [&] {
+                const bool there = both_wait(M.acc_full[x][rx.slot], rx.phase, M.log_full[x][rl.slot],
+                                             rl.phase, wc, 53);
+                tc_fence_after();
+                return there;
+            };
+            auto pass = [&](int from, int to) {      // the other half's tiles of units [from, to)
+                for (int u = max(from, ob); u < min(to, oe); ++u) ra.next();
+            };
+            auto add = [&](const uint32_t(&v)[32], const float4* log) {
+                const float2 c2 = make_float2(p.c, p.c);
+#pragma unroll
+                for (int y = 0; y < 32; y += 4) {
+                    const float4 t = log[y / 4];
+                    const float2 w0 = __ffma2_rn(make_float2(as_f(v[y]), as_f(v[y + 1])), c2,
+                                                 make_float2(t.x, t.y));
+                    const float2 w1 = __ffma2_rn(make_float2(as_f(v[y + 2]), as_f(v[y + 3])), c2,
+                                                 make_float2(t.z, t.w));
+                    l[y / 4 % 2] = __fadd2_rn(l[y / 4 % 2],
+                                              make_float2(exp2_approx(w0.x), exp2_approx(w0.y)));
+                    l[2 + y / 4 % 2] = __fadd2_rn(
+                        l[2 + y / 4 % 2], make_float2(exp2_approx(w1.x), exp2_approx(w1.y)));
+                }
+            };
+            if (mine) {
+                uint32_t s[2][32];
+                if (other) pass(ob, b + x);
+                if (!(ok = wait_tile())) break;
+                tmem_ld_32x32b_x32(base + C::T_ACC + ra.slot * 128 + half * 64, s[0]);
+                for (int u = b; u < e; ++u) {
                     const int p0 = gap + u * tpt;         // first token's position less the warp's first key
                     const int rest = left - u * tpt;      // tokens from it on
                     const bool edge = p0 < 31 || rest < tpt ||
                                       (a.window > 0 && p0 + tpt - 1 >= a.window);
                     // columns [lo, hi) see the thread's key: those of the tokens from its own on, as far
                     // as the window reaches
-                    int lo = 0, hi = 128;
+                    uint32_t see[2] = {~0u, ~0u};
                     if (edge) {
-                        lo = min(max(lane - p0, 0), 128) * a.G;
-                        hi = min(rest, tpt);
+                        const int lo = min(max(lane - p0, 0), 128) * a.G;
+                        int hi = min(rest, tpt);
                         if (a.window > 0 && key >= a.n_sink) hi = min(hi, lane + a.window - p0);
                         hi = max(hi, 0) * a.G;
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const int first = 64 * half + 32 * i;
+                            see[i] = bits_below(hi - first) & ~bits_below(lo - first);
+                        }
                     }
                     const float4* log = reinterpret_cast<const float4*>(smem + C::OFF_LOG +
                                                                         (x * kLogSlots + rl.slot) * 512 +
                                                                         half * 256);
-                    const float2 c2 = make_float2(p.c, p.c);
-                    float2 l[4] = {};
-                    tmem_wait_ld();
-                    reg_fence(s[0]);
-                    reg_fence(s[1]);
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&M.acc_empty[ra.slot]);
-                    ra.next();
-                    if (edge) {
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const int first = 64 * half + 32 * i;
-                            const uint32_t see = bits_below(hi - first) & ~bits_below(lo - first);
+                    for (int i = 0; i < 2; ++i) {
+                        tmem_wait_ld();
+                        reg_fence(s[i]);
+                        if (i == 0) {
+                            tmem_ld_32x32b_x32(base + C::T_ACC + ra.slot * 128 + half * 64 + 32, s[1]);
+                        } else {
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&M.acc_empty[ra.slot]);
+                            ra.next();
+                            rx.next();
+                            rl.next();
+                            if (u + 1 < e) {
+                                if (other) pass(u + x, u + x + 1);
+                                if (!(ok = wait_tile())) break;
+                                tmem_ld_32x32b_x32(base + C::T_ACC + ra.slot * 128 + half * 64, s[0]);
+                            }
+                        }
+                        if (edge) {
 #pragma unroll
                             for (int y = 0; y < 32; ++y)
-                                s[i][y] = see >> y & 1u ? s[i][y] : 0xff800000u;
+                                s[i][y] = see[i] >> y & 1u ? s[i][y] : 0xff800000u;
                         }
+                        add(s[i], log + 8 * i);
                     }
+                    if (!ok) break;
+                    if ((u & 31) == 31) {
+                        const float2 l2 = __fadd2_rn(__fadd2_rn(l[0], l[1]), __fadd2_rn(l[2], l[3]));
+                        sum += l2.x + l2.y;
 #pragma unroll
-                    for (int y = 0; y < 64; y += 4) {
-                        const uint32_t(&v)[32] = s[y / 32];
-                        const float4 t = log[y / 4];
-                        const float2 w0 = __ffma2_rn(
-                            make_float2(as_f(v[y % 32]), as_f(v[y % 32 + 1])), c2,
-                            make_float2(t.x, t.y));
-                        const float2 w1 = __ffma2_rn(
-                            make_float2(as_f(v[y % 32 + 2]), as_f(v[y % 32 + 3])), c2,
-                            make_float2(t.z, t.w));
-                        l[y / 4 % 2] = __fadd2_rn(l[y / 4 % 2],
-                                                  make_float2(exp2_approx(w0.x), exp2_approx(w0.y)));
-                        l[2 + y / 4 % 2] = __fadd2_rn(
-                            l[2 + y / 4 % 2], make_float2(exp2_approx(w1.x), exp2_approx(w1.y)));
+                        for (int i = 0; i < 4; ++i) l[i] = make_float2(0.0f, 0.0f);
                     }
-                    const float2 l2 = __fadd2_rn(__fadd2_rn(l[0], l[1]), __fadd2_rn(l[2], l[3]));
-                    sum += l2.x + l2.y;
-                    rl.next();
                 }
-                if (x == 0 && also) ra.next();
+                if (!ok) break;
+                if (other) pass(e - 1 + x, oe);
+            } else if (other) {
+                pass(ob, oe);
             }
-            if (!ok) break;
-            if (other) {
-                // what the other half takes after this one's last unit
-                for (int u = max(ob, mine ? e : ob); u < oe; ++u) ra.next();
-            }
+            const float2 l2 = __fadd2_rn(__fadd2_rn(l[0], l[1]), __fadd2_rn(l[2], l[3]));
+            sum += l2.x + l2.y;
             // the two halves of the columns, in order
             if (half == 1) {
                 if (!(ok = all_wait(&M.half_empty[x], (joins++ & 1u) ^ 1u, wc, 55))) break;
