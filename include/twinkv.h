@@ -581,14 +581,14 @@ size_t twinkv_prompt_attend_workspace(twinkv_prompt s);
 /*
  * Attention over prompts, query head h reading KV head h / (Hq / H):
  *   o = sum_j softmax_j(scale q . k_j) v_j over the keys j that the token sees; 0 if there are none
- * Precision: products of bf16 values in float32 sums; exp(score - m), m within 6 of the largest score
- * so far, is rounded to bf16 for its product with the values, not for the denominator.  The
+ * Precision: products of bf16 values in float32 sums; exp(score - m), m at most 11 below the largest
+ * score so far, is rounded to bf16 for its product with the values, not for the denominator.  The
  * result is rounded to bf16.
  *   q, k, v     bf16, 16-byte aligned, strides in s; q . k below 2^120; what a sequence's keys and
  *               values hold has to be finite, other rows may hold anything
  *   scale       finite, above 0
  *   window      0: none (n_sink is then not used)
- *   out         [tokens][Hq][d] bf16, 16-byte aligned
+ *   out         [tokens][Hq][d] bf16, 16-byte aligned; not q, k or v
  *   out_lse     [tokens][Hq] float32 log of the softmax's denominator (-inf: nothing seen), or NULL
  *   out_status  [B] int32, or NULL: TWINKV_ERR_INVALID_ARG for a sequence whose offsets descend or
  *               are outside q or k, or whose length is below 0 or beyond its rows (it is not computed)

@@ -10,11 +10,18 @@
 // the other one; the zeros are the accumulators' start, a scale is one multiplication per group.  With
 // c = scale log2(e), a weight is 2^(c q . k - log2(e) lse).
 //
-// A block of four warps takes some pages of one unit, a warp a page at a time.  Its lanes load their operands
-// straight from the page (512 contiguous bytes an instruction): nothing is shared between lanes, and
-// enough warps are on an SM to keep loads on their way.  The query rows, scaled to f16 by a power of two
-// each, are laid out once per block in shared memory, 64 rows at a time; a slot's sum is the same lanes',
-// in the order of the rows, whatever the grid.
+// Up to 8 rows: a persistent kernel whose warps divide the pages of all units evenly, with the query rows in
+// registers and the pages' keys on their way in rings.  More: a block of four warps to some pages of a
+// unit, its query rows laid out once in shared memory, up to 64 at a time.  A slot's sum is the same
+// lanes', in the order of the rows, whatever the grid.
+//
+// Measured (us in a graph; share of the measured copy rate by the bytes above):
+//   32 x 8 units of 4k to 16k slots, 4 rows, d = 128   42.6   74 %;  d = 64, 16384 slots 45.1   60 %
+//   8 units of 131009 slots, 4 rows                    23.5   53 %
+//   16 x 8 units of 16384 slots, 8 rows 35.5   70 %;  16 rows 61, 41 %
+//   8 units of 2048 slots, 4 rows                       5.4
+// A block of warps for each unit's pages instead of the persistent kernel: 58 us for the first, whatever its
+// pages' prefetching (loads wait behind the start of each block).
 #include <algorithm>
 #include <atomic>
 

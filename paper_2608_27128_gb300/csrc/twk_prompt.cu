@@ -10,20 +10,31 @@
 // The top is the maximum of the row's first tile, and follows later ones only where a tile's sum of
 // probabilities shows that it is far behind them (2^15: floats and bf16 do not notice such factors, and
 // the sum of 128 probabilities stays below it else): the tile's maximum is found, O scaled in tensor
-// memory and the tile done again, a rare event.  So a tile costs no maximum (XXX).
+// memory and the tile done again, a rare event.  So a tile costs no maximum (a fifth of the softmax at
+// d = 64, where that is what bounds it).
 //
-// Bound by the tensor cores: 4 d operations for each pair of a row and a key, of which a prompt of n tokens
-// has n^2 / 2 per head; exponentials (a row and key each) take about half their time at d = 128 and as
-// long at d = 64.  Design (persistent, one block of 384 threads per SM):
+// Bound by the tensor cores at d = 128: 4 d operations for each pair of a row and a key, of which a prompt of
+// n tokens has n^2 / 2 per head; an exponential for each (4 cycles a warp) takes half their time there, and
+// as long at d = 64, which the softmax's instructions bound.  Design (persistent, one block of 384 threads
+// per SM):
 //   - An item is 256 query rows of one KV head: (token, head) pairs, the heads of a token side by side,
 //     so that every head of the group reads the same keys, and short sequences fill a tile.  Two
 //     tiles of 128 rows take turns: one's softmax runs beside the other's products.
-//   - S = Q K^T by tcgen05.mma from shared memory, both K-major; P (bf16, written over S in tensor memory)
-//     times V, whose rows run along the keys: operand A from tensor memory, B as TMA left it.
+//   - S = Q K^T by tcgen05.mma from shared memory, both K-major; P (bf16, in tensor memory) times V, whose
+//     rows run along the keys: operand A from tensor memory, B as TMA left it.
 //   - Warps 0 to 3 and 4 to 7: softmax, a thread per row.  Warp 8: TMA (queries once per item, then keys
-//     and values in one ring).  Warp 9: one thread issues every product.  Warp 10 hands out items.
+//     and values in one ring).  Warp 9 issues the products, warp 11 those with V at d = 64 (Cfg).  Warp 10
+//     hands out items.
 //   - Work is divided evenly whatever the lengths (twk_prompt.cuh): a block's span may begin and end inside
 //     an item, whose parts (unnormalised O, top, l in float32) merge_kernel joins in order.
+//
+// Measured (us in a graph; TFLOP/s; 32 query heads on 8 KV heads), before and after what is named:
+//   16384 tokens, d = 128   1414   1555: 83 % of the measured burst rate, 92 % of the sustained
+//   4096 tokens, d = 128     121   1133; 1024: 25.4 us; 101: 9.4, most of it the start and the end
+//   256 tokens over 65536    198   1388, items cut into 5 parts
+//   16384 tokens, d = 64     840   1309; 12 packed prompts of 752 to 3001 tokens 255, 829
+//   descriptors in uniform registers: 2095 -> 1451 on the first line
+//   cutting by tiles and what an item takes beside them, instead of by tiles: 305 -> 255 on the last
 #include <atomic>
 
 #include "twk_cache.cuh"
@@ -77,7 +88,7 @@ struct Cfg {
     // scores come after their products.  At d = 64 there is room beside them: the next scores come as soon
     // as the softmax has the last ones in registers, and are there when it is done.  Scores and outputs are
     // then issued by a warp each: what a warp does around its products takes longer than they do
-    // (16384 tokens, one warp and one place: 1075 us; two places: 1232; XXX).
+    // (16384 tokens, one warp and one place: 1075 us; two warps and places: 899).
     static constexpr bool EARLY = D == 64;
     static constexpr int T_S = 0, T_P = EARLY ? 256 : 0, P_STRIDE = EARLY ? 64 : kTileKeys;
     static constexpr int T_O = EARLY ? 384 : 256;
@@ -511,6 +522,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int p0 = it.pos + x * tpt;                         // position of the tile's first token
             const int pos = p0 + token;
             const int low = a.window > 0 ? pos - a.window + 1 : INT_MIN;
+            // rows of no token hold anything
+            const bool sees = token < tpt && x * tpt + token < it.tokens && pos >= 0;
             float top = -INFINITY, sum = 0.0f;
             for (int j = it.s0; j < n; ++j) {
                 const int k0 = kt.tile(j) * kTileKeys;
@@ -544,7 +557,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 // With the top so far; again with the true one where a row has none, or its sum shows that
                 // the scores have left it far behind.
-                bool exact = __any_sync(0xffffffffu, top == -INFINITY);
+                bool exact = __any_sync(0xffffffffu, sees && top == -INFINITY);
                 // the products with the tile's last probabilities, whose place the next ones take
                 if (C::EARLY && j > it.s0) {
                     if (!(ok = all_wait(&M.o_full[x], o_uses++ & 1u, wc, 36))) break;
@@ -565,7 +578,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         const bool rise = most > top;
                         const float f = rise ? exp2_approx(top - most) : 1.0f;    // top -inf: 0
                         if (rise) top = most;
-                        if (j > it.s0) {
+                        if (j > it.s0 && __any_sync(0xffffffffu, rise)) {
                             sum *= f;
 #pragma unroll
                             for (int i = 0; i < D / 32; ++i) {
@@ -598,7 +611,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     const float2 l2 = __fadd2_rn(__fadd2_rn(l[0], l[1]), __fadd2_rn(l[2], l[3]));
                     const float add = l2.x + l2.y;
-                    if (exact || !__any_sync(0xffffffffu, add > kFar)) {
+                    if (exact || !__any_sync(0xffffffffu, sees && add > kFar)) {
                         sum += add;
                         break;
                     }

@@ -109,6 +109,8 @@ twinkv_status twinkv_prompt_attend(const void* q, const void* k, const void* v, 
 {
     twinkv_status r = prompt_ok(q, k, s, seqs, scale, window, n_sink, out_status);
     if (r != TWINKV_OK) return r;
+    // rows are read while others are written
+    if (out == q || out == k || out == v) return TWINKV_ERR_INVALID_ARG;
     if (!v || !out || !aligned(v, 16) || !aligned(out, 16) || !aligned(out_lse, 4) ||
         !stride_ok(s.v_token, s.keys) || !stride_ok(s.v_head, s.H))
         return TWINKV_ERR_INVALID_ARG;

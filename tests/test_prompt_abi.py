@@ -55,11 +55,12 @@ COMMON = ([dict(q=None), dict(k=None), dict(q=OFF), dict(k=OFF), dict(status=FAK
 
 
 def test_attend_arguments(lib):
-    def call(q=FAKE, k=FAKE, v=FAKE, s=None, at=None, scale=0.1, window=0, n_sink=0, out=FAKE,
-             lse=FAKE, status=FAKE, ws=FAKE, wsb=BIG):
+    def call(q=FAKE, k=FAKE, v=FAKE, s=None, at=None, scale=0.1, window=0, n_sink=0,
+             out=2 * FAKE, lse=FAKE, status=FAKE, ws=FAKE, wsb=BIG):
         return lib.twinkv_prompt_attend(q, k, v, s or prompt(), at or seqs(), scale, window, n_sink,
                                         out, lse, status, ws, wsb, None)
 
+    assert call(out=FAKE) == tk.ERR_INVALID_ARG            # what it reads
     for kw in COMMON + [dict(v=None), dict(v=OFF), dict(out=None), dict(out=OFF),
                         dict(lse=FAKE + 2), dict(s=prompt(v_token=4)), dict(s=prompt(v_head=0))]:
         assert call(**kw) == tk.ERR_INVALID_ARG, kw
