@@ -472,7 +472,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (at.take < at.length) {
                         // heads and middles in slot 2 c, the item that begins in the block in 2 c + 1
                         it.slot = 2 * static_cast<int>(blockIdx.x) + (at.off == 0 ? 1 : 0);
-                        if (at.off == 0) join = make_int4(at.parts(), it.t0, it.tokens, it.head);
+                        if (at.off == 0) join = make_int4(at.parts(a), it.t0, it.tokens, it.head);
                     }
                     ok = mbar_wait(&M.item_empty[ri.slot], ri.phase ^ 1u, wc, 31);
                     if (!ok) break;
@@ -777,8 +777,10 @@ __global__ void __launch_bounds__(32 * kMergeWarps)
         a.out_lse[at] = sum > 0.0f ? fmaf(top, 0.6931471805599453f, logf(sum)) : -INFINITY;
 }
 
-// An item that reads this many keys or fewer is never cut.
-constexpr int whole_keys(int d) { return (2 * kSnap + 1 - RowPairs::more(d)) * kTileKeys; }
+// Where no item is longer than 13 units none is cut: the longest takes no longer than shares and a second
+// kernel (1024 tokens, d = 128: 25.4 -> 21.6 us).
+constexpr int kSnapFew = 6;
+constexpr int whole_keys(int d) { return (2 * kSnapFew + 1 - RowPairs::more(d)) * kTileKeys; }
 
 template <int D>
 cudaError_t launch(const PromptArgs& a, int sms, const WaitFacts& w, cudaStream_t st)
@@ -805,9 +807,10 @@ cudaError_t launch(const PromptArgs& a, int sms, const WaitFacts& w, cudaStream_
         !encode_rows(&v, a.v, D, a.s.H, a.s.keys, a.s.v_head, a.s.v_token, 1, kTileKeys))
         return cudaErrorInvalidValue;
     AttendKernelArgs p{};
-    p.a = a;
-    p.c = a.scale * 1.4426950408889634f;
     const bool shared = a.s.keys > whole_keys(D);
+    p.a = a;
+    p.a.snap = shared ? kSnap : kSnapFew;
+    p.c = a.scale * 1.4426950408889634f;
     if (shared) {
         p.join = static_cast<int4*>(a.ws);
         p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(a.ws) + 16 * kPromptBlocks);

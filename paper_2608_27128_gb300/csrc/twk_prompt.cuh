@@ -125,12 +125,12 @@ struct Ring {
 // ---- work among blocks
 //
 // A call's items (of a sequence and KV head) follow one another, each as long as W::length says: its tiles,
-// and up to kSnap more for what it takes beside them, at least 1.  All units are cut into even spans, one for each block.  An item that spans
-// share is done in parts, which a second kernel joins in order: what is cut where depends on the sizes
-// alone.  A cut within kSnap units of an item's end moves there, since a part costs about as much as so
-// many units.
+// and up to kSnap more for what it takes beside them, at least 1.  All units are cut into even spans, one for
+// each block.  An item that spans share is done in parts, which a second kernel joins in order: what is cut
+// where depends on the sizes alone.  A cut within a.snap units of an item's end moves there, since a part
+// costs about as much as so many units (and a cut that stays inside an item is at one of its tiles).
 
-constexpr int kSnap = 3;           // so a cut that stays inside an item is at one of its tiles
+constexpr int kSnap = 3;            // least a.snap
 constexpr int kChunks = 256;        // groups of sequences with their sums in shared memory
 
 // x / y, both above 0
@@ -342,9 +342,9 @@ struct Walk {
         }
         begin = g - off;
         more = true;
-        if (off <= kSnap) off = 0;
-        else if (length - off <= kSnap) advance(a);
-        part();
+        if (off <= a.snap) off = 0;
+        else if (length - off <= a.snap) advance(a);
+        part(a);
     }
 
     // The part after this one, by any one lane.
@@ -352,14 +352,14 @@ struct Walk {
     {
         if (off + take < length) more = false;
         else advance(a);
-        part();
+        part(a);
     }
 
     // Blocks that share the item, this one being the first.
-    __device__ __forceinline__ int parts() const
+    __device__ __forceinline__ int parts(const PromptArgs& a) const
     {
         int n = 1;
-        while (cut(blockIdx.x + n) + kSnap < begin + length) ++n;
+        while (cut(blockIdx.x + n) + a.snap < begin + length) ++n;
         return n;
     }
 
@@ -390,13 +390,13 @@ private:
         length = W::length(a, s, item);
     }
     // how far the span takes the item
-    __device__ __forceinline__ void part()
+    __device__ __forceinline__ void part(const PromptArgs& a)
     {
         if (!more) return;
         take = length - off;
         if (end < begin + length) {
-            if (end - begin <= kSnap) more = false;
-            else if (begin + length - end > kSnap) take = static_cast<int>(end - begin) - off;
+            if (end - begin <= a.snap) more = false;
+            else if (begin + length - end > a.snap) take = static_cast<int>(end - begin) - off;
         }
     }
 };

@@ -17,6 +17,7 @@ struct PromptArgs {
     twinkv_sequences seqs;
     int G;                         // query heads per KV head
     int tile_tokens;               // 128 / G: tokens of a tile of query rows
+    int snap;                      // how the work is cut, see twk_prompt.cuh
     float scale;
     int window, n_sink;            // window 0: none
     int* out_status;               // [B] or null

@@ -361,7 +361,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         // heads and middles in slot 2 c, the item that begins in the block in 2 c + 1
                         it.slot = 2 * static_cast<int>(blockIdx.x) + (at.off == 0 ? 1 : 0);
                         if (at.off == 0)
-                            join = make_int4(at.parts(), it.j0 + it.j, min(kPairKeys, it.m - it.j),
+                            join = make_int4(at.parts(a), it.j0 + it.j, min(kPairKeys, it.m - it.j),
                                              it.head);
                     }
                     ok = mbar_wait(&M.item_empty[ri.slot], ri.phase ^ 1u, wc, 48);
@@ -662,6 +662,7 @@ cudaError_t launch(const PromptArgs& a, int sms, const WaitFacts& w, cudaStream_
         return cudaErrorInvalidValue;
     WeightsKernelArgs p{};
     p.a = a;
+    p.a.snap = kSnap;
     p.c = a.scale * 1.4426950408889634f;
     const int tokens = a.last > 0 ? std::min(a.last, a.s.tokens) : a.s.tokens;
     const bool shared = tokens > whole_tokens(a);
