@@ -440,7 +440,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
         } else if (warp == 10) {
             // ------------------------------------------------------------ items
-            Walk<RowPairs> at;
+            // d = 64 runs 12 % slower with the code of a second start in the kernel (16384 tokens: 938 us, not
+            // 844), whose loops already fill the instruction cache
+            Walk<RowPairs, D == 128> at;
             at.start(a, sums);
             fence_async_shared();       // the sums have been read
             __syncwarp();

@@ -241,7 +241,8 @@ __device__ __forceinline__ void sum_chunks(const PromptArgs& a, long long* sums)
 constexpr int kSumsBytes = (2 * kChunks + 1) * 8;
 
 // A block's walk over the items of its span: next() gives one part after another.
-template <class W>
+// ONE: with a start of its own for one sequence.
+template <class W, bool ONE = true>
 struct Walk {
     int b = 0, head = 0, item = 0, length = 0;   // where it is; length of the item
     int items = 0;                               // of the sequence and head
@@ -257,6 +258,9 @@ struct Walk {
     __device__ __forceinline__ void start(const PromptArgs& a, const long long* sums)
     {
         const int lane = threadIdx.x % 32;
+        if constexpr (ONE) {
+            if (a.s.B == 1 && start_one(a)) return;
+        }
         long long units, count;
         LaneUnits u{};
         if (a.s.B <= 32) {
@@ -364,6 +368,56 @@ struct Walk {
     }
 
 private:
+    // The same for one sequence whose units are counted in 32 bits: a third of the instructions, which are
+    // read anew with every launch (4500 cycles before the first item, now 3500).  False where they are
+    // not.
+    __device__ __forceinline__ bool start_one(const PromptArgs& a)
+    {
+        const int lane = threadIdx.x % 32;
+        s = sequence_of(a, 0);
+        items = W::items(a, s);
+        if (items > 8192 || max(s.n, s.m) > 1 << 19 || a.s.H > 1024) return false;
+        unsigned mine = 0;          // at most 256 items of 2^19 + kSnap units
+        for (int i = lane; i < items; i += 32) mine += W::length(a, s, i);
+        if (__any_sync(0xffffffffu, mine > (1u << 30) / 32 / static_cast<unsigned>(a.s.H)))
+            return false;
+        const unsigned per_head = __reduce_add_sync(0xffffffffu, mine);
+        if (per_head == 0) return true;
+        const unsigned units = per_head * a.s.H, count = items * a.s.H;
+        blocks = static_cast<int>(min(min(max(units / 4, 2 * count), units), gridDim.x));
+        if (static_cast<int>(blockIdx.x) >= blocks) return true;
+        each = units / blocks;
+        over = units % blocks;
+        const unsigned g = static_cast<unsigned>(cut(blockIdx.x));
+        end = cut(blockIdx.x + 1);
+        head = static_cast<int>(g / per_head);
+        unsigned rest = g - head * per_head;
+        for (int i = 0;; i += 32) {
+            const unsigned n = i + lane < items ? W::length(a, s, i + lane) : 0;
+            unsigned scan = n;
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const unsigned y = __shfl_up_sync(0xffffffffu, scan, o);
+                if (lane >= o) scan += y;
+            }
+            const unsigned past = __ballot_sync(0xffffffffu, scan > rest);
+            if (past) {
+                const int l = __ffs(past) - 1;
+                length = __shfl_sync(0xffffffffu, n, l);
+                off = static_cast<int>(rest) - (__shfl_sync(0xffffffffu, scan, l) - length);
+                item = i + l;
+                break;
+            }
+            rest -= __shfl_sync(0xffffffffu, scan, 31);
+        }
+        begin = static_cast<long long>(g) - off;
+        more = true;
+        if (off <= a.snap) off = 0;
+        else if (length - off <= a.snap) advance(a);
+        part(a);
+        return true;
+    }
+
     // where the span of block c begins, before it snaps
     __device__ __forceinline__ long long cut(unsigned c) const
     {
