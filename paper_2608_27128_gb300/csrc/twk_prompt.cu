@@ -29,10 +29,10 @@
 //     an item, whose parts (unnormalised O, top, l in float32) merge_kernel joins in order.
 //
 // Measured (us in a graph; TFLOP/s; 32 query heads on 8 KV heads), before and after what is named:
-//   16384 tokens, d = 128   1414   1555: 83 % of the measured burst rate, 92 % of the sustained
-//   4096 tokens, d = 128     121   1133; 1024: 25.4 us; 101: 9.4, most of it the start and the end
-//   256 tokens over 65536    198   1388, items cut into 5 parts
-//   16384 tokens, d = 64     840   1309; 12 packed prompts of 752 to 3001 tokens 255, 829
+//   16384 tokens, d = 128   1382   1591: 85 % of the measured burst rate, 94 % of the sustained
+//   4096 tokens, d = 128     115   1195; 2048: 44 us, 1024: 21; 101: 8.8, most of it the start and the end
+//   256 tokens over 65536    196   1401, items cut into 5 parts
+//   16384 tokens, d = 64     843   1304; 12 packed prompts of 752 to 3001 tokens 252, 838
 //   descriptors in uniform registers: 2095 -> 1451 on the first line
 //   cutting by tiles and what an item takes beside them, instead of by tiles: 305 -> 255 on the last
 #include <atomic>
@@ -706,7 +706,9 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 // Joins the parts of an item that several blocks took, in order: a block per block that such an item
-// begins in and 32 rows of it, a warp for every eighth group of four values.
+// begins in and 32 rows of it, a warp for every eighth group of four values.  Rows leave through shared
+// memory, whole ones side by side (4096 tokens, 40 MB of parts: 7 us beside the rest, with 8 bytes of 32 rows
+// in a store 11).
 constexpr int kMergeWarps = 8;
 
 template <int D>
@@ -714,6 +716,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps)
     merge_kernel(const __grid_constant__ AttendKernelArgs p)
 {
     constexpr int kVec = D / 4 / kMergeWarps;
+    __shared__ __align__(16) uint8_t rows[32][2 * D + 16];
     wait_for_previous();
     const PromptArgs& a = p.a;
     const int4 join = p.join[blockIdx.x];
@@ -722,10 +725,10 @@ __global__ void __launch_bounds__(32 * kMergeWarps)
     const int r = blockIdx.y * 32 + lane;
     const int x = r / kTileRows, row = r % kTileRows, tpt = a.tile_tokens;
     const int token = row / a.G;
-    if (token >= tpt || x * tpt + token >= join.z) return;
+    const bool held = token < tpt && x * tpt + token < join.z;
     float top = -INFINITY, sum = 0.0f, acc[kVec][4] = {};
     constexpr int kAhead = 4;
-    for (int k0 = 0; k0 < join.x; k0 += kAhead) {
+    for (int k0 = 0; held && k0 < join.x; k0 += kAhead) {
         float m[kAhead], l[kAhead];
         float4 y[kAhead][kVec];
 #pragma unroll
@@ -767,16 +770,26 @@ __global__ void __launch_bounds__(32 * kMergeWarps)
             }
         }
     }
-    const int64_t at = static_cast<int64_t>(join.y + x * tpt + token) * a.s.Hq + join.w * a.G +
-                       row - token * a.G;
+    const int64_t first = static_cast<int64_t>(join.y) * a.s.Hq + join.w * a.G;
+    const int at = held ? (x * tpt + token) * a.s.Hq + row - token * a.G : -1;
     const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
 #pragma unroll
     for (int v = 0; v < kVec; ++v)
-        *reinterpret_cast<uint2*>(a.out + at * D + 4 * (warp + kMergeWarps * v)) =
+        *reinterpret_cast<uint2*>(rows[lane] + 8 * (warp + kMergeWarps * v)) =
             make_uint2(bf16_pair(acc[v][0] * inv, acc[v][1] * inv),
                        bf16_pair(acc[v][2] * inv, acc[v][3] * inv));
-    if (warp == 0 && a.out_lse)
-        a.out_lse[at] = sum > 0.0f ? fmaf(top, 0.6931471805599453f, logf(sum)) : -INFINITY;
+    if (warp == 0 && held && a.out_lse)
+        a.out_lse[first + at] = sum > 0.0f ? fmaf(top, 0.6931471805599453f, logf(sum)) : -INFINITY;
+    __syncthreads();
+    constexpr int kRowLanes = D / 8;
+#pragma unroll
+    for (int i = 0; i < 32 * kRowLanes; i += 32 * kMergeWarps) {
+        const int n = (i + static_cast<int>(threadIdx.x)) / kRowLanes, e = threadIdx.x % kRowLanes;
+        const int to = __shfl_sync(0xffffffffu, at, n);
+        if (to >= 0)
+            *reinterpret_cast<uint4*>(a.out + (first + to) * D + 8 * e) =
+                *reinterpret_cast<const uint4*>(rows[n] + 16 * e);
+    }
 }
 
 // Where no item is longer than 13 units none is cut: the longest takes no longer than shares and a second

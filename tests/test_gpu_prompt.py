@@ -78,6 +78,14 @@ def test_chunks_of_long_prompts(d, n, m):
 
 
 @pytest.mark.parametrize("d", [64, 128])
+def test_shared_items(d):
+    """Prompts whose items of all lengths are cut where the division falls, odd groups among them."""
+    check(Prompts([(1700, 1700), (40, 40)], 6, 2, d, device(), seed=3))
+    check(Prompts([(130, 130), (1, 1601), (1900, 1950)], 4, 1, d, device(), seed=4, gap=3), window=700,
+          n_sink=130)
+
+
+@pytest.mark.parametrize("d", [64, 128])
 def test_many_short_sequences(d):
     rng = np.random.default_rng(d)
     seqs = [(int(n), int(n)) for n in rng.integers(0, 4, 300)] + [(200, 200)]
