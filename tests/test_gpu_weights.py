@@ -347,6 +347,26 @@ def test_policy_ties_and_odd_values():
     check_policy(score, [700] * len(rows), n_sink=10, n_recent=10 ** 6)
 
 
+@pytest.mark.parametrize("N", [100, 196, 197, 4100, 16385, 40000])
+def test_policy_ranges(N):
+    """Scores over the whole range of floats and in the smallest corner of it, one far from all others
+    among them; as few between the protected positions as are compared with one another, and one more."""
+    rng = np.random.default_rng(N)
+    big = np.float32(3e38)
+    near = 1.0 + rng.integers(0, 2000, N) * 2.0 ** -23
+    rows = [rng.standard_normal(N) * big / 8, -np.abs(rng.standard_normal(N)),
+            np.where(rng.random(N) < 0.2, np.nan, -np.abs(rng.standard_normal(N)) * 1e30),
+            rng.choice([np.nan, -np.inf, -big], N), rng.choice([np.inf, big], N),
+            near, np.where(np.arange(N) == N // 2, np.inf, near),
+            np.where(np.arange(N) == N // 2, np.nan, near),
+            np.where(np.arange(N) == N // 2, -np.inf, rng.integers(0, 9, N))]
+    score = np.array(rows, np.float32)
+    for budget in (69, 70, N // 2, N - 7, N - 1):
+        check_policy(score, [min(budget, N)] * len(rows))
+    check_policy(score, [N // 3] * len(rows), n_sink=0, n_recent=0)
+    check_policy(score, [N // 3] * len(rows), n_sink=N // 3 - 1, n_recent=0)
+
+
 def test_policy_data_errors():
     rng = np.random.default_rng(2)
     check_policy(heavy(rng, 6, 500), [-1, 501, 100, 100, 100, 100],
