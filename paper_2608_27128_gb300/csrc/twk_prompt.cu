@@ -31,7 +31,7 @@
 // Measured (us in a graph; TFLOP/s; 32 query heads on 8 KV heads), before and after what is named:
 //   16384 tokens, d = 128   1382   1591: 85 % of the measured burst rate, 94 % of the sustained
 //   4096 tokens, d = 128     115   1195; 2048: 44 us, 1024: 21; 101: 8.8, most of it the start and the end
-//   256 tokens over 65536    196   1401, items cut into 5 parts
+//   256 tokens over 65536    195   1405, items cut into 5 parts
 //   16384 tokens, d = 64     843   1304; 12 packed prompts of 752 to 3001 tokens 252, 838
 //   descriptors in uniform registers: 2095 -> 1451 on the first line
 //   cutting by tiles and what an item takes beside them, instead of by tiles: 305 -> 255 on the last

@@ -23,13 +23,16 @@
 //     an item that blocks share, in order.
 //
 // Measured (us in a graph; TFLOP/s; 32 query heads on 8 KV heads):
-//   every token of 16384, d = 128   776   1416: 75 % of the measured burst rate
-//   every token of 8192             207   1329, of 4096 65, of 2048 26; of 8192 at d = 64 210
-//   the last 32 of 16384            16.5  2.1 us an item of 256 keys, three to four of them a block
+//   every token of 16384, d = 128   788   1395: 74 % of the measured burst rate
+//   every token of 8192             210   1309, of 4096 64.5, of 2048 25.3; of 8192 at d = 64 209
+//   the last 32 of 16384            16.3  four items of 256 keys a block at most, one after another: 4300
+//                                         cycles each for moving keys, products, sums and their joining
 //   six prompts of up to 3001, window of 1024, d = 64   91: most tiles are at an edge
 // With 16 warps a unit of two tiles takes about 1900 cycles where exponentials alone take 1050: the four warps
 // of a quarter of the SM wait for tiles, and load them, at the same time, since there are three
-// accumulators for four.
+// accumulators for four.  The next item's keys moved beside an item's last sums: 16.3 -> 15.7 us on the fourth
+// line, 210 -> 218 on the second, for the registers.  One ring for keys and queries, with keys of three
+// items on their way: 17.2, the keys are not what items wait for.
 #include <atomic>
 
 #include "twk_prompt.cuh"
