@@ -56,7 +56,9 @@ def test_warpgroups_trade_what_the_launch_has(reports, d, src, kernel, others, s
 @pytest.mark.parametrize("src", ["twk_prompt.cu", "twk_weights.cu"])
 def test_merges_do_not_spill(reports, src):
     hits = {k: v for k, v in reports[src].items() if re.search(r"\dmerge_", k)}
-    assert hits and all(spill == 0 and smem == 0 for _, spill, smem in hits.values())
+    assert hits and all(spill == 0 for _, spill, _ in hits.values())
+    for regs, _, smem in hits.values():               # two blocks an SM at least, rows in passing
+        assert 2 * _registers(regs, 256) <= SM_REGS and 2 * (smem + 1024) <= SM_SMEM
 
 
 @pytest.mark.parametrize("d", [64, 128])
@@ -73,9 +75,11 @@ def test_cache_weights_blocks(reports, d):
     assert spill <= 16 and 4 * _registers(regs, 128) <= SM_REGS and 4 * (smem + 1024) <= SM_SMEM
 
 
-@pytest.mark.parametrize("v,threads", [(8, 768), (16, 512), (32, 512), (32, 1024)])
-def test_policy_blocks(reports, v, threads):
+@pytest.mark.parametrize("v,threads,blocks", [(8, 512, 3), (16, 512, 3), (32, 512, 2), (32, 1024, 1)])
+def test_policy_blocks(reports, v, threads, blocks):
+    """As many blocks as the launch counts on share an SM."""
     regs, spill, smem = _one(reports["twk_weight_policy.cu"],
-                             rf"weight_policy_kernelILi{v}ELi{threads}E")
-    assert spill <= 16 and _registers(regs, threads) <= SM_REGS
+                             rf"weight_policy_kernelILi{v}ELi{threads}ELi{blocks}E")
+    assert spill <= 16 and blocks * _registers(regs, threads) <= SM_REGS
     assert smem + 4 * v * threads <= BLOCK_SMEM
+    assert blocks * (smem + 4 * v * threads + 1024) <= SM_SMEM
