@@ -52,6 +52,7 @@ constexpr int kAccs = 3, kItemSlots = 4;
 // start: every tile three and more before it, of either half, is then released.  So the half's tile
 // kAccs before it, at least as far back, is released, and the one before that, whose slot is taken, is done.
 constexpr int kLogSlots = kAccs + 1;
+static_assert((kLogSlots & (kLogSlots - 1)) == 0);
 
 // The tokens that see some key of [j, last]: the first, and the end; of those that count.
 __device__ __forceinline__ int2 tokens_of(const PromptArgs& a, const Sequence& s, int j, int last)
@@ -112,8 +113,9 @@ static_assert(sizeof(Item) == 64);
 
 struct Misc {
     uint64_t k_full[2], k_empty[2], kt_full[2], half_full[2], half_empty[2], drain;
-    // acc_full: by half and its own count, since a half that skips another's phases would lose track
-    uint64_t acc_full[2][kAccs], acc_empty[kAccs], log_full[2][kLogSlots];
+    // acc_full: products and lse of a tile; by half and its own count, since a half that skips another's
+    // phases would lose track
+    uint64_t acc_full[2][kAccs], acc_empty[kAccs];
     uint64_t q_full[8], q_empty[8], item_full[kItemSlots], item_empty[kItemSlots];
     Item items[kItemSlots];
     uint32_t tmem;
@@ -130,15 +132,6 @@ struct WeightsKernelArgs {
     int* err;
     unsigned long long timeout_ns;
 };
-
-// Both barriers' phases, as all_wait.
-__device__ __forceinline__ bool both_wait(uint64_t& a, uint32_t a_parity, uint64_t& b, uint32_t b_parity,
-                                          const WaitCtl& w, int where)
-{
-    if (__all_sync(0xffffffffu, mbar_test2(smem_u32(&a), a_parity, smem_u32(&b), b_parity) != 0))
-        return true;
-    return all_wait(&b, b_parity, w, where + 1) && all_wait(&a, a_parity, w, where);
-}
 
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -164,13 +157,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         mbar_init(&M.drain, 1);
         for (int i = 0; i < kAccs; ++i) {
-            mbar_init(&M.acc_full[0][i], 1);
-            mbar_init(&M.acc_full[1][i], 1);
+            mbar_init(&M.acc_full[0][i], 2);         // the products and the lse
+            mbar_init(&M.acc_full[1][i], 2);
             mbar_init(&M.acc_empty[i], 8);
-        }
-        for (int i = 0; i < kLogSlots; ++i) {
-            mbar_init(&M.log_full[0][i], 1);
-            mbar_init(&M.log_full[1][i], 1);
         }
         for (int i = 0; i < C::STAGES; ++i) {
             mbar_init(&M.q_full[i], 1);
@@ -386,8 +375,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int b = lane; b < a.s.B; b += 32)
                     a.out_status[b] = sequence_of(a, b).ok ? TWINKV_OK : TWINKV_ERR_INVALID_ARG;
             Ring<kItemSlots> ri;
-            Ring<kLogSlots> rl[2];
-            Ring<kAccs> ra;
+            Ring<kAccs> ra, rx[2];
+            int log_at[2] = {};
             bool ok = true;
             int token[4], sub[4];                    // of the lane's columns
 #pragma unroll
@@ -435,10 +424,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                         if (!(ok = all_wait(&M.acc_empty[ra.slot], ra.phase ^ 1u, wc, 50))) continue;
                         ra.next();
                         *reinterpret_cast<float4*>(smem + C::OFF_LOG +
-                                                   (x * kLogSlots + rl[x].slot) * 512 + lane * 16) = w;
+                                                   (x * kLogSlots + log_at[x]) * 512 + lane * 16) = w;
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(&M.log_full[x][rl[x].slot]);
-                        rl[x].next();
+                        if (lane == 0) mbar_arrive(&M.acc_full[x][rx[x].slot]);
+                        log_at[x] = (log_at[x] + 1) % kLogSlots;
+                        rx[x].next();
                     }
 #pragma unroll
                     for (int k = 0; k < 4; ++k) y[k] = next[k];
@@ -458,8 +448,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int row = q * 32 + lane;
         const uint32_t base = tmem + (static_cast<uint32_t>(q * 32) << 16);
         Ring<kItemSlots> ri;
-        Ring<kLogSlots> rl;
         Ring<kAccs> ra, rx;
+        int log_at = 0;
         float* halves = reinterpret_cast<float*>(smem + C::OFF_HALF) + x * kTileKeys + row;
         uint32_t k_uses = 0, joins = 0;
         bool ok = true;
@@ -508,8 +498,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             float2 l[4] = {};
             float sum = 0.0f;            // what l had every 32 units: short sums of sums
             auto wait_tile = [&] {
-                const bool there = both_wait(M.acc_full[x][rx.slot], rx.phase, M.log_full[x][rl.slot],
-                                             rl.phase, wc, 53);
+                const bool there = all_wait(&M.acc_full[x][rx.slot], rx.phase, wc, 53);
                 tc_fence_after();
                 return there;
             };
@@ -556,7 +545,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                     }
                     const float4* log = reinterpret_cast<const float4*>(smem + C::OFF_LOG +
-                                                                        (x * kLogSlots + rl.slot) * 512 +
+                                                                        (x * kLogSlots + log_at) * 512 +
                                                                         half * 256);
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
@@ -570,9 +559,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                             if (lane == 0) mbar_arrive(&M.acc_empty[ra.slot]);
                             ra.next();
                             rx.next();
-                            rl.next();
+                            log_at = (log_at + 1) % kLogSlots;
                             if (u + 1 < e) {
-                                if (other) pass(u + x, u + x + 1);
+                                if (u + x >= ob && u + x < oe) ra.next();       // the other half's tile
                                 if (!(ok = wait_tile())) break;
                                 tmem_ld_32x32b_x32(base + C::T_ACC + ra.slot * 128 + half * 64, s[0]);
                             }
