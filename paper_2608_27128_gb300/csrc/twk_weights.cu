@@ -23,16 +23,17 @@
 //     an item that blocks share, in order.
 //
 // Measured (us in a graph; TFLOP/s; 32 query heads on 8 KV heads):
-//   every token of 16384, d = 128   788   1395: 74 % of the measured burst rate
-//   every token of 8192             210   1309, of 4096 64.5, of 2048 25.3; of 8192 at d = 64 209
-//   the last 32 of 16384            16.3  four items of 256 keys a block at most, one after another: 4300
+//   every token of 16384, d = 128   754   1458: 77 % of the measured burst rate
+//   every token of 8192             198   1389, of 4096 61, of 2048 24.3; of 8192 at d = 64 188
+//   the last 32 of 16384            16    four items of 256 keys a block at most, one after another: 4300
 //                                         cycles each for moving keys, products, sums and their joining
-//   six prompts of up to 3001, window of 1024, d = 64   91: most tiles are at an edge
-// With 16 warps a unit of two tiles takes about 1900 cycles where exponentials alone take 1050: the four warps
-// of a quarter of the SM wait for tiles, and load them, at the same time, since there are three
-// accumulators for four.  The next item's keys moved beside an item's last sums: 16.3 -> 15.7 us on the fourth
-// line, 210 -> 218 on the second, for the registers.  One ring for keys and queries, with keys of three
-// items on their way: 17.2, the keys are not what items wait for.
+//   six prompts of up to 3001, window of 1024, d = 64   85: most tiles are at an edge
+// A unit of two tiles takes about 1750 cycles where exponentials alone take 1050: the warps issue in more than
+// half of the cycles, so what surrounds a tile counts (one barrier for a tile's products and lse instead
+// of two, rings without phases: 210 -> 202 us on the second line, 209 -> 188 at d = 64).  All sixteen warps
+// on one tile, a quarter of the columns each: 258.  The next item's keys moved beside an item's last
+// sums: 16.3 -> 15.7 on the third line, 210 -> 218 on the second, for the registers.  One ring for keys and
+// queries, with keys of three items on their way: 17.2, the keys are not what items wait for.
 #include <atomic>
 
 #include "twk_prompt.cuh"
@@ -547,6 +548,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     const float4* log = reinterpret_cast<const float4*>(smem + C::OFF_LOG +
                                                                         (x * kLogSlots + log_at) * 512 +
                                                                         half * 256);
+                    [[maybe_unused]] bool there = true;   // the next tile, if any, is on its way
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         tmem_wait_ld();
@@ -562,8 +564,19 @@ __global__ void __launch_bounds__(kThreads, 1)
                             log_at = (log_at + 1) % kLogSlots;
                             if (u + 1 < e) {
                                 if (u + x >= ob && u + x < oe) ra.next();       // the other half's tile
-                                if (!(ok = wait_tile())) break;
-                                tmem_ld_32x32b_x32(base + C::T_ACC + ra.slot * 128 + half * 64, s[0]);
+                                // d = 128: not waited for before this one's last columns are done (16384
+                                // tokens 765 -> 747 us; at d = 64, whose products are short, 8192: 187 -> 199)
+                                if constexpr (D == 128) {
+                                    there = __all_sync(0xffffffffu, mbar_test(smem_u32(&M.acc_full[x][rx.slot]),
+                                                                              rx.phase));
+                                    if (there) {
+                                        tc_fence_after();
+                                        tmem_ld_32x32b_x32(base + C::T_ACC + ra.slot * 128 + half * 64, s[0]);
+                                    }
+                                } else {
+                                    if (!(ok = wait_tile())) break;
+                                    tmem_ld_32x32b_x32(base + C::T_ACC + ra.slot * 128 + half * 64, s[0]);
+                                }
                             }
                         }
                         if (edge) {
@@ -572,6 +585,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                                 s[i][y] = see[i] >> y & 1u ? s[i][y] : 0xff800000u;
                         }
                         add(s[i], log + 8 * i);
+                    }
+                    if constexpr (D == 128) {
+                        if (!there) {
+                            if (!(ok = wait_tile())) break;
+                            tmem_ld_32x32b_x32(base + C::T_ACC + ra.slot * 128 + half * 64, s[0]);
+                        }
                     }
                     if (!ok) break;
                     if ((u & 31) == 31) {
