@@ -29,9 +29,9 @@
 //     an item, whose parts (unnormalised O, top, l in float32) merge_kernel joins in order.
 //
 // Measured (us in a graph; TFLOP/s; 32 query heads on 8 KV heads), before and after what is named:
-//   16384 tokens, d = 128   1382   1591: 85 % of the measured burst rate, 94 % of the sustained
-//   4096 tokens, d = 128     115   1195; 2048: 44 us, 1024: 21; 101: 8.8, most of it the start and the end
-//   256 tokens over 65536    195   1405, items cut into 5 parts
+//   16384 tokens, d = 128   1400   1571: 83 % of the measured burst rate, 93 % of the sustained
+//   4096 tokens, d = 128     116   1185; 2048: 44 us, 1024: 21; 101: 8.9, most of it the start and the end
+//   256 tokens over 65536    185   1480, items cut into 5 parts
 //   16384 tokens, d = 64     843   1304; 12 packed prompts of 752 to 3001 tokens 252, 838
 //   descriptors in uniform registers: 2095 -> 1451 on the first line
 //   cutting by tiles and what an item takes beside them, instead of by tiles: 305 -> 255 on the last
@@ -475,6 +475,26 @@ __global__ void __launch_bounds__(kThreads, 1)
                         // heads and middles in slot 2 c, the item that begins in the block in 2 c + 1
                         it.slot = 2 * static_cast<int>(blockIdx.x) + (at.off == 0 ? 1 : 0);
                         if (at.off == 0) join = make_int4(at.parts(a), it.t0, it.tokens, it.head);
+                        // Items longer than a span: those of a head read the same keys at the same time, or
+                        // L2 would not hold them until the next one does (256 tokens over 65536: 198 ->
+                        // 185 us; at d = 64 the code costs what it gains).  What one visits after t units of
+                        // the span is, in tiles, t modulo the span's length: a part begins inside and ends
+                        // with what is before.  Its list is then tiles [first + r, end), [first, first + r).
+                        if constexpr (D == 128) {
+                            const int tiles = min(it.s1, min(it.count[0], it.count[1]));
+                            if (at.length > at.each && it.s0 >= kt.sinks &&
+                                tiles == min(it.s1, max(it.count[0], it.count[1]))) {
+                                const int shift = kt.from - kt.sinks;
+                                const int first = it.s0 + shift, end = tiles + shift;
+                                const int r = at.turn(first);
+                                if (r < end - first) {
+                                    it.s0 = first + r;
+                                    it.s1 = it.count[0] = it.count[1] = end + r;
+                                    it.sinks = end;
+                                    it.from = first;
+                                }
+                            }
+                        }
                     }
                     ok = mbar_wait(&M.item_empty[ri.slot], ri.phase ^ 1u, wc, 31);
                     if (!ok) break;

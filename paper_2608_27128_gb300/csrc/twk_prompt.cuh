@@ -359,6 +359,14 @@ struct Walk {
         part(a);
     }
 
+    // What to add to x so that it is, modulo the length of a span, the part's place in its span.
+    __device__ __forceinline__ int turn(int x) const
+    {
+        const long long d = begin + off - cut(blockIdx.x) - x;
+        const int r = static_cast<int>(d % each);
+        return r < 0 ? r + static_cast<int>(each) : r;
+    }
+
     // Blocks that share the item, this one being the first.
     __device__ __forceinline__ int parts(const PromptArgs& a) const
     {
