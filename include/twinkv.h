@@ -582,8 +582,9 @@ size_t twinkv_prompt_attend_workspace(twinkv_prompt s);
  * Attention over prompts, query head h reading KV head h / (Hq / H):
  *   o = sum_j softmax_j(scale q . k_j) v_j over the keys j that the token sees; 0 if there are none
  * Precision: products of bf16 values in float32 sums; exp(score - m), m at most 11 below the largest
- * score so far, is rounded to bf16 for its product with the values, not for the denominator.  The
- * result is rounded to bf16.
+ * score so far, is rounded to bf16 for its product with the values, not for the denominator.  Scores
+ * may be of any size that q . k allows: beyond 2^12 in units of log 2 their differences are taken
+ * first.  The result is rounded to bf16.
  *   q, k, v     bf16, 16-byte aligned, strides in s; q . k below 2^120; what a sequence's keys and
  *               values hold has to be finite, other rows may hold anything
  *   scale       finite, above 0

@@ -13,6 +13,11 @@
 // memory and the tile done again, a rare event.  So a tile costs no maximum (a fifth of the softmax at
 // d = 64, where that is what bounds it).
 //
+// t is rounded, by 2^-24 of itself: a factor that the row's probabilities have in common, and that its sum and lse
+// take out again, as long as it is about 1.  A row's top is kept as the q . k that it comes from, and where one
+// of a warp's is beyond 2^12 in units of log 2 (kLarge) the difference is taken first, p_j = 2^(c (q . k_j - top)),
+// which is right for scores of any size; every tile then has its maximum found.
+//
 // Bound by the tensor cores at d = 128: 4 d operations for each pair of a row and a key, of which a prompt of
 // n tokens has n^2 / 2 per head; an exponential for each (4 cycles a warp) takes half their time there, and
 // as long at d = 64, which the softmax's instructions bound.  Design (persistent, one block of 384 threads
@@ -51,6 +56,7 @@ static_assert(4 * kHelperRegs + 8 * kSoftmaxRegs <= 12 * kLaunchRegs,
               "the split draws on the registers of the launch");
 constexpr int kPairRows = 2 * kTileRows;
 constexpr float kFar = 0x1p15f;          // sum of a tile's probabilities from which the top follows
+constexpr float kLarge = 0x1p12f;        // |c top| up to which c top enters rounded
 
 // Items of attention: pairs of row tiles; as long as their list of key tiles.
 struct RowPairs {
@@ -142,6 +148,22 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
+
+// c (x - y) of two tops (-inf: none yet), with their products rounded as they enter the probabilities.
+__device__ __forceinline__ float top_gap(float x, float y, float c)
+{
+    const float u = __fmul_rn(x, c), v = __fmul_rn(y, c);
+    return fabsf(u) <= kLarge && fabsf(v) <= kLarge ? u - v : (x - y) * c;
+}
+
+// The logarithm of a row's denominator.
+__device__ __forceinline__ float log_sum(float top, float sum, float c, float scale)
+{
+    if (!(sum > 0.0f)) return -INFINITY;
+    const float t = __fmul_rn(top, c);
+    return fabsf(t) <= kLarge ? fmaf(t, 0.6931471805599453f, logf(sum)) : fmaf(top, scale, logf(sum));
+}
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
     prompt_attend_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
@@ -547,6 +569,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             // rows of no token hold anything
             const bool sees = token < tpt && x * tpt + token < it.tokens && pos >= 0;
             float top = -INFINITY, sum = 0.0f;
+            bool large = false;                                      // one of the warp's tops is
             for (int j = it.s0; j < n; ++j) {
                 const int k0 = kt.tile(j) * kTileKeys;
                 if (!(ok = all_wait(&M.s_full[x], s_uses++ & 1u, wc, 35))) break;
@@ -579,7 +602,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 // With the top so far; again with the true one where a row has none, or its sum shows that
                 // the scores have left it far behind.
-                bool exact = __any_sync(0xffffffffu, sees && top == -INFINITY);
+                bool exact = large || __any_sync(0xffffffffu, sees && top == -INFINITY);
                 // the products with the tile's last probabilities, whose place the next ones take
                 if (C::EARLY && j > it.s0) {
                     if (!(ok = all_wait(&M.o_full[x], o_uses++ & 1u, wc, 36))) break;
@@ -596,9 +619,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                                 m[i] = max3(m[i], as_f(s[i][e]), as_f(s[i][e + 1]));
                             m[i] = fmaxf(m[i], as_f(s[i][31]));
                         }
-                        const float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * p.c;
+                        const float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
                         const bool rise = most > top;
-                        const float f = rise ? exp2_approx(top - most) : 1.0f;    // top -inf: 0
+                        const float f = rise ? exp2_approx(top_gap(top, most, p.c)) : 1.0f;    // top -inf: 0
                         if (rise) top = most;
                         if (j > it.s0 && __any_sync(0xffffffffu, rise)) {
                             sum *= f;
@@ -613,8 +636,22 @@ __global__ void __launch_bounds__(kThreads, 1)
                                 tmem_st_32x32b_x32(t_o + 32 * i, o);
                             }
                         }
+                        large = __any_sync(0xffffffffu, sees && top > -INFINITY &&
+                                                            fabsf(top * p.c) > kLarge);
+                        if (large) {             // the tile is not done again: s may change
+                            const float y = top == -INFINITY ? 0.0f : -top;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                                for (int e = 0; e < 32; e += 2) {
+                                    const float2 z = __fadd2_rn(
+                                        make_float2(as_f(s[i][e]), as_f(s[i][e + 1])), make_float2(y, y));
+                                    s[i][e] = __float_as_uint(z.x);
+                                    s[i][e + 1] = __float_as_uint(z.y);
+                                }
+                        }
                     }
-                    const float t = top == -INFINITY ? 0.0f : top;
+                    const float t = large || top == -INFINITY ? 0.0f : __fmul_rn(top, p.c);
                     const float2 c2 = make_float2(p.c, p.c), t2 = make_float2(-t, -t);
                     float2 l[4] = {};
 #pragma unroll
@@ -696,8 +733,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     __syncwarp();
                 }
                 if (held && a.out_lse)
-                    a.out_lse[at_row] = sum > 0.0f ? fmaf(top, 0.6931471805599453f, logf(sum))
-                                                   : -INFINITY;
+                    a.out_lse[at_row] = log_sum(top, sum, p.c, a.scale);
             } else {
                 float* part = p.part + static_cast<int64_t>(it.slot) * kPartFloats<D>;
                 const int r = x * kTileRows + row;
@@ -769,7 +805,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps)
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) most = fmaxf(most, m[k]);
         if (most == -INFINITY) continue;
-        const float f = exp2_approx(top - most);
+        const float f = exp2_approx(top_gap(top, most, p.c));
         sum *= f;
 #pragma unroll
         for (int v = 0; v < kVec; ++v)
@@ -779,7 +815,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps)
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             if (m[k] == -INFINITY) continue;          // what it holds is no number
-            const float w = exp2_approx(m[k] - top);
+            const float w = exp2_approx(top_gap(m[k], top, p.c));
             sum = fmaf(l[k], w, sum);
 #pragma unroll
             for (int v = 0; v < kVec; ++v) {
@@ -799,7 +835,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps)
             make_uint2(bf16_pair(acc[v][0] * inv, acc[v][1] * inv),
                        bf16_pair(acc[v][2] * inv, acc[v][3] * inv));
     if (warp == 0 && held && a.out_lse)
-        a.out_lse[first + at] = sum > 0.0f ? fmaf(top, 0.6931471805599453f, logf(sum)) : -INFINITY;
+        a.out_lse[first + at] = log_sum(top, sum, p.c, a.scale);
     __syncthreads();
     constexpr int kRowLanes = D / 8;
 #pragma unroll
