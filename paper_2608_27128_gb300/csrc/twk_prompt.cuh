@@ -38,10 +38,10 @@ __device__ __forceinline__ Sequence sequence_of(const PromptArgs& a, int b)
     Sequence q;
     q.ok = true;
     rows_of(a.seqs.offsets, a.seqs.lens, b, a.s.tokens, q.t0, q.n, q.ok);
-    const bool own = a.seqs.k_offsets || !a.seqs.offsets;
-    rows_of(own ? a.seqs.k_offsets : a.seqs.offsets,
-            a.seqs.k_lens ? a.seqs.k_lens : own ? nullptr : a.seqs.lens, b, a.s.keys, q.j0, q.m,
-            q.ok);
+    // without offsets of their own the keys are as the tokens: also their number, where lens gives that
+    rows_of(a.seqs.k_offsets ? a.seqs.k_offsets : a.seqs.offsets,
+            a.seqs.k_lens ? a.seqs.k_lens : a.seqs.k_offsets ? nullptr : a.seqs.lens, b, a.s.keys, q.j0,
+            q.m, q.ok);
     if (!q.ok) q.n = q.m = 0;
     return q;
 }
