@@ -143,15 +143,23 @@ class PageCache:
 
     def evict(self, b: int, score, budget, *, n_sink=None, n_recent=None) -> dict:
         """Sequence b keeps, per unit, the budget's worth of slots with the highest score
-        [L,H,N] float32 (N at least the longest unit), sinks and recent ones first
-        (twinkv_weight_policy), in new pages; a unit with fewer slots keeps all of them.  Returns a
-        dict: status [L,H] as pack's, mask [L,H,N], and score [L,H,N], the kept slots' in order."""
+        [L,H,N] float32 (N at least the longest unit, else ValueError), sinks and recent ones first
+        (twinkv_weight_policy), in new pages; a unit with fewer slots keeps all of them.  Between steps:
+        not after a reserve whose appends are still to come.  Returns a dict: status [L,H], the
+        policy's or, where that is 0, as pack's; mask [L,H,N], and score [L,H,N], the kept slots' in
+        order."""
         units = self._sequence(b)
         counts = [min(n, self._used[u]) for n, u in zip(self._counts(budget, units), units)]
+        # a unit longer than its scores would be a data error, and lose its slots
+        most = max(self._used[u] for u in units)
+        if (not isinstance(score, torch.Tensor) or score.dim() != 3
+                or score.shape[:2] != (self.L, self.H) or score.shape[2] < most):
+            raise ValueError(f"score must be [{self.L}, {self.H}, N], N at least {most}")
         want = torch.tensor(counts, dtype=torch.int32).view(self.L, self.H).to(self.pool.device)
         out = tk.twinkv_weight_policy(score, want, lens=self.lens[:, b].contiguous(), n_sink=n_sink,
                                       n_recent=n_recent, want_score=True)
-        out["status"] = self.compact(b, out["mask"], counts)
+        policy = out["status"]
+        out["status"] = torch.where(policy != 0, policy, self.compact(b, out["mask"], counts))
         return out
 
     def fork(self, b: int, to: int):
