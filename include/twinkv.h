@@ -587,7 +587,7 @@ size_t twinkv_prompt_attend_workspace(twinkv_prompt s);
  * first.  The result is rounded to bf16.
  *   q, k, v     bf16, 16-byte aligned, strides in s; q . k below 2^120; what a sequence's keys and
  *               values hold has to be finite, other rows may hold anything
- *   scale       finite, above 0
+ *   scale       above 0, below 2^127
  *   window      0: none (n_sink is then not used)
  *   out         [tokens][Hq][d] bf16, 16-byte aligned; not q, k or v
  *   out_lse     [tokens][Hq] float32 log of the softmax's denominator (-inf: nothing seen), or NULL
@@ -628,7 +628,8 @@ size_t twinkv_cache_weights_workspace(twinkv_queries s, int32_t d);
  * lens[u] - n + i, and sees what it sees in twinkv_cache_attend): per unit u and slot j
  *   out_score = score + sum over the tokens i and query heads g that see j of
  *               exp(scale q_ig . k_j - lse_ig)
- *   q, s, scale, window, n_sink, pool, table, lens   as in twinkv_cache_attend
+ *   q, s, window, n_sink, pool, table, lens   as in twinkv_cache_attend
+ *   scale       above 0, below 2^127
  *   lse         [B][n][Hq] float32, as twinkv_cache_attend gives it
  *   score       [B*H][N] float32: the slots' sums so far
  *   out_score   [B*H][N] float32; may be `score` itself.  Entries from lens[u] on are left as they were

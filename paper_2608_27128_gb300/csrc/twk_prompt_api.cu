@@ -16,6 +16,9 @@ constexpr int kMaxRows = 1 << 20;      // positions of a unit, as for the audit
 constexpr int kMaxUnits = 65535;
 constexpr int kMaxGroup = 128;         // query heads per KV head over prompts
 
+// above 0, and a float32 as a multiple of log 2 too
+bool scale_ok(float scale) { return std::isfinite(scale) && scale > 0.0f && scale < 0x1p127f; }
+
 bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
 size_t up256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
@@ -57,7 +60,7 @@ twinkv_status prompt_ok(const void* q, const void* k, const twinkv_prompt& s,
     if (!stride_ok(s.q_token, s.tokens) || !stride_ok(s.q_head, s.Hq) ||
         !stride_ok(s.k_token, s.keys) || !stride_ok(s.k_head, s.H))
         return TWINKV_ERR_INVALID_ARG;
-    if (!std::isfinite(scale) || scale <= 0.0f || window < 0 || n_sink < 0)
+    if (!scale_ok(scale) || window < 0 || n_sink < 0)
         return TWINKV_ERR_INVALID_ARG;
     return TWINKV_OK;
 }
@@ -165,7 +168,7 @@ twinkv_status twinkv_cache_weights(const void* q, const float* lse, twinkv_queri
         pool.n_pages < 1 || !table || !aligned(table, 4) || max_pages < 1 ||
         max_pages > kMaxRows / kPage)
         return TWINKV_ERR_INVALID_ARG;
-    if (!std::isfinite(scale) || scale <= 0.0f || window < 0 || n_sink < 0 || N < 1 ||
+    if (!scale_ok(scale) || window < 0 || n_sink < 0 || N < 1 ||
         N > kMaxRows)
         return TWINKV_ERR_INVALID_ARG;
     if (s.B < 1 || s.H < 1 || s.Hq < 1 || s.n < 1 || s.Hq % s.H != 0 || s.q_batch % 8 ||
