@@ -606,6 +606,8 @@ size_t twinkv_prompt_weights_workspace(twinkv_prompt s);
  * What the attention over prompts pays to each key: per KV head h and key j the sum
  *   [score +] sum over tokens i that see j, query heads g of h:  exp(scale q_ig . k_j - lse_ig)
  * in float32, in an order that the sizes alone decide.
+ * Range: |scale q . k| and |lse| below 2^20.  An exponent is off by up to 2^-23 (|scale q . k| + |lse|)
+ * and what the float32 sums of its score are, a weight by that much of itself.
  *   q, k, s, seqs, scale, window, n_sink   as in twinkv_prompt_attend (the strides of v are not used)
  *   lse         [tokens][Hq] float32, as twinkv_prompt_attend gives it
  *   last        > 0: only the last `last` tokens of each sequence count (the observation window of
@@ -628,6 +630,7 @@ size_t twinkv_cache_weights_workspace(twinkv_queries s, int32_t d);
  * lens[u] - n + i, and sees what it sees in twinkv_cache_attend): per unit u and slot j
  *   out_score = score + sum over the tokens i and query heads g that see j of
  *               exp(scale q_ig . k_j - lse_ig)
+ * Range and precision as there; scale times the values of q below 2^116.
  *   q, s, window, n_sink, pool, table, lens   as in twinkv_cache_attend
  *   scale       above 0, below 2^127
  *   lse         [B][n][Hq] float32, as twinkv_cache_attend gives it
