@@ -585,8 +585,9 @@ size_t twinkv_prompt_attend_workspace(twinkv_prompt s);
  * score so far, is rounded to bf16 for its product with the values, not for the denominator.  Scores
  * may be of any size that q . k allows: beyond 2^12 in units of log 2 their differences are taken
  * first.  The result is rounded to bf16.
- *   q, k, v     bf16, 16-byte aligned, strides in s; q . k below 2^120; what a sequence's keys and
- *               values hold has to be finite, other rows may hold anything
+ *   q, k, v     bf16, 16-byte aligned, strides in s; q . k below 2^120, values below 2^95 (a sum of
+ *               products is up to 2^15 times what it comes to, for each tile of 128 keys); what a
+ *               sequence's keys and values hold has to be finite, other rows may hold anything
  *   scale       above 0, below 2^127
  *   window      0: none (n_sink is then not used)
  *   out         [tokens][Hq][d] bf16, 16-byte aligned; not q, k or v

@@ -146,3 +146,22 @@ def test_equal_large_scores_share_the_output(d):
     want = (p.v64[p.j0[0] + 90, 0] + p.v64[p.j0[0] + 40, 0]) / 2
     out = got["out"][:30, 0].double().cpu().numpy()
     assert (np.abs(out - want) <= 2.0 ** -8 * np.abs(want) + 1e-30).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_large_values(d):
+    """Values up to the largest that the header allows, whose products with probabilities of up to
+    2^15 (a tile's sum before the top follows) and their sums stay finite."""
+    size = 2.0 ** 92
+    for n, m in ((300, 300), (64, 3000)):
+        p = Prompts([(n, m)], 2, 1, d, device(), seed=d)
+        p.k64[:] = 0
+        p.k64[:, 0, 0] = np.linspace(0, 60, m)         # rises by less than the top follows at, for long
+        p.q64[:] = 0
+        p.q64[:, 0, 0], p.q64[:, 1, 0] = d ** 0.5, -d ** 0.5
+        p.k, p.q = (torch.from_numpy(x).to(torch.bfloat16).to(device()) for x in (p.k64, p.q64))
+        p.k64, p.q64 = p.k.double().cpu().numpy(), p.q.double().cpu().numpy()
+        p.v64 = p.v64 * size
+        p.v = torch.from_numpy(p.v64).to(torch.bfloat16).to(device())
+        assert np.abs(p.v64).max() < 2.0 ** 95
+        check(p)
