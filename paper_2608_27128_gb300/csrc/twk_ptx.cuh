@@ -324,9 +324,10 @@ __device__ __forceinline__ void umma_commit_own(uint64_t* bar)
 }
 
 // The forms of one CTA, for operands as umma_desc_sw128 and umma_desc_sw128_rows describe them (low words
-// of the descriptors, the high word being the same): D[tmem] (+)= A B, bf16 -> f32, in steps of 16 along
+// of the descriptors, the high word being kDescHigh): D[tmem] (+)= A B, bf16 -> f32, in steps of 16 along
 // K.  The steps' descriptors are made inside: as C++ values the compiler keeps them all in registers.
-constexpr uint32_t kDescHigh = 0x40004040u;
+// The high word: stride byte offset >> 4 of 1024 B from bit 0, version 1 at bit 14, layout type 2 at bit 29.
+constexpr uint32_t kDescHigh = 1024u >> 4 | 1u << 14 | 2u << 29;
 
 // A and B K-major in shared memory, K = 64 kChunks: rows of 64 values, chunks of 64 of them 16 KB apart.
 template <int kChunks>
@@ -337,19 +338,19 @@ __device__ __forceinline__ void umma_rows(uint32_t d_tmem, uint32_t a_low, uint3
     "add.u32 a, %1, " #offset ";\n\tadd.u32 b, %2, " #offset ";\n\t"                       \
     "mov.b64 x, {a, h};\n\tmov.b64 y, {b, h};\n\t"                                        \
     "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, " #sum ";\n\t"
-#define TWK_BEGIN                                                                          \
+#define TWK_BEGIN(high)                                                                    \
     "{\n\t.reg .pred p, q;\n\t.reg .b32 a, b, h;\n\t.reg .b64 x, y;\n\t"                   \
-    "mov.b32 h, 0x40004040;\n\tsetp.ne.b32 p, h, 0;\n\t"
+    "mov.b32 h, %" #high ";\n\tsetp.ne.b32 p, h, 0;\n\t"
     if constexpr (kChunks == 2)
-        asm volatile(TWK_BEGIN "setp.eq.b32 q, h, 0;\n\t" TWK_STEP(0, q) TWK_STEP(2, p)
+        asm volatile(TWK_BEGIN(4) "setp.eq.b32 q, h, 0;\n\t" TWK_STEP(0, q) TWK_STEP(2, p)
                          TWK_STEP(4, p) TWK_STEP(6, p) TWK_STEP(1024, p) TWK_STEP(1026, p)
                              TWK_STEP(1028, p) TWK_STEP(1030, p) "}" ::"r"(d_tmem),
-                     "r"(a_low), "r"(b_low), "r"(idesc)
+                     "r"(a_low), "r"(b_low), "r"(idesc), "n"(kDescHigh)
                      : "memory");
     else
-        asm volatile(TWK_BEGIN "setp.eq.b32 q, h, 0;\n\t" TWK_STEP(0, q) TWK_STEP(2, p)
+        asm volatile(TWK_BEGIN(4) "setp.eq.b32 q, h, 0;\n\t" TWK_STEP(0, q) TWK_STEP(2, p)
                          TWK_STEP(4, p) TWK_STEP(6, p) "}" ::"r"(d_tmem),
-                     "r"(a_low), "r"(b_low), "r"(idesc)
+                     "r"(a_low), "r"(b_low), "r"(idesc), "n"(kDescHigh)
                      : "memory");
 #undef TWK_STEP
 }
@@ -362,11 +363,11 @@ __device__ __forceinline__ void umma_tmem_128(uint32_t d_tmem, uint32_t a_tmem, 
 #define TWK_STEP(i, column, offset, sum)                                                   \
     "add.u32 a, %1, " #column ";\n\tadd.u32 b, %2, " #offset ";\n\tmov.b64 y, {b, h};\n\t" \
     "tcgen05.mma.cta_group::1.kind::f16 [%0], [a], y, %3, " #sum ";\n\t"
-    asm volatile(TWK_BEGIN "setp.ne.b32 q, %4, 0;\n\t" TWK_STEP(0, 0, 0, q) TWK_STEP(1, 8, 128, p)
+    asm volatile(TWK_BEGIN(5) "setp.ne.b32 q, %4, 0;\n\t" TWK_STEP(0, 0, 0, q) TWK_STEP(1, 8, 128, p)
                      TWK_STEP(2, 16, 256, p) TWK_STEP(3, 24, 384, p) TWK_STEP(4, 32, 512, p)
                          TWK_STEP(5, 40, 640, p) TWK_STEP(6, 48, 768, p)
                              TWK_STEP(7, 56, 896, p) "}" ::"r"(d_tmem),
-                 "r"(a_tmem), "r"(b_low), "r"(idesc), "r"(add)
+                 "r"(a_tmem), "r"(b_low), "r"(idesc), "r"(add), "n"(kDescHigh)
                  : "memory");
 #undef TWK_STEP
 }
@@ -380,16 +381,16 @@ __device__ __forceinline__ void umma_tmem_rows(uint32_t d_tmem, uint32_t a_tmem,
     "add.u32 a, %1, " #column ";\n\tadd.u32 b, %2, " #offset ";\n\tmov.b64 y, {b, h};\n\t" \
     "tcgen05.mma.cta_group::1.kind::f16 [%0], [a], y, %3, " #sum ";\n\t"
     if constexpr (kChunks == 2)
-        asm volatile(TWK_BEGIN "setp.eq.b32 q, h, 0;\n\t" TWK_STEP(0, 0, q) TWK_STEP(8, 2, p)
+        asm volatile(TWK_BEGIN(4) "setp.eq.b32 q, h, 0;\n\t" TWK_STEP(0, 0, q) TWK_STEP(8, 2, p)
                          TWK_STEP(16, 4, p) TWK_STEP(24, 6, p) TWK_STEP(32, 1024, p)
                              TWK_STEP(40, 1026, p) TWK_STEP(48, 1028, p)
                                  TWK_STEP(56, 1030, p) "}" ::"r"(d_tmem),
-                     "r"(a_tmem), "r"(b_low), "r"(idesc)
+                     "r"(a_tmem), "r"(b_low), "r"(idesc), "n"(kDescHigh)
                      : "memory");
     else
-        asm volatile(TWK_BEGIN "setp.eq.b32 q, h, 0;\n\t" TWK_STEP(0, 0, q) TWK_STEP(8, 2, p)
+        asm volatile(TWK_BEGIN(4) "setp.eq.b32 q, h, 0;\n\t" TWK_STEP(0, 0, q) TWK_STEP(8, 2, p)
                          TWK_STEP(16, 4, p) TWK_STEP(24, 6, p) "}" ::"r"(d_tmem),
-                     "r"(a_tmem), "r"(b_low), "r"(idesc)
+                     "r"(a_tmem), "r"(b_low), "r"(idesc), "n"(kDescHigh)
                      : "memory");
 #undef TWK_STEP
 #undef TWK_BEGIN
@@ -465,9 +466,7 @@ __device__ __forceinline__ uint64_t umma_desc_sw128(uint32_t saddr)
     uint64_t d = 0;
     d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
     d |= static_cast<uint64_t>(1u) << 16;
-    d |= static_cast<uint64_t>(1024u >> 4) << 32;
-    d |= static_cast<uint64_t>(1u) << 46;
-    d |= static_cast<uint64_t>(2u) << 61;
+    d |= static_cast<uint64_t>(kDescHigh) << 32;
     return d;
 }
 
