@@ -18,7 +18,8 @@
 // Measured (us in a graph; share of the measured copy rate by the bytes above):
 //   32 x 8 units of 4k to 16k slots, 4 rows, d = 128   42.6   74 %;  d = 64, 16384 slots 45.1   60 %
 //   8 units of 131009 slots, 4 rows                    23.5   53 %
-//   16 x 8 units of 16384 slots, 8 rows 35.5   70 %;  16 rows 61, 41 %
+//   16 x 8 units of 16384 slots, 8 rows 35.4   70 %;  16 rows 61, 41 %: blocks that start anew for some pages
+//                                                each, with one page on its way
 //   8 units of 2048 slots, 4 rows                       5.4
 // A block of warps for each unit's pages instead of the persistent kernel: 58 us for the first, whatever its
 // pages' prefetching (loads wait behind the start of each block).

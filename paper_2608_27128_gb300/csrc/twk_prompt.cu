@@ -10,8 +10,8 @@
 // The top is the maximum of the row's first tile, and follows later ones only where a tile's sum of
 // probabilities shows that it is far behind them (2^15: floats and bf16 do not notice such factors, and
 // the sum of 128 probabilities stays below it else): the tile's maximum is found, O scaled in tensor
-// memory and the tile done again, a rare event.  So a tile costs no maximum (a fifth of the softmax at
-// d = 64, where that is what bounds it).
+// memory and the tile done again, a rare event.  So a tile costs no maximum (a fifth of the softmax's
+// instructions at d = 64).
 //
 // t is rounded, by 2^-24 of itself: a factor that the row's probabilities have in common, and that its sum and lse
 // take out again, as long as it is about 1.  A row's top is kept as the q . k that it comes from, and where one
@@ -20,8 +20,9 @@
 //
 // Bound by the tensor cores at d = 128: 4 d operations for each pair of a row and a key, of which a prompt of
 // n tokens has n^2 / 2 per head; an exponential for each (4 cycles a warp) takes half their time there, and
-// as long at d = 64, which the softmax's instructions bound.  Design (persistent, one block of 384 threads
-// per SM):
+// as long at d = 64.  There no pipe is above 41 % and an instruction issues in 39 % of the cycles: latency bounds
+// it, two softmax warps to a quarter of the SM, each in a chain of load, exponentials, store and wait.  Design
+// (persistent, one block of 384 threads per SM):
 //   - An item is 256 query rows of one KV head: (token, head) pairs, the heads of a token side by side,
 //     so that every head of the group reads the same keys, and short sequences fill a tile.  Two
 //     tiles of 128 rows take turns: one's softmax runs beside the other's products.
@@ -34,12 +35,14 @@
 //     an item, whose parts (unnormalised O, top, l in float32) merge_kernel joins in order.
 //
 // Measured (us in a graph; TFLOP/s; 32 query heads on 8 KV heads), before and after what is named:
-//   16384 tokens, d = 128   1400   1571: 83 % of the measured burst rate, 93 % of the sustained
-//   4096 tokens, d = 128     116   1185; 2048: 44 us, 1024: 21; 101: 8.9, most of it the start and the end
-//   256 tokens over 65536    185   1480, items cut into 5 parts
-//   16384 tokens, d = 64     843   1304; 12 packed prompts of 752 to 3001 tokens 252, 838
+//   16384 tokens, d = 128   1370   1605: 85 % of the measured burst rate, 95 % of the sustained (1474 us
+//                           from call to call, under the power limit)
+//   4096 tokens, d = 128     116   1180; 2048: 44.5 us, 1024: 21; 101: 9.0, most of it the start and the end
+//   256 tokens over 65536    185   1483, items cut into 5 parts (199 us from call to call)
+//   16384 tokens, d = 64     862   1275; 12 packed prompts of 752 to 3001 tokens 246, 858
 //   descriptors in uniform registers: 2095 -> 1451 on the first line
 //   cutting by tiles and what an item takes beside them, instead of by tiles: 305 -> 255 on the last
+//   tops kept as q . k, for scores of any size: 1404 -> 1379 on the first, 843 -> 861 and 252 -> 246 on the last
 #include <atomic>
 
 #include "twk_cache.cuh"
@@ -462,8 +465,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
         } else if (warp == 10) {
             // ------------------------------------------------------------ items
-            // d = 64 runs 12 % slower with the code of a second start in the kernel (16384 tokens: 938 us, not
-            // 844), whose loops already fill the instruction cache
+            // d = 64 ran 12 % slower with the code of a second start in the kernel (16384 tokens: 938 us, not
+            // 844); why is not known: code, registers or their scheduling
             Walk<RowPairs, D == 128> at;
             at.start(a, sums);
             fence_async_shared();       // the sums have been read
@@ -499,7 +502,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         if (at.off == 0) join = make_int4(at.parts(a), it.t0, it.tokens, it.head);
                         // Items longer than a span: those of a head read the same keys at the same time, or
                         // L2 would not hold them until the next one does (256 tokens over 65536: 198 ->
-                        // 185 us; at d = 64 the code costs what it gains).  What one visits after t units of
+                        // 185 us; at d = 64 packed prompts lose what it gains there).  What one visits after t units of
                         // the span is, in tiles, t modulo the span's length: a part begins inside and ends
                         // with what is before.  Its list is then tiles [first + r, end), [first, first + r).
                         if constexpr (D == 128) {
@@ -849,7 +852,8 @@ __global__ void __launch_bounds__(32 * kMergeWarps)
 }
 
 // Where no item is longer than 13 units none is cut: the longest takes no longer than shares and a second
-// kernel (1024 tokens, d = 128: 25.4 -> 21.6 us).
+// kernel (d = 128: 512 tokens 15.8 -> 13.7 us, 1024 24.7 -> 21.0, 1500 35.3 -> 29.0; d = 64: 1024 19.4 -> 16.2).
+// The lengths being on the device, all rows of k decide: a batch of short prompts gets the second kernel.
 constexpr int kSnapFew = 6;
 constexpr int whole_keys(int d) { return (2 * kSnapFew + 1 - RowPairs::more(d)) * kTileKeys; }
 

@@ -23,11 +23,13 @@
 //     an item that blocks share, in order.
 //
 // Measured (us in a graph; TFLOP/s; 32 query heads on 8 KV heads):
-//   every token of 16384, d = 128   754   1458: 77 % of the measured burst rate
-//   every token of 8192             198   1389, of 4096 61, of 2048 24.3; of 8192 at d = 64 188
+//   every token of 16384, d = 128   744   1478: 79 % of the measured burst rate
+//   every token of 8192             197   1393, of 4096 61, of 2048 24.4; of 8192 at d = 64 187
 //   the last 32 of 16384            16    four items of 256 keys a block at most, one after another: 4300
 //                                         cycles each for moving keys, products, sums and their joining
-//   six prompts of up to 3001, window of 1024, d = 64   85: most tiles are at an edge
+//   six prompts of up to 3001, window of 1024, d = 64   85: at the rate of the unwindowed ones their tiles are 64;
+//                                         21 % of a warp's tiles are at an edge, 12 % show it nothing and are
+//                                         done all the same (half of them where the sinks stretch an item)
 // A unit of two tiles takes about 1750 cycles where exponentials alone take 1050: the warps issue in more than
 // half of the cycles, so what surrounds a tile counts (one barrier for a tile's products and lse instead
 // of two, rings without phases: 210 -> 202 us on the second line, 209 -> 188 at d = 64).  All sixteen warps
