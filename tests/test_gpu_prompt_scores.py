@@ -130,7 +130,8 @@ def test_scores_that_pass_from_small_to_large(d, e, down):
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("scale,k,q", [(1.0, 80, 0), (2.0 ** 20, 80, 0), (2.0 ** 100, 0, 0),
                                        (2.0 ** 110, -56, -56), (2.0 ** 126, -60, -60),
-                                       (1e-30, 100, 0), (1e-38, 0, 0)])
+                                       (1e-30, 100, 0), (1e-38, 0, 0), (1e-40, 0, 0),
+                                       (1e-45, 60, 0)])
 def test_scales(d, scale, k, q):
     """From scores that are alike to the largest ones, by the scale."""
     check(prompt(40, 200, d, k, [q] * 4, 1), scale=scale)

@@ -85,3 +85,32 @@ def test_large_scores_over_pages(d, G, n):
     for u, length in enumerate(lens):
         a = got["score"][u, 0, :length].double().cpu().numpy()
         assert (np.abs(a - want[u, :length]) <= off[u, :length]).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("scale", [1e-12, 1e-38, 1e-40, 1e-45])
+def test_scales_down_to_the_smallest(d, scale):
+    """Scores that are all but nothing, also where the scale has few bits or none beside log 2: a token pays
+    alike to every key that it sees, and nothing to the others.  Off by lse's rounding and its
+    product's, 2^-23 |lse| with |lse| < 8, the exponential's 2^-22, and the sum's 2^-23 a step; the
+    scores themselves are below 2^-21."""
+    p = prompt(100, 700, d, 0, [0, 0, -3, 2], 1, more=[(33, 33)])
+    lse = np.full((p.T, p.Hq), np.nan, np.float32)
+    want, steps = np.zeros(p.Tk), np.zeros(p.Tk)
+    for (n, m), t, j in zip(p.seqs, p.t0, p.j0):
+        see = R.sees(n, m)
+        lse[t:t + n] = np.log(see.sum(1))[:, None]
+        want[j:j + m] = p.Hq * (see / see.sum(1)[:, None]).sum(0)
+        steps[j:j + m] = n * p.Hq
+    off = want * (8 * 2.0 ** -22 + 2.0 ** -21 + 2.0 ** -22 + (steps + 4) * 2.0 ** -23)
+    got = tk.twinkv_prompt_weights(p.q, p.k, put(lse), **p.where, scale=scale)
+    score = got["score"].double().cpu().numpy()[0]
+    assert (np.abs(score - want) <= off)[p.key].all()
+
+    pool, table, _ = make_cache(np.random.default_rng(d), [300], d)
+    q = torch.from_numpy(np.random.default_rng(1).standard_normal((1, 1, 4, d))).to(torch.bfloat16)
+    log = torch.full((1, 1, 4), float(np.log(300)), device=device())
+    score = tk.twinkv_cache_weights(q.to(device()), log, pool, table.view(1, 1, -1),
+                                    torch.full((1, 1), 300, dtype=torch.int32, device=device()),
+                                    torch.zeros(1, 1, 300, device=device()), scale=scale)["score"]
+    assert (score.double() - 4 / 300).abs().max() <= 4 / 300 * (8 * 2.0 ** -22 + 2.0 ** -20)
